@@ -436,6 +436,106 @@ int iv_merkle_root_noalloc(const uint8_t *d_leaves, uint64_t n_leaves, uint8_t *
                            void *cuda_stream);
 
 /* ---------------------------------------------------------------------------
+ * A training step on verified weights -- the paper verifies a model before and
+ * between the steps of a training pipeline and, after an update that "touches
+ * some chunks", re-verifies only those (iv_tree_update).  The calls below are
+ * the parts of such a step that touch few rows or all gradients at once: the
+ * embedding lookup, its gradient, the global gradient norm and clipping.
+ * Results are functions of the inputs alone, bit for bit: no floating-point
+ * atomics, every sum in an order fixed by the data, so replicas that make the
+ * same step keep the same digests and root.
+ *
+ * Element types; 16-bit values are widened to 32 bits, sums and products are
+ * taken in 32 bits or more and rounded once (to nearest, ties to even).  An
+ * input and an output type may be the same, or one of them IV_F32.  Tensors may
+ * start at any multiple of their element size (a tensor inside a weight file
+ * rarely starts at a multiple of 16 bytes); sizes and strides are in elements.
+ */
+typedef enum iv_dtype { IV_F32 = 0, IV_F16 = 1, IV_BF16 = 2 } iv_dtype;
+
+/* Embedding lookup with scaling: out[t, :] = round(scale * table[token[t], :]).
+ *   d_table      n_rows rows of dim elements, row r at d_table + r * row_stride
+ *                (row_stride >= dim when there is more than one row)
+ *   d_tokens     n_tokens row numbers of token_bytes (4 or 8) bytes, signed
+ *   d_out        n_tokens rows of dim elements, out_stride apart; must not
+ *                overlap the table
+ * A token outside [0, n_rows) gives a row of zeros and sets the device status
+ * to 2.  n_tokens == 0 or dim == 0 launches nothing. */
+int iv_embedding(iv_ctx *ctx, const void *d_table, int table_type, uint64_t n_rows, uint64_t dim, uint64_t row_stride,
+                 const void *d_tokens, int token_bytes, uint64_t n_tokens, float scale, void *d_out, int out_type,
+                 uint64_t out_stride, void *cuda_stream);
+
+/* Its gradient: grad[r, :] = round(old + scale * sum of grad_out[t, :] over the tokens t of row r), old = grad[r, :]
+ * when accumulate != 0 (rows without a token are then left alone) and 0 otherwise (they are set to zero).
+ * The sum of a row runs over its tokens in ascending order of t: 64 terms make
+ * a piece, 32 pieces a group; terms, pieces and groups are added first to last
+ * in 32 bits, then scaled.
+ *   d_grad_out    n_tokens rows of dim elements, grad_stride apart
+ *   padding_row   tokens equal to it give no gradient; -1 for none
+ *   d_grad        n_rows rows of dim elements, out_stride apart
+ * Tokens outside [0, n_rows) give no gradient and set the device status to 2.
+ * IV_ERR_TOO_LARGE for n_tokens > 2^30, n_rows or dim > 2^31 or n_tokens * dim
+ * > 2^45 or so (also the other calls of this section). */
+int iv_embedding_grad(iv_ctx *ctx, const void *d_grad_out, int grad_type, uint64_t grad_stride, uint64_t dim,
+                      const void *d_tokens, int token_bytes, uint64_t n_tokens, uint64_t n_rows, int64_t padding_row,
+                      float scale, int accumulate, void *d_grad, int out_type, uint64_t out_stride, void *cuda_stream);
+
+/* The same gradient with only the rows that have a token, for a table of which a
+ * step touches little (the touched rows are also what makes chunks dirty):
+ *   d_rows     receives the distinct rows in ascending order, then -1
+ *   d_grad     receives row d_rows[i]'s gradient as row i, then zeros (so norms
+ *              over the whole array are right)
+ *   cap        rows of both arrays, all written; >= min(n_tokens, n_rows)
+ *   d_count    receives the number of distinct rows (device memory) */
+int iv_embedding_grad_rows(iv_ctx *ctx, const void *d_grad_out, int grad_type, uint64_t grad_stride, uint64_t dim,
+                           const void *d_tokens, int token_bytes, uint64_t n_tokens, uint64_t n_rows,
+                           int64_t padding_row, float scale, int64_t *d_rows, void *d_grad, int out_type,
+                           uint64_t out_stride, uint64_t cap, uint64_t *d_count, void *cuda_stream);
+
+/* Global gradient norm over a ragged tensor set.  The set is given as for
+ * iv_hash_ragged: tensor k is the d_lengths[k] BYTES at d_base + d_offsets[k]
+ * (modulo 2^64, so a tensor of another allocation has the offset address -
+ * d_base).
+ *   d_types    one byte per tensor, its iv_dtype; NULL: all are of `type`
+ *   d_norms    optional: n floats, the norm of each tensor
+ *   d_result   device memory for one record:
+ *     norm = sqrt(sum of squares over all tensors); scale = 1;
+ *     n_nonfinite = tensors that hold an infinity or a NaN.
+ * Finite gradients of any size have a right norm (squares that leave the range
+ * of 32 bits are taken in 64).  A tensor whose offset or length is not a
+ * multiple of its element size, or whose type is unknown, is left out and sets
+ * the device status to 2.  n == 0 gives norm 0.
+ * For gradients sharded over several GPUs, add up sum_squares over them. */
+typedef struct iv_norm_result {
+    uint32_t status;      /* device-side status, as iv_device_status */
+    uint32_t n_nonfinite; /* tensors with an infinity or a NaN */
+    float norm;
+    float scale;          /* what the gradients are multiplied by (1 for iv_grad_norm) */
+    double sum_squares;
+    uint64_t n_elements;
+} iv_norm_result;
+int iv_grad_norm(iv_ctx *ctx, const void *d_base, const uint64_t *d_offsets, const uint64_t *d_lengths,
+                 const uint8_t *d_types, int type, uint64_t n, float *d_norms, iv_norm_result *d_result,
+                 void *cuda_stream);
+
+/* Clipping: the norm as above, scale = norm <= max_norm ? 1 : max_norm / norm
+ * (so an infinite norm gives 0 and NaN gives NaN: n_nonfinite tells to skip the
+ * step), then every tensor times scale, rounded once.
+ *   max_norm        >= 0, not NaN
+ *   d_out           NULL: in place.  Otherwise tensor k goes to d_out +
+ *                   d_out_offsets[k] (bytes) as out_type, or as its own type when
+ *                   out_type < 0; the output must not overlap the input */
+int iv_grad_clip(iv_ctx *ctx, void *d_base, const uint64_t *d_offsets, const uint64_t *d_lengths, const uint8_t *d_types,
+                 int type, uint64_t n, float max_norm, void *d_out, const uint64_t *d_out_offsets, int out_type,
+                 float *d_norms, iv_norm_result *d_result, void *cuda_stream);
+
+/* Its second half alone, with a factor from device memory (gradients sharded over several GPUs, whose norm is known
+ * after a reduction).  Arguments as iv_grad_clip. */
+int iv_grad_scale(iv_ctx *ctx, void *d_base, const uint64_t *d_offsets, const uint64_t *d_lengths, const uint8_t *d_types,
+                  int type, uint64_t n, const float *d_scale, void *d_out, const uint64_t *d_out_offsets, int out_type,
+                  void *cuda_stream);
+
+/* ---------------------------------------------------------------------------
  * Roofline probe (a measurement aid; the paper has no counterpart).  Runs a
  * register-only microbenchmark on every SM and reports, from the SM cycle
  * counter, how many lane-operations of one instruction kind an SM retires per

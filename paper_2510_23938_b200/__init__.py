@@ -5,5 +5,5 @@ hand-written CUDA kernels behind the C ABI declared in ``include/iv.h``.  This p
 the thin Python binding (``binding``), the in-tree build (``build``) and the synthetic
 input generators used by the tests and the benchmark (``inputs``).
 """
-from .binding import (Context, IvError, Manifest, VerifyResult, load_library, n_chunks,  # noqa: F401
-                      new_result, read_result, read_results)
+from .binding import (Context, IvError, Manifest, NormResult, VerifyResult, load_library, n_chunks,  # noqa: F401
+                      new_norm_result, new_result, read_norm_result, read_result, read_results, tensor_ranges)

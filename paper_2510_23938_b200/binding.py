@@ -34,7 +34,11 @@ EXPORTS = (
     "iv_hash_chunks_sha384", "iv_merkle_root_sha384", "iv_verify_manifest_sha384",
     "iv_hash_chunks_sha512", "iv_merkle_root_sha512", "iv_verify_manifest_sha512",
     "iv_hash_chunks_rfc6962", "iv_merkle_root_rfc6962", "iv_verify_manifest_rfc6962",
+    "iv_embedding", "iv_embedding_grad", "iv_embedding_grad_rows", "iv_grad_norm", "iv_grad_clip", "iv_grad_scale",
 )
+
+# iv_dtype of the training-step operators
+DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
 class IvError(RuntimeError):
@@ -82,6 +86,12 @@ class VerifyResult(ctypes.Structure):
     """iv_verify_result as laid out in device memory (48 bytes)."""
     _fields_ = [("status", ctypes.c_uint32), ("root_ok", ctypes.c_uint32),
                 ("n_mismatch", ctypes.c_uint64), ("root", ctypes.c_uint8 * 32)]
+
+
+class NormResult(ctypes.Structure):
+    """iv_norm_result as laid out in device memory (32 bytes)."""
+    _fields_ = [("status", ctypes.c_uint32), ("n_nonfinite", ctypes.c_uint32), ("norm", ctypes.c_float),
+                ("scale", ctypes.c_float), ("sum_squares", ctypes.c_double), ("n_elements", ctypes.c_uint64)]
 
 
 _lib = None
@@ -172,6 +182,19 @@ def load_library() -> ctypes.CDLL:
     lib.iv_probe_alu.argtypes = [vp, i32, ctypes.c_uint32, ctypes.c_uint32, ctypes.c_uint32, ctypes.c_uint32,
                                  ctypes.POINTER(ctypes.c_double)]
     lib.iv_probe_alu.restype = i32
+    i64, f32 = ctypes.c_int64, ctypes.c_float
+    lib.iv_embedding.argtypes = [vp, vp, i32, u64, u64, u64, vp, i32, u64, f32, vp, i32, u64, vp]
+    lib.iv_embedding.restype = i32
+    lib.iv_embedding_grad.argtypes = [vp, vp, i32, u64, u64, vp, i32, u64, u64, i64, f32, i32, vp, i32, u64, vp]
+    lib.iv_embedding_grad.restype = i32
+    lib.iv_embedding_grad_rows.argtypes = [vp, vp, i32, u64, u64, vp, i32, u64, u64, i64, f32, vp, vp, i32, u64, u64, vp, vp]
+    lib.iv_embedding_grad_rows.restype = i32
+    lib.iv_grad_norm.argtypes = [vp, vp, vp, vp, vp, i32, u64, vp, vp, vp]
+    lib.iv_grad_norm.restype = i32
+    lib.iv_grad_clip.argtypes = [vp, vp, vp, vp, vp, i32, u64, f32, vp, vp, i32, vp, vp, vp]
+    lib.iv_grad_clip.restype = i32
+    lib.iv_grad_scale.argtypes = [vp, vp, vp, vp, vp, i32, u64, vp, vp, vp, i32, vp]
+    lib.iv_grad_scale.restype = i32
     _lib = lib
     return lib
 
@@ -201,6 +224,59 @@ def _dev_ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 def _nbytes(t: torch.Tensor) -> int:
     return t.numel() * t.element_size()
+
+
+def _ptr(t: torch.Tensor) -> int:
+    assert t.is_cuda, "device tensors must be CUDA tensors"
+    return t.data_ptr()
+
+
+def _row_ptr(t: torch.Tensor) -> int:
+    """Device pointer of a (rows, dim) tensor whose rows are contiguous."""
+    assert t.is_cuda and t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1), "rows must be contiguous CUDA memory"
+    return t.data_ptr()
+
+
+def _stride_of(t: torch.Tensor) -> int:
+    """Elements from one row of a (rows, dim) tensor to the next."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _rows_of(t: torch.Tensor, n: int, dim: int) -> int:
+    """Checks that `t` is n rows of `dim` elements one fixed stride apart; returns the stride."""
+    assert t.is_cuda and t.numel() == n * dim and t.shape[-1] == dim, "wrong number of rows or columns"
+    if t.dim() == 2:
+        assert dim <= 1 or t.stride(1) == 1, "rows must be contiguous"
+        return t.stride(0) if n > 1 else dim
+    assert t.is_contiguous(), "tensors of more than two dimensions must be contiguous"
+    return dim
+
+
+def _token_bytes(tokens: torch.Tensor) -> int:
+    assert tokens.dtype in (torch.int32, torch.int64), "tokens are int32 or int64"
+    return tokens.element_size()
+
+
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _result_ptr(result: torch.Tensor) -> int:
+    assert result.is_cuda and result.is_contiguous() and _nbytes(result) >= ctypes.sizeof(NormResult)
+    return result.data_ptr()
+
+
+def _out_args(out, out_offsets, out_dtype, types, n):
+    """(d_out, d_out_offsets, out_type) of iv_grad_clip and iv_grad_scale."""
+    if out is None:
+        assert out_offsets is None and out_dtype is None, "in place needs no output arguments"
+        return None, None, -1
+    assert out_offsets.dtype == torch.int64 and out_offsets.numel() == n
+    code = DTYPES[out_dtype] if out_dtype is not None else (DTYPES[out.dtype] if types is None else -1)
+    return _ptr(out), _dev_ptr(out_offsets), code
 
 
 class Context:
@@ -556,6 +632,111 @@ class Context:
         self._check(rc, "iv_hash_ragged_update")
         return out if finish else None
 
+    # -- training-step operators --------------------------------------------------------------
+    # Tensors the calls allocate come from the stream the work runs on; a caller that passes `stream` keeps its other
+    # tensors alive until that stream has reached the work, as everywhere in this binding.
+
+    def embedding(self, table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out: torch.Tensor | None = None,
+                  out_dtype: torch.dtype | None = None, stream=None) -> torch.Tensor:
+        """iv_embedding: scale * table[tokens] (tokens int32 or int64, any shape), rounded once to `out_dtype`
+        (default: the table's).  `table` is (rows, dim) with contiguous rows, at any element alignment."""
+        rows, dim = table.shape
+        if out is None:
+            out = _empty((*tokens.shape, dim), out_dtype or table.dtype, table.device, stream)
+        n = tokens.numel()
+        out_stride = _rows_of(out, n, dim)
+        rc = self._lib.iv_embedding(self._h, _row_ptr(table), DTYPES[table.dtype], rows, dim, _stride_of(table),
+                                    _dev_ptr(tokens), _token_bytes(tokens), n, scale, _ptr(out), DTYPES[out.dtype],
+                                    out_stride, _stream_ptr(stream))
+        self._check(rc, "iv_embedding")
+        return out
+
+    def embedding_grad(self, grad_out: torch.Tensor, tokens: torch.Tensor, n_rows: int, scale: float = 1.0,
+                       padding_row: int | None = None, out: torch.Tensor | None = None,
+                       out_dtype: torch.dtype | None = None, accumulate: bool = False, stream=None) -> torch.Tensor:
+        """iv_embedding_grad: the (n_rows, dim) gradient of `embedding`'s table, `grad_out` (..., dim) being the
+        gradient of its result; with `accumulate`, added to `out`."""
+        dim, n = grad_out.shape[-1], tokens.numel()
+        grad_stride = _rows_of(grad_out, n, dim)
+        if out is None:
+            assert not accumulate, "accumulate needs the gradient to add to"
+            out = _empty((n_rows, dim), out_dtype or grad_out.dtype, grad_out.device, stream)
+        assert out.shape == (n_rows, dim), "out must be (n_rows, dim)"
+        rc = self._lib.iv_embedding_grad(self._h, _ptr(grad_out), DTYPES[grad_out.dtype], grad_stride, dim,
+                                         _dev_ptr(tokens), _token_bytes(tokens), n, n_rows,
+                                         -1 if padding_row is None else padding_row, scale, int(accumulate), _row_ptr(out),
+                                         DTYPES[out.dtype], _stride_of(out), _stream_ptr(stream))
+        self._check(rc, "iv_embedding_grad")
+        return out
+
+    def embedding_grad_rows(self, grad_out: torch.Tensor, tokens: torch.Tensor, n_rows: int, scale: float = 1.0,
+                            padding_row: int | None = None, rows: torch.Tensor | None = None,
+                            out: torch.Tensor | None = None, count: torch.Tensor | None = None,
+                            out_dtype: torch.dtype | None = None, stream=None):
+        """iv_embedding_grad_rows: (rows, grad, count) -- the distinct rows ascending (int64, -1 behind them), their
+        gradients (zero rows behind them) and their number (int64, on the device).  min(tokens, n_rows) rows in all."""
+        dim, n = grad_out.shape[-1], tokens.numel()
+        grad_stride = _rows_of(grad_out, n, dim)
+        cap = min(n, n_rows) if out is None else out.shape[0]
+        if out is None:
+            out = _empty((cap, dim), out_dtype or grad_out.dtype, grad_out.device, stream)
+        if rows is None:
+            rows = _empty((cap,), torch.int64, grad_out.device, stream)
+        if count is None:
+            count = _empty((1,), torch.int64, grad_out.device, stream)
+        assert out.shape == (cap, dim) and rows.shape == (cap,) and rows.dtype == count.dtype == torch.int64
+        assert rows.is_cuda and rows.is_contiguous() and count.is_cuda and count.numel() == 1
+        rc = self._lib.iv_embedding_grad_rows(self._h, _ptr(grad_out), DTYPES[grad_out.dtype], grad_stride, dim,
+                                              _dev_ptr(tokens), _token_bytes(tokens), n, n_rows,
+                                              -1 if padding_row is None else padding_row, scale,
+                                              rows.data_ptr() or count.data_ptr(), _row_ptr(out), DTYPES[out.dtype],
+                                              _stride_of(out), cap, count.data_ptr(), _stream_ptr(stream))
+        self._check(rc, "iv_embedding_grad_rows")
+        return rows, out, count
+
+    def _set_args(self, base, offsets, lengths, dtype, types):
+        n = offsets.numel()
+        assert lengths.numel() == n and offsets.dtype == lengths.dtype == torch.int64
+        if types is not None:
+            assert types.dtype == torch.uint8 and types.numel() == n
+        return (_ptr(base), _dev_ptr(offsets), _dev_ptr(lengths), _dev_ptr(types),
+                DTYPES[base.dtype if dtype is None else dtype] if types is None else 0, n)
+
+    def grad_norm(self, base: torch.Tensor, offsets: torch.Tensor, lengths: torch.Tensor, result: torch.Tensor,
+                  norms: torch.Tensor | None = None, dtype: torch.dtype | None = None,
+                  types: torch.Tensor | None = None, stream=None) -> None:
+        """iv_grad_norm (asynchronous): `offsets`, `lengths` in bytes as for hash_ragged (see tensor_ranges for tensors
+        of their own); `result` is a 32-byte uint8 device tensor (new_norm_result, read_norm_result), `norms` an
+        optional float32 tensor for the tensors' own norms; element type `dtype` (default: base's) or `types`, one
+        DTYPES code per tensor (uint8)."""
+        args = self._set_args(base, offsets, lengths, dtype, types)
+        assert norms is None or (norms.dtype == torch.float32 and norms.numel() == args[-1])
+        rc = self._lib.iv_grad_norm(self._h, *args, _dev_ptr(norms), _result_ptr(result), _stream_ptr(stream))
+        self._check(rc, "iv_grad_norm")
+
+    def grad_clip(self, base: torch.Tensor, offsets: torch.Tensor, lengths: torch.Tensor, max_norm: float,
+                  result: torch.Tensor, norms: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                  out_offsets: torch.Tensor | None = None, dtype: torch.dtype | None = None,
+                  types: torch.Tensor | None = None, out_dtype: torch.dtype | None = None, stream=None) -> None:
+        """iv_grad_clip (asynchronous): grad_norm, then every tensor times min(1, max_norm / norm), in place or to
+        `out` + `out_offsets` (bytes) as `out_dtype` (default: out's type, or with `types` each tensor's own)."""
+        args = self._set_args(base, offsets, lengths, dtype, types)
+        assert norms is None or (norms.dtype == torch.float32 and norms.numel() == args[-1])
+        rc = self._lib.iv_grad_clip(self._h, *args, max_norm, *_out_args(out, out_offsets, out_dtype, types, args[-1]),
+                                    _dev_ptr(norms), _result_ptr(result), _stream_ptr(stream))
+        self._check(rc, "iv_grad_clip")
+
+    def grad_scale(self, base: torch.Tensor, offsets: torch.Tensor, lengths: torch.Tensor, scale: torch.Tensor,
+                   out: torch.Tensor | None = None, out_offsets: torch.Tensor | None = None,
+                   dtype: torch.dtype | None = None, types: torch.Tensor | None = None,
+                   out_dtype: torch.dtype | None = None, stream=None) -> None:
+        """iv_grad_scale (asynchronous): every tensor times the float32 device scalar `scale`; output as grad_clip."""
+        args = self._set_args(base, offsets, lengths, dtype, types)
+        assert scale.is_cuda and scale.dtype == torch.float32 and scale.numel() == 1
+        rc = self._lib.iv_grad_scale(self._h, *args, scale.data_ptr(),
+                                     *_out_args(out, out_offsets, out_dtype, types, args[-1]), _stream_ptr(stream))
+        self._check(rc, "iv_grad_scale")
+
     def last_digests(self, n: int) -> torch.Tensor:
         """Copy of the chunk digests the last verification on this context computed."""
         ptr = self._lib.iv_ctx_digests(self._h)
@@ -596,6 +777,28 @@ def read_result(result: torch.Tensor) -> dict:
     r = VerifyResult.from_buffer_copy(raw)
     return {"status": int(r.status), "root_ok": bool(r.root_ok), "n_mismatch": int(r.n_mismatch),
             "root": bytes(r.root)}
+
+
+def new_norm_result(device) -> torch.Tensor:
+    return torch.zeros(ctypes.sizeof(NormResult), dtype=torch.uint8, device=device)
+
+
+def read_norm_result(result: torch.Tensor) -> dict:
+    """Decodes a 32-byte iv_norm_result tensor (synchronises on the copy to the host)."""
+    r = NormResult.from_buffer_copy(bytes(result.cpu().numpy().tobytes()))
+    return {name: getattr(r, name) for name, _ in NormResult._fields_}
+
+
+def tensor_ranges(tensors) -> tuple:
+    """(base, offsets, lengths, types) of tensors of their own, as grad_norm, grad_clip and hash_ragged take a set: the
+    first tensor and, per tensor, the bytes from it, the length in bytes (int64 device tensors) and the DTYPES code."""
+    base = tensors[0]
+    assert all(t.is_cuda and t.is_contiguous() for t in tensors), "device tensors must be contiguous CUDA tensors"
+    signed = [(t.data_ptr() - base.data_ptr() + (1 << 63)) % (1 << 64) - (1 << 63) for t in tensors]
+    device = base.device
+    return (base, torch.tensor(signed, dtype=torch.int64, device=device),
+            torch.tensor([_nbytes(t) for t in tensors], dtype=torch.int64, device=device),
+            torch.tensor([DTYPES[t.dtype] for t in tensors], dtype=torch.uint8, device=device))
 
 
 def read_results(results: torch.Tensor) -> list:

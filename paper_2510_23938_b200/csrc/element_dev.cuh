@@ -1,0 +1,174 @@
+// Elements of the training-step operators: 32-bit floats and the two 16-bit types, read and written as vectors at any
+// element alignment.  Tensors inside a weight file or a packed gradient buffer start at any multiple of their element
+// size, so a vector may straddle two aligned pieces of memory: both are loaded (the second is the neighbouring lane's
+// first, an L1 hit) and the wanted bytes are shifted out.  Every aligned piece that is touched holds at least one
+// byte that was asked for, so nothing outside the 16-byte granules of the tensor is read.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cstdint>
+
+#include "iv_internal.h"
+
+namespace ivk {
+namespace elem {
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// V elements of type T as 32-bit words.
+template <typename T, int V>
+struct Packed {
+    static constexpr int kBytes = V * (int)sizeof(T);
+    static constexpr int kWords = kBytes / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0u;
+    }
+    __device__ __forceinline__ void unpack(float (&v)[V]) const {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = __uint_as_float(w[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                T lo, hi;
+                *reinterpret_cast<uint16_t *>(&lo) = (uint16_t)(w[i] & 0xffffu);
+                *reinterpret_cast<uint16_t *>(&hi) = (uint16_t)(w[i] >> 16);
+                v[2 * i] = to_float(lo);
+                v[2 * i + 1] = to_float(hi);
+            }
+        }
+    }
+    __device__ __forceinline__ void pack(const float (&v)[V]) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) w[i] = __float_as_uint(v[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                const T lo = from_float<T>(v[2 * i]), hi = from_float<T>(v[2 * i + 1]);
+                w[i] = (uint32_t)*reinterpret_cast<const uint16_t *>(&lo) |
+                       ((uint32_t)*reinterpret_cast<const uint16_t *>(&hi) << 16);
+            }
+        }
+    }
+};
+
+// Aligned vector access of 8 or 16 bytes.
+template <int WORDS>
+__device__ __forceinline__ void load_aligned(const void *p, uint32_t *w) {
+    if constexpr (WORDS == 4) {
+        const uint4 q = *static_cast<const uint4 *>(p);
+        w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+    } else {
+        static_assert(WORDS == 2, "8 or 16 bytes");
+        const uint2 q = *static_cast<const uint2 *>(p);
+        w[0] = q.x; w[1] = q.y;
+    }
+}
+template <int WORDS>
+__device__ __forceinline__ void store_aligned(void *p, const uint32_t *w) {
+    if constexpr (WORDS == 4) *static_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    else {
+        static_assert(WORDS == 2, "8 or 16 bytes");
+        *static_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+    }
+}
+
+// V consecutive elements at any element alignment.  The branch on the misalignment is the same for all lanes that walk
+// one tensor with a stride of whole vectors.
+template <typename T, int V>
+__device__ __forceinline__ void load_any(const T *p, Packed<T, V> &out) {
+    constexpr int W = Packed<T, V>::kWords;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    const uint32_t off = (uint32_t)a & (4u * W - 1u);
+    if (off == 0u) {
+        load_aligned<W>(p, out.w);
+        return;
+    }
+    const uint32_t *q = reinterpret_cast<const uint32_t *>(a - off);
+    uint32_t w[2 * W];
+    load_aligned<W>(q, w);
+    load_aligned<W>(q + W, w + W);
+    const uint32_t words = off >> 2, bits = (off & 3u) * 8u;
+    if constexpr (W == 4) {
+        if (words & 2u) {
+#pragma unroll
+            for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+        }
+    }
+    if (words & 1u) {
+#pragma unroll
+        for (int i = 0; i < W + 1; ++i) w[i] = i + 1 < 2 * W ? w[i + 1] : 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i) out.w[i] = __funnelshift_r(w[i], i + 1 < 2 * W ? w[i + 1] : 0u, bits);
+}
+
+// out[i] = f(in[i]) for i < n by the `lanes` threads of which this is number `lane`: single elements up to the first
+// aligned vector of the output, aligned vectors (UNROLL of them in flight per thread), single elements at the end.
+template <typename Tin, typename Tout, int UNROLL, typename F>
+__device__ __forceinline__ void map_span(const Tin *in, Tout *out, uint32_t n, uint32_t lane, uint32_t lanes, F f) {
+    constexpr int V = 16 / (int)(sizeof(Tin) > sizeof(Tout) ? sizeof(Tin) : sizeof(Tout));
+    constexpr uint32_t kOut = V * sizeof(Tout);
+    uint32_t head = (uint32_t)((kOut - (reinterpret_cast<uintptr_t>(out) & (kOut - 1u))) & (kOut - 1u)) / (uint32_t)sizeof(Tout);
+    if (head > n) head = n;
+    if (lane < head) out[lane] = from_float<Tout>(f(to_float(in[lane])));
+    in += head;
+    out += head;
+    n -= head;
+    const uint32_t vecs = n / V;
+    for (uint32_t v0 = lane; v0 < vecs; v0 += lanes * UNROLL) {
+        Packed<Tin, V> raw[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const uint32_t v = v0 + u * lanes;
+            if (v < vecs) load_any<Tin, V>(in + (uint64_t)v * V, raw[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const uint32_t v = v0 + u * lanes;
+            if (v < vecs) {
+                float x[V];
+                raw[u].unpack(x);
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[i] = f(x[i]);
+                Packed<Tout, V> y;
+                y.pack(x);
+                store_aligned<Packed<Tout, V>::kWords>(out + (uint64_t)v * V, y.w);
+            }
+        }
+    }
+    const uint32_t done = vecs * V;
+    if (lane < n - done) out[done + lane] = from_float<Tout>(f(to_float(in[done + lane])));
+}
+
+}  // namespace elem
+
+// Calls f(tag of the input type, tag of the output type) for the pairs of element types the operators support: equal
+// ones, and a 16-bit type with 32 bits on the other side.
+template <typename T> struct TypeTag { using type = T; };
+template <typename F>
+inline cudaError_t by_types(int in, int out, F f) {
+    using f32 = TypeTag<float>;
+    using f16 = TypeTag<__half>;
+    using bf16 = TypeTag<__nv_bfloat16>;
+    switch (in * 3 + out) {
+        case IV_F32 * 3 + IV_F32: return f(f32{}, f32{});
+        case IV_F32 * 3 + IV_F16: return f(f32{}, f16{});
+        case IV_F32 * 3 + IV_BF16: return f(f32{}, bf16{});
+        case IV_F16 * 3 + IV_F32: return f(f16{}, f32{});
+        case IV_F16 * 3 + IV_F16: return f(f16{}, f16{});
+        case IV_BF16 * 3 + IV_F32: return f(bf16{}, f32{});
+        case IV_BF16 * 3 + IV_BF16: return f(bf16{}, bf16{});
+        default: return cudaErrorInvalidValue;     // checked at the entry points
+    }
+}
+}  // namespace ivk

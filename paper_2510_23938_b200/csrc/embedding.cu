@@ -1,0 +1,65 @@
+// Embedding lookup with scaling: out[t, :] = round(scale * table[token[t], :]), the product in 32 bits, rounded once.
+//
+// A gather of rows: what bounds it is memory (the distinct rows read once, every output row written once), for a few
+// tokens the latency of the chain token -> row -> store.  A warp takes one tile of kTile columns of one token, so that
+// a single token's row is spread over several warps and every lane has four vector loads in flight.
+#include "element_dev.cuh"
+#include "iv_internal.h"
+
+namespace ivk {
+
+namespace {
+
+constexpr uint32_t kTile = 1024;      // columns per warp: 4 vectors of 8 (16-bit types) or 8 of 4 (32-bit) per lane
+constexpr uint32_t kWarps = 8;
+
+template <typename Tin, typename Tout, typename Token>
+__global__ void __launch_bounds__(kWarps * 32)
+embedding_kernel(const Tin *table, uint64_t n_rows, uint64_t dim, uint64_t row_stride, const Token *tokens, uint64_t n_tokens,
+                 float scale, Tout *out, uint64_t out_stride, uint32_t tiles, uint32_t *status) {
+    const uint32_t lane = threadIdx.x & 31u;
+    const uint64_t units = n_tokens * tiles;
+    for (uint64_t unit = (uint64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); unit < units;
+         unit += (uint64_t)gridDim.x * kWarps) {
+        const uint64_t t = unit / tiles;
+        const uint64_t c0 = (unit - t * tiles) * kTile;
+        const uint32_t cols = (uint32_t)(dim - c0 < kTile ? dim - c0 : kTile);
+        const uint64_t row = (uint64_t)(int64_t)tokens[t];       // a negative token becomes a large number
+        Tout *o = out + t * out_stride + c0;
+        if (row < n_rows) {
+            elem::map_span<Tin, Tout, 4>(table + row * row_stride + c0, o, cols, lane, 32u, [scale](float x) { return x * scale; });
+        } else {
+            for (uint32_t i = lane; i < cols; i += 32u) o[i] = elem::from_float<Tout>(0.f);
+            if (lane == 0 && c0 == 0) atomicMax(status, (uint32_t)IVK_DEV_BOUNDS);
+        }
+    }
+}
+
+template <typename Tin, typename Tout, typename Token>
+cudaError_t launch_typed(const EmbeddingArgs &a, uint32_t *d_status, cudaStream_t stream) {
+    const uint32_t tiles = (uint32_t)((a.dim + kTile - 1) / kTile);
+    const uint64_t blocks = (a.n_tokens * tiles + kWarps - 1) / kWarps;
+    const uint32_t grid = (uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30));
+    embedding_kernel<Tin, Tout, Token><<<grid, kWarps * 32, 0, stream>>>(
+        static_cast<const Tin *>(a.d_table), a.n_rows, a.dim, a.row_stride, static_cast<const Token *>(a.d_tokens), a.n_tokens,
+        a.scale, static_cast<Tout *>(a.d_out), a.out_stride, tiles, d_status);
+    return cudaGetLastError();
+}
+
+template <typename Tin, typename Tout>
+cudaError_t launch_token(const EmbeddingArgs &a, uint32_t *d_status, cudaStream_t stream) {
+    return a.token_bytes == 4 ? launch_typed<Tin, Tout, int32_t>(a, d_status, stream)
+                              : launch_typed<Tin, Tout, int64_t>(a, d_status, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_embedding(const EmbeddingArgs &a, uint32_t *d_status, cudaStream_t stream, uint64_t *launches) {
+    if (a.n_tokens == 0 || a.dim == 0) return cudaSuccess;
+    ++*launches;
+    return by_types(a.table_type, a.out_type, [&](auto in, auto out) {
+        return launch_token<typename decltype(in)::type, typename decltype(out)::type>(a, d_status, stream);
+    });
+}
+
+}  // namespace ivk

@@ -48,6 +48,16 @@ struct iv_ctx {
     uint8_t *d_slices = nullptr;              // FIFO, slice counters and parked chaining values of the sliced leaf kernel
     uint64_t slices_cap = 0;                  // bytes
 
+    // training-step operators
+    uint8_t *d_sort = nullptr;                // sorted tokens of iv_embedding_grad
+    uint64_t sort_cap = 0;                    // bytes
+    uint32_t *d_arrivals = nullptr;           // its arrival counters, zero between calls
+    uint64_t arrivals_cap = 0;                // bytes
+    float *d_partial = nullptr;               // its partial sums
+    uint64_t partial_cap = 0;                 // bytes
+    uint8_t *d_plan = nullptr;                // pieces and their sums of iv_grad_norm
+    uint64_t plan_cap = 0;                    // bytes
+
     // streaming windows
     uint8_t *d_digests384 = nullptr;          // chunk digests of iv_verify_manifest_sha384 / _sha512, then the root
     uint64_t digests384_cap = 0;              // records of 64 bytes
@@ -405,6 +415,10 @@ int iv_destroy(iv_ctx *ctx) {
     cudaFree(ctx->d_pairs512);
     cudaFree(ctx->d_sub);
     cudaFree(ctx->d_batch);
+    cudaFree(ctx->d_sort);
+    cudaFree(ctx->d_arrivals);
+    cudaFree(ctx->d_partial);
+    cudaFree(ctx->d_plan);
     cudaFree(ctx->d_tree384[0]);
     cudaFree(ctx->d_tree384[1]);
     cudaFree(ctx->d_window[0]);
@@ -979,6 +993,154 @@ int iv_merkle_root_rfc6962(iv_ctx *ctx, const uint8_t *d_leaves, uint64_t n_leav
     if (rc != IV_OK) return rc;
     IV_TRY(ctx, ivk::launch_merkle_root_rfc6962(d_leaves, n_leaves, d_root, ctx->d_tree384[0], ctx->d_tree384[1],
                                                 static_cast<cudaStream_t>(cuda_stream), &ctx->launches));
+    return IV_OK;
+}
+
+namespace {
+
+bool is_dtype(int type) { return type == IV_F32 || type == IV_F16 || type == IV_BF16; }
+bool type_pair_ok(int in, int out) { return is_dtype(in) && is_dtype(out) && (in == out || in == IV_F32 || out == IV_F32); }
+uint64_t dtype_bytes(int type) { return type == IV_F32 ? 4u : 2u; }
+bool aligned_to(const void *p, uint64_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1u)) == 0u; }
+
+constexpr uint64_t kMaxTokens = 1ull << 30;
+constexpr uint64_t kMaxRows = 1ull << 31;
+
+// Arguments that both forms of the gradient have in common, then scratch and launch.
+int embedding_grad(iv_ctx *ctx, const ivk::EmbeddingGradArgs &a, void *cuda_stream) {
+    if (!type_pair_ok(a.grad_type, a.out_type) || (a.token_bytes != 4 && a.token_bytes != 8)) return IV_ERR_INVALID_ARG;
+    if (a.padding_row < -1) return IV_ERR_INVALID_ARG;
+    if (a.n_tokens > kMaxTokens || a.n_rows > kMaxRows || a.dim > kMaxRows) return IV_ERR_TOO_LARGE;
+    if ((a.n_tokens / 8u + 1u) * (a.dim / 256u + 1u) / 8u > 0x7ffffff0ull) return IV_ERR_TOO_LARGE;   // one launch's blocks
+    if (a.n_tokens > 1 && a.grad_stride < a.dim) return IV_ERR_INVALID_ARG;
+    if (a.n_tokens && (!a.d_tokens || !aligned_to(a.d_tokens, a.token_bytes))) return IV_ERR_INVALID_ARG;
+    if (a.n_tokens && a.dim && (!a.d_grad_out || !aligned_to(a.d_grad_out, dtype_bytes(a.grad_type)))) return IV_ERR_INVALID_ARG;
+    const uint64_t out_rows = a.d_rows ? a.cap : a.n_rows;
+    if (out_rows > 1 && a.out_stride < a.dim) return IV_ERR_INVALID_ARG;
+    if (out_rows && a.dim && (!a.d_grad || !aligned_to(a.d_grad, dtype_bytes(a.out_type)))) return IV_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (a.n_tokens || a.d_rows) {
+        int rc = grow(ctx, &ctx->d_sort, &ctx->sort_cap, ivk::embedding_grad_sort_bytes(a.n_tokens), 1);
+        if (rc != IV_OK) return rc;
+        rc = grow(ctx, &ctx->d_partial, &ctx->partial_cap, ivk::embedding_grad_partial_bytes(a.n_tokens, a.dim), 1);
+        if (rc != IV_OK) return rc;
+        const uint64_t before = ctx->arrivals_cap;
+        rc = grow(ctx, &ctx->d_arrivals, &ctx->arrivals_cap, ivk::embedding_grad_arrival_bytes(a.n_tokens, a.dim), 1);
+        if (rc != IV_OK) return rc;
+        if (ctx->arrivals_cap != before) IV_TRY(ctx, cudaMemsetAsync(ctx->d_arrivals, 0, ctx->arrivals_cap, stream));
+    }
+    IV_TRY(ctx, ivk::launch_embedding_grad(a, ctx->d_sort, ctx->d_arrivals, ctx->d_partial, ctx->d_status, stream, &ctx->launches));
+    return IV_OK;
+}
+
+// The set as the kernels take it, with room for its pieces.
+int tensor_set(iv_ctx *ctx, const void *d_base, const uint64_t *d_offsets, const uint64_t *d_lengths, const uint8_t *d_types,
+               int type, uint64_t n, ivk::TensorSet *set) {
+    if (n && (!d_base || !d_offsets || !d_lengths)) return IV_ERR_INVALID_ARG;
+    if (!aligned_to(d_offsets, 8) || !aligned_to(d_lengths, 8)) return IV_ERR_INVALID_ARG;
+    if (!d_types && !is_dtype(type)) return IV_ERR_INVALID_ARG;
+    if (n > kMaxTokens) return IV_ERR_TOO_LARGE;
+    *set = {static_cast<uint8_t *>(const_cast<void *>(d_base)), d_offsets, d_lengths, d_types, type, n};
+    return IV_OK;
+}
+
+int check_scaled_output(const void *d_out, const uint64_t *d_out_offsets, int out_type, const uint8_t *d_types, int type, uint64_t n) {
+    if (!d_out) return out_type < 0 || (!d_types && out_type == type) ? IV_OK : IV_ERR_INVALID_ARG;   // in place
+    if (n && (!d_out_offsets || !aligned_to(d_out_offsets, 8))) return IV_ERR_INVALID_ARG;
+    if (out_type >= 0 && !is_dtype(out_type)) return IV_ERR_INVALID_ARG;
+    if (out_type >= 0 && !d_types && !type_pair_ok(type, out_type)) return IV_ERR_INVALID_ARG;
+    return IV_OK;
+}
+
+}  // namespace
+
+int iv_embedding(iv_ctx *ctx, const void *d_table, int table_type, uint64_t n_rows, uint64_t dim, uint64_t row_stride,
+                 const void *d_tokens, int token_bytes, uint64_t n_tokens, float scale, void *d_out, int out_type,
+                 uint64_t out_stride, void *cuda_stream) {
+    if (!ctx || !type_pair_ok(table_type, out_type) || (token_bytes != 4 && token_bytes != 8)) return IV_ERR_INVALID_ARG;
+    if (n_tokens == 0 || dim == 0) return IV_OK;
+    if (n_tokens > kMaxTokens || dim > kMaxRows) return IV_ERR_TOO_LARGE;
+    if (!d_tokens || !d_out || (n_rows && !d_table)) return IV_ERR_INVALID_ARG;
+    if ((n_rows > 1 && row_stride < dim) || (n_tokens > 1 && out_stride < dim)) return IV_ERR_INVALID_ARG;
+    if (!aligned_to(d_table, dtype_bytes(table_type)) || !aligned_to(d_out, dtype_bytes(out_type)) ||
+        !aligned_to(d_tokens, token_bytes))
+        return IV_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    const ivk::EmbeddingArgs a = {d_table, table_type, n_rows, dim, row_stride, d_tokens, token_bytes, n_tokens, scale,
+                                  d_out, out_type, out_stride};
+    IV_TRY(ctx, ivk::launch_embedding(a, ctx->d_status, static_cast<cudaStream_t>(cuda_stream), &ctx->launches));
+    return IV_OK;
+}
+
+int iv_embedding_grad(iv_ctx *ctx, const void *d_grad_out, int grad_type, uint64_t grad_stride, uint64_t dim,
+                      const void *d_tokens, int token_bytes, uint64_t n_tokens, uint64_t n_rows, int64_t padding_row,
+                      float scale, int accumulate, void *d_grad, int out_type, uint64_t out_stride, void *cuda_stream) {
+    if (!ctx) return IV_ERR_INVALID_ARG;
+    const ivk::EmbeddingGradArgs a = {d_grad_out, grad_type, grad_stride, dim, d_tokens, token_bytes, n_tokens, n_rows,
+                                      padding_row, scale, accumulate != 0, d_grad, out_type, out_stride, nullptr, 0, nullptr};
+    return embedding_grad(ctx, a, cuda_stream);
+}
+
+int iv_embedding_grad_rows(iv_ctx *ctx, const void *d_grad_out, int grad_type, uint64_t grad_stride, uint64_t dim,
+                           const void *d_tokens, int token_bytes, uint64_t n_tokens, uint64_t n_rows,
+                           int64_t padding_row, float scale, int64_t *d_rows, void *d_grad, int out_type,
+                           uint64_t out_stride, uint64_t cap, uint64_t *d_count, void *cuda_stream) {
+    if (!ctx || !d_rows || !d_count) return IV_ERR_INVALID_ARG;
+    if (!aligned_to(d_rows, 8) || !aligned_to(d_count, 8)) return IV_ERR_INVALID_ARG;
+    if (cap < (n_tokens < n_rows ? n_tokens : n_rows)) return IV_ERR_INVALID_ARG;
+    const ivk::EmbeddingGradArgs a = {d_grad_out, grad_type, grad_stride, dim, d_tokens, token_bytes, n_tokens, n_rows,
+                                      padding_row, scale, false, d_grad, out_type, out_stride, d_rows, cap, d_count};
+    return embedding_grad(ctx, a, cuda_stream);
+}
+
+int iv_grad_norm(iv_ctx *ctx, const void *d_base, const uint64_t *d_offsets, const uint64_t *d_lengths,
+                 const uint8_t *d_types, int type, uint64_t n, float *d_norms, iv_norm_result *d_result,
+                 void *cuda_stream) {
+    if (!ctx || !d_result || !aligned_to(d_result, 8) || !aligned_to(d_norms, 4)) return IV_ERR_INVALID_ARG;
+    ivk::TensorSet set;
+    int rc = tensor_set(ctx, d_base, d_offsets, d_lengths, d_types, type, n, &set);
+    if (rc != IV_OK) return rc;
+    DeviceGuard guard(ctx->device);
+    if ((rc = grow(ctx, &ctx->d_plan, &ctx->plan_cap, ivk::grad_norm_scratch_bytes(n), 1)) != IV_OK) return rc;
+    IV_TRY(ctx, ivk::launch_grad_norm(set, false, 0.f, d_norms, d_result, ctx->d_plan, ctx->d_status, ctx->sm_count,
+                                      static_cast<cudaStream_t>(cuda_stream), &ctx->launches));
+    return IV_OK;
+}
+
+int iv_grad_clip(iv_ctx *ctx, void *d_base, const uint64_t *d_offsets, const uint64_t *d_lengths, const uint8_t *d_types,
+                 int type, uint64_t n, float max_norm, void *d_out, const uint64_t *d_out_offsets, int out_type,
+                 float *d_norms, iv_norm_result *d_result, void *cuda_stream) {
+    if (!ctx || !d_result || !aligned_to(d_result, 8) || !aligned_to(d_norms, 4)) return IV_ERR_INVALID_ARG;
+    if (!(max_norm >= 0.f)) return IV_ERR_INVALID_ARG;
+    ivk::TensorSet set;
+    int rc = tensor_set(ctx, d_base, d_offsets, d_lengths, d_types, type, n, &set);
+    if (rc == IV_OK) rc = check_scaled_output(d_out, d_out_offsets, out_type, d_types, type, n);
+    if (rc != IV_OK) return rc;
+    DeviceGuard guard(ctx->device);
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if ((rc = grow(ctx, &ctx->d_plan, &ctx->plan_cap, ivk::grad_norm_scratch_bytes(n), 1)) != IV_OK) return rc;
+    IV_TRY(ctx, ivk::launch_grad_norm(set, true, max_norm, d_norms, d_result, ctx->d_plan, ctx->d_status, ctx->sm_count,
+                                      stream, &ctx->launches));
+    IV_TRY(ctx, ivk::launch_grad_scale(set, false, &d_result->scale, d_out ? static_cast<uint8_t *>(d_out) : set.d_base,
+                                       d_out ? d_out_offsets : d_offsets, out_type, ctx->d_plan, ctx->d_status, ctx->sm_count,
+                                       stream, &ctx->launches));
+    return IV_OK;
+}
+
+int iv_grad_scale(iv_ctx *ctx, void *d_base, const uint64_t *d_offsets, const uint64_t *d_lengths, const uint8_t *d_types,
+                  int type, uint64_t n, const float *d_scale, void *d_out, const uint64_t *d_out_offsets, int out_type,
+                  void *cuda_stream) {
+    if (!ctx || !d_scale || !aligned_to(d_scale, 4)) return IV_ERR_INVALID_ARG;
+    ivk::TensorSet set;
+    int rc = tensor_set(ctx, d_base, d_offsets, d_lengths, d_types, type, n, &set);
+    if (rc == IV_OK) rc = check_scaled_output(d_out, d_out_offsets, out_type, d_types, type, n);
+    if (rc != IV_OK) return rc;
+    DeviceGuard guard(ctx->device);
+    if ((rc = grow(ctx, &ctx->d_plan, &ctx->plan_cap, ivk::grad_norm_scratch_bytes(n), 1)) != IV_OK) return rc;
+    IV_TRY(ctx, ivk::launch_grad_scale(set, true, d_scale, d_out ? static_cast<uint8_t *>(d_out) : set.d_base,
+                                       d_out ? d_out_offsets : d_offsets, out_type, ctx->d_plan, ctx->d_status, ctx->sm_count,
+                                       static_cast<cudaStream_t>(cuda_stream), &ctx->launches));
     return IV_OK;
 }
 

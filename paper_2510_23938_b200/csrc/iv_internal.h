@@ -191,6 +191,74 @@ cudaError_t launch_hash_chunks_rfc6962(const uint8_t *d_data, uint64_t nbytes, u
 cudaError_t launch_merkle_root_rfc6962(const uint8_t *d_leaves, uint64_t n, uint8_t *d_root, uint8_t *d_scratch_a,
                                        uint8_t *d_scratch_b, cudaStream_t stream, uint64_t *launches);
 
+// embedding.cu ---------------------------------------------------------------
+// Arguments as in iv.h (checked there); strides in elements.
+struct EmbeddingArgs {
+    const void *d_table;
+    int table_type;
+    uint64_t n_rows, dim, row_stride;
+    const void *d_tokens;
+    int token_bytes;
+    uint64_t n_tokens;
+    float scale;
+    void *d_out;
+    int out_type;
+    uint64_t out_stride;
+};
+cudaError_t launch_embedding(const EmbeddingArgs &a, uint32_t *d_status, cudaStream_t stream, uint64_t *launches);
+
+// embedding_grad.cu ----------------------------------------------------------
+// d_rows != NULL asks for the compact form (cap rows, d_count), NULL for the whole table.
+struct EmbeddingGradArgs {
+    const void *d_grad_out;
+    int grad_type;
+    uint64_t grad_stride, dim;
+    const void *d_tokens;
+    int token_bytes;
+    uint64_t n_tokens, n_rows;
+    int64_t padding_row;
+    float scale;
+    bool accumulate;
+    void *d_grad;
+    int out_type;
+    uint64_t out_stride;
+    int64_t *d_rows;
+    uint64_t cap;
+    uint64_t *d_count;
+};
+constexpr uint32_t kPiece = 64;      // terms that are added up without a break
+constexpr uint32_t kGroup = 32;      // pieces whose sums are added up without a break
+struct SortBuffers {
+    uint32_t *key[2], *index[2];     // ping-pong of the radix sort
+    uint32_t *rank, *start, *totals; // distinct row of each sorted position, its first position, {sorted tokens that count, distinct rows}
+    uint32_t *arrivals;              // zero between calls
+    float *partial;
+};
+uint64_t embedding_grad_sort_bytes(uint64_t n);
+uint64_t embedding_grad_arrival_bytes(uint64_t n, uint64_t dim);
+uint64_t embedding_grad_partial_bytes(uint64_t n, uint64_t dim);
+cudaError_t launch_embedding_grad(const EmbeddingGradArgs &a, void *d_sort, uint32_t *d_arrivals, float *d_partial,
+                                  uint32_t *d_status, cudaStream_t stream, uint64_t *launches);
+
+// grad_norm.cu ---------------------------------------------------------------
+// A set of n tensors: tensor k is the d_lengths[k] bytes at d_base + d_offsets[k], of type d_types[k] (or `type`).
+struct TensorSet {
+    uint8_t *d_base;
+    const uint64_t *d_offsets, *d_lengths;
+    const uint8_t *d_types;          // NULL: all of `type`
+    int type;
+    uint64_t n;
+};
+uint64_t grad_norm_scratch_bytes(uint64_t n);
+// Norms, result record (scale 1, or what clipping to max_norm asks for when `clip`).
+cudaError_t launch_grad_norm(const TensorSet &set, bool clip, float max_norm, float *d_norms, iv_norm_result *d_result,
+                             void *d_scratch, uint32_t *d_status, int sm_count, cudaStream_t stream, uint64_t *launches);
+// out tensor k = round(tensor k * *d_scale) at d_out + d_out_offsets[k], of type out_type (< 0: tensor k's own).
+// with_plan: lays out the pieces first (launch_grad_norm has done so for the same set otherwise).
+cudaError_t launch_grad_scale(const TensorSet &set, bool with_plan, const float *d_scale, uint8_t *d_out,
+                              const uint64_t *d_out_offsets, int out_type, void *d_scratch, uint32_t *d_status, int sm_count,
+                              cudaStream_t stream, uint64_t *launches);
+
 // selftest.cu --------------------------------------------------------------
 // One warp waits (bounded by limit_cycles SM clocks) on a barrier nobody arrives at, then sets *d_status to
 // IVK_DEV_TIMEOUT and returns; *d_waited (may be NULL) receives the clocks it waited.
