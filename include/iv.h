@@ -467,15 +467,15 @@ int iv_embedding(iv_ctx *ctx, const void *d_table, int table_type, uint64_t n_ro
 
 /* Its gradient: grad[r, :] = round(old + scale * sum of grad_out[t, :] over the tokens t of row r), old = grad[r, :]
  * when accumulate != 0 (rows without a token are then left alone) and 0 otherwise (they are set to zero).
- * The sum of a row runs over its tokens in ascending order of t: 64 terms make
+ * The sum of a row runs over its tokens in ascending order of t: 32 terms make
  * a piece, 32 pieces a group; terms, pieces and groups are added first to last
  * in 32 bits, then scaled.
  *   d_grad_out    n_tokens rows of dim elements, grad_stride apart
  *   padding_row   tokens equal to it give no gradient; -1 for none
  *   d_grad        n_rows rows of dim elements, out_stride apart
  * Tokens outside [0, n_rows) give no gradient and set the device status to 2.
- * IV_ERR_TOO_LARGE for n_tokens > 2^30, n_rows or dim > 2^31 or n_tokens * dim
- * > 2^45 or so (also the other calls of this section). */
+ * IV_ERR_TOO_LARGE for n_tokens or cap > 2^30, n_rows > 2^31 or dim > 2^24 (also
+ * the other calls of this section). */
 int iv_embedding_grad(iv_ctx *ctx, const void *d_grad_out, int grad_type, uint64_t grad_stride, uint64_t dim,
                       const void *d_tokens, int token_bytes, uint64_t n_tokens, uint64_t n_rows, int64_t padding_row,
                       float scale, int accumulate, void *d_grad, int out_type, uint64_t out_stride, void *cuda_stream);

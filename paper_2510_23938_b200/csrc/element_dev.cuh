@@ -21,6 +21,27 @@ template <> __device__ __forceinline__ float from_float<float>(float v) { return
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+// Two 16-bit values in a word.
+template <typename T> __device__ __forceinline__ void unpack2(uint32_t w, float &lo, float &hi);
+template <> __device__ __forceinline__ void unpack2<__nv_bfloat16>(uint32_t w, float &lo, float &hi) {
+    lo = __uint_as_float(w << 16);                    // bf16 is the upper half of a 32-bit float
+    hi = __uint_as_float(w & 0xffff0000u);
+}
+template <> __device__ __forceinline__ void unpack2<__half>(uint32_t w, float &lo, float &hi) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+    lo = f.x;
+    hi = f.y;
+}
+template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
+    const __nv_bfloat162 x = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&x);
+}
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) {
+    const __half2 x = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&x);
+}
+
 // V elements of type T as 32-bit words.
 template <typename T, int V>
 struct Packed {
@@ -37,13 +58,7 @@ struct Packed {
             for (int i = 0; i < V; ++i) v[i] = __uint_as_float(w[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < V / 2; ++i) {
-                T lo, hi;
-                *reinterpret_cast<uint16_t *>(&lo) = (uint16_t)(w[i] & 0xffffu);
-                *reinterpret_cast<uint16_t *>(&hi) = (uint16_t)(w[i] >> 16);
-                v[2 * i] = to_float(lo);
-                v[2 * i + 1] = to_float(hi);
-            }
+            for (int i = 0; i < V / 2; ++i) unpack2<T>(w[i], v[2 * i], v[2 * i + 1]);
         }
     }
     __device__ __forceinline__ void pack(const float (&v)[V]) {
@@ -52,11 +67,7 @@ struct Packed {
             for (int i = 0; i < V; ++i) w[i] = __float_as_uint(v[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < V / 2; ++i) {
-                const T lo = from_float<T>(v[2 * i]), hi = from_float<T>(v[2 * i + 1]);
-                w[i] = (uint32_t)*reinterpret_cast<const uint16_t *>(&lo) |
-                       ((uint32_t)*reinterpret_cast<const uint16_t *>(&hi) << 16);
-            }
+            for (int i = 0; i < V / 2; ++i) w[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
         }
     }
 };

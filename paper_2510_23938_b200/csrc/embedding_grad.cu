@@ -6,11 +6,11 @@
 //
 //   1. sort_tokens_kernel      stable radix sort of (token, t) by one cluster, then the list of distinct rows
 //   2. sum_rows_kernel         one warp per (8 sorted positions, tile of columns): adds up the pieces that begin there
-//   3. fill_tail_kernel        compact form: what lies behind the last distinct row
 #include <cooperative_groups.h>
 
 #include "element_dev.cuh"
 #include "iv_internal.h"
+#include "tma_dev.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -22,24 +22,31 @@ namespace {
 
 constexpr uint32_t kSortThreads = 1024;
 constexpr uint32_t kSortWarps = kSortThreads / 32;
-constexpr uint32_t kItems = 8;                             // keys per thread and tile
-constexpr uint32_t kTileKeys = kSortThreads * kItems;
+constexpr uint32_t kMaxItems = 8;                          // keys per thread and tile
 constexpr uint32_t kDigitBits = 9;                         // two passes for tables of up to 262,143 rows
 constexpr uint32_t kBins = 1u << kDigitBits;
-constexpr uint32_t kMaxCluster = 8;
+constexpr uint32_t kMaxCluster = 16;
 
 struct SortShared {
-    uint16_t warp_bins[kSortWarps][kBins];   // keys of each digit in a warp's part of the tile, then their prefix over the warps
-    uint32_t count[kBins];                   // keys of each digit in this CTA's range (read by the whole cluster)
-    uint32_t tile_count[kBins];              // keys of each digit in the current tile
-    uint32_t base[kBins];                    // where this CTA's next key of each digit goes
+    union {
+        uint32_t peers[kSortWarps][kBins];                 // ranking: lanes of the warp that hold each digit
+        uint2 sorted[kSortThreads * kMaxItems];            // afterwards: the tile's keys and indices by digit
+    };
+    uint2 incoming[kSortThreads * kMaxItems];              // one tile per CTA: the keys at this CTA's positions after the pass
+    uint16_t warp_bins[kSortWarps][kBins];                 // keys of each digit in a warp's part of the tile, then their prefix over half of the warps
+    uint32_t from[kMaxCluster][kBins];                     // keys of each digit in every CTA's share
+    uint4 rows_from[kMaxCluster];                          // of every CTA's share: rows that begin, valid keys, 1 + the last place a row begins
+    uint32_t half_count[kBins];                            // keys of each digit in the first half of the warps
+    uint32_t count[kBins];                                 // keys of each digit in this CTA's share
+    uint32_t tile_first[kBins];                            // place of the first key of each digit in the current tile, sorted
+    uint32_t base[kBins];                                  // where this CTA's next key of each digit goes
     uint32_t scan[kSortWarps];
-    uint32_t heads;                          // distinct rows that begin in this CTA's range (read by the whole cluster)
-    uint32_t valid;                          // keys below n_rows in this CTA's range (read by the whole cluster)
+    uint32_t warp_heads[kSortWarps], warp_last[kSortWarps];
+    uint32_t heads, valid, last_head;                      // of this CTA's share
 };
 
-// Exclusive prefix sum over the CTA; every thread also gets the total.
-__device__ __forceinline__ uint32_t block_exclusive(uint32_t v, uint32_t *scan, uint32_t &total) {
+// Exclusive prefix sum over the CTA.
+__device__ __forceinline__ uint32_t block_exclusive(uint32_t v, uint32_t *scan) {
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     uint32_t x = v;
 #pragma unroll
@@ -49,33 +56,64 @@ __device__ __forceinline__ uint32_t block_exclusive(uint32_t v, uint32_t *scan, 
     }
     if (lane == 31u) scan[warp] = x;
     __syncthreads();
-    uint32_t w = scan[lane];
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const uint32_t y = __shfl_up_sync(0xffffffffu, w, d);
-        if (lane >= (uint32_t)d) w += y;
-    }
-    total = __shfl_sync(0xffffffffu, w, 31);
-    const uint32_t before = warp ? __shfl_sync(0xffffffffu, w, (warp - 1u) & 31u) : 0u;
+    const uint32_t before = __reduce_add_sync(0xffffffffu, lane < warp ? scan[lane] : 0u);
     __syncthreads();
     return before + x - v;
 }
 
-template <typename Token>
-__device__ __forceinline__ uint32_t key_of(const Token *tokens, uint32_t i, uint64_t n_rows, int64_t padding_row, uint32_t *status) {
-    const int64_t t = (int64_t)tokens[i];
-    if (t == padding_row) return (uint32_t)n_rows;             // sorts behind every row and is left out
-    if ((uint64_t)t >= n_rows) {
-        atomicMax(status, (uint32_t)IVK_DEV_BOUNDS);
-        return (uint32_t)n_rows;
-    }
-    return (uint32_t)t;
-}
+// The rows of a fresh table gradient that no token names are set to zero beside the sort: each CTA takes a range of
+// rows, marks those with a token (it reads all tokens) and writes the others.
+constexpr uint32_t kFillThreads = 1024;
+constexpr uint32_t kFillRows = 1u << 18;                   // rows marked at a time: 32 KiB of bits
 
 template <typename Token>
+__global__ void __launch_bounds__(kFillThreads)
+fill_rows_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t padding_row, uint8_t *out, uint64_t row_bytes,
+                 uint64_t stride_bytes) {
+    __shared__ uint32_t marks[kFillRows / 32];
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const uint64_t begin = n_rows * blockIdx.x / gridDim.x, end = n_rows * (blockIdx.x + 1u) / gridDim.x;
+    for (uint64_t r0 = begin; r0 < end; r0 += kFillRows) {
+        const uint32_t rows = (uint32_t)(end - r0 < kFillRows ? end - r0 : kFillRows);
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < (rows + 31u) / 32u; i += kFillThreads) marks[i] = 0u;
+        __syncthreads();
+        constexpr uint32_t kAhead = 8;
+        for (uint32_t i0 = threadIdx.x; i0 < n; i0 += kFillThreads * kAhead) {
+            int64_t t[kAhead];
+#pragma unroll
+            for (uint32_t u = 0; u < kAhead; ++u) t[u] = i0 + u * kFillThreads < n ? (int64_t)tokens[i0 + u * kFillThreads] : -1;
+#pragma unroll
+            for (uint32_t u = 0; u < kAhead; ++u) {
+                const uint64_t at = (uint64_t)t[u] - r0;
+                if (at < rows && t[u] != padding_row) atomicOr(&marks[at >> 5], 1u << (at & 31u));
+            }
+        }
+        __syncthreads();
+        for (uint32_t r = warp; r < rows; r += kFillThreads / 32) {
+            if (marks[r >> 5] >> (r & 31u) & 1u) continue;
+            uint8_t *p = out + (r0 + r) * stride_bytes;
+            const uint64_t head = (16u - (reinterpret_cast<uintptr_t>(p) & 15u)) & 15u;
+            const uint64_t start = head < row_bytes ? head : row_bytes, body = (row_bytes - start) & ~15ull;
+            if (lane < start / 2u) reinterpret_cast<uint16_t *>(p)[lane] = 0;
+            uint4 *q = reinterpret_cast<uint4 *>(p + start);
+#pragma unroll 4
+            for (uint64_t i = lane; i < body / 16u; i += 32u) q[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (lane < (row_bytes - start - body) / 2u) reinterpret_cast<uint16_t *>(p + start + body)[lane] = 0;
+        }
+    }
+}
+
+// One cluster sorts all tokens; CTA r owns the r-th share of the positions, cut into tiles of kSortThreads * ITEMS keys
+// of which each warp owns a consecutive part.  Per pass: digits counted over the share, written into the shared memory
+// of every CTA of the cluster, then every key's place = keys of smaller digits + same digit in earlier CTAs, tiles,
+// warps and lanes.  With one tile per CTA the keys stay in shared memory, each written into that of the CTA whose
+// position it takes; with more they go through global memory.
+template <typename Token, uint32_t ITEMS>
 __global__ void __launch_bounds__(kSortThreads, 1)
 sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t padding_row, uint32_t passes, SortBuffers b,
                    int64_t *rows_out, uint64_t *count_out, uint32_t *status) {
+    constexpr uint32_t kTileKeys = kSortThreads * ITEMS;
     extern __shared__ __align__(16) unsigned char raw_smem[];
     SortShared &s = *reinterpret_cast<SortShared *>(raw_smem);
     cg::cluster_group cluster = cg::this_cluster();
@@ -84,127 +122,278 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
     const uint32_t share = ((n + ranks - 1) / ranks + 31u) & ~31u;
     const uint32_t lo = me * share < n ? me * share : n;
     const uint32_t hi = lo + share < n ? lo + share : n;
+    const bool one_tile = share <= kTileKeys;
+    const uint32_t mine = warp * (ITEMS * 32u) + lane;               // this lane's first key in a tile; the next are 32 apart
+    bool bad = false;
+    auto all_sync = [&]() {
+        if (ranks > 1) cluster.sync();
+        else __syncthreads();
+    };
+    // padding and rows that are not there sort behind every row and are left out
+    auto to_key = [&](Token token) {
+        const int64_t t = (int64_t)token;
+        const bool there = (uint64_t)t < n_rows;
+        bad |= !there && t != padding_row;
+        return there && t != padding_row ? (uint32_t)t : (uint32_t)n_rows;
+    };
 
     for (uint32_t pass = 0; pass < passes; ++pass) {
         const uint32_t shift = pass * kDigitBits;
         const uint32_t *in_key = b.key[(pass + 1) & 1], *in_idx = b.index[(pass + 1) & 1];
         uint32_t *out_key = b.key[pass & 1], *out_idx = b.index[pass & 1];
-        // digits of the whole range
-        for (uint32_t i = threadIdx.x; i < kBins; i += kSortThreads) s.count[i] = 0;
-        __syncthreads();
-        for (uint32_t i = lo + threadIdx.x; i < hi; i += kSortThreads) {
-            const uint32_t key = pass == 0 ? key_of(tokens, i, n_rows, padding_row, status) : in_key[i];
-            atomicAdd(&s.count[(key >> shift) & (kBins - 1)], 1u);
+        uint32_t key[ITEMS], idx[ITEMS], rank[ITEMS];
+
+        auto load_tile = [&](uint32_t t0) {
+            if (pass == 0) {
+                Token token[ITEMS];
+#pragma unroll
+                for (uint32_t j = 0; j < ITEMS; ++j) {
+                    const uint32_t i = t0 + mine + j * 32u;
+                    token[j] = i < hi ? tokens[i] : Token(0);
+                    idx[j] = i;
+                }
+#pragma unroll
+                for (uint32_t j = 0; j < ITEMS; ++j) key[j] = idx[j] < hi ? to_key(token[j]) : 0u;
+            } else if (one_tile) {
+#pragma unroll
+                for (uint32_t j = 0; j < ITEMS; ++j) {
+                    const uint2 k = t0 + mine + j * 32u < hi ? s.incoming[mine + j * 32u] : make_uint2(0u, 0u);
+                    key[j] = k.x;
+                    idx[j] = k.y;
+                }
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < ITEMS; ++j) {
+                    const uint32_t i = t0 + mine + j * 32u;
+                    key[j] = i < hi ? in_key[i] : 0u;
+                    idx[j] = i < hi ? in_idx[i] : 0u;
+                }
+            }
+        };
+        // The tile sorted by this pass's digit into s.sorted; returns the tile's keys of digit threadIdx.x.
+        auto sort_tile = [&](uint32_t t0) {
+            const uint32_t keys = hi - t0 < kTileKeys ? hi - t0 : kTileKeys;
+            const uint32_t warps = (keys + ITEMS * 32u - 1) / (ITEMS * 32u);          // that have keys
+            for (uint32_t i = threadIdx.x; i < warps * (kBins / 8); i += kSortThreads)
+                reinterpret_cast<uint4 *>(&s.warp_bins[0][0])[i] = make_uint4(0u, 0u, 0u, 0u);
+            for (uint32_t i = threadIdx.x; i < warps * (kBins / 4); i += kSortThreads)
+                reinterpret_cast<uint4 *>(&s.peers[0][0])[i] = make_uint4(0u, 0u, 0u, 0u);
+            __syncthreads();
+#pragma unroll
+            for (uint32_t j = 0; j < ITEMS; ++j) {
+                rank[j] = 0;
+                if (warp * (ITEMS * 32u) + j * 32u < keys) {                           // the same for the whole warp
+                    const bool live = mine + j * 32u < keys;
+                    const uint32_t digit = (key[j] >> shift) & (kBins - 1);
+                    uint32_t *mask = &s.peers[warp][digit];
+                    if (live) atomicOr(mask, 1u << lane);
+                    __syncwarp();
+                    const uint32_t peers = live ? *mask : 0u, old = s.warp_bins[warp][digit];
+                    const uint32_t below = __popc(peers & ((1u << lane) - 1u));
+                    rank[j] = old + below;
+                    __syncwarp();
+                    if (live && below == 0) {
+                        s.warp_bins[warp][digit] = (uint16_t)(old + __popc(peers));
+                        *mask = 0u;
+                    }
+                    __syncwarp();
+                }
+            }
+            __syncthreads();
+            // prefix over the warps, two digits (16 bits each) and half of the warps per thread
+            constexpr uint32_t kHalf = kSortWarps / 2;
+            if (threadIdx.x < kBins) {
+                const uint32_t pair = threadIdx.x % (kBins / 2), half = threadIdx.x / (kBins / 2);
+                const uint32_t from = half * kHalf, to = warps < from + kHalf ? warps : from + kHalf;
+                uint32_t run = 0;
+#pragma unroll 8
+                for (uint32_t w = from; w < to; ++w) {
+                    uint32_t *p = reinterpret_cast<uint32_t *>(&s.warp_bins[w][0]) + pair;
+                    const uint32_t c = *p;
+                    *p = run;
+                    run += c;
+                }
+                uint32_t *total = half == 0 ? s.half_count : s.tile_first;             // tile_first: of the second half for now
+                total[2 * pair] = run & 0xffffu;
+                total[2 * pair + 1] = run >> 16;
+            }
+            __syncthreads();
+            const uint32_t total = threadIdx.x < kBins ? s.half_count[threadIdx.x] + s.tile_first[threadIdx.x] : 0u;
+            const uint32_t first = block_exclusive(total, s.scan);
+            if (threadIdx.x < kBins) s.tile_first[threadIdx.x] = first;
+            __syncthreads();
+            // by digit in shared memory first: keys of one digit then leave for consecutive addresses
+#pragma unroll
+            for (uint32_t j = 0; j < ITEMS; ++j) {
+                if (mine + j * 32u < keys) {
+                    const uint32_t digit = (key[j] >> shift) & (kBins - 1);
+                    const uint32_t at = s.tile_first[digit] + (warp >= kHalf ? s.half_count[digit] : 0u) +
+                                        s.warp_bins[warp][digit] + rank[j];
+                    s.sorted[at] = make_uint2(key[j], idx[j]);
+                }
+            }
+            return total;
+        };
+
+        uint32_t digits = 0;                                   // of digit threadIdx.x: keys in the share
+        if (one_tile) {
+            load_tile(lo);
+            digits = sort_tile(lo);
+        } else {
+            for (uint32_t i = threadIdx.x; i < kBins; i += kSortThreads) s.count[i] = 0;
+            __syncthreads();
+            for (uint32_t t0 = lo; t0 < hi; t0 += kTileKeys) {
+                load_tile(t0);
+#pragma unroll
+                for (uint32_t j = 0; j < ITEMS; ++j)
+                    if (t0 + mine + j * 32u < hi) atomicAdd(&s.count[(key[j] >> shift) & (kBins - 1)], 1u);
+            }
+            __syncthreads();
+            if (threadIdx.x < kBins) digits = s.count[threadIdx.x];
         }
-        cluster.sync();
-        {
+        if (ranks > 1) {
+            if (threadIdx.x < kBins)
+                for (uint32_t r = 0; r < ranks; ++r) *cluster.map_shared_rank(&s.from[me][threadIdx.x], r) = digits;
+            cluster.sync();
             uint32_t all = 0, before = 0;
             if (threadIdx.x < kBins) {
                 for (uint32_t r = 0; r < ranks; ++r) {
-                    const uint32_t c = *cluster.map_shared_rank(&s.count[threadIdx.x], r);
+                    const uint32_t c = s.from[r][threadIdx.x];
                     all += c;
                     before += r < me ? c : 0u;
                 }
             }
-            uint32_t total;
-            const uint32_t start = block_exclusive(all, s.scan, total);
+            const uint32_t start = block_exclusive(all, s.scan);
             if (threadIdx.x < kBins) s.base[threadIdx.x] = start + before;
+        } else {
+            const uint32_t start = block_exclusive(digits, s.scan);
+            if (threadIdx.x < kBins) s.base[threadIdx.x] = start;
         }
         __syncthreads();
-        // stable ranks, tile by tile: a warp owns kItems * 32 consecutive keys
         for (uint32_t t0 = lo; t0 < hi; t0 += kTileKeys) {
-            uint32_t key[kItems], idx[kItems], rank[kItems];
-            for (uint32_t i = threadIdx.x; i < kSortWarps * kBins / 2; i += kSortThreads)
-                reinterpret_cast<uint32_t *>(&s.warp_bins[0][0])[i] = 0u;
-            __syncthreads();
+            uint32_t tile_count = 0;
+            if (!one_tile) {
+                load_tile(t0);
+                tile_count = sort_tile(t0);
+                __syncthreads();
+            }
+            const uint32_t keys = hi - t0 < kTileKeys ? hi - t0 : kTileKeys;
 #pragma unroll
-            for (uint32_t j = 0; j < kItems; ++j) {
-                const uint32_t i = t0 + warp * (kItems * 32u) + j * 32u + lane;
-                key[j] = 0xffffffffu;
-                idx[j] = i;
-                if (i < hi) {
-                    key[j] = pass == 0 ? key_of(tokens, i, n_rows, padding_row, status) : in_key[i];
-                    if (pass) idx[j] = in_idx[i];
+            for (uint32_t j = 0; j < ITEMS; ++j) {
+                const uint32_t at = j * kSortThreads + threadIdx.x;
+                if (at < keys) {
+                    const uint2 k = s.sorted[at];
+                    const uint32_t digit = (k.x >> shift) & (kBins - 1);
+                    const uint32_t pos = s.base[digit] + at - s.tile_first[digit];
+                    if (one_tile) {
+                        const uint32_t r = pos / share;
+                        *cluster.map_shared_rank(&s.incoming[pos - r * share], r) = k;
+                    } else {
+                        out_key[pos] = k.x;
+                        out_idx[pos] = k.y;
+                    }
                 }
             }
-#pragma unroll
-            for (uint32_t j = 0; j < kItems; ++j) {
-                const uint32_t i = t0 + warp * (kItems * 32u) + j * 32u + lane;
-                const bool live = i < hi;
-                const uint32_t digit = live ? (key[j] >> shift) & (kBins - 1) : kBins + lane;   // dead lanes match nobody
-                const uint32_t peers = __match_any_sync(0xffffffffu, digit);
-                uint32_t old = 0;
-                if (live) old = s.warp_bins[warp][digit];
-                __syncwarp();
-                const uint32_t below = __popc(peers & ((1u << lane) - 1u));
-                if (live && below == 0) s.warp_bins[warp][digit] = (uint16_t)(old + __popc(peers));
-                __syncwarp();
-                rank[j] = old + below;
+            if (!one_tile) {
+                __syncthreads();
+                if (threadIdx.x < kBins) s.base[threadIdx.x] += tile_count;
+                __syncthreads();
             }
-            __syncthreads();
-            if (threadIdx.x < kBins) {
-                uint32_t run = 0;
-                for (uint32_t w = 0; w < kSortWarps; ++w) {
-                    const uint32_t c = s.warp_bins[w][threadIdx.x];
-                    s.warp_bins[w][threadIdx.x] = (uint16_t)run;
-                    run += c;
-                }
-                s.tile_count[threadIdx.x] = run;
-            }
-            __syncthreads();
-#pragma unroll
-            for (uint32_t j = 0; j < kItems; ++j) {
-                const uint32_t i = t0 + warp * (kItems * 32u) + j * 32u + lane;
-                if (i < hi) {
-                    const uint32_t digit = (key[j] >> shift) & (kBins - 1);
-                    const uint32_t pos = s.base[digit] + s.warp_bins[warp][digit] + rank[j];
-                    out_key[pos] = key[j];
-                    out_idx[pos] = idx[j];
-                }
-            }
-            __syncthreads();
-            if (threadIdx.x < kBins) s.base[threadIdx.x] += s.tile_count[threadIdx.x];
-            __syncthreads();
         }
-        cluster.sync();                                        // orders this pass's stores before the next pass's loads
+        all_sync();                                            // orders this pass's stores before the next pass's loads
     }
+    if (bad) atomicMax(status, (uint32_t)IVK_DEV_BOUNDS);
 
-    // distinct rows: rank[i] = number of the row among the distinct ones, start[rank] = its first sorted position
-    const uint32_t *key = b.key[(passes + 1) & 1];
-    if (threadIdx.x == 0) s.heads = s.valid = 0;
-    __syncthreads();
-    for (uint32_t i = lo + threadIdx.x; i < hi; i += kSortThreads) {
-        const uint32_t k = key[i];
-        const bool valid = k < n_rows;
-        if (valid) atomicAdd(&s.valid, 1u);
-        if (valid && (i == 0 || key[i - 1] != k)) atomicAdd(&s.heads, 1u);
-    }
-    cluster.sync();
-    uint32_t before = 0, distinct = 0, valid = 0;
-    for (uint32_t r = 0; r < ranks; ++r) {
-        const uint32_t h = *cluster.map_shared_rank(&s.heads, r);
-        distinct += h;
-        before += r < me ? h : 0u;
-        valid += *cluster.map_shared_rank(&s.valid, r);
-    }
-    for (uint32_t t0 = lo; t0 < hi; t0 += kSortThreads) {
-        const uint32_t i = t0 + threadIdx.x;
-        bool head = false;
-        uint32_t k = 0;
-        if (i < hi) {
-            k = key[i];
-            head = k < n_rows && (i == 0 || key[i - 1] != k);
-        }
-        uint32_t total;
-        const uint32_t r = before + block_exclusive(head ? 1u : 0u, s.scan, total);
-        if (i < hi && k < n_rows) {
-            b.rank[i] = head ? r : r - 1u;
-            if (head) {
-                b.start[r] = i;
-                if (rows_out) rows_out[r] = (int64_t)k;
+    // distinct rows: each sorted position's record {token, first position of its row, number of its row among the
+    // distinct ones, row}, and start[number] = the first position
+    const uint32_t *key = b.key[(passes + 1) & 1], *index = b.index[(passes + 1) & 1];
+    uint32_t k[ITEMS], idx[ITEMS], heads[ITEMS];               // heads: where rows begin among the warp's 32 positions
+    uint32_t my_heads, my_last, my_valid;                      // of the warp: rows that begin, 1 + the last such place, valid keys
+    auto load_sorted = [&](uint32_t t0) {
+        uint32_t prev[ITEMS];
+#pragma unroll
+        for (uint32_t j = 0; j < ITEMS; ++j) {
+            const uint32_t i = t0 + mine + j * 32u;
+            k[j] = prev[j] = 0xffffffffu;
+            idx[j] = 0;
+            if (i < hi) {
+                if (one_tile) {
+                    const uint2 x = s.incoming[i - lo];
+                    k[j] = x.x;
+                    idx[j] = x.y;
+                    if (i > lo) prev[j] = s.incoming[i - lo - 1u].x;
+                    else if (i) prev[j] = cluster.map_shared_rank(&s.incoming[share - 1u], me - 1u)->x;
+                } else {
+                    k[j] = key[i];
+                    idx[j] = index[i];
+                    if (i) prev[j] = key[i - 1];
+                }
             }
         }
-        before += total;
+        my_heads = my_last = my_valid = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < ITEMS; ++j) {
+            heads[j] = __ballot_sync(0xffffffffu, k[j] < n_rows && prev[j] != k[j]);
+            my_valid += __popc(__ballot_sync(0xffffffffu, k[j] < n_rows));
+            my_heads += __popc(heads[j]);
+            if (heads[j]) my_last = t0 + warp * (ITEMS * 32u) + j * 32u + 32u - __clz(heads[j]);
+        }
+    };
+    if (threadIdx.x == 0) s.heads = s.valid = s.last_head = 0;
+    __syncthreads();
+    uint32_t sum_heads = 0, sum_valid = 0, max_last = 0;
+    for (uint32_t t0 = lo; t0 < hi; t0 += kTileKeys) {
+        load_sorted(t0);
+        sum_heads += my_heads;
+        sum_valid += my_valid;
+        max_last = max(max_last, my_last);
+    }
+    if (lane == 0 && sum_valid) {
+        atomicAdd(&s.heads, sum_heads);
+        atomicAdd(&s.valid, sum_valid);
+        atomicMax(&s.last_head, max_last);
+    }
+    __syncthreads();
+    uint32_t before = 0, distinct = s.heads, valid = s.valid, last = 0;
+    if (ranks > 1) {                                           // nothing is read from or written to another CTA after this
+        if (threadIdx.x < ranks)
+            *cluster.map_shared_rank(&s.rows_from[me], threadIdx.x) = make_uint4(s.heads, s.valid, s.last_head, 0u);
+        cluster.sync();
+        const uint4 x = lane < ranks ? s.rows_from[lane] : make_uint4(0u, 0u, 0u, 0u);
+        distinct = __reduce_add_sync(0xffffffffu, x.x);
+        valid = __reduce_add_sync(0xffffffffu, x.y);
+        before = __reduce_add_sync(0xffffffffu, lane < me ? x.x : 0u);
+        last = __reduce_max_sync(0xffffffffu, lane < me ? x.z : 0u);
+    }
+    for (uint32_t t0 = lo; t0 < hi; t0 += kTileKeys) {
+        if (!one_tile) load_sorted(t0);
+        if (lane == 0) {
+            s.warp_heads[warp] = my_heads;
+            s.warp_last[warp] = my_last;
+        }
+        __syncthreads();
+        const uint32_t h = s.warp_heads[lane], p = s.warp_last[lane];
+        uint32_t number = before + __reduce_add_sync(0xffffffffu, lane < warp ? h : 0u);
+        uint32_t start = max(last, __reduce_max_sync(0xffffffffu, lane < warp ? p : 0u));
+        before += __reduce_add_sync(0xffffffffu, h);
+        last = max(last, __reduce_max_sync(0xffffffffu, p));
+        __syncthreads();
+#pragma unroll
+        for (uint32_t j = 0; j < ITEMS; ++j) {
+            const uint32_t i0 = t0 + warp * (ITEMS * 32u) + j * 32u, i = i0 + lane;
+            const uint32_t upto = heads[j] & (0xffffffffu >> (31u - lane));            // rows that begin here or before
+            const uint32_t my_number = number + __popc(upto) - 1u;
+            const uint32_t my_start = upto ? i0 + 31u - __clz(upto) : start - 1u;
+            if (k[j] < n_rows) {
+                if (my_start == i) {
+                    b.start[my_number] = i;
+                    if (rows_out) rows_out[my_number] = (int64_t)k[j];
+                }
+                b.record[i] = make_uint4(idx[j], my_start, my_number, k[j]);
+            }
+            number += __popc(heads[j]);
+            if (heads[j]) start = i0 + 32u - __clz(heads[j]);
+        }
     }
     if (me == 0 && threadIdx.x == 0) {
         b.start[distinct] = valid;
@@ -212,55 +401,73 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
         b.totals[1] = distinct;
         if (count_out) *count_out = distinct;
     }
-    cluster.sync();                                            // nobody leaves while its shared memory is still read
 }
 
 // ------------------------------------------------------------------------------------------------- sums
 
 constexpr uint32_t kWindow = 8;        // sorted positions per warp
-constexpr uint32_t kSumWarps = 8;
-constexpr uint32_t kTileCols = 256;    // columns per warp: 8 per lane
+constexpr uint32_t kSumWarps = 4;
+constexpr uint32_t kParts = 2;         // a lane holds this many vectors of 16 bytes of a row, a warp 1 KiB
+constexpr uint32_t kStageRows = 4;     // rows per stage of the ring, two stages: eight rows in flight
 
-// 8 columns of one row for this lane, the ones behind the last column as zeros.
-template <typename T>
-__device__ __forceinline__ void load_cols(const T *p, uint32_t cols, float (&v)[8]) {
-    if (cols >= 8u) {
-        if constexpr (sizeof(T) == 4) {
-            elem::Packed<T, 4> a, b;
-            elem::load_any<T, 4>(p, a);
-            elem::load_any<T, 4>(p + 4, b);
-            float x[4], y[4];
-            a.unpack(x);
-            b.unpack(y);
+template <typename T> struct Tile {
+    static constexpr uint32_t V = 16 / sizeof(T);                 // columns of a vector
+    static constexpr uint32_t kCols = kParts * 32 * V;            // columns per warp: 512 (16-bit types) or 256
+};
+
+// V columns of type T, `have` of them: the rest reads as zero and is not written.
+template <typename T, uint32_t V>
+__device__ __forceinline__ void load_cols(const T *p, uint32_t have, float (&v)[V]) {
+    if (have == V) {
+        constexpr uint32_t W = 16 / sizeof(T) < V ? 16 / sizeof(T) : V;   // 16 bytes at a time, or all of fewer
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i] = x[i]; v[4 + i] = y[i]; }
-        } else {
-            elem::Packed<T, 8> a;
-            elem::load_any<T, 8>(p, a);
-            a.unpack(v);
+        for (uint32_t i = 0; i < V; i += W) {
+            elem::Packed<T, (int)W> x;
+            float y[W];
+            elem::load_any<T, (int)W>(p + i, x);
+            x.unpack(y);
+#pragma unroll
+            for (uint32_t j = 0; j < W; ++j) v[i + j] = y[j];
         }
     } else {
 #pragma unroll
-        for (uint32_t i = 0; i < 8u; ++i) v[i] = i < cols ? elem::to_float(p[i]) : 0.f;
+        for (uint32_t i = 0; i < V; ++i) v[i] = i < have ? elem::to_float(p[i]) : 0.f;
     }
 }
-template <typename T>
-__device__ __forceinline__ void store_cols(T *p, uint32_t cols, const float (&v)[8]) {
-    if (cols >= 8u && (reinterpret_cast<uintptr_t>(p) & 15u) == 0u) {
-        if constexpr (sizeof(T) == 4) {
-            reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-        } else {
-            elem::Packed<T, 8> a;
-            a.pack(v);
-            elem::store_aligned<4>(p, a.w);
+template <typename T, uint32_t V>
+__device__ __forceinline__ void store_cols(T *p, uint32_t have, const float (&v)[V]) {
+    constexpr uint32_t W = 16 / sizeof(T) < V ? 16 / sizeof(T) : V;
+    if (have == V && (reinterpret_cast<uintptr_t>(p) & (W * sizeof(T) - 1u)) == 0u) {
+#pragma unroll
+        for (uint32_t i = 0; i < V; i += W) {
+            elem::Packed<T, (int)W> x;
+            float y[W];
+#pragma unroll
+            for (uint32_t j = 0; j < W; ++j) y[j] = v[i + j];
+            x.pack(y);
+            elem::store_aligned<elem::Packed<T, (int)W>::kWords>(p + i, x.w);
         }
     } else {
 #pragma unroll
-        for (uint32_t i = 0; i < 8u; ++i)
-            if (i < cols) p[i] = elem::from_float<T>(v[i]);
+        for (uint32_t i = 0; i < V; ++i)
+            if (i < have) p[i] = elem::from_float<T>(v[i]);
     }
 }
+
+// Asynchronous copy of 16 bytes into shared memory, the last 16 - bytes of them zeros; both addresses 16-byte aligned.
+template <int SHARED_OFFSET, int GLOBAL_OFFSET>
+__device__ __forceinline__ void copy_async16(uint32_t shared, uint64_t global, uint32_t bytes) {
+    asm volatile("cp.async.cg.shared.global [%0+%3], [%1+%4], 16, %2;" ::"r"(shared), "l"(global), "r"(bytes), "n"(SHARED_OFFSET),
+                 "n"(GLOBAL_OFFSET) : "memory");
+}
+// (x0, x1) += (y0, y1), each rounded as a 32-bit addition of its own
+__device__ __forceinline__ void add2(float &x0, float &x1, float y0, float y1) {
+    asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %3};\n\tadd.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "+f"(x0), "+f"(x1) : "f"(y0), "f"(y1));
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 
 struct SumArgs {
     const void *grad_out;
@@ -268,65 +475,98 @@ struct SumArgs {
     void *out;
     uint64_t out_stride;
     float scale;
-    uint32_t n, tiles;
+    uint32_t tiles, tile_shift;
+    bool aligned;          // every row of grad_out starts at a multiple of 16 bytes
+    int64_t *rows;         // compact form: row numbers and how many rows there is room for
+    uint64_t cap;
 };
 
-// Adds partial sums slot(first), slot(first + 1), ... in order: pieces begin kPiece positions apart.
+// Where the partial sum of a piece lies: at most two pieces of rows with several pieces begin in kPiece consecutive
+// sorted positions, the last one of a row and the first one of the next.
 __device__ __forceinline__ uint32_t slot_of(uint32_t piece_begin, bool first_of_row) {
     return 2u * (piece_begin / kPiece) + (first_of_row ? 1u : 0u);
 }
 
 template <typename Tin, typename Tout, bool COMPACT, bool ADD>
-__global__ void __launch_bounds__(kSumWarps * 32)
-sum_rows_kernel(SumArgs a, SortBuffers b, uint32_t final_buffer) {
-    const uint32_t lane = threadIdx.x & 31u;
-    const uint64_t unit = (uint64_t)blockIdx.x * kSumWarps + (threadIdx.x >> 5);
-    const uint32_t tile = (uint32_t)(unit % a.tiles);
-    const uint64_t window64 = unit / a.tiles;
+__global__ void __launch_bounds__(kSumWarps * 32, 6)
+sum_rows_kernel(SumArgs a, SortBuffers b) {
+    constexpr uint32_t V = Tile<Tin>::V, kCols = Tile<Tin>::kCols;
+    __shared__ __align__(16) uint4 ring[kSumWarps][2][kStageRows][kParts][32];             // a lane reads back its own copies only
+    // a CTA's warps take consecutive tiles of one window, or, where a row has fewer tiles, several windows
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const uint32_t tile = (blockIdx.y << a.tile_shift) + (warp & ((1u << a.tile_shift) - 1u));
+    const uint64_t window = ((uint64_t)blockIdx.x * kSumWarps + warp) >> a.tile_shift;
+    if (tile >= a.tiles) return;
     const uint32_t valid = b.totals[0];
-    if (window64 * kWindow >= valid) return;
-    const uint32_t w0 = (uint32_t)window64 * kWindow, w1 = w0 + kWindow;
-    const uint32_t *key = b.key[final_buffer], *index = b.index[final_buffer];
-    const uint32_t col = tile * kTileCols + lane * 8u;
-    const uint32_t cols = col < a.dim ? (a.dim - col < 8u ? (uint32_t)(a.dim - col) : 8u) : 0u;
-    const Tin *g = static_cast<const Tin *>(a.grad_out) + col;
-    Tout *out = static_cast<Tout *>(a.out) + col;
-
-    float acc[8];
-    bool open = false;                                  // a piece of ours is being added up
-    uint32_t begin = 0, row_rank = 0, row_start = 0, row_end = 0;
-
-    auto write_row = [&](uint32_t rank, uint32_t row, const float (&sum)[8]) {
-        if (cols == 0u) return;
-        Tout *o = out + (uint64_t)(COMPACT ? rank : row) * a.out_stride;
-        float v[8];
-        if (ADD) {
-            load_cols<Tout>(o, cols, v);
+    // this lane's columns: V from col[q], have[q] of them there
+    uint32_t col[kParts], have[kParts];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = fmaf(a.scale, sum[i], v[i]);
-        } else {
+    for (uint32_t q = 0; q < kParts; ++q) {
+        col[q] = tile * kCols + (q * 32u + lane) * V;
+        have[q] = col[q] < a.dim ? (a.dim - col[q] < V ? (uint32_t)(a.dim - col[q]) : V) : 0u;
+    }
+    Tout *out = static_cast<Tout *>(a.out);
+
+    if (COMPACT) {                                      // what lies behind the last distinct row: number -1, gradient zero
+        const float zero[V] = {};
+        const uint64_t distinct = b.totals[1];
+        for (uint64_t r = window * kWindow > distinct ? window * kWindow : distinct; r < (window + 1) * kWindow && r < a.cap; ++r) {
+            if (tile == 0 && lane == 0) a.rows[r] = -1;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = a.scale * sum[i];
+            for (uint32_t q = 0; q < kParts; ++q)
+                if (have[q]) store_cols<Tout, V>(out + r * a.out_stride + col[q], have[q], zero);
         }
-        store_cols<Tout>(o, cols, v);
-    };
-    // partial sums are kept column-major per tile: slot, tile, 8 x 32 columns
-    auto partial = [&](uint32_t slot) { return b.partial + ((uint64_t)slot * a.tiles + tile) * kTileCols + lane * 8u; };
-    auto put_partial = [&](uint32_t slot, const float (&v)[8]) {
-        float4 *p = reinterpret_cast<float4 *>(partial(slot));
-        __stcg(p, make_float4(v[0], v[1], v[2], v[3]));
-        __stcg(p + 1, make_float4(v[4], v[5], v[6], v[7]));
-    };
-    auto add_partials = [&](uint32_t first, uint32_t count, uint32_t step, uint32_t start, float (&sum)[8]) {
+    }
+    if (window * kWindow >= valid) return;
+    const uint32_t w0 = (uint32_t)window * kWindow, w1 = valid - w0 < kWindow ? valid : w0 + kWindow;
+    const Tin *g = static_cast<const Tin *>(a.grad_out);
+
+    uint4 *mine = &ring[warp][0][0][0][lane];
+    float acc[kParts][V];
+    bool open = false;                                  // a piece of ours is being added up
+    uint32_t begin = 0, row_start = 0, row_number = 0, row = 0;
+
+    auto write_row = [&](const float (&sum)[kParts][V]) {
+        Tout *o = out + (uint64_t)(COMPACT ? row_number : row) * a.out_stride;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+        for (uint32_t q = 0; q < kParts; ++q) {
+            if (have[q] == 0u) continue;
+            float v[V];
+            if (ADD) {
+                load_cols<Tout, V>(o + col[q], have[q], v);
+#pragma unroll
+                for (uint32_t i = 0; i < V; ++i) v[i] = fmaf(a.scale, sum[q][i], v[i]);
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < V; ++i) v[i] = a.scale * sum[q][i];
+            }
+            store_cols<Tout, V>(o + col[q], have[q], v);
+        }
+    };
+    auto partial = [&](uint32_t slot, uint32_t q) {
+        return reinterpret_cast<float4 *>(b.partial + ((uint64_t)slot * a.tiles + tile) * kCols + (q * 32u + lane) * V);
+    };
+    auto put_partial = [&](uint32_t slot, const float (&v)[kParts][V]) {
+#pragma unroll
+        for (uint32_t q = 0; q < kParts; ++q)
+#pragma unroll
+            for (uint32_t i = 0; i < V; i += 4) __stcg(partial(slot, q) + i / 4, make_float4(v[q][i], v[q][i + 1], v[q][i + 2], v[q][i + 3]));
+    };
+    auto add_partials = [&](uint32_t first, uint32_t count, uint32_t step) {
+#pragma unroll
+        for (uint32_t q = 0; q < kParts; ++q)
+#pragma unroll
+            for (uint32_t i = 0; i < V; ++i) acc[q][i] = 0.f;
 #pragma unroll 4
         for (uint32_t j = 0; j < count; ++j) {
-            const uint32_t begin_j = first + j * step;
-            const float4 *p = reinterpret_cast<const float4 *>(partial(slot_of(begin_j, begin_j == start)));
-            const float4 x = __ldcg(p), y = __ldcg(p + 1);
-            sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
-            sum[4] += y.x; sum[5] += y.y; sum[6] += y.z; sum[7] += y.w;
+            const uint32_t at = first + j * step, slot = slot_of(at, at == row_start);
+#pragma unroll
+            for (uint32_t q = 0; q < kParts; ++q)
+#pragma unroll
+                for (uint32_t i = 0; i < V; i += 4) {
+                    const float4 x = __ldcg(partial(slot, q) + i / 4);
+                    acc[q][i] += x.x; acc[q][i + 1] += x.y; acc[q][i + 2] += x.z; acc[q][i + 3] += x.w;
+                }
         }
     };
     // true for the warp that arrives last of `members`; leaves the counter at zero for the next call
@@ -342,72 +582,108 @@ sum_rows_kernel(SumArgs a, SortBuffers b, uint32_t final_buffer) {
         __threadfence();
         return last != 0u;
     };
-    auto flush = [&]() {
-        const uint32_t row = key[row_start];
-        if (row_end - row_start <= kPiece) {
-            write_row(row_rank, row, acc);
-            return;
+    auto counter = [&](uint32_t slot, uint32_t level) { return b.arrivals + ((uint64_t)slot * a.tiles + tile) * 2u + level; };
+    // the open piece is complete; row_ends: and no further piece of its row follows
+    auto flush = [&](bool row_ends) {
+        if (begin != row_start || !row_ends) {
+            const uint32_t terms = b.start[row_number + 1] - row_start;
+            const uint32_t pieces = (terms + kPiece - 1) / kPiece, piece = (begin - row_start) / kPiece;
+            const uint32_t group = piece / kGroup, groups = (pieces + kGroup - 1) / kGroup;
+            const uint32_t first = row_start + group * (kGroup * kPiece);    // first position of the group
+            const uint32_t members = pieces - group * kGroup < kGroup ? pieces - group * kGroup : kGroup;
+            put_partial(slot_of(begin, begin == row_start), acc);
+            if (!arrive(counter(slot_of(first, first == row_start), 0u), members)) return;
+            add_partials(first, members, kPiece);
+            if (groups > 1) {
+                put_partial(slot_of(first, first == row_start), acc);
+                if (!arrive(counter(slot_of(row_start, true), 1u), groups)) return;
+                add_partials(row_start, groups, kGroup * kPiece);
+            }
         }
-        const uint32_t pieces = (row_end - row_start + kPiece - 1) / kPiece;
-        const uint32_t piece = (begin - row_start) / kPiece;
-        const uint32_t group = piece / kGroup, groups = (pieces + kGroup - 1) / kGroup;
-        const uint32_t first = row_start + group * kGroup * kPiece;      // first position of the group
-        const uint32_t members = pieces - group * kGroup < kGroup ? pieces - group * kGroup : kGroup;
-        put_partial(slot_of(begin, begin == row_start), acc);
-        if (!arrive(b.arrivals + ((uint64_t)slot_of(first, first == row_start) * a.tiles + tile) * 2u, members)) return;
-        float sum[8];
-        add_partials(first, members, kPiece, row_start, sum);
-        if (groups > 1) {
-            put_partial(slot_of(first, first == row_start), sum);
-            if (!arrive(b.arrivals + ((uint64_t)slot_of(row_start, true) * a.tiles + tile) * 2u + 1u, groups)) return;
-            add_partials(row_start, groups, kGroup * kPiece, row_start, sum);
-        }
-        write_row(row_rank, row, sum);
+        write_row(acc);
     };
 
     for (uint32_t i0 = w0;; i0 += 32u) {
-        // 32 sorted positions: token index and row of each, one per lane
+        // 32 sorted positions, one per lane; behind the last one everything begins anew
         const uint32_t i = i0 + lane;
-        const bool live = i < valid;
-        const uint32_t my_rank = live ? b.rank[i] : 0u;
-        const uint32_t my_index = live ? index[i] : 0u;
-        const uint32_t my_start = live ? b.start[my_rank] : 0u;
-        const uint32_t my_end = live ? b.start[my_rank + 1] : 0u;
-        const bool my_begin = live && (i - my_start) % kPiece == 0u;
-        for (uint32_t j = 0; j < 32u; ++j) {
-            const uint32_t at = i0 + j;
-            const bool piece_begin = __shfl_sync(0xffffffffu, my_begin ? 1u : 0u, j) != 0u;
-            if (at >= valid || piece_begin) {
-                if (open) flush();
-                open = false;
-                if (at >= valid || at >= w1) return;
-                open = true;
-                begin = at;
-                row_rank = __shfl_sync(0xffffffffu, my_rank, j);
-                row_start = __shfl_sync(0xffffffffu, my_start, j);
-                row_end = __shfl_sync(0xffffffffu, my_end, j);
-#pragma unroll
-                for (int c = 0; c < 8; ++c) acc[c] = 0.f;
-            }
-            if (!open) {
-                if (at + 1u >= w1) return;              // no piece begins in this window
-                continue;
-            }
-            const uint32_t t = __shfl_sync(0xffffffffu, my_index, j);
-            float v[8];
-            load_cols<Tin>(g + (uint64_t)t * a.grad_stride, cols, v);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) acc[c] += v[c];
+        uint4 rec = make_uint4(0u, i, 0u, 0u);
+        if (i < valid) rec = b.record[i];
+        const uint32_t begins = __ballot_sync(0xffffffffu, (i - rec.y) % kPiece == 0u);
+        const uint32_t row_begins = __ballot_sync(0xffffffffu, i == rec.y);
+        // ours: from the first piece that begins in the window to the first that begins behind it
+        uint32_t from = 0, to = 32u;
+        if (!open) {
+            from = begins ? __ffs(begins) - 1u : 32u;
+            if (i0 + from >= w1) return;
         }
-    }
-}
-
-// Rows behind the last distinct one: number -1, gradient zero.
-template <typename Tout>
-__global__ void fill_tail_kernel(Tout *out, uint64_t out_stride, uint64_t dim, uint64_t cap, int64_t *rows, const uint32_t *totals) {
-    for (uint64_t r = (uint64_t)totals[1] + blockIdx.x; r < cap; r += gridDim.x) {
-        if (threadIdx.x == 0) rows[r] = -1;
-        for (uint64_t c = threadIdx.x; c < dim; c += blockDim.x) out[r * out_stride + c] = elem::from_float<Tout>(0.f);
+        const uint32_t inside = w1 > i0 ? w1 - i0 : 0u;
+        const uint32_t behind = inside < 32u ? begins >> inside << inside : 0u;
+        if (behind) to = __ffs(behind) - 1u;
+        // rows j .. j + kStageRows - 1 of them into a stage of the ring
+        const uint64_t my_row = reinterpret_cast<uint64_t>(g) + (uint64_t)rec.x * a.grad_stride * sizeof(Tin);
+        auto fetch = [&](uint32_t j, uint32_t stage) {
+            uint4 *dst = mine + stage * (kStageRows * kParts * 32u);
+#pragma unroll
+            for (uint32_t u = 0; u < kStageRows; ++u) {
+                const uint64_t src = __shfl_sync(0xffffffffu, my_row, (j + u) & 31u) + col[0] * sizeof(Tin);
+                if (j + u < to) {
+                    if (a.aligned) {
+                        const uint32_t shared = tma::smem_u32(dst + u * kParts * 32u);
+                        if (have[0]) copy_async16<0, 0>(shared, src, have[0] * (uint32_t)sizeof(Tin));
+                        if (have[1]) copy_async16<512, 512>(shared, src, have[1] * (uint32_t)sizeof(Tin));
+                    } else {
+#pragma unroll
+                        for (uint32_t q = 0; q < kParts; ++q) {
+                            float v[V] = {};
+                            if (have[q]) load_cols<Tin, V>(reinterpret_cast<const Tin *>(src) + q * 32u * V, have[q], v);
+                            elem::Packed<Tin, (int)V> x;
+                            x.pack(v);
+                            dst[(u * kParts + q) * 32u] = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+                        }
+                    }
+                }
+            }
+            copy_commit();
+        };
+        uint32_t stage = 0;
+        fetch(from, 0u);
+        for (uint32_t j0 = from; j0 < to; j0 += kStageRows) {
+            fetch(j0 + kStageRows, stage ^ 1u);
+            copy_wait<1>();
+            const uint4 *src = mine + stage * (kStageRows * kParts * 32u);
+            const uint32_t end = to < j0 + kStageRows ? to : j0 + kStageRows;
+#pragma unroll 1
+            for (uint32_t j = j0; j < end; ++j, src += kParts * 32u) {
+                if (begins >> j & 1u) {
+                    if (open) flush(row_begins >> j & 1u);
+                    open = true;
+                    begin = i0 + j;
+                    row_start = __shfl_sync(0xffffffffu, rec.y, j);
+                    row_number = __shfl_sync(0xffffffffu, rec.z, j);
+                    row = __shfl_sync(0xffffffffu, rec.w, j);
+#pragma unroll
+                    for (uint32_t q = 0; q < kParts; ++q)
+#pragma unroll
+                        for (uint32_t c = 0; c < V; ++c) acc[q][c] = 0.f;
+                }
+#pragma unroll
+                for (uint32_t q = 0; q < kParts; ++q) {
+                    const uint4 x = src[q * 32u];
+                    elem::Packed<Tin, (int)V> c;
+                    c.w[0] = x.x; c.w[1] = x.y; c.w[2] = x.z; c.w[3] = x.w;
+                    float v[V];
+                    c.unpack(v);
+#pragma unroll
+                    for (uint32_t k = 0; k < V; k += 2) add2(acc[q][k], acc[q][k + 1], v[k], v[k + 1]);
+                }
+            }
+            stage ^= 1u;
+        }
+        copy_wait<0>();                                 // nothing but empty groups is left
+        if (to < 32u) {
+            flush(row_begins >> to & 1u);
+            return;
+        }
     }
 }
 
@@ -417,14 +693,15 @@ uint32_t sort_passes(uint64_t n_rows) {
     return (bits + kDigitBits - 1) / kDigitBits;
 }
 
-template <typename Token>
+template <typename Token, uint32_t ITEMS>
 cudaError_t launch_sort(const EmbeddingGradArgs &a, const SortBuffers &b, uint32_t passes, uint32_t *d_status,
                         cudaStream_t stream) {
     static bool smem_done[kMaxDevices];
-    cudaError_t e = ensure_dynamic_smem(sort_tokens_kernel<Token>, sizeof(SortShared), smem_done);
+    cudaError_t e = ensure_dynamic_smem(sort_tokens_kernel<Token, ITEMS>, sizeof(SortShared), smem_done);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(sort_tokens_kernel<Token, ITEMS>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
     uint32_t ranks = 1;
-    while (ranks < kMaxCluster && (uint64_t)ranks * kTileKeys < a.n_tokens) ranks *= 2;
+    while (ranks < kMaxCluster && (uint64_t)ranks * kSortThreads * ITEMS < a.n_tokens) ranks *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ranks);
     cfg.blockDim = dim3(kSortThreads);
@@ -436,13 +713,23 @@ cudaError_t launch_sort(const EmbeddingGradArgs &a, const SortBuffers &b, uint32
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, sort_tokens_kernel<Token>, static_cast<const Token *>(a.d_tokens), (uint32_t)a.n_tokens,
+    return cudaLaunchKernelEx(&cfg, sort_tokens_kernel<Token, ITEMS>, static_cast<const Token *>(a.d_tokens), (uint32_t)a.n_tokens,
                               a.n_rows, a.padding_row, passes, b, a.d_rows, a.d_count, d_status);
 }
 
+template <typename Token>
+cudaError_t launch_sort_sized(const EmbeddingGradArgs &a, const SortBuffers &b, uint32_t passes, uint32_t *d_status,
+                              cudaStream_t stream) {
+    // first all CTAs of a cluster, then more keys per thread: what a pass costs is the keys of ONE multiprocessor
+    const uint64_t row = (uint64_t)kMaxCluster * kSortThreads;
+    if (a.n_tokens <= row) return launch_sort<Token, 1>(a, b, passes, d_status, stream);
+    if (a.n_tokens <= 2 * row) return launch_sort<Token, 2>(a, b, passes, d_status, stream);
+    if (a.n_tokens <= 4 * row) return launch_sort<Token, 4>(a, b, passes, d_status, stream);
+    return launch_sort<Token, kMaxItems>(a, b, passes, d_status, stream);
+}
+
 template <typename Tin, typename Tout>
-cudaError_t launch_sums(const EmbeddingGradArgs &a, const SortBuffers &b, uint32_t final_buffer, cudaStream_t stream,
-                        uint64_t *launches) {
+cudaError_t launch_sums(const EmbeddingGradArgs &a, const SortBuffers &b, cudaStream_t stream, uint64_t *launches) {
     SumArgs s;
     s.grad_out = a.d_grad_out;
     s.grad_stride = a.grad_stride;
@@ -450,70 +737,90 @@ cudaError_t launch_sums(const EmbeddingGradArgs &a, const SortBuffers &b, uint32
     s.out = a.d_grad;
     s.out_stride = a.out_stride;
     s.scale = a.scale;
-    s.n = (uint32_t)a.n_tokens;
-    s.tiles = (uint32_t)((a.dim + kTileCols - 1) / kTileCols);
-    const uint64_t units = (a.n_tokens + kWindow - 1) / kWindow * s.tiles;
-    const uint64_t blocks = (units + kSumWarps - 1) / kSumWarps;      // none without tokens or columns
-    if (blocks > 0x7fffffffull) return cudaErrorInvalidConfiguration;
-    const dim3 grid((uint32_t)blocks), block(kSumWarps * 32);
-    if (blocks) {
-        ++*launches;
-        if (a.d_rows) sum_rows_kernel<Tin, Tout, true, false><<<grid, block, 0, stream>>>(s, b, final_buffer);
-        else if (a.accumulate) sum_rows_kernel<Tin, Tout, false, true><<<grid, block, 0, stream>>>(s, b, final_buffer);
-        else sum_rows_kernel<Tin, Tout, false, false><<<grid, block, 0, stream>>>(s, b, final_buffer);
-    }
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess || !a.d_rows) return e;
+    s.aligned = ((reinterpret_cast<uintptr_t>(a.d_grad_out) | (a.n_tokens > 1 ? a.grad_stride * sizeof(Tin) : 0u)) & 15u) == 0u;
+    s.rows = a.d_rows;
+    s.cap = a.cap;
+    s.tiles = a.dim ? (uint32_t)((a.dim + Tile<Tin>::kCols - 1) / Tile<Tin>::kCols) : 1u;     // without columns: the row numbers alone
+    const uint64_t positions = a.n_tokens > a.cap ? a.n_tokens : a.cap;
+    s.tile_shift = s.tiles >= 4u ? 2u : s.tiles >= 2u ? 1u : 0u;
+    const uint64_t windows = (positions + kWindow - 1) / kWindow;
+    const uint64_t blocks = ((windows << s.tile_shift) + kSumWarps - 1) / kSumWarps;
+    const uint64_t groups = (s.tiles + (1u << s.tile_shift) - 1) >> s.tile_shift;
+    if (blocks == 0) return cudaSuccess;
+    if (blocks > 0x7fffffffull || groups > 65535u) return cudaErrorInvalidConfiguration;   // refused at the entry points
     ++*launches;
-    fill_tail_kernel<Tout><<<592, 256, 0, stream>>>(static_cast<Tout *>(a.d_grad), a.out_stride, a.dim, a.cap, a.d_rows, b.totals);
+    const dim3 grid((uint32_t)blocks, (uint32_t)groups), block(kSumWarps * 32);
+    if (a.d_rows) sum_rows_kernel<Tin, Tout, true, false><<<grid, block, 0, stream>>>(s, b);
+    else if (a.accumulate) sum_rows_kernel<Tin, Tout, false, true><<<grid, block, 0, stream>>>(s, b);
+    else sum_rows_kernel<Tin, Tout, false, false><<<grid, block, 0, stream>>>(s, b);
     return cudaGetLastError();
 }
 
 }  // namespace
 
-// Scratch: two key and two index arrays of n, rank[n], start[n + 1], totals, then the arrival counters and the partial sums of rows with
-// more than kPiece tokens (at most two pieces begin in kPiece consecutive sorted positions: the last piece of one row
-// and the first of the next).
+// Scratch: a record for each sorted position, two key and two index arrays, start[n + 1], totals; then the arrival
+// counters and the partial sums of rows with more than kPiece tokens.
 namespace {
 uint64_t round16(uint64_t x) { return (x + 15u) & ~15ull; }
 uint64_t slot_count(uint64_t n) { return 2u * (n / kPiece + 1u); }
-uint64_t tile_count(uint64_t dim) { return (dim + kTileCols - 1) / kTileCols; }
+constexpr uint64_t kLeastCols = Tile<float>::kCols, kMostCols = Tile<__half>::kCols;
+uint64_t tile_count(uint64_t dim) { return (dim + kLeastCols - 1) / kLeastCols; }
 }  // namespace
 
-uint64_t embedding_grad_sort_bytes(uint64_t n) { return 6u * round16(4u * (n + 1u)) + 64u; }
+uint64_t embedding_grad_sort_bytes(uint64_t n) { return 16u * (n + 1u) + 5u * round16(4u * (n + 1u)) + 64u; }
 uint64_t embedding_grad_arrival_bytes(uint64_t n, uint64_t dim) { return round16(8u * slot_count(n) * tile_count(dim)); }
 uint64_t embedding_grad_partial_bytes(uint64_t n, uint64_t dim) {
-    return n <= kPiece ? 16u : 4u * slot_count(n) * tile_count(dim) * kTileCols;     // one piece at most: no partial sums
+    return n <= kPiece ? 16u : 4u * slot_count(n) * ((dim + kMostCols - 1) / kMostCols * kMostCols);     // one piece at most: no partial sums
 }
 
-cudaError_t launch_embedding_grad(const EmbeddingGradArgs &a, void *d_sort, uint32_t *d_arrivals, float *d_partial,
-                                  uint32_t *d_status, cudaStream_t stream, uint64_t *launches) {
-    const uint64_t out_size = a.out_type == IV_F32 ? 4u : 2u;
-    if (!a.d_rows && !a.accumulate && a.n_rows) {
-        cudaError_t e = cudaMemset2DAsync(a.d_grad, a.out_stride * out_size, 0, a.dim * out_size, a.n_rows, stream);
-        if (e != cudaSuccess) return e;
-    }
-    if (a.n_tokens == 0 && !a.d_rows) return cudaSuccess;      // the compact form still has its count and its tail to write
+namespace {
+SortBuffers sort_buffers(const EmbeddingGradArgs &a, const EmbeddingGradScratch &scratch) {
     const uint64_t array = round16(4u * (a.n_tokens + 1u));
-    uint8_t *p = static_cast<uint8_t *>(d_sort);
+    uint8_t *p = static_cast<uint8_t *>(scratch.d_sort);
     SortBuffers b;
+    b.record = reinterpret_cast<uint4 *>(p);
+    p += 16u * (a.n_tokens + 1u);
     b.key[0] = reinterpret_cast<uint32_t *>(p);
     b.key[1] = reinterpret_cast<uint32_t *>(p + array);
     b.index[0] = reinterpret_cast<uint32_t *>(p + 2 * array);
     b.index[1] = reinterpret_cast<uint32_t *>(p + 3 * array);
-    b.rank = reinterpret_cast<uint32_t *>(p + 4 * array);
-    b.start = reinterpret_cast<uint32_t *>(p + 5 * array);
-    b.totals = reinterpret_cast<uint32_t *>(p + 6 * array);
-    b.arrivals = d_arrivals;
-    b.partial = d_partial;
+    b.start = reinterpret_cast<uint32_t *>(p + 4 * array);
+    b.totals = reinterpret_cast<uint32_t *>(p + 5 * array);
+    b.arrivals = scratch.d_arrivals;
+    b.partial = scratch.d_partial;
+    return b;
+}
+
+template <typename Token>
+cudaError_t launch_fill(const EmbeddingGradArgs &a, int sm_count, cudaStream_t stream) {
+    const uint64_t size = a.out_type == IV_F32 ? 4u : 2u;
+    const uint32_t grid = (uint32_t)(sm_count > 2 * (int)kMaxCluster ? sm_count - (int)kMaxCluster : sm_count);   // the SMs the sort leaves
+    fill_rows_kernel<Token><<<grid, kFillThreads, 0, stream>>>(static_cast<const Token *>(a.d_tokens), (uint32_t)a.n_tokens, a.n_rows,
+                                                               a.padding_row, static_cast<uint8_t *>(a.d_grad), a.dim * size,
+                                                               a.out_stride * size);
+    return cudaGetLastError();
+}
+}  // namespace
+
+cudaError_t launch_embedding_grad_sort(const EmbeddingGradArgs &a, const EmbeddingGradScratch &scratch, uint32_t *d_status,
+                                       cudaStream_t stream, uint64_t *launches) {
+    const SortBuffers b = sort_buffers(a, scratch);
     const uint32_t passes = sort_passes(a.n_rows);
-    cudaError_t e = a.token_bytes == 4 ? launch_sort<int32_t>(a, b, passes, d_status, stream)
-                                       : launch_sort<int64_t>(a, b, passes, d_status, stream);
-    if (e != cudaSuccess) return e;
     ++*launches;
-    if (a.dim == 0 && !a.d_rows) return cudaSuccess;
+    return a.token_bytes == 4 ? launch_sort_sized<int32_t>(a, b, passes, d_status, stream)
+                              : launch_sort_sized<int64_t>(a, b, passes, d_status, stream);
+}
+
+cudaError_t launch_embedding_grad_fill(const EmbeddingGradArgs &a, int sm_count, cudaStream_t stream, uint64_t *launches) {
+    ++*launches;
+    return a.token_bytes == 4 ? launch_fill<int32_t>(a, sm_count, stream) : launch_fill<int64_t>(a, sm_count, stream);
+}
+
+cudaError_t launch_embedding_grad_sums(const EmbeddingGradArgs &a, const EmbeddingGradScratch &scratch, cudaStream_t stream,
+                                       uint64_t *launches) {
+    const SortBuffers b = sort_buffers(a, scratch);
     return by_types(a.grad_type, a.out_type, [&](auto in, auto out) {
-        return launch_sums<typename decltype(in)::type, typename decltype(out)::type>(a, b, (passes + 1) & 1, stream, launches);
+        return launch_sums<typename decltype(in)::type, typename decltype(out)::type>(a, b, stream, launches);
     });
 }
 

@@ -1005,13 +1005,16 @@ bool aligned_to(const void *p, uint64_t bytes) { return (reinterpret_cast<uintpt
 
 constexpr uint64_t kMaxTokens = 1ull << 30;
 constexpr uint64_t kMaxRows = 1ull << 31;
+constexpr uint64_t kMaxColumns = 1ull << 24;
+constexpr uint64_t kForkFillBytes = 8ull << 20;
 
 // Arguments that both forms of the gradient have in common, then scratch and launch.
 int embedding_grad(iv_ctx *ctx, const ivk::EmbeddingGradArgs &a, void *cuda_stream) {
     if (!type_pair_ok(a.grad_type, a.out_type) || (a.token_bytes != 4 && a.token_bytes != 8)) return IV_ERR_INVALID_ARG;
     if (a.padding_row < -1) return IV_ERR_INVALID_ARG;
-    if (a.n_tokens > kMaxTokens || a.n_rows > kMaxRows || a.dim > kMaxRows) return IV_ERR_TOO_LARGE;
-    if ((a.n_tokens / 8u + 1u) * (a.dim / 256u + 1u) / 8u > 0x7ffffff0ull) return IV_ERR_TOO_LARGE;   // one launch's blocks
+    const uint64_t positions = a.n_tokens > a.cap ? a.n_tokens : a.cap;
+    if (a.n_rows > kMaxRows) return IV_ERR_TOO_LARGE;
+    if (positions > kMaxTokens || a.dim > kMaxColumns) return IV_ERR_TOO_LARGE;
     if (a.n_tokens > 1 && a.grad_stride < a.dim) return IV_ERR_INVALID_ARG;
     if (a.n_tokens && (!a.d_tokens || !aligned_to(a.d_tokens, a.token_bytes))) return IV_ERR_INVALID_ARG;
     if (a.n_tokens && a.dim && (!a.d_grad_out || !aligned_to(a.d_grad_out, dtype_bytes(a.grad_type)))) return IV_ERR_INVALID_ARG;
@@ -1020,17 +1023,24 @@ int embedding_grad(iv_ctx *ctx, const ivk::EmbeddingGradArgs &a, void *cuda_stre
     if (out_rows && a.dim && (!a.d_grad || !aligned_to(a.d_grad, dtype_bytes(a.out_type)))) return IV_ERR_INVALID_ARG;
     DeviceGuard guard(ctx->device);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (a.n_tokens || a.d_rows) {
-        int rc = grow(ctx, &ctx->d_sort, &ctx->sort_cap, ivk::embedding_grad_sort_bytes(a.n_tokens), 1);
-        if (rc != IV_OK) return rc;
-        rc = grow(ctx, &ctx->d_partial, &ctx->partial_cap, ivk::embedding_grad_partial_bytes(a.n_tokens, a.dim), 1);
-        if (rc != IV_OK) return rc;
-        const uint64_t before = ctx->arrivals_cap;
-        rc = grow(ctx, &ctx->d_arrivals, &ctx->arrivals_cap, ivk::embedding_grad_arrival_bytes(a.n_tokens, a.dim), 1);
-        if (rc != IV_OK) return rc;
-        if (ctx->arrivals_cap != before) IV_TRY(ctx, cudaMemsetAsync(ctx->d_arrivals, 0, ctx->arrivals_cap, stream));
-    }
-    IV_TRY(ctx, ivk::launch_embedding_grad(a, ctx->d_sort, ctx->d_arrivals, ctx->d_partial, ctx->d_status, stream, &ctx->launches));
+    int rc = grow(ctx, &ctx->d_sort, &ctx->sort_cap, ivk::embedding_grad_sort_bytes(a.n_tokens), 1);
+    if (rc != IV_OK) return rc;
+    rc = grow(ctx, &ctx->d_partial, &ctx->partial_cap, ivk::embedding_grad_partial_bytes(a.n_tokens, a.dim), 1);
+    if (rc != IV_OK) return rc;
+    const uint64_t before = ctx->arrivals_cap;
+    rc = grow(ctx, &ctx->d_arrivals, &ctx->arrivals_cap, ivk::embedding_grad_arrival_bytes(a.n_tokens, a.dim), 1);
+    if (rc != IV_OK) return rc;
+    if (ctx->arrivals_cap != before) IV_TRY(ctx, cudaMemsetAsync(ctx->d_arrivals, 0, ctx->arrivals_cap, stream));
+    const ivk::EmbeddingGradScratch scratch = {ctx->d_sort, ctx->d_arrivals, ctx->d_partial};
+
+    const uint64_t fill_bytes = !a.d_rows && !a.accumulate ? a.n_rows * a.dim * dtype_bytes(a.out_type) : 0;
+    const bool sums = a.d_rows || (a.n_tokens && a.dim && a.n_rows);
+    const bool fork = sums && fill_bytes >= kForkFillBytes;
+    if (fork && (rc = fork_tail_stream(ctx, stream)) != IV_OK) return rc;
+    if (sums) IV_TRY(ctx, ivk::launch_embedding_grad_sort(a, scratch, ctx->d_status, stream, &ctx->launches));
+    if (fill_bytes) IV_TRY(ctx, ivk::launch_embedding_grad_fill(a, ctx->sm_count, fork ? ctx->tail_stream : stream, &ctx->launches));
+    if (sums) IV_TRY(ctx, ivk::launch_embedding_grad_sums(a, scratch, stream, &ctx->launches));
+    if (fork && (rc = join_tail_stream(ctx, stream)) != IV_OK) return rc;
     return IV_OK;
 }
 
@@ -1060,7 +1070,7 @@ int iv_embedding(iv_ctx *ctx, const void *d_table, int table_type, uint64_t n_ro
                  uint64_t out_stride, void *cuda_stream) {
     if (!ctx || !type_pair_ok(table_type, out_type) || (token_bytes != 4 && token_bytes != 8)) return IV_ERR_INVALID_ARG;
     if (n_tokens == 0 || dim == 0) return IV_OK;
-    if (n_tokens > kMaxTokens || dim > kMaxRows) return IV_ERR_TOO_LARGE;
+    if (n_tokens > kMaxTokens || dim > kMaxColumns) return IV_ERR_TOO_LARGE;
     if (!d_tokens || !d_out || (n_rows && !d_table)) return IV_ERR_INVALID_ARG;
     if ((n_rows > 1 && row_stride < dim) || (n_tokens > 1 && out_stride < dim)) return IV_ERR_INVALID_ARG;
     if (!aligned_to(d_table, dtype_bytes(table_type)) || !aligned_to(d_out, dtype_bytes(out_type)) ||

@@ -226,19 +226,30 @@ struct EmbeddingGradArgs {
     uint64_t cap;
     uint64_t *d_count;
 };
-constexpr uint32_t kPiece = 64;      // terms that are added up without a break
+constexpr uint32_t kPiece = 32;      // terms that are added up without a break
 constexpr uint32_t kGroup = 32;      // pieces whose sums are added up without a break
 struct SortBuffers {
+    uint4 *record;                   // of each sorted position: token, first position of its row, number of its row, row
     uint32_t *key[2], *index[2];     // ping-pong of the radix sort
-    uint32_t *rank, *start, *totals; // distinct row of each sorted position, its first position, {sorted tokens that count, distinct rows}
+    uint32_t *start, *totals;        // first position of each distinct row; {sorted tokens that count, distinct rows}
     uint32_t *arrivals;              // zero between calls
     float *partial;
 };
 uint64_t embedding_grad_sort_bytes(uint64_t n);
 uint64_t embedding_grad_arrival_bytes(uint64_t n, uint64_t dim);
 uint64_t embedding_grad_partial_bytes(uint64_t n, uint64_t dim);
-cudaError_t launch_embedding_grad(const EmbeddingGradArgs &a, void *d_sort, uint32_t *d_arrivals, float *d_partial,
-                                  uint32_t *d_status, cudaStream_t stream, uint64_t *launches);
+struct EmbeddingGradScratch {
+    void *d_sort;
+    uint32_t *d_arrivals;
+    float *d_partial;
+};
+// The tokens sorted (and the compact form's row numbers and count), then the sums of the rows with a token; the rows
+// without one of a fresh table gradient are the fill's, which needs neither of the others.
+cudaError_t launch_embedding_grad_sort(const EmbeddingGradArgs &a, const EmbeddingGradScratch &scratch, uint32_t *d_status,
+                                       cudaStream_t stream, uint64_t *launches);
+cudaError_t launch_embedding_grad_sums(const EmbeddingGradArgs &a, const EmbeddingGradScratch &scratch, cudaStream_t stream,
+                                       uint64_t *launches);
+cudaError_t launch_embedding_grad_fill(const EmbeddingGradArgs &a, int sm_count, cudaStream_t stream, uint64_t *launches);
 
 // grad_norm.cu ---------------------------------------------------------------
 // A set of n tensors: tensor k is the d_lengths[k] bytes at d_base + d_offsets[k], of type d_types[k] (or `type`).
