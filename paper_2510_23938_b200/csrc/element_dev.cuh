@@ -93,71 +93,121 @@ __device__ __forceinline__ void store_aligned(void *p, const uint32_t *w) {
     }
 }
 
-// V consecutive elements at any element alignment.  The branch on the misalignment is the same for all lanes that walk
-// one tensor with a stride of whole vectors.
+// V consecutive elements (a multiple of 16 bytes) with the aligned 16-byte pieces of memory they lie in; load() only
+// loads, get() shifts the wanted bytes out, so that several loads can be in flight.  ALIGNED: starts at a piece.
+template <typename T, int V, bool ALIGNED>
+struct Vector {
+    static constexpr int W = Packed<T, V>::kWords;
+    static_assert(W % 4 == 0, "whole pieces of 16 bytes");
+    uint32_t w[ALIGNED ? W : W + 4];
+    __device__ __forceinline__ void load(const T *p, uint32_t off) {
+        const uint8_t *q = reinterpret_cast<const uint8_t *>(p) - (ALIGNED ? 0u : off);
+#pragma unroll
+        for (int i = 0; i < (ALIGNED ? W : W + 4); i += 4) load_aligned<4>(q + 4 * i, w + i);
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < (ALIGNED ? W : W + 4); ++i) w[i] = 0u;
+    }
+    // `off`: bytes from the piece's start, the same for all lanes that walk one tensor with a stride of whole vectors
+    __device__ __forceinline__ Packed<T, V> get(uint32_t off) const {
+        Packed<T, V> out;
+        if constexpr (ALIGNED) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) out.w[i] = w[i];
+        } else {
+            uint32_t x[W + 4];
+#pragma unroll
+            for (int i = 0; i < W + 4; ++i) x[i] = w[i];
+            if (off & 8u) {
+#pragma unroll
+                for (int i = 0; i < W + 2; ++i) x[i] = x[i + 2];
+            }
+            if (off & 4u) {
+#pragma unroll
+                for (int i = 0; i < W + 1; ++i) x[i] = x[i + 1];
+            }
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int i = 0; i < W; ++i) out.w[i] = x[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < W; ++i) out.w[i] = __funnelshift_r(x[i], x[i + 1], (off & 2u) * 8u);
+            }
+        }
+        return out;
+    }
+};
+
+__device__ __forceinline__ uint32_t misalignment(const void *p) { return (uint32_t)reinterpret_cast<uintptr_t>(p) & 15u; }
+
+// V consecutive elements at any element alignment, at once.
 template <typename T, int V>
 __device__ __forceinline__ void load_any(const T *p, Packed<T, V> &out) {
-    constexpr int W = Packed<T, V>::kWords;
-    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
-    const uint32_t off = (uint32_t)a & (4u * W - 1u);
+    const uint32_t off = misalignment(p);
     if (off == 0u) {
-        load_aligned<W>(p, out.w);
-        return;
+        Vector<T, V, true> x;
+        x.load(p, 0u);
+        out = x.get(0u);
+    } else {
+        Vector<T, V, false> x;
+        x.load(p, off);
+        out = x.get(off);
     }
-    const uint32_t *q = reinterpret_cast<const uint32_t *>(a - off);
-    uint32_t w[2 * W];
-    load_aligned<W>(q, w);
-    load_aligned<W>(q + W, w + W);
-    const uint32_t words = off >> 2, bits = (off & 3u) * 8u;
-    if constexpr (W == 4) {
-        if (words & 2u) {
-#pragma unroll
-            for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
-        }
-    }
-    if (words & 1u) {
-#pragma unroll
-        for (int i = 0; i < W + 1; ++i) w[i] = i + 1 < 2 * W ? w[i + 1] : 0u;
-    }
-#pragma unroll
-    for (int i = 0; i < W; ++i) out.w[i] = __funnelshift_r(w[i], i + 1 < 2 * W ? w[i + 1] : 0u, bits);
 }
 
-// out[i] = f(in[i]) for i < n by the `lanes` threads of which this is number `lane`: single elements up to the first
-// aligned vector of the output, aligned vectors (UNROLL of them in flight per thread), single elements at the end.
-template <typename Tin, typename Tout, int UNROLL, typename F>
-__device__ __forceinline__ void map_span(const Tin *in, Tout *out, uint32_t n, uint32_t lane, uint32_t lanes, F f) {
-    constexpr int V = 16 / (int)(sizeof(Tin) > sizeof(Tout) ? sizeof(Tin) : sizeof(Tout));
-    constexpr uint32_t kOut = V * sizeof(Tout);
-    uint32_t head = (uint32_t)((kOut - (reinterpret_cast<uintptr_t>(out) & (kOut - 1u))) & (kOut - 1u)) / (uint32_t)sizeof(Tout);
-    if (head > n) head = n;
-    if (lane < head) out[lane] = from_float<Tout>(f(to_float(in[lane])));
-    in += head;
-    out += head;
-    n -= head;
-    const uint32_t vecs = n / V;
+template <typename Tin, typename Tout, bool ALIGNED, typename F>
+__device__ __forceinline__ void map_vectors(const Tin *in, Tout *out, uint32_t vecs, uint32_t lane, uint32_t lanes, F f) {
+    constexpr int V = 16 / (int)(sizeof(Tin) < sizeof(Tout) ? sizeof(Tin) : sizeof(Tout));
+    constexpr int UNROLL = (ALIGNED ? 64 : 32) / (V * (int)sizeof(Tin)); // 64 bytes in flight per thread; 32 where their neighbours come along
+    const uint32_t off = misalignment(in);
     for (uint32_t v0 = lane; v0 < vecs; v0 += lanes * UNROLL) {
-        Packed<Tin, V> raw[UNROLL];
+        Vector<Tin, V, ALIGNED> raw[UNROLL];
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             const uint32_t v = v0 + u * lanes;
-            if (v < vecs) load_any<Tin, V>(in + (uint64_t)v * V, raw[u]);
+            if (v < vecs) raw[u].load(in + (uint64_t)v * V, off);
         }
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             const uint32_t v = v0 + u * lanes;
             if (v < vecs) {
                 float x[V];
-                raw[u].unpack(x);
+                raw[u].get(off).unpack(x);
 #pragma unroll
                 for (int i = 0; i < V; ++i) x[i] = f(x[i]);
                 Packed<Tout, V> y;
                 y.pack(x);
-                store_aligned<Packed<Tout, V>::kWords>(out + (uint64_t)v * V, y.w);
+#pragma unroll
+                for (int i = 0; i < Packed<Tout, V>::kWords; i += 4)
+                    store_aligned<4>(reinterpret_cast<uint32_t *>(out + (uint64_t)v * V) + i, y.w + i);
             }
         }
     }
-    const uint32_t done = vecs * V;
+}
+
+// out[i] = f(in[i]) for i < n by the `lanes` threads (at least 8) of which this is number `lane`, in vectors of 16 bytes
+// of the smaller type.  Both ends start at a 16-byte boundary.
+template <typename Tin, typename Tout, typename F>
+__device__ __forceinline__ void map_aligned(const Tin *in, Tout *out, uint32_t n, uint32_t lane, uint32_t lanes, F f) {
+    constexpr int V = 16 / (int)(sizeof(Tin) < sizeof(Tout) ? sizeof(Tin) : sizeof(Tout));
+    const uint32_t vecs = n / V, done = vecs * V;
+    map_vectors<Tin, Tout, true>(in, out, vecs, lane, lanes, f);
+    if (lane < n - done) out[done + lane] = from_float<Tout>(f(to_float(in[done + lane])));
+}
+// The same at any element alignment: single elements up to the first 16-byte boundary of the output.
+template <typename Tin, typename Tout, typename F>
+__device__ __forceinline__ void map_any(const Tin *in, Tout *out, uint32_t n, uint32_t lane, uint32_t lanes, F f) {
+    constexpr int V = 16 / (int)(sizeof(Tin) < sizeof(Tout) ? sizeof(Tin) : sizeof(Tout));
+    uint32_t head = ((16u - misalignment(out)) & 15u) / (uint32_t)sizeof(Tout);
+    if (head > n) head = n;
+    if (lane < head) out[lane] = from_float<Tout>(f(to_float(in[lane])));
+    in += head;
+    out += head;
+    n -= head;
+    const uint32_t vecs = n / V, done = vecs * V;
+    if (misalignment(in) == 0u) map_vectors<Tin, Tout, true>(in, out, vecs, lane, lanes, f);
+    else map_vectors<Tin, Tout, false>(in, out, vecs, lane, lanes, f);
     if (lane < n - done) out[done + lane] = from_float<Tout>(f(to_float(in[done + lane])));
 }
 

@@ -418,10 +418,10 @@ template <typename T> struct Tile {
 // V columns of type T, `have` of them: the rest reads as zero and is not written.
 template <typename T, uint32_t V>
 __device__ __forceinline__ void load_cols(const T *p, uint32_t have, float (&v)[V]) {
-    if (have == V) {
-        constexpr uint32_t W = 16 / sizeof(T) < V ? 16 / sizeof(T) : V;   // 16 bytes at a time, or all of fewer
+    constexpr uint32_t W = 16 / sizeof(T);                               // 16 bytes at a time
+    if (V % W == 0 && have == V) {
 #pragma unroll
-        for (uint32_t i = 0; i < V; i += W) {
+        for (uint32_t i = 0; i + W <= V; i += W) {
             elem::Packed<T, (int)W> x;
             float y[W];
             elem::load_any<T, (int)W>(p + i, x);

@@ -10,10 +10,13 @@
 // small that squares may have been lost below the smallest 32-bit number is added up again in 64 bits, so any finite
 // gradient has a right norm.
 //
-//   1. plan_kernel     pieces of each tensor and their running sum; ill-formed tensors are left out (device status 2)
-//   2. norm_kernel     one sum per piece
-//   3. finish_kernel   per-tensor sums, the norm, the scale
-//   4. scale_kernel    clipping: piece by piece
+//   1. plan_kernel     sets of more than kSmallSet tensors only: the pieces' running number before each tensor; smaller
+//                      sets are laid out by every CTA for itself, in shared memory
+//   2. norm_kernel     one sum per piece; the CTA that completes a tensor adds up its pieces, the one that completes the
+//                      set adds up the tensors
+//   3. scale_kernel    clipping: piece by piece
+#include <type_traits>
+
 #include "element_dev.cuh"
 #include "iv_internal.h"
 
@@ -21,35 +24,29 @@ namespace ivk {
 
 namespace {
 
-constexpr uint32_t kNormThreads = 256;
-constexpr uint32_t kMinShift = 12, kMaxShift = 31;      // pieces of 4,096 elements and more
-constexpr uint64_t kPieceTarget = 65536;                // a set has at most this many pieces and one more per tensor
-
-// Scratch: header, running number of pieces before each tensor (n + 1), one sum per piece.
-struct PlanHeader {
-    uint64_t pieces;
-    uint64_t elements;
-    uint32_t shift;
-    uint32_t pad;
-};
+constexpr uint32_t kThreads = 256;
+constexpr uint32_t kWarps = kThreads / 32;
+constexpr uint32_t kMinShift = 13, kMaxShift = 31;      // pieces of 8,192 elements and more
+constexpr uint64_t kPieceTarget = 32768;                // a set has at most this many pieces and one more per tensor
+constexpr uint32_t kSmallSet = 2048;
 
 __device__ __forceinline__ int type_of(const TensorSet &set, uint64_t k) { return set.d_types ? (int)set.d_types[k] : set.type; }
 
 // Elements of tensor k, 0 for one that is ill-formed (unknown type, offset or length not a multiple of the element).
-__device__ __forceinline__ uint64_t elements_of(const TensorSet &set, uint64_t k, uint32_t *status) {
+__device__ __forceinline__ uint64_t elements_of(const TensorSet &set, uint64_t k, bool &bad) {
     const int type = type_of(set, k);
     const uint64_t bytes = set.d_lengths[k];
     const uint64_t size = type == IV_F32 ? 4u : 2u;
     const uint64_t address = reinterpret_cast<uint64_t>(set.d_base) + set.d_offsets[k];
     if (type > IV_BF16 || type < 0 || ((bytes | address) & (size - 1u)) != 0u) {
-        atomicMax(status, (uint32_t)IVK_DEV_BOUNDS);
+        bad = true;
         return 0;
     }
     return bytes / size;
 }
 
-constexpr uint32_t kPlanThreads = 1024;
-
+// Exclusive prefix sum over a CTA of THREADS threads, and the total.
+template <uint32_t THREADS>
 __device__ __forceinline__ uint64_t block_exclusive64(uint64_t v, uint64_t *scan, uint64_t &total) {
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     uint64_t x = v;
@@ -62,7 +59,8 @@ __device__ __forceinline__ uint64_t block_exclusive64(uint64_t v, uint64_t *scan
     __syncthreads();
     uint64_t before = 0;
     total = 0;
-    for (uint32_t w = 0; w < kPlanThreads / 32; ++w) {
+#pragma unroll
+    for (uint32_t w = 0; w < THREADS / 32; ++w) {
         if (w == warp) before = total;
         total += scan[w];
     }
@@ -70,72 +68,148 @@ __device__ __forceinline__ uint64_t block_exclusive64(uint64_t v, uint64_t *scan
     return before + x - v;
 }
 
-__global__ void __launch_bounds__(kPlanThreads)
-plan_kernel(TensorSet set, PlanHeader *header, uint64_t *first, uint32_t *status) {
-    __shared__ uint64_t scan[kPlanThreads / 32];
-    uint64_t elements = 0;
-    for (uint64_t k = threadIdx.x; k < set.n; k += kPlanThreads) elements += elements_of(set, k, status);
-    uint64_t total;
-    block_exclusive64(elements, scan, total);
+__device__ __forceinline__ uint32_t shift_for(uint64_t elements) {
     uint32_t shift = kMinShift;
-    while (shift < kMaxShift && (total >> shift) > kPieceTarget) ++shift;
-    uint64_t before = 0;
-    for (uint64_t k0 = 0; k0 < set.n; k0 += kPlanThreads) {
-        const uint64_t k = k0 + threadIdx.x;
-        const uint64_t pieces = k < set.n ? (elements_of(set, k, status) + (1ull << shift) - 1) >> shift : 0;
-        uint64_t here;
-        const uint64_t at = block_exclusive64(pieces, scan, here);
-        if (k < set.n) first[k] = before + at;
-        before += here;
-    }
-    if (threadIdx.x == 0) {
-        first[set.n] = before;
-        header->pieces = before;
-        header->elements = total;
-        header->shift = shift;
-    }
+    while (shift < kMaxShift && (elements >> shift) > kPieceTarget) ++shift;
+    return shift;
 }
 
-// The tensor that piece p belongs to: first[k] <= p < first[k + 1].
-__device__ __forceinline__ uint64_t tensor_of(const uint64_t *first, uint64_t n, uint64_t p) {
-    uint64_t lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const uint64_t mid = (lo + hi) / 2;
-        if (first[mid] <= p) lo = mid;
-        else hi = mid;
+struct Plan {
+    uint64_t pieces, elements;
+    uint32_t shift;
+    uint32_t live;               // tensors that have pieces
+};
+
+// The set laid out by one CTA: first[k] = number of pieces before tensor k, first[n] = all; thread 0 .. all get the plan.
+template <uint32_t THREADS, typename Index>
+__device__ __forceinline__ Plan lay_out(const TensorSet &set, Index *first, uint64_t *scan, uint32_t *status) {
+    bool bad = false;
+    uint64_t elements = 0;
+    for (uint64_t k = threadIdx.x; k < set.n; k += THREADS) elements += elements_of(set, k, bad);
+    Plan plan;
+    block_exclusive64<THREADS>(elements, scan, plan.elements);
+    plan.shift = shift_for(plan.elements);
+    uint64_t before = 0;
+    uint32_t live = 0;
+    for (uint64_t k0 = 0; k0 < set.n; k0 += THREADS) {
+        const uint64_t k = k0 + threadIdx.x;
+        const uint64_t pieces = k < set.n ? (elements_of(set, k, bad) + (1ull << plan.shift) - 1) >> plan.shift : 0;
+        uint64_t here;
+        const uint64_t at = block_exclusive64<THREADS>(pieces, scan, here);
+        if (k < set.n) first[k] = (Index)(before + at);
+        before += here;
+        live += __syncthreads_count(pieces != 0);
+    }
+    if (bad) atomicMax(status, (uint32_t)IVK_DEV_BOUNDS);
+    if (threadIdx.x == 0) first[set.n] = (Index)before;
+    plan.pieces = before;
+    plan.live = live;
+    __syncthreads();
+    return plan;
+}
+
+constexpr uint32_t kPlanThreads = 1024;
+
+__global__ void __launch_bounds__(kPlanThreads)
+plan_kernel(TensorSet set, Plan *header, uint32_t *first, uint32_t *status) {
+    __shared__ uint64_t scan[kPlanThreads / 32];
+    const Plan plan = lay_out<kPlanThreads>(set, first, scan, status);
+    if (threadIdx.x == 0) *header = plan;
+}
+
+// Where the norm and scale kernels find the plan: in their own shared memory (small sets) or in global memory.
+struct PlanAt {
+    const Plan *header;          // NULL: lay out in shared memory
+    const uint32_t *first;
+};
+
+struct Walk {
+    Plan plan;
+    const uint32_t *first;
+};
+
+// The tensor k with first[k] <= p < first[k + 1]; by the whole warp, 32 places at a time.
+__device__ __forceinline__ uint64_t tensor_of(const uint32_t *first, uint64_t n, uint64_t p) {
+    const uint32_t lane = threadIdx.x & 31u;
+    uint64_t lo = 0, count = n;
+    while (count > 1) {
+        const uint64_t step = (count + 31u) / 32u, at = lane * step;
+        const bool before = at < count && first[lo + at] <= p;
+        const uint32_t part = __popc(__ballot_sync(0xffffffffu, before)) - 1u;    // true for a first few lanes, lane 0 among them
+        lo += part * step;
+        count = count - part * step < step ? count - part * step : step;
     }
     return lo;
 }
 
-// Sum of squares of `count` elements by the CTA; the result is in thread 0.  An element's place in the piece decides
-// which thread and accumulator it goes to, whatever the alignment.
+__device__ __forceinline__ Walk start_walk(const TensorSet &set, const PlanAt &at, uint32_t *shared_first, uint64_t *scan, uint32_t *status) {
+    Walk w;
+    if (at.header) {
+        w.plan = *at.header;
+        w.first = at.first;
+    } else {
+        w.plan = lay_out<kThreads>(set, shared_first, scan, status);
+        w.first = shared_first;
+    }
+    return w;
+}
+
+// Sum over the CTA in a fixed order; every thread gets it.  `shared`: kWarps doubles, free again after the next barrier.
+__device__ __forceinline__ double block_sum(double x, double *shared) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+    if ((threadIdx.x & 31u) == 0u) shared[threadIdx.x >> 5] = x;
+    __syncthreads();
+    double total = 0.0;
+#pragma unroll
+    for (uint32_t w = 0; w < kWarps; ++w) total += shared[w];
+    return total;
+}
+
+// Squares of `vecs` vectors by the CTA, added to acc; the bits that are set anywhere in them added to `bits`.
+template <typename T, int V, bool ALIGNED>
+__device__ __forceinline__ void add_squares(const T *p, uint32_t vecs, float (&acc)[V], uint32_t &bits) {
+    constexpr uint32_t kUnroll = 4;
+    const uint32_t off = elem::misalignment(p);
+    for (uint32_t v0 = threadIdx.x; v0 < vecs; v0 += kThreads * kUnroll) {
+        elem::Vector<T, V, ALIGNED> raw[kUnroll];
+#pragma unroll
+        for (uint32_t u = 0; u < kUnroll; ++u) {
+            const uint32_t v = v0 + u * kThreads;
+            if (v < vecs) raw[u].load(p + (uint64_t)v * V, off);
+            else raw[u].zero();
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < kUnroll; ++u) {
+            const elem::Packed<T, V> w = raw[u].get(off);
+            float x[V];
+            w.unpack(x);
+#pragma unroll
+            for (int i = 0; i < V; ++i) acc[i] = fmaf(x[i], x[i], acc[i]);
+#pragma unroll
+            for (int i = 0; i < elem::Packed<T, V>::kWords; ++i) bits |= w.w[i];
+        }
+    }
+}
+
+// Two of them take turns, so that one barrier per piece is enough.
+struct PieceShared {
+    double sum[kWarps];
+    uint32_t any[kWarps];
+};
+
+// Sum of squares of `count` elements by the CTA.  An element's place in the piece decides which thread and accumulator
+// it goes to, whatever the alignment.
 template <typename T>
-__device__ double piece_squares(const T *p, uint32_t count, double *shared) {
+__device__ __forceinline__ double piece_squares(const T *p, uint32_t count, PieceShared &shared) {
     constexpr int V = 16 / (int)sizeof(T);
     float acc[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = 0.f;
     uint32_t bits = 0;
     const uint32_t vecs = count / V;
-    constexpr uint32_t kUnroll = 4;
-    for (uint32_t v0 = threadIdx.x; v0 < vecs; v0 += kNormThreads * kUnroll) {
-        elem::Packed<T, V> raw[kUnroll];
-#pragma unroll
-        for (uint32_t u = 0; u < kUnroll; ++u) {
-            const uint32_t v = v0 + u * kNormThreads;
-            if (v < vecs) elem::load_any<T, V>(p + (uint64_t)v * V, raw[u]);
-            else raw[u].zero();
-        }
-#pragma unroll
-        for (uint32_t u = 0; u < kUnroll; ++u) {
-            float x[V];
-            raw[u].unpack(x);
-#pragma unroll
-            for (int i = 0; i < V; ++i) acc[i] = fmaf(x[i], x[i], acc[i]);
-#pragma unroll
-            for (int i = 0; i < elem::Packed<T, V>::kWords; ++i) bits |= raw[u].w[i];
-        }
-    }
+    if (elem::misalignment(p) == 0u) add_squares<T, V, true>(p, vecs, acc, bits);
+    else add_squares<T, V, false>(p, vecs, acc, bits);
     float tail = 0.f;
     if (threadIdx.x < count - vecs * V) {
         tail = elem::to_float(p[vecs * V + threadIdx.x]);
@@ -144,171 +218,259 @@ __device__ double piece_squares(const T *p, uint32_t count, double *shared) {
     double sum = (double)tail * (double)tail;
 #pragma unroll
     for (int i = 0; i < V; ++i) sum += (double)acc[i];
+    bits &= sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
+    // sum over the CTA in a fixed order
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    const bool any = __any_sync(0xffffffffu, bits != 0u);
+    if ((threadIdx.x & 31u) == 0u) {
+        shared.sum[threadIdx.x >> 5] = sum;
+        shared.any[threadIdx.x >> 5] = any ? 1u : 0u;
+    }
+    __syncthreads();
+    double total = 0.0;
+    uint32_t some = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < kWarps; ++w) {
+        total += shared.sum[w];
+        some |= shared.any[w];
+    }
     // fine: a finite 32-bit sum that is large against what rounding below the smallest normal number may have cost
     // (each square off by at most 2^-150), or nothing but zeros
-    bits &= sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
-    auto reduce = [&](double x) {
-#pragma unroll
-        for (int d = 16; d; d >>= 1) x += __shfl_down_sync(0xffffffffu, x, d);
-        if ((threadIdx.x & 31u) == 0u) shared[threadIdx.x >> 5] = x;
-        __syncthreads();
-        double total = 0.0;
-#pragma unroll
-        for (uint32_t w = 0; w < kNormThreads / 32; ++w) total += shared[w];
-        return total;
-    };
-    const double total = reduce(sum);
     const bool fine = total < 3e38 && total > 0x1p-90;
-    const int some = __syncthreads_or(bits != 0u);          // also: everybody has read `shared`
     if (fine || !some) return some ? total : 0.0;
     double slow = 0.0;
-    for (uint32_t i = threadIdx.x; i < count; i += kNormThreads) {
+    for (uint32_t i = threadIdx.x; i < count; i += kThreads) {
         const double x = (double)elem::to_float(p[i]);
         slow = fma(x, x, slow);
     }
-    const double exact = reduce(slow);
-    __syncthreads();
-    return exact;
+    __syncthreads();                                      // everybody has read `shared`
+    return block_sum(slow, shared.sum);
 }
 
-__global__ void __launch_bounds__(kNormThreads)
-norm_kernel(TensorSet set, const PlanHeader *header, const uint64_t *first, double *sums) {
-    __shared__ double shared[kNormThreads / 32];
-    const uint64_t pieces = header->pieces;
-    const uint32_t shift = header->shift;
-    for (uint64_t p = blockIdx.x; p < pieces; p += gridDim.x) {
-        const uint64_t k = tensor_of(first, set.n, p);
-        const uint64_t e0 = (p - first[k]) << shift;
-        const int type = type_of(set, k);
-        const uint64_t total = set.d_lengths[k] >> (type == IV_F32 ? 2 : 1);
-        const uint32_t count = (uint32_t)(total - e0 < (1ull << shift) ? total - e0 : (1ull << shift));
-        const uint8_t *base = set.d_base + set.d_offsets[k];
-        double sum;
-        if (type == IV_F32) sum = piece_squares(reinterpret_cast<const float *>(base) + e0, count, shared);
-        else if (type == IV_F16) sum = piece_squares(reinterpret_cast<const __half *>(base) + e0, count, shared);
-        else sum = piece_squares(reinterpret_cast<const __nv_bfloat16 *>(base) + e0, count, shared);
-        if (threadIdx.x == 0) sums[p] = sum;
-    }
-}
+// Scratch in global memory: sums[pieces], squares[n] of the tensors, arrived[n] pieces and one word for the set (both
+// zero between calls).
+struct NormScratch {
+    double *sums, *squares;
+    uint32_t *arrived, *arrived_set;
+};
 
-constexpr uint32_t kFinishThreads = 1024;
-
-// One warp per tensor adds up its pieces (lane l takes pieces l, l + 32, ...), then the tensors are added up likewise.
-__global__ void __launch_bounds__(kFinishThreads)
-finish_kernel(uint64_t n, const PlanHeader *header, const uint64_t *first, const double *sums, bool clip, float max_norm,
-              float *norms, iv_norm_result *result, const uint32_t *status) {
-    __shared__ double shared[kFinishThreads / 32];
-    __shared__ uint32_t bad;
-    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    if (threadIdx.x == 0) bad = 0;
-    __syncthreads();
-    double mine = 0.0;                                   // of the tensors warp, warp + 32, ...
-    for (uint64_t k = warp; k < n; k += kFinishThreads / 32) {
-        double s = 0.0;
-        for (uint64_t p = first[k] + lane; p < first[k + 1]; p += 32u) s += sums[p];
-#pragma unroll
-        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-        if (lane == 0) {
-            if (norms) norms[k] = (float)sqrt(s);
-            if (!isfinite(s)) atomicAdd(&bad, 1u);
-        }
-        mine += s;
-    }
-    if (lane == 0) shared[warp] = mine;
-    __syncthreads();
-    if (threadIdx.x == 0) {
+// T: the tensors' type, void for a set of several types.
+template <typename T>
+__global__ void __launch_bounds__(kThreads, std::is_void_v<T> ? 2 : 4)
+norm_kernel(TensorSet set, PlanAt at, NormScratch scratch, bool clip, float max_norm, float *norms, iv_norm_result *result,
+            uint32_t *status) {
+    extern __shared__ uint32_t shared_first[];
+    __shared__ uint64_t scan[kWarps];
+    __shared__ double shared[kWarps];
+    __shared__ PieceShared piece_shared[2];
+    __shared__ uint32_t flag;
+    const Walk w = start_walk(set, at, shared_first, scan, status);
+    const uint32_t *first = w.first;
+    auto finish_set = [&]() {
         double total = 0.0;
-        for (uint32_t w = 0; w < kFinishThreads / 32; ++w) total += shared[w];
-        const double norm = sqrt(total);
-        result->status = *status;
-        result->n_nonfinite = bad;
-        result->norm = (float)norm;
-        result->scale = !clip || norm <= (double)max_norm ? 1.f : (float)((double)max_norm / norm);
-        result->sum_squares = total;
-        result->n_elements = header->elements;
+        uint32_t bad = 0;
+        for (uint64_t k = threadIdx.x; k < set.n; k += kThreads) {
+            const double s = first[k + 1] != first[k] ? __ldcg(&scratch.squares[k]) : 0.0;
+            bad += isfinite(s) ? 0u : 1u;
+            total += s;
+        }
+        total = block_sum(total, shared);
+        __syncthreads();
+        const double bad_tensors = block_sum((double)bad, shared);
+        if (threadIdx.x == 0) {
+            const double norm = sqrt(total);
+            result->status = *reinterpret_cast<volatile uint32_t *>(status);
+            result->n_nonfinite = (uint32_t)bad_tensors;
+            result->norm = (float)norm;
+            result->scale = !clip || norm <= (double)max_norm ? 1.f : (float)((double)max_norm / norm);
+            result->sum_squares = total;
+            result->n_elements = w.plan.elements;
+        }
+    };
+    if (blockIdx.x == 0) {
+        if (norms)
+            for (uint64_t k = threadIdx.x; k < set.n; k += kThreads)
+                if (first[k] == first[k + 1]) norms[k] = 0.f;
+        if (w.plan.pieces == 0) finish_set();
+    }
+    const uint64_t range_begin = w.plan.pieces * blockIdx.x / gridDim.x;       // this CTA's pieces
+    const uint64_t range_end = w.plan.pieces * (blockIdx.x + 1u) / gridDim.x;
+    if (range_begin == range_end) return;
+    // pieces done of tensor k; true for the CTA whose pieces complete it (and likewise the set)
+    auto arrive = [&](uint32_t *counter, uint32_t mine, uint32_t all) {
+        if (threadIdx.x == 0) {
+            __threadfence();
+            flag = atomicAdd(counter, mine) + mine == all ? 1u : 0u;
+            if (flag) *counter = 0u;
+            __threadfence();
+        }
+        __syncthreads();
+        const bool last = flag != 0u;
+        __syncthreads();
+        return last;
+    };
+    for (uint64_t p = range_begin, k = tensor_of(first, set.n, range_begin); p < range_end; ++k) {
+        const uint64_t from = first[k], next = first[k + 1];
+        if (p >= next) continue;
+        const int type = type_of(set, k);
+        const uint64_t elements = set.d_lengths[k] >> (type == IV_F32 ? 2 : 1);
+        const uint8_t *base = set.d_base + set.d_offsets[k];
+        const uint64_t stop = next < range_end ? next : range_end, begin = p;
+        for (; p < stop; ++p) {
+            const uint64_t e0 = (p - from) << w.plan.shift;
+            const uint32_t count = (uint32_t)(elements - e0 < (1ull << w.plan.shift) ? elements - e0 : (1ull << w.plan.shift));
+            double sum;
+            if constexpr (!std::is_void_v<T>) sum = piece_squares(reinterpret_cast<const T *>(base) + e0, count, piece_shared[p & 1u]);
+            else if (type == IV_F32) sum = piece_squares(reinterpret_cast<const float *>(base) + e0, count, piece_shared[p & 1u]);
+            else if (type == IV_F16) sum = piece_squares(reinterpret_cast<const __half *>(base) + e0, count, piece_shared[p & 1u]);
+            else sum = piece_squares(reinterpret_cast<const __nv_bfloat16 *>(base) + e0, count, piece_shared[p & 1u]);
+            if (threadIdx.x == 0) __stcg(&scratch.sums[p], sum);
+        }
+        if (!arrive(&scratch.arrived[k], (uint32_t)(stop - begin), (uint32_t)(next - from))) continue;
+        double s = 0.0;
+        for (uint64_t q = from + threadIdx.x; q < next; q += kThreads) s += __ldcg(&scratch.sums[q]);
+        s = block_sum(s, shared);
+        if (threadIdx.x == 0) {
+            __stcg(&scratch.squares[k], s);
+            if (norms) norms[k] = (float)sqrt(s);
+        }
+        if (arrive(scratch.arrived_set, 1u, w.plan.live)) finish_set();
     }
 }
 
 template <typename Tin, typename Tout>
-__device__ __forceinline__ void scale_piece(const uint8_t *in, uint8_t *out, uint64_t e0, uint32_t count, float scale) {
-    elem::map_span<Tin, Tout, 4>(reinterpret_cast<const Tin *>(in) + e0, reinterpret_cast<Tout *>(out) + e0, count, threadIdx.x,
-                                 kNormThreads, [scale](float x) { return x * scale; });
+__device__ __forceinline__ void scale_piece(const uint8_t *in8, uint8_t *out8, uint64_t e0, uint32_t count, float scale) {
+    const Tin *in = reinterpret_cast<const Tin *>(in8) + e0;
+    Tout *out = reinterpret_cast<Tout *>(out8) + e0;
+    elem::map_any<Tin, Tout>(in, out, count, threadIdx.x, kThreads, [scale](float x) { return x * scale; });
 }
 
-__global__ void __launch_bounds__(kNormThreads)
-scale_kernel(TensorSet set, const PlanHeader *header, const uint64_t *first, const float *scale_at, uint8_t *out_base,
-             const uint64_t *out_offsets, int out_type, uint32_t *status) {
-    const uint64_t pieces = header->pieces;
-    const uint32_t shift = header->shift;
+// Tin, Tout: the types of all tensors, void for a set of several types.
+template <typename Tin, typename Tout>
+__global__ void __launch_bounds__(kThreads, std::is_void_v<Tin> ? 2 : 4)
+scale_kernel(TensorSet set, PlanAt at, const float *scale_at, uint8_t *out_base, const uint64_t *out_offsets, int out_type,
+             uint32_t *status) {
+    extern __shared__ uint32_t shared_first[];
+    __shared__ uint64_t scan[kWarps];
+    const Walk w = start_walk(set, at, shared_first, scan, status);
     const float scale = *scale_at;
     if (scale == 1.f && out_base == set.d_base && out_offsets == set.d_offsets) return;   // in place, nothing to change
-    for (uint64_t q = blockIdx.x; q < pieces; q += gridDim.x) {
-        const uint64_t p = pieces - 1 - q;               // backwards: the norm's last pieces are still in the L2 cache
-        const uint64_t k = tensor_of(first, set.n, p);
-        const uint64_t e0 = (p - first[k]) << shift;
+    // backwards: what the norm read last is still in the L2 cache
+    for (uint64_t q = blockIdx.x; q < w.plan.pieces; q += gridDim.x) {
+        const uint64_t p = w.plan.pieces - 1u - q;
+        const uint64_t k = tensor_of(w.first, set.n, p);
+        const uint64_t e0 = (p - w.first[k]) << w.plan.shift;
         const int type = type_of(set, k);
         const int to = out_type < 0 ? type : out_type;
-        const uint64_t total = set.d_lengths[k] >> (type == IV_F32 ? 2 : 1);
-        const uint32_t count = (uint32_t)(total - e0 < (1ull << shift) ? total - e0 : (1ull << shift));
+        const uint64_t elements = set.d_lengths[k] >> (type == IV_F32 ? 2 : 1);
+        const uint32_t count = (uint32_t)(elements - e0 < (1ull << w.plan.shift) ? elements - e0 : (1ull << w.plan.shift));
         const uint8_t *in = set.d_base + set.d_offsets[k];
         uint8_t *out = out_base + out_offsets[k];
-        if ((reinterpret_cast<uintptr_t>(out) & (to == IV_F32 ? 3u : 1u)) != 0u) {
+        const bool aligned = (reinterpret_cast<uintptr_t>(out) & (to == IV_F32 ? 3u : 1u)) == 0u;
+        const bool pair = type == to || type == IV_F32 || to == IV_F32;
+        if (!aligned || !pair) {                         // not one 16-bit type to the other
             if (threadIdx.x == 0) atomicMax(status, (uint32_t)IVK_DEV_BOUNDS);
             continue;
         }
-        switch (type * 3 + to) {
+        if constexpr (!std::is_void_v<Tin>) scale_piece<Tin, Tout>(in, out, e0, count, scale);
+        else switch (type * 3 + to) {
             case IV_F32 * 3 + IV_F32: scale_piece<float, float>(in, out, e0, count, scale); break;
             case IV_F32 * 3 + IV_F16: scale_piece<float, __half>(in, out, e0, count, scale); break;
             case IV_F32 * 3 + IV_BF16: scale_piece<float, __nv_bfloat16>(in, out, e0, count, scale); break;
             case IV_F16 * 3 + IV_F32: scale_piece<__half, float>(in, out, e0, count, scale); break;
             case IV_F16 * 3 + IV_F16: scale_piece<__half, __half>(in, out, e0, count, scale); break;
             case IV_BF16 * 3 + IV_F32: scale_piece<__nv_bfloat16, float>(in, out, e0, count, scale); break;
-            case IV_BF16 * 3 + IV_BF16: scale_piece<__nv_bfloat16, __nv_bfloat16>(in, out, e0, count, scale); break;
-            default:
-                if (threadIdx.x == 0) atomicMax(status, (uint32_t)IVK_DEV_BOUNDS);   // one 16-bit type to the other
+            default: scale_piece<__nv_bfloat16, __nv_bfloat16>(in, out, e0, count, scale); break;
         }
     }
 }
 
 uint64_t round256(uint64_t x) { return (x + 255u) & ~255ull; }
 
-struct Plan {
-    PlanHeader *header;
-    uint64_t *first;
-    double *sums;
+// Plan header | first[n + 1] | sums[kPieceTarget + n] | squares[n]
+struct Layout {
+    Plan *header;
+    uint32_t *first;
+    double *sums, *squares;
 };
-Plan plan_at(void *scratch, uint64_t n) {
+Layout layout_at(void *scratch, uint64_t n) {
     uint8_t *p = static_cast<uint8_t *>(scratch);
-    return {reinterpret_cast<PlanHeader *>(p), reinterpret_cast<uint64_t *>(p + 256),
-            reinterpret_cast<double *>(p + 256 + round256(8u * (n + 1u)))};
+    Layout l;
+    l.header = reinterpret_cast<Plan *>(p);
+    p += 256;
+    l.first = reinterpret_cast<uint32_t *>(p);
+    p += round256(4u * (n + 1u));
+    l.sums = reinterpret_cast<double *>(p);
+    p += round256(8u * (kPieceTarget + n));
+    l.squares = reinterpret_cast<double *>(p);
+    return l;
+}
+
+cudaError_t make_plan(const TensorSet &set, const Layout &l, PlanAt *at, size_t *shared, uint32_t *d_status, cudaStream_t stream,
+                      uint64_t *launches) {
+    if (set.n <= kSmallSet) {
+        *at = {nullptr, nullptr};
+        *shared = 4u * (set.n + 1u);
+        return cudaSuccess;
+    }
+    *at = {l.header, l.first};
+    *shared = 0;
+    plan_kernel<<<1, kPlanThreads, 0, stream>>>(set, l.header, l.first, d_status);
+    ++*launches;
+    return cudaGetLastError();
 }
 
 }  // namespace
 
-uint64_t grad_norm_scratch_bytes(uint64_t n) { return 256u + round256(8u * (n + 1u)) + 8u * (kPieceTarget + n); }
+uint64_t grad_norm_scratch_bytes(uint64_t n) { return 256u + round256(4u * (n + 1u)) + round256(8u * (kPieceTarget + n)) + 8u * n; }
+uint64_t grad_norm_arrival_bytes(uint64_t n) { return 4u * (n + 1u); }
 
 cudaError_t launch_grad_norm(const TensorSet &set, bool clip, float max_norm, float *d_norms, iv_norm_result *d_result,
-                             void *d_scratch, uint32_t *d_status, int sm_count, cudaStream_t stream, uint64_t *launches) {
-    const Plan plan = plan_at(d_scratch, set.n);
-    plan_kernel<<<1, kPlanThreads, 0, stream>>>(set, plan.header, plan.first, d_status);
-    norm_kernel<<<sm_count * 8, kNormThreads, 0, stream>>>(set, plan.header, plan.first, plan.sums);
-    finish_kernel<<<1, kFinishThreads, 0, stream>>>(set.n, plan.header, plan.first, plan.sums, clip, max_norm, d_norms,
-                                                    d_result, d_status);
-    *launches += 3;
+                             void *d_scratch, uint32_t *d_arrivals, uint32_t *d_status, int sm_count, cudaStream_t stream,
+                             uint64_t *launches) {
+    const Layout l = layout_at(d_scratch, set.n);
+    PlanAt at;
+    size_t shared;
+    cudaError_t e = make_plan(set, l, &at, &shared, d_status, stream, launches);
+    if (e != cudaSuccess) return e;
+    const NormScratch scratch = {l.sums, l.squares, d_arrivals + 1, d_arrivals};
+    const uint32_t grid = (uint32_t)sm_count * 4u;
+    if (set.d_types) norm_kernel<void><<<grid, kThreads, shared, stream>>>(set, at, scratch, clip, max_norm, d_norms, d_result, d_status);
+    else
+        e = by_types(set.type, set.type, [&](auto in, auto) {
+            norm_kernel<typename decltype(in)::type><<<grid, kThreads, shared, stream>>>(set, at, scratch, clip, max_norm, d_norms, d_result, d_status);
+            return cudaSuccess;
+        });
+    if (e != cudaSuccess) return e;
+    ++*launches;
     return cudaGetLastError();
 }
 
-cudaError_t launch_grad_scale(const TensorSet &set, bool with_plan, const float *d_scale, uint8_t *d_out,
+cudaError_t launch_grad_scale(const TensorSet &set, bool planned, const float *d_scale, uint8_t *d_out,
                               const uint64_t *d_out_offsets, int out_type, void *d_scratch, uint32_t *d_status, int sm_count,
                               cudaStream_t stream, uint64_t *launches) {
     if (set.n == 0) return cudaSuccess;
-    const Plan plan = plan_at(d_scratch, set.n);
-    if (with_plan) {
-        plan_kernel<<<1, kPlanThreads, 0, stream>>>(set, plan.header, plan.first, d_status);
-        ++*launches;
+    const Layout l = layout_at(d_scratch, set.n);
+    PlanAt at;
+    size_t shared;
+    if (planned && set.n > kSmallSet) {
+        at = {l.header, l.first};
+        shared = 0;
+    } else {
+        cudaError_t e = make_plan(set, l, &at, &shared, d_status, stream, launches);
+        if (e != cudaSuccess) return e;
     }
-    scale_kernel<<<sm_count * 8, kNormThreads, 0, stream>>>(set, plan.header, plan.first, d_scale, d_out, d_out_offsets, out_type,
-                                                            d_status);
+    const uint32_t grid = (uint32_t)sm_count * 4u;
+    cudaError_t e = cudaSuccess;
+    if (set.d_types) scale_kernel<void, void><<<grid, kThreads, shared, stream>>>(set, at, d_scale, d_out, d_out_offsets, out_type, d_status);
+    else
+        e = by_types(set.type, out_type < 0 ? set.type : out_type, [&](auto in, auto out) {
+            scale_kernel<typename decltype(in)::type, typename decltype(out)::type><<<grid, kThreads, shared, stream>>>(
+                set, at, d_scale, d_out, d_out_offsets, out_type, d_status);
+            return cudaSuccess;
+        });
+    if (e != cudaSuccess) return e;
     ++*launches;
     return cudaGetLastError();
 }

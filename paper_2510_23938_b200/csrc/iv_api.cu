@@ -57,6 +57,8 @@ struct iv_ctx {
     uint64_t partial_cap = 0;                 // bytes
     uint8_t *d_plan = nullptr;                // pieces and their sums of iv_grad_norm
     uint64_t plan_cap = 0;                    // bytes
+    uint32_t *d_norm_arrivals = nullptr;      // its arrival counters, zero between calls
+    uint64_t norm_arrivals_cap = 0;           // bytes
 
     // streaming windows
     uint8_t *d_digests384 = nullptr;          // chunk digests of iv_verify_manifest_sha384 / _sha512, then the root
@@ -419,6 +421,7 @@ int iv_destroy(iv_ctx *ctx) {
     cudaFree(ctx->d_arrivals);
     cudaFree(ctx->d_partial);
     cudaFree(ctx->d_plan);
+    cudaFree(ctx->d_norm_arrivals);
     cudaFree(ctx->d_tree384[0]);
     cudaFree(ctx->d_tree384[1]);
     cudaFree(ctx->d_window[0]);
@@ -1044,7 +1047,18 @@ int embedding_grad(iv_ctx *ctx, const ivk::EmbeddingGradArgs &a, void *cuda_stre
     return IV_OK;
 }
 
-// The set as the kernels take it, with room for its pieces.
+// Scratch of the norm over n tensors.
+int ensure_norm_scratch(iv_ctx *ctx, uint64_t n, cudaStream_t stream) {
+    int rc = grow(ctx, &ctx->d_plan, &ctx->plan_cap, ivk::grad_norm_scratch_bytes(n), 1);
+    if (rc != IV_OK) return rc;
+    const uint64_t before = ctx->norm_arrivals_cap;
+    rc = grow(ctx, &ctx->d_norm_arrivals, &ctx->norm_arrivals_cap, ivk::grad_norm_arrival_bytes(n), 1);
+    if (rc != IV_OK) return rc;
+    if (ctx->norm_arrivals_cap != before) IV_TRY(ctx, cudaMemsetAsync(ctx->d_norm_arrivals, 0, ctx->norm_arrivals_cap, stream));
+    return IV_OK;
+}
+
+// The set as the kernels take it.
 int tensor_set(iv_ctx *ctx, const void *d_base, const uint64_t *d_offsets, const uint64_t *d_lengths, const uint8_t *d_types,
                int type, uint64_t n, ivk::TensorSet *set) {
     if (n && (!d_base || !d_offsets || !d_lengths)) return IV_ERR_INVALID_ARG;
@@ -1112,9 +1126,10 @@ int iv_grad_norm(iv_ctx *ctx, const void *d_base, const uint64_t *d_offsets, con
     int rc = tensor_set(ctx, d_base, d_offsets, d_lengths, d_types, type, n, &set);
     if (rc != IV_OK) return rc;
     DeviceGuard guard(ctx->device);
-    if ((rc = grow(ctx, &ctx->d_plan, &ctx->plan_cap, ivk::grad_norm_scratch_bytes(n), 1)) != IV_OK) return rc;
-    IV_TRY(ctx, ivk::launch_grad_norm(set, false, 0.f, d_norms, d_result, ctx->d_plan, ctx->d_status, ctx->sm_count,
-                                      static_cast<cudaStream_t>(cuda_stream), &ctx->launches));
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if ((rc = ensure_norm_scratch(ctx, n, stream)) != IV_OK) return rc;
+    IV_TRY(ctx, ivk::launch_grad_norm(set, false, 0.f, d_norms, d_result, ctx->d_plan, ctx->d_norm_arrivals, ctx->d_status,
+                                      ctx->sm_count, stream, &ctx->launches));
     return IV_OK;
 }
 
@@ -1129,10 +1144,10 @@ int iv_grad_clip(iv_ctx *ctx, void *d_base, const uint64_t *d_offsets, const uin
     if (rc != IV_OK) return rc;
     DeviceGuard guard(ctx->device);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if ((rc = grow(ctx, &ctx->d_plan, &ctx->plan_cap, ivk::grad_norm_scratch_bytes(n), 1)) != IV_OK) return rc;
-    IV_TRY(ctx, ivk::launch_grad_norm(set, true, max_norm, d_norms, d_result, ctx->d_plan, ctx->d_status, ctx->sm_count,
-                                      stream, &ctx->launches));
-    IV_TRY(ctx, ivk::launch_grad_scale(set, false, &d_result->scale, d_out ? static_cast<uint8_t *>(d_out) : set.d_base,
+    if ((rc = ensure_norm_scratch(ctx, n, stream)) != IV_OK) return rc;
+    IV_TRY(ctx, ivk::launch_grad_norm(set, true, max_norm, d_norms, d_result, ctx->d_plan, ctx->d_norm_arrivals, ctx->d_status,
+                                      ctx->sm_count, stream, &ctx->launches));
+    IV_TRY(ctx, ivk::launch_grad_scale(set, true, &d_result->scale, d_out ? static_cast<uint8_t *>(d_out) : set.d_base,
                                        d_out ? d_out_offsets : d_offsets, out_type, ctx->d_plan, ctx->d_status, ctx->sm_count,
                                        stream, &ctx->launches));
     return IV_OK;
@@ -1148,7 +1163,7 @@ int iv_grad_scale(iv_ctx *ctx, void *d_base, const uint64_t *d_offsets, const ui
     if (rc != IV_OK) return rc;
     DeviceGuard guard(ctx->device);
     if ((rc = grow(ctx, &ctx->d_plan, &ctx->plan_cap, ivk::grad_norm_scratch_bytes(n), 1)) != IV_OK) return rc;
-    IV_TRY(ctx, ivk::launch_grad_scale(set, true, d_scale, d_out ? static_cast<uint8_t *>(d_out) : set.d_base,
+    IV_TRY(ctx, ivk::launch_grad_scale(set, false, d_scale, d_out ? static_cast<uint8_t *>(d_out) : set.d_base,
                                        d_out ? d_out_offsets : d_offsets, out_type, ctx->d_plan, ctx->d_status, ctx->sm_count,
                                        static_cast<cudaStream_t>(cuda_stream), &ctx->launches));
     return IV_OK;

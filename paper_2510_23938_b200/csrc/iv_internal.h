@@ -261,12 +261,14 @@ struct TensorSet {
     uint64_t n;
 };
 uint64_t grad_norm_scratch_bytes(uint64_t n);
+uint64_t grad_norm_arrival_bytes(uint64_t n);      // words that are zero between calls
 // Norms, result record (scale 1, or what clipping to max_norm asks for when `clip`).
 cudaError_t launch_grad_norm(const TensorSet &set, bool clip, float max_norm, float *d_norms, iv_norm_result *d_result,
-                             void *d_scratch, uint32_t *d_status, int sm_count, cudaStream_t stream, uint64_t *launches);
+                             void *d_scratch, uint32_t *d_arrivals, uint32_t *d_status, int sm_count, cudaStream_t stream,
+                             uint64_t *launches);
 // out tensor k = round(tensor k * *d_scale) at d_out + d_out_offsets[k], of type out_type (< 0: tensor k's own).
-// with_plan: lays out the pieces first (launch_grad_norm has done so for the same set otherwise).
-cudaError_t launch_grad_scale(const TensorSet &set, bool with_plan, const float *d_scale, uint8_t *d_out,
+// planned: launch_grad_norm has just laid out the same set in d_scratch.
+cudaError_t launch_grad_scale(const TensorSet &set, bool planned, const float *d_scale, uint8_t *d_out,
                               const uint64_t *d_out_offsets, int out_type, void *d_scratch, uint32_t *d_status, int sm_count,
                               cudaStream_t stream, uint64_t *launches);
 
