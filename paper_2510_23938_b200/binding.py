@@ -211,8 +211,9 @@ def n_chunks(nbytes: int, chunk_bytes: int) -> int:
 
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    if stream is None:                # the current stream's handle, without a Stream object around it
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream
 
 
 def _dev_ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -231,25 +232,23 @@ def _ptr(t: torch.Tensor) -> int:
     return t.data_ptr()
 
 
-def _row_ptr(t: torch.Tensor) -> int:
-    """Device pointer of a (rows, dim) tensor whose rows are contiguous."""
-    assert t.is_cuda and t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1), "rows must be contiguous CUDA memory"
-    return t.data_ptr()
+def _matrix(t: torch.Tensor) -> tuple:
+    """(device pointer, rows, columns, elements from one row to the next) of a tensor whose rows are contiguous."""
+    assert t.is_cuda, "device tensors must be CUDA tensors"
+    rows, dim = t.shape
+    stride, unit = t.stride()
+    assert unit == 1 or dim <= 1, "rows must be contiguous"
+    return t.data_ptr(), rows, dim, stride if rows > 1 else dim
 
 
-def _stride_of(t: torch.Tensor) -> int:
-    """Elements from one row of a (rows, dim) tensor to the next."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
-
-
-def _rows_of(t: torch.Tensor, n: int, dim: int) -> int:
-    """Checks that `t` is n rows of `dim` elements one fixed stride apart; returns the stride."""
-    assert t.is_cuda and t.numel() == n * dim and t.shape[-1] == dim, "wrong number of rows or columns"
+def _rows_of(t: torch.Tensor, n: int, dim: int) -> tuple:
+    """(device pointer, elements from one row to the next) of n rows of `dim` elements."""
     if t.dim() == 2:
-        assert dim <= 1 or t.stride(1) == 1, "rows must be contiguous"
-        return t.stride(0) if n > 1 else dim
-    assert t.is_contiguous(), "tensors of more than two dimensions must be contiguous"
-    return dim
+        ptr, rows, columns, stride = _matrix(t)
+        assert (rows, columns) == (n, dim), "wrong number of rows or columns"
+        return ptr, stride
+    assert t.is_cuda and t.is_contiguous() and t.numel() == n * dim and t.shape[-1] == dim, "wrong number of rows or columns"
+    return t.data_ptr(), dim
 
 
 def _token_bytes(tokens: torch.Tensor) -> int:
@@ -640,15 +639,16 @@ class Context:
                   out_dtype: torch.dtype | None = None, stream=None) -> torch.Tensor:
         """iv_embedding: scale * table[tokens] (tokens int32 or int64, any shape), rounded once to `out_dtype`
         (default: the table's).  `table` is (rows, dim) with contiguous rows, at any element alignment."""
-        rows, dim = table.shape
+        table_ptr, rows, dim, row_stride = _matrix(table)
         if out is None:
             out = _empty((*tokens.shape, dim), out_dtype or table.dtype, table.device, stream)
         n = tokens.numel()
-        out_stride = _rows_of(out, n, dim)
-        rc = self._lib.iv_embedding(self._h, _row_ptr(table), DTYPES[table.dtype], rows, dim, _stride_of(table),
-                                    _dev_ptr(tokens), _token_bytes(tokens), n, scale, _ptr(out), DTYPES[out.dtype],
-                                    out_stride, _stream_ptr(stream))
-        self._check(rc, "iv_embedding")
+        out_ptr, out_stride = _rows_of(out, n, dim)
+        rc = self._lib.iv_embedding(self._h, table_ptr, DTYPES[table.dtype], rows, dim, row_stride, _dev_ptr(tokens),
+                                    _token_bytes(tokens), n, scale, out_ptr, DTYPES[out.dtype], out_stride,
+                                    _stream_ptr(stream))
+        if rc:
+            self._check(rc, "iv_embedding")
         return out
 
     def embedding_grad(self, grad_out: torch.Tensor, tokens: torch.Tensor, n_rows: int, scale: float = 1.0,
@@ -657,16 +657,18 @@ class Context:
         """iv_embedding_grad: the (n_rows, dim) gradient of `embedding`'s table, `grad_out` (..., dim) being the
         gradient of its result; with `accumulate`, added to `out`."""
         dim, n = grad_out.shape[-1], tokens.numel()
-        grad_stride = _rows_of(grad_out, n, dim)
+        grad_ptr, grad_stride = _rows_of(grad_out, n, dim)
         if out is None:
             assert not accumulate, "accumulate needs the gradient to add to"
             out = _empty((n_rows, dim), out_dtype or grad_out.dtype, grad_out.device, stream)
-        assert out.shape == (n_rows, dim), "out must be (n_rows, dim)"
-        rc = self._lib.iv_embedding_grad(self._h, _ptr(grad_out), DTYPES[grad_out.dtype], grad_stride, dim,
+        out_ptr, out_rows, out_dim, out_stride = _matrix(out)
+        assert (out_rows, out_dim) == (n_rows, dim), "out must be (n_rows, dim)"
+        rc = self._lib.iv_embedding_grad(self._h, grad_ptr, DTYPES[grad_out.dtype], grad_stride, dim,
                                          _dev_ptr(tokens), _token_bytes(tokens), n, n_rows,
-                                         -1 if padding_row is None else padding_row, scale, int(accumulate), _row_ptr(out),
-                                         DTYPES[out.dtype], _stride_of(out), _stream_ptr(stream))
-        self._check(rc, "iv_embedding_grad")
+                                         -1 if padding_row is None else padding_row, scale, accumulate, out_ptr,
+                                         DTYPES[out.dtype], out_stride, _stream_ptr(stream))
+        if rc:
+            self._check(rc, "iv_embedding_grad")
         return out
 
     def embedding_grad_rows(self, grad_out: torch.Tensor, tokens: torch.Tensor, n_rows: int, scale: float = 1.0,
@@ -676,7 +678,7 @@ class Context:
         """iv_embedding_grad_rows: (rows, grad, count) -- the distinct rows ascending (int64, -1 behind them), their
         gradients (zero rows behind them) and their number (int64, on the device).  min(tokens, n_rows) rows in all."""
         dim, n = grad_out.shape[-1], tokens.numel()
-        grad_stride = _rows_of(grad_out, n, dim)
+        grad_ptr, grad_stride = _rows_of(grad_out, n, dim)
         cap = min(n, n_rows) if out is None else out.shape[0]
         if out is None:
             out = _empty((cap, dim), out_dtype or grad_out.dtype, grad_out.device, stream)
@@ -684,14 +686,17 @@ class Context:
             rows = _empty((cap,), torch.int64, grad_out.device, stream)
         if count is None:
             count = _empty((1,), torch.int64, grad_out.device, stream)
-        assert out.shape == (cap, dim) and rows.shape == (cap,) and rows.dtype == count.dtype == torch.int64
-        assert rows.is_cuda and rows.is_contiguous() and count.is_cuda and count.numel() == 1
-        rc = self._lib.iv_embedding_grad_rows(self._h, _ptr(grad_out), DTYPES[grad_out.dtype], grad_stride, dim,
+        out_ptr, _, out_dim, out_stride = _matrix(out)
+        assert out_dim == dim and rows.numel() == cap and rows.dtype == count.dtype == torch.int64 and count.numel() == 1
+        assert rows.is_cuda and rows.is_contiguous() and count.is_cuda
+        count_ptr = count.data_ptr()
+        rc = self._lib.iv_embedding_grad_rows(self._h, grad_ptr, DTYPES[grad_out.dtype], grad_stride, dim,
                                               _dev_ptr(tokens), _token_bytes(tokens), n, n_rows,
                                               -1 if padding_row is None else padding_row, scale,
-                                              rows.data_ptr() or count.data_ptr(), _row_ptr(out), DTYPES[out.dtype],
-                                              _stride_of(out), cap, count.data_ptr(), _stream_ptr(stream))
-        self._check(rc, "iv_embedding_grad_rows")
+                                              rows.data_ptr() or count_ptr, out_ptr, DTYPES[out.dtype], out_stride, cap,
+                                              count_ptr, _stream_ptr(stream))
+        if rc:
+            self._check(rc, "iv_embedding_grad_rows")
         return rows, out, count
 
     def _set_args(self, base, offsets, lengths, dtype, types):

@@ -139,6 +139,12 @@ struct Vector {
     }
 };
 
+// (a0, a1) += (x0^2, x1^2), each rounded as a multiply-add of its own.
+__device__ __forceinline__ void add_squares2(float &a0, float &a1, float x0, float x1) {
+    asm("{\n\t.reg .b64 a, x;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 x, {%2, %3};\n\tfma.rn.f32x2 a, x, x, a;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "+f"(a0), "+f"(a1) : "f"(x0), "f"(x1));
+}
+
 __device__ __forceinline__ uint32_t misalignment(const void *p) { return (uint32_t)reinterpret_cast<uintptr_t>(p) & 15u; }
 
 // V consecutive elements at any element alignment, at once.

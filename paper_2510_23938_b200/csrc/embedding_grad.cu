@@ -116,6 +116,7 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
     constexpr uint32_t kTileKeys = kSortThreads * ITEMS;
     extern __shared__ __align__(16) unsigned char raw_smem[];
     SortShared &s = *reinterpret_cast<SortShared *>(raw_smem);
+    allow_next_kernel();
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t ranks = cluster.num_blocks(), me = cluster.block_rank();
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
@@ -497,7 +498,8 @@ sum_rows_kernel(SumArgs a, SortBuffers b) {
     const uint32_t tile = (blockIdx.y << a.tile_shift) + (warp & ((1u << a.tile_shift) - 1u));
     const uint64_t window = ((uint64_t)blockIdx.x * kSumWarps + warp) >> a.tile_shift;
     if (tile >= a.tiles) return;
-    const uint32_t valid = b.totals[0];
+    wait_for_previous_kernel();
+    const uint32_t valid = *reinterpret_cast<const volatile uint32_t *>(b.totals);
     // this lane's columns: V from col[q], have[q] of them there
     uint32_t col[kParts], have[kParts];
 #pragma unroll
@@ -696,9 +698,9 @@ uint32_t sort_passes(uint64_t n_rows) {
 template <typename Token, uint32_t ITEMS>
 cudaError_t launch_sort(const EmbeddingGradArgs &a, const SortBuffers &b, uint32_t passes, uint32_t *d_status,
                         cudaStream_t stream) {
-    static bool smem_done[kMaxDevices];
+    static bool smem_done[kMaxDevices], cluster_done[kMaxDevices];
     cudaError_t e = ensure_dynamic_smem(sort_tokens_kernel<Token, ITEMS>, sizeof(SortShared), smem_done);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(sort_tokens_kernel<Token, ITEMS>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) e = ensure_large_clusters(sort_tokens_kernel<Token, ITEMS>, cluster_done);
     if (e != cudaSuccess) return e;
     uint32_t ranks = 1;
     while (ranks < kMaxCluster && (uint64_t)ranks * kSortThreads * ITEMS < a.n_tokens) ranks *= 2;
@@ -750,9 +752,9 @@ cudaError_t launch_sums(const EmbeddingGradArgs &a, const SortBuffers &b, cudaSt
     if (blocks > 0x7fffffffull || groups > 65535u) return cudaErrorInvalidConfiguration;   // refused at the entry points
     ++*launches;
     const dim3 grid((uint32_t)blocks, (uint32_t)groups), block(kSumWarps * 32);
-    if (a.d_rows) sum_rows_kernel<Tin, Tout, true, false><<<grid, block, 0, stream>>>(s, b);
-    else if (a.accumulate) sum_rows_kernel<Tin, Tout, false, true><<<grid, block, 0, stream>>>(s, b);
-    else sum_rows_kernel<Tin, Tout, false, false><<<grid, block, 0, stream>>>(s, b);
+    if (a.d_rows) return launch_overlapping(sum_rows_kernel<Tin, Tout, true, false>, grid, block, 0, stream, s, b);
+    if (a.accumulate) return launch_overlapping(sum_rows_kernel<Tin, Tout, false, true>, grid, block, 0, stream, s, b);
+    sum_rows_kernel<Tin, Tout, false, false><<<grid, block, 0, stream>>>(s, b);          // the fill needs the SMs meanwhile
     return cudaGetLastError();
 }
 

@@ -3,8 +3,8 @@
 //     out_k = round(scale * tensor_k)
 //
 // Both passes are bound by memory: two (four) operations per element read.  Tensors of very different sizes are cut
-// into pieces of one size, a power of two that the total size alone decides; a CTA adds up one piece, so the order of
-// every sum is a function of the lengths and not of the launch, the alignment or the GPU: the same gradients give the
+// into pieces of one size, a power of two that the total size alone decides; a CTA adds up one piece, each of its eight
+// warps every eighth run of 32 vectors, without waiting for the others.  So the order of every sum is a function of the lengths and not of the launch, the alignment or the GPU: the same gradients give the
 // same norm bit for bit.  Squares are added in 32 bits inside a thread's share of a piece (64 of them in one accumulator
 // for every 2^16 elements of 32 bits or 2^17 of 16), everything above that in 64 bits.  A piece whose 32-bit sum overflowed or came out so
 // small that squares may have been lost below the smallest 32-bit number is added up again in 64 bits, so any finite
@@ -29,6 +29,8 @@ constexpr uint32_t kWarps = kThreads / 32;
 constexpr uint32_t kMinShift = 13, kMaxShift = 31;      // pieces of 8,192 elements and more
 constexpr uint64_t kPieceTarget = 32768;                // a set has at most this many pieces and one more per tensor
 constexpr uint32_t kSmallSet = 2048;
+constexpr uint32_t kFewPieces = 2048;                   // of a set whose tensors the last CTA adds up on its own
+constexpr uint32_t kPending = 256;                       // pieces a CTA adds up between two barriers, one per thread
 
 __device__ __forceinline__ int type_of(const TensorSet &set, uint64_t k) { return set.d_types ? (int)set.d_types[k] : set.type; }
 
@@ -80,31 +82,40 @@ struct Plan {
     uint32_t live;               // tensors that have pieces
 };
 
-// The set laid out by one CTA: first[k] = number of pieces before tensor k, first[n] = all; thread 0 .. all get the plan.
-template <uint32_t THREADS, typename Index>
-__device__ __forceinline__ Plan lay_out(const TensorSet &set, Index *first, uint64_t *scan, uint32_t *status) {
+// The set laid out by one CTA: first[k] = number of pieces before tensor k, first[n] = all.  A thread takes consecutive
+// tensors; every thread gets the plan.
+template <uint32_t THREADS>
+__device__ __forceinline__ Plan lay_out(const TensorSet &set, uint32_t *first, uint64_t *scan, uint32_t *live_shared, uint32_t *status) {
+    const uint64_t per = (set.n + THREADS - 1) / THREADS;
+    const uint64_t begin = threadIdx.x * per < set.n ? threadIdx.x * per : set.n;
+    const uint64_t end = begin + per < set.n ? begin + per : set.n;
+    if (threadIdx.x == 0) *live_shared = 0u;
     bool bad = false;
     uint64_t elements = 0;
-    for (uint64_t k = threadIdx.x; k < set.n; k += THREADS) elements += elements_of(set, k, bad);
+#pragma unroll 4
+    for (uint64_t k = begin; k < end; ++k) elements += elements_of(set, k, bad);
     Plan plan;
     block_exclusive64<THREADS>(elements, scan, plan.elements);
     plan.shift = shift_for(plan.elements);
-    uint64_t before = 0;
+    auto pieces_of = [&](uint64_t k) { return (elements_of(set, k, bad) + (1ull << plan.shift) - 1) >> plan.shift; };
+    uint64_t pieces = 0;
     uint32_t live = 0;
-    for (uint64_t k0 = 0; k0 < set.n; k0 += THREADS) {
-        const uint64_t k = k0 + threadIdx.x;
-        const uint64_t pieces = k < set.n ? (elements_of(set, k, bad) + (1ull << plan.shift) - 1) >> plan.shift : 0;
-        uint64_t here;
-        const uint64_t at = block_exclusive64<THREADS>(pieces, scan, here);
-        if (k < set.n) first[k] = (Index)(before + at);
-        before += here;
-        live += __syncthreads_count(pieces != 0);
+    for (uint64_t k = begin; k < end; ++k) {
+        const uint64_t here = pieces_of(k);
+        pieces += here;
+        live += here ? 1u : 0u;
+    }
+    live = __reduce_add_sync(0xffffffffu, live);
+    if ((threadIdx.x & 31u) == 0u) atomicAdd(live_shared, live);
+    uint64_t at = block_exclusive64<THREADS>(pieces, scan, plan.pieces);
+    for (uint64_t k = begin; k < end; ++k) {
+        first[k] = (uint32_t)at;
+        at += pieces_of(k);
     }
     if (bad) atomicMax(status, (uint32_t)IVK_DEV_BOUNDS);
-    if (threadIdx.x == 0) first[set.n] = (Index)before;
-    plan.pieces = before;
-    plan.live = live;
+    if (threadIdx.x == 0) first[set.n] = (uint32_t)plan.pieces;
     __syncthreads();
+    plan.live = *live_shared;
     return plan;
 }
 
@@ -113,7 +124,8 @@ constexpr uint32_t kPlanThreads = 1024;
 __global__ void __launch_bounds__(kPlanThreads)
 plan_kernel(TensorSet set, Plan *header, uint32_t *first, uint32_t *status) {
     __shared__ uint64_t scan[kPlanThreads / 32];
-    const Plan plan = lay_out<kPlanThreads>(set, first, scan, status);
+    __shared__ uint32_t live;
+    const Plan plan = lay_out<kPlanThreads>(set, first, scan, &live, status);
     if (threadIdx.x == 0) *header = plan;
 }
 
@@ -142,13 +154,13 @@ __device__ __forceinline__ uint64_t tensor_of(const uint32_t *first, uint64_t n,
     return lo;
 }
 
-__device__ __forceinline__ Walk start_walk(const TensorSet &set, const PlanAt &at, uint32_t *shared_first, uint64_t *scan, uint32_t *status) {
+__device__ __forceinline__ Walk start_walk(const TensorSet &set, const PlanAt &at, uint32_t *shared_first, uint64_t *scan, uint32_t *live, uint32_t *status) {
     Walk w;
     if (at.header) {
         w.plan = *at.header;
         w.first = at.first;
     } else {
-        w.plan = lay_out<kThreads>(set, shared_first, scan, status);
+        w.plan = lay_out<kThreads>(set, shared_first, scan, live, status);
         w.first = shared_first;
     }
     return w;
@@ -185,23 +197,17 @@ __device__ __forceinline__ void add_squares(const T *p, uint32_t vecs, float (&a
             float x[V];
             w.unpack(x);
 #pragma unroll
-            for (int i = 0; i < V; ++i) acc[i] = fmaf(x[i], x[i], acc[i]);
+            for (int i = 0; i < V; i += 2) elem::add_squares2(acc[i], acc[i + 1], x[i], x[i + 1]);
 #pragma unroll
             for (int i = 0; i < elem::Packed<T, V>::kWords; ++i) bits |= w.w[i];
         }
     }
 }
 
-// Two of them take turns, so that one barrier per piece is enough.
-struct PieceShared {
-    double sum[kWarps];
-    uint32_t any[kWarps];
-};
-
-// Sum of squares of `count` elements by the CTA.  An element's place in the piece decides which thread and accumulator
-// it goes to, whatever the alignment.
+// Sum of squares of this warp's share of `count` elements.  An element's place in the piece decides which thread and
+// accumulator it goes to, whatever the alignment.
 template <typename T>
-__device__ __forceinline__ double piece_squares(const T *p, uint32_t count, PieceShared &shared) {
+__device__ __forceinline__ double piece_squares(const T *p, uint32_t count) {
     constexpr int V = 16 / (int)sizeof(T);
     float acc[V];
 #pragma unroll
@@ -215,37 +221,28 @@ __device__ __forceinline__ double piece_squares(const T *p, uint32_t count, Piec
         tail = elem::to_float(p[vecs * V + threadIdx.x]);
         bits |= __float_as_uint(tail);
     }
-    double sum = (double)tail * (double)tail;
+    // the thread's accumulators, then the warp's, in 32 bits; from there on in 64
 #pragma unroll
-    for (int i = 0; i < V; ++i) sum += (double)acc[i];
+    for (int d = V / 2; d; d >>= 1)
+#pragma unroll
+        for (int i = 0; i < d; ++i) acc[i] += acc[i + d];
+    float sum = fmaf(tail, tail, acc[0]);
     bits &= sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
-    // sum over the CTA in a fixed order
 #pragma unroll
     for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    const bool any = __any_sync(0xffffffffu, bits != 0u);
-    if ((threadIdx.x & 31u) == 0u) {
-        shared.sum[threadIdx.x >> 5] = sum;
-        shared.any[threadIdx.x >> 5] = any ? 1u : 0u;
-    }
-    __syncthreads();
-    double total = 0.0;
-    uint32_t some = 0;
-#pragma unroll
-    for (uint32_t w = 0; w < kWarps; ++w) {
-        total += shared.sum[w];
-        some |= shared.any[w];
-    }
     // fine: a finite 32-bit sum that is large against what rounding below the smallest normal number may have cost
     // (each square off by at most 2^-150), or nothing but zeros
-    const bool fine = total < 3e38 && total > 0x1p-90;
-    if (fine || !some) return some ? total : 0.0;
-    double slow = 0.0;
-    for (uint32_t i = threadIdx.x; i < count; i += kThreads) {
-        const double x = (double)elem::to_float(p[i]);
-        slow = fma(x, x, slow);
-    }
-    __syncthreads();                                      // everybody has read `shared`
-    return block_sum(slow, shared.sum);
+    if (sum < 3e38f && sum > 0x1p-90f) return (double)sum;
+    if (!__any_sync(0xffffffffu, bits != 0u)) return 0.0;
+    double slow = (double)tail * (double)tail;
+    for (uint32_t v = threadIdx.x; v < vecs; v += kThreads)
+        for (int i = 0; i < V; ++i) {
+            const double x = (double)elem::to_float(p[(uint64_t)v * V + i]);
+            slow = fma(x, x, slow);
+        }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) slow += __shfl_xor_sync(0xffffffffu, slow, d);
+    return slow;
 }
 
 // Scratch in global memory: sums[pieces], squares[n] of the tensors, arrived[n] pieces and one word for the set (both
@@ -262,18 +259,51 @@ norm_kernel(TensorSet set, PlanAt at, NormScratch scratch, bool clip, float max_
             uint32_t *status) {
     extern __shared__ uint32_t shared_first[];
     __shared__ uint64_t scan[kWarps];
+    __shared__ uint32_t live;
     __shared__ double shared[kWarps];
-    __shared__ PieceShared piece_shared[2];
+    __shared__ double pending[kPending][kWarps];     // of pieces this CTA has added up and not written yet
     __shared__ uint32_t flag;
-    const Walk w = start_walk(set, at, shared_first, scan, status);
+    allow_next_kernel();                                 // the scale kernel may lay out its set
+    const Walk w = start_walk(set, at, shared_first, scan, &live, status);
     const uint32_t *first = w.first;
+    const bool few = w.plan.pieces <= kFewPieces;
     auto finish_set = [&]() {
         double total = 0.0;
         uint32_t bad = 0;
-        for (uint64_t k = threadIdx.x; k < set.n; k += kThreads) {
-            const double s = first[k + 1] != first[k] ? __ldcg(&scratch.squares[k]) : 0.0;
-            bad += isfinite(s) ? 0u : 1u;
-            total += s;
+        if (few) {
+            double *piece_sums = reinterpret_cast<double *>(&pending[0][0]);
+            static_assert(sizeof(pending) >= kFewPieces * sizeof(double), "room for the sums of all pieces");
+#pragma unroll
+            for (uint32_t i = 0; i < kFewPieces / kThreads; ++i) {
+                const uint32_t p = i * kThreads + threadIdx.x;
+                if (p < w.plan.pieces) piece_sums[p] = __ldcg(&scratch.sums[p]);
+            }
+            __syncthreads();
+            auto take = [&](uint64_t k, double s) {
+                if (norms) norms[k] = (float)sqrt(s);
+                bad += isfinite(s) ? 0u : 1u;
+                total += s;
+            };
+            for (uint64_t k = threadIdx.x; k < set.n; k += kThreads) {                 // a thread per small tensor
+                if (first[k + 1] - first[k] > 32u) continue;
+                double s = 0.0;
+                for (uint32_t p = first[k]; p < first[k + 1]; ++p) s += piece_sums[p];
+                take(k, s);
+            }
+            for (uint64_t k = threadIdx.x >> 5; k < set.n; k += kWarps) {              // a warp per large one
+                if (first[k + 1] - first[k] <= 32u) continue;
+                double s = 0.0;
+                for (uint32_t p = first[k] + (threadIdx.x & 31u); p < first[k + 1]; p += 32u) s += piece_sums[p];
+#pragma unroll
+                for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+                if ((threadIdx.x & 31u) == 0u) take(k, s);
+            }
+        } else {
+            for (uint64_t k = threadIdx.x; k < set.n; k += kThreads) {
+                const double s = first[k + 1] != first[k] ? __ldcg(&scratch.squares[k]) : 0.0;
+                bad += isfinite(s) ? 0u : 1u;
+                total += s;
+            }
         }
         total = block_sum(total, shared);
         __syncthreads();
@@ -289,7 +319,7 @@ norm_kernel(TensorSet set, PlanAt at, NormScratch scratch, bool clip, float max_
         }
     };
     if (blockIdx.x == 0) {
-        if (norms)
+        if (norms && !few)
             for (uint64_t k = threadIdx.x; k < set.n; k += kThreads)
                 if (first[k] == first[k + 1]) norms[k] = 0.f;
         if (w.plan.pieces == 0) finish_set();
@@ -299,8 +329,9 @@ norm_kernel(TensorSet set, PlanAt at, NormScratch scratch, bool clip, float max_
     if (range_begin == range_end) return;
     // pieces done of tensor k; true for the CTA whose pieces complete it (and likewise the set)
     auto arrive = [&](uint32_t *counter, uint32_t mine, uint32_t all) {
+        __threadfence();
+        __syncthreads();
         if (threadIdx.x == 0) {
-            __threadfence();
             flag = atomicAdd(counter, mine) + mine == all ? 1u : 0u;
             if (flag) *counter = 0u;
             __threadfence();
@@ -310,6 +341,19 @@ norm_kernel(TensorSet set, PlanAt at, NormScratch scratch, bool clip, float max_
         __syncthreads();
         return last;
     };
+    // the warps' sums of pieces flushed .. end - 1 added up and written
+    uint64_t flushed = 0;
+    auto flush = [&](uint64_t end) {
+        __syncthreads();
+        if (threadIdx.x < (uint32_t)(end - flushed)) {
+            double s = 0.0;
+#pragma unroll
+            for (uint32_t v = 0; v < kWarps; ++v) s += pending[threadIdx.x][v];
+            __stcg(&scratch.sums[flushed + threadIdx.x], s);
+        }
+        flushed = end;
+        __syncthreads();
+    };
     for (uint64_t p = range_begin, k = tensor_of(first, set.n, range_begin); p < range_end; ++k) {
         const uint64_t from = first[k], next = first[k + 1];
         if (p >= next) continue;
@@ -317,18 +361,25 @@ norm_kernel(TensorSet set, PlanAt at, NormScratch scratch, bool clip, float max_
         const uint64_t elements = set.d_lengths[k] >> (type == IV_F32 ? 2 : 1);
         const uint8_t *base = set.d_base + set.d_offsets[k];
         const uint64_t stop = next < range_end ? next : range_end, begin = p;
+        flushed = p;
         for (; p < stop; ++p) {
             const uint64_t e0 = (p - from) << w.plan.shift;
             const uint32_t count = (uint32_t)(elements - e0 < (1ull << w.plan.shift) ? elements - e0 : (1ull << w.plan.shift));
             double sum;
-            if constexpr (!std::is_void_v<T>) sum = piece_squares(reinterpret_cast<const T *>(base) + e0, count, piece_shared[p & 1u]);
-            else if (type == IV_F32) sum = piece_squares(reinterpret_cast<const float *>(base) + e0, count, piece_shared[p & 1u]);
-            else if (type == IV_F16) sum = piece_squares(reinterpret_cast<const __half *>(base) + e0, count, piece_shared[p & 1u]);
-            else sum = piece_squares(reinterpret_cast<const __nv_bfloat16 *>(base) + e0, count, piece_shared[p & 1u]);
-            if (threadIdx.x == 0) __stcg(&scratch.sums[p], sum);
+            if constexpr (!std::is_void_v<T>) sum = piece_squares(reinterpret_cast<const T *>(base) + e0, count);
+            else if (type == IV_F32) sum = piece_squares(reinterpret_cast<const float *>(base) + e0, count);
+            else if (type == IV_F16) sum = piece_squares(reinterpret_cast<const __half *>(base) + e0, count);
+            else sum = piece_squares(reinterpret_cast<const __nv_bfloat16 *>(base) + e0, count);
+            if ((threadIdx.x & 31u) == 0u) pending[p - flushed][threadIdx.x >> 5] = sum;
+            if (p - flushed + 1u == kPending) flush(p + 1u);
         }
-        if (!arrive(&scratch.arrived[k], (uint32_t)(stop - begin), (uint32_t)(next - from))) continue;
+        flush(stop);
+        if (few) continue;
+        if (stop - begin != next - from) {               // a tensor of several CTAs
+            if (!arrive(&scratch.arrived[k], (uint32_t)(stop - begin), (uint32_t)(next - from))) continue;
+        }
         double s = 0.0;
+#pragma unroll 16
         for (uint64_t q = from + threadIdx.x; q < next; q += kThreads) s += __ldcg(&scratch.sums[q]);
         s = block_sum(s, shared);
         if (threadIdx.x == 0) {
@@ -337,6 +388,7 @@ norm_kernel(TensorSet set, PlanAt at, NormScratch scratch, bool clip, float max_
         }
         if (arrive(scratch.arrived_set, 1u, w.plan.live)) finish_set();
     }
+    if (few && arrive(scratch.arrived_set, (uint32_t)(range_end - range_begin), (uint32_t)w.plan.pieces)) finish_set();
 }
 
 template <typename Tin, typename Tout>
@@ -353,8 +405,10 @@ scale_kernel(TensorSet set, PlanAt at, const float *scale_at, uint8_t *out_base,
              uint32_t *status) {
     extern __shared__ uint32_t shared_first[];
     __shared__ uint64_t scan[kWarps];
-    const Walk w = start_walk(set, at, shared_first, scan, status);
-    const float scale = *scale_at;
+    __shared__ uint32_t live;
+    const Walk w = start_walk(set, at, shared_first, scan, &live, status);
+    wait_for_previous_kernel();
+    const float scale = *reinterpret_cast<const volatile float *>(scale_at);
     if (scale == 1.f && out_base == set.d_base && out_offsets == set.d_offsets) return;   // in place, nothing to change
     // backwards: what the norm read last is still in the L2 cache
     for (uint64_t q = blockIdx.x; q < w.plan.pieces; q += gridDim.x) {
@@ -463,12 +517,16 @@ cudaError_t launch_grad_scale(const TensorSet &set, bool planned, const float *d
     }
     const uint32_t grid = (uint32_t)sm_count * 4u;
     cudaError_t e = cudaSuccess;
-    if (set.d_types) scale_kernel<void, void><<<grid, kThreads, shared, stream>>>(set, at, d_scale, d_out, d_out_offsets, out_type, d_status);
+    auto launch = [&](auto kernel) {
+        if (planned) return launch_overlapping(kernel, dim3(grid), dim3(kThreads), shared, stream, set, at, d_scale, d_out, d_out_offsets, out_type, d_status);
+        kernel<<<grid, kThreads, shared, stream>>>(set, at, d_scale, d_out, d_out_offsets, out_type, d_status);
+        return cudaGetLastError();
+    };
+    if (set.d_types) e = launch(scale_kernel<void, void>);
     else
         e = by_types(set.type, out_type < 0 ? set.type : out_type, [&](auto in, auto out) {
-            scale_kernel<typename decltype(in)::type, typename decltype(out)::type><<<grid, kThreads, shared, stream>>>(
-                set, at, d_scale, d_out, d_out_offsets, out_type, d_status);
-            return cudaSuccess;
+            auto kernel = scale_kernel<typename decltype(in)::type, typename decltype(out)::type>;
+            return launch(kernel);
         });
     if (e != cudaSuccess) return e;
     ++*launches;

@@ -23,6 +23,40 @@ inline cudaError_t ensure_dynamic_smem(Kernel kernel, size_t bytes, bool (&done)
     return e;
 }
 
+// Opts a kernel into clusters of 16 CTAs, likewise.
+template <typename Kernel>
+inline cudaError_t ensure_large_clusters(Kernel kernel, bool (&done)[kMaxDevices]) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    if (done[dev]) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) done[dev] = true;
+    return e;
+}
+
+// Launches a kernel that may begin while the one before it on the stream is still running (it was told so by that
+// kernel's allow_next_kernel); everything that depends on the earlier kernel comes after wait_for_previous_kernel.
+template <typename... Params, typename... Args>
+inline cudaError_t launch_overlapping(void (*kernel)(Params...), dim3 grid, dim3 block, size_t shared, cudaStream_t stream, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+#ifdef __CUDACC__
+__device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;"); }
+__device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+#endif
+
 // Device-side status values written to iv_verify_result::status.
 enum : uint32_t { IVK_DEV_OK = 0, IVK_DEV_TIMEOUT = 1, IVK_DEV_BOUNDS = 2 };
 
