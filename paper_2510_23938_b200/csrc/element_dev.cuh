@@ -93,26 +93,29 @@ __device__ __forceinline__ void store_aligned(void *p, const uint32_t *w) {
     }
 }
 
-// V consecutive elements (a multiple of 16 bytes) with the aligned 16-byte pieces of memory they lie in; load() only
-// loads, get() shifts the wanted bytes out, so that several loads can be in flight.  ALIGNED: starts at a piece.
-template <typename T, int V, bool ALIGNED>
+// V consecutive elements (a multiple of 16 bytes) with the aligned pieces of memory they lie in; load() only loads,
+// get() shifts the wanted bytes out, so that several loads can be in flight.  ALIGN: 16 or 8 bytes (tables of weight
+// files: their header is a multiple of 8), which need no shifting; 0 for any element alignment.
+template <typename T, int V, int ALIGN>
 struct Vector {
     static constexpr int W = Packed<T, V>::kWords;
+    static constexpr int kLoaded = ALIGN ? W : W + 4;
     static_assert(W % 4 == 0, "whole pieces of 16 bytes");
-    uint32_t w[ALIGNED ? W : W + 4];
+    uint32_t w[kLoaded];
     __device__ __forceinline__ void load(const T *p, uint32_t off) {
-        const uint8_t *q = reinterpret_cast<const uint8_t *>(p) - (ALIGNED ? 0u : off);
+        const uint8_t *q = reinterpret_cast<const uint8_t *>(p) - (ALIGN ? 0u : off);
+        constexpr int kStep = ALIGN == 8 ? 2 : 4;
 #pragma unroll
-        for (int i = 0; i < (ALIGNED ? W : W + 4); i += 4) load_aligned<4>(q + 4 * i, w + i);
+        for (int i = 0; i < kLoaded; i += kStep) load_aligned<kStep>(q + 4 * i, w + i);
     }
     __device__ __forceinline__ void zero() {
 #pragma unroll
-        for (int i = 0; i < (ALIGNED ? W : W + 4); ++i) w[i] = 0u;
+        for (int i = 0; i < kLoaded; ++i) w[i] = 0u;
     }
-    // `off`: bytes from the piece's start, the same for all lanes that walk one tensor with a stride of whole vectors
+    // `off`: bytes from the 16-byte boundary, the same for all lanes that walk one tensor with a stride of whole vectors
     __device__ __forceinline__ Packed<T, V> get(uint32_t off) const {
         Packed<T, V> out;
-        if constexpr (ALIGNED) {
+        if constexpr (ALIGN != 0) {
 #pragma unroll
             for (int i = 0; i < W; ++i) out.w[i] = w[i];
         } else {
@@ -152,23 +155,23 @@ template <typename T, int V>
 __device__ __forceinline__ void load_any(const T *p, Packed<T, V> &out) {
     const uint32_t off = misalignment(p);
     if (off == 0u) {
-        Vector<T, V, true> x;
+        Vector<T, V, 16> x;
         x.load(p, 0u);
         out = x.get(0u);
     } else {
-        Vector<T, V, false> x;
+        Vector<T, V, 0> x;
         x.load(p, off);
         out = x.get(off);
     }
 }
 
-template <typename Tin, typename Tout, bool ALIGNED, typename F>
+template <typename Tin, typename Tout, int ALIGN, typename F>
 __device__ __forceinline__ void map_vectors(const Tin *in, Tout *out, uint32_t vecs, uint32_t lane, uint32_t lanes, F f) {
     constexpr int V = 16 / (int)(sizeof(Tin) < sizeof(Tout) ? sizeof(Tin) : sizeof(Tout));
-    constexpr int UNROLL = (ALIGNED ? 64 : 32) / (V * (int)sizeof(Tin)); // 64 bytes in flight per thread; 32 where their neighbours come along
+    constexpr int UNROLL = (ALIGN ? 64 : 32) / (V * (int)sizeof(Tin)); // 64 bytes in flight per thread; 32 where their neighbours come along
     const uint32_t off = misalignment(in);
     for (uint32_t v0 = lane; v0 < vecs; v0 += lanes * UNROLL) {
-        Vector<Tin, V, ALIGNED> raw[UNROLL];
+        Vector<Tin, V, ALIGN> raw[UNROLL];
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             const uint32_t v = v0 + u * lanes;
@@ -193,28 +196,27 @@ __device__ __forceinline__ void map_vectors(const Tin *in, Tout *out, uint32_t v
 }
 
 // out[i] = f(in[i]) for i < n by the `lanes` threads (at least 8) of which this is number `lane`, in vectors of 16 bytes
-// of the smaller type.  Both ends start at a 16-byte boundary.
-template <typename Tin, typename Tout, typename F>
+// of the smaller type.  The input starts at a multiple of ALIGN bytes (0: of an element), the output of 16.
+template <typename Tin, typename Tout, int ALIGN, typename F>
 __device__ __forceinline__ void map_aligned(const Tin *in, Tout *out, uint32_t n, uint32_t lane, uint32_t lanes, F f) {
     constexpr int V = 16 / (int)(sizeof(Tin) < sizeof(Tout) ? sizeof(Tin) : sizeof(Tout));
     const uint32_t vecs = n / V, done = vecs * V;
-    map_vectors<Tin, Tout, true>(in, out, vecs, lane, lanes, f);
+    map_vectors<Tin, Tout, ALIGN>(in, out, vecs, lane, lanes, f);
     if (lane < n - done) out[done + lane] = from_float<Tout>(f(to_float(in[done + lane])));
 }
 // The same at any element alignment: single elements up to the first 16-byte boundary of the output.
 template <typename Tin, typename Tout, typename F>
 __device__ __forceinline__ void map_any(const Tin *in, Tout *out, uint32_t n, uint32_t lane, uint32_t lanes, F f) {
-    constexpr int V = 16 / (int)(sizeof(Tin) < sizeof(Tout) ? sizeof(Tin) : sizeof(Tout));
     uint32_t head = ((16u - misalignment(out)) & 15u) / (uint32_t)sizeof(Tout);
     if (head > n) head = n;
     if (lane < head) out[lane] = from_float<Tout>(f(to_float(in[lane])));
     in += head;
     out += head;
     n -= head;
-    const uint32_t vecs = n / V, done = vecs * V;
-    if (misalignment(in) == 0u) map_vectors<Tin, Tout, true>(in, out, vecs, lane, lanes, f);
-    else map_vectors<Tin, Tout, false>(in, out, vecs, lane, lanes, f);
-    if (lane < n - done) out[done + lane] = from_float<Tout>(f(to_float(in[done + lane])));
+    const uint32_t off = misalignment(in);
+    if (off == 0u) map_aligned<Tin, Tout, 16>(in, out, n, lane, lanes, f);
+    else if (off == 8u) map_aligned<Tin, Tout, 8>(in, out, n, lane, lanes, f);
+    else map_aligned<Tin, Tout, 0>(in, out, n, lane, lanes, f);
 }
 
 }  // namespace elem

@@ -13,8 +13,9 @@ namespace {
 constexpr uint32_t kTile = 1024;      // columns per warp: 4 vectors of 8 (16-bit types) or 8 of 4 (32-bit) per lane
 constexpr uint32_t kWarps = 8;
 
-// ALIGNED: every row of the table and of the output starts at a 16-byte boundary.
-template <typename Tin, typename Tout, typename Token, bool ALIGNED>
+// ALIGN: every row of the output starts at a 16-byte boundary and every row of the table at one of ALIGN (16 or 8) bytes;
+// 0: anywhere.
+template <typename Tin, typename Tout, typename Token, int ALIGN>
 __global__ void __launch_bounds__(kWarps * 32)
 embedding_kernel(const Tin *table, uint64_t n_rows, uint64_t dim, uint64_t row_stride, const Token *tokens, uint64_t n_tokens,
                  float scale, Tout *out, uint64_t out_stride, uint32_t tiles, uint32_t *status) {
@@ -30,7 +31,7 @@ embedding_kernel(const Tin *table, uint64_t n_rows, uint64_t dim, uint64_t row_s
         if (row < n_rows) {
             const Tin *in = table + row * row_stride + c0;
             auto scaled = [scale](float x) { return x * scale; };
-            if constexpr (ALIGNED) elem::map_aligned<Tin, Tout>(in, o, cols, lane, 32u, scaled);
+            if constexpr (ALIGN != 0) elem::map_aligned<Tin, Tout, ALIGN>(in, o, cols, lane, 32u, scaled);
             else elem::map_any<Tin, Tout>(in, o, cols, lane, 32u, scaled);
         } else {
             for (uint32_t i = lane; i < cols; i += 32u) o[i] = elem::from_float<Tout>(0.f);
@@ -39,12 +40,12 @@ embedding_kernel(const Tin *table, uint64_t n_rows, uint64_t dim, uint64_t row_s
     }
 }
 
-template <typename Tin, typename Tout, typename Token, bool ALIGNED>
+template <typename Tin, typename Tout, typename Token, int ALIGN>
 cudaError_t launch_instance(const EmbeddingArgs &a, uint32_t *d_status, cudaStream_t stream) {
     const uint32_t tiles = (uint32_t)((a.dim + kTile - 1) / kTile);
     const uint64_t blocks = (a.n_tokens * tiles + kWarps - 1) / kWarps;
     const uint32_t grid = (uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30));
-    embedding_kernel<Tin, Tout, Token, ALIGNED><<<grid, kWarps * 32, 0, stream>>>(
+    embedding_kernel<Tin, Tout, Token, ALIGN><<<grid, kWarps * 32, 0, stream>>>(
         static_cast<const Tin *>(a.d_table), a.n_rows, a.dim, a.row_stride, static_cast<const Token *>(a.d_tokens), a.n_tokens,
         a.scale, static_cast<Tout *>(a.d_out), a.out_stride, tiles, d_status);
     return cudaGetLastError();
@@ -54,8 +55,9 @@ template <typename Tin, typename Tout, typename Token>
 cudaError_t launch_typed(const EmbeddingArgs &a, uint32_t *d_status, cudaStream_t stream) {
     const uintptr_t table = reinterpret_cast<uintptr_t>(a.d_table) | (a.n_rows > 1 ? a.row_stride * sizeof(Tin) : 0u);
     const uintptr_t out = reinterpret_cast<uintptr_t>(a.d_out) | (a.n_tokens > 1 ? a.out_stride * sizeof(Tout) : 0u);
-    return ((table | out) & 15u) == 0u ? launch_instance<Tin, Tout, Token, true>(a, d_status, stream)
-                                       : launch_instance<Tin, Tout, Token, false>(a, d_status, stream);
+    if ((out & 15u) || (table & 7u)) return launch_instance<Tin, Tout, Token, 0>(a, d_status, stream);
+    return table & 15u ? launch_instance<Tin, Tout, Token, 8>(a, d_status, stream)
+                       : launch_instance<Tin, Tout, Token, 16>(a, d_status, stream);
 }
 
 template <typename Tin, typename Tout>

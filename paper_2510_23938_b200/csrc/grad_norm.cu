@@ -179,12 +179,12 @@ __device__ __forceinline__ double block_sum(double x, double *shared) {
 }
 
 // Squares of `vecs` vectors by the CTA, added to acc; the bits that are set anywhere in them added to `bits`.
-template <typename T, int V, bool ALIGNED>
+template <typename T, int V, int ALIGN>
 __device__ __forceinline__ void add_squares(const T *p, uint32_t vecs, float (&acc)[V], uint32_t &bits) {
     constexpr uint32_t kUnroll = 4;
     const uint32_t off = elem::misalignment(p);
     for (uint32_t v0 = threadIdx.x; v0 < vecs; v0 += kThreads * kUnroll) {
-        elem::Vector<T, V, ALIGNED> raw[kUnroll];
+        elem::Vector<T, V, ALIGN> raw[kUnroll];
 #pragma unroll
         for (uint32_t u = 0; u < kUnroll; ++u) {
             const uint32_t v = v0 + u * kThreads;
@@ -214,8 +214,10 @@ __device__ __forceinline__ double piece_squares(const T *p, uint32_t count) {
     for (int i = 0; i < V; ++i) acc[i] = 0.f;
     uint32_t bits = 0;
     const uint32_t vecs = count / V;
-    if (elem::misalignment(p) == 0u) add_squares<T, V, true>(p, vecs, acc, bits);
-    else add_squares<T, V, false>(p, vecs, acc, bits);
+    const uint32_t off = elem::misalignment(p);
+    if (off == 0u) add_squares<T, V, 16>(p, vecs, acc, bits);
+    else if (off == 8u) add_squares<T, V, 8>(p, vecs, acc, bits);
+    else add_squares<T, V, 0>(p, vecs, acc, bits);
     float tail = 0.f;
     if (threadIdx.x < count - vecs * V) {
         tail = elem::to_float(p[vecs * V + threadIdx.x]);
