@@ -93,18 +93,23 @@ __device__ __forceinline__ void store_aligned(void *p, const uint32_t *w) {
     }
 }
 
+__device__ __forceinline__ void store_32_bytes(void *p, const uint32_t *w) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+
 // V consecutive elements (a multiple of 16 bytes) with the aligned pieces of memory they lie in; load() only loads,
 // get() shifts the wanted bytes out, so that several loads can be in flight.  ALIGN: 16 or 8 bytes (tables of weight
 // files: their header is a multiple of 8), which need no shifting; 0 for any element alignment.
 template <typename T, int V, int ALIGN>
 struct Vector {
     static constexpr int W = Packed<T, V>::kWords;
-    static constexpr int kLoaded = ALIGN ? W : W + 4;
-    static_assert(W % 4 == 0, "whole pieces of 16 bytes");
+    static constexpr int P = W % 4 == 0 ? 4 : 2;                          // words of an aligned piece: 16 bytes, or 8 of a vector of 8
+    static constexpr int kLoaded = ALIGN ? W : W + P;
     uint32_t w[kLoaded];
     __device__ __forceinline__ void load(const T *p, uint32_t off) {
-        const uint8_t *q = reinterpret_cast<const uint8_t *>(p) - (ALIGN ? 0u : off);
-        constexpr int kStep = ALIGN == 8 ? 2 : 4;
+        const uint8_t *q = reinterpret_cast<const uint8_t *>(p) - (ALIGN ? 0u : off & (4u * P - 1u));
+        constexpr int kStep = ALIGN == 8 ? 2 : P;
 #pragma unroll
         for (int i = 0; i < kLoaded; i += kStep) load_aligned<kStep>(q + 4 * i, w + i);
     }
@@ -121,8 +126,8 @@ struct Vector {
         } else {
             uint32_t x[W + 4];
 #pragma unroll
-            for (int i = 0; i < W + 4; ++i) x[i] = w[i];
-            if (off & 8u) {
+            for (int i = 0; i < W + 4; ++i) x[i] = i < kLoaded ? w[i] : 0u;
+            if (P == 4 && (off & 8u)) {
 #pragma unroll
                 for (int i = 0; i < W + 2; ++i) x[i] = x[i + 2];
             }
@@ -165,9 +170,17 @@ __device__ __forceinline__ void load_any(const T *p, Packed<T, V> &out) {
     }
 }
 
+// Elements per vector of a map.  Widening: 8 bytes in, 16 out, so that a warp's stores are contiguous (two 16-byte stores
+// 32 bytes apart from lane to lane write half sectors: 284 against 240 us for 65,536 rows of 4096); narrowing: 32 in, 16 out (loads that
+// share sectors meet in L1).
+template <typename Tin, typename Tout>
+struct MapShape {
+    static constexpr int V = sizeof(Tout) == 4 ? 4 : 8;
+};
+
 template <typename Tin, typename Tout, int ALIGN, typename F>
 __device__ __forceinline__ void map_vectors(const Tin *in, Tout *out, uint32_t vecs, uint32_t lane, uint32_t lanes, F f) {
-    constexpr int V = 16 / (int)(sizeof(Tin) < sizeof(Tout) ? sizeof(Tin) : sizeof(Tout));
+    constexpr int V = MapShape<Tin, Tout>::V;
     constexpr int UNROLL = (ALIGN ? 64 : 32) / (V * (int)sizeof(Tin)); // 64 bytes in flight per thread; 32 where their neighbours come along
     const uint32_t off = misalignment(in);
     for (uint32_t v0 = lane; v0 < vecs; v0 += lanes * UNROLL) {
@@ -195,11 +208,11 @@ __device__ __forceinline__ void map_vectors(const Tin *in, Tout *out, uint32_t v
     }
 }
 
-// out[i] = f(in[i]) for i < n by the `lanes` threads (at least 8) of which this is number `lane`, in vectors of 16 bytes
-// of the smaller type.  The input starts at a multiple of ALIGN bytes (0: of an element), the output of 16.
+// out[i] = f(in[i]) for i < n by the `lanes` threads (at least 8) of which this is number `lane`, in vectors.
+// The input starts at a multiple of ALIGN bytes (0: of an element), the output of 16.
 template <typename Tin, typename Tout, int ALIGN, typename F>
 __device__ __forceinline__ void map_aligned(const Tin *in, Tout *out, uint32_t n, uint32_t lane, uint32_t lanes, F f) {
-    constexpr int V = 16 / (int)(sizeof(Tin) < sizeof(Tout) ? sizeof(Tin) : sizeof(Tout));
+    constexpr int V = MapShape<Tin, Tout>::V;
     const uint32_t vecs = n / V, done = vecs * V;
     map_vectors<Tin, Tout, ALIGN>(in, out, vecs, lane, lanes, f);
     if (lane < n - done) out[done + lane] = from_float<Tout>(f(to_float(in[done + lane])));

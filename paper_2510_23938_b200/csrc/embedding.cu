@@ -2,7 +2,8 @@
 //
 // A gather of rows: what bounds it is memory (the distinct rows read once, every output row written once), for a few
 // tokens the latency of the chain token -> row -> store.  A warp takes one tile of kTile columns of one token, so that
-// a single token's row is spread over several warps and every lane has four vector loads in flight.
+// a single token's row is spread over several warps and every lane has four vector loads in flight; rows of few
+// columns are taken by a half or a quarter of a warp.
 #include "element_dev.cuh"
 #include "iv_internal.h"
 
@@ -16,25 +17,27 @@ constexpr uint32_t kWarps = 8;
 // ALIGN: every row of the output starts at a 16-byte boundary and every row of the table at one of ALIGN (16 or 8) bytes;
 // 0: anywhere.
 template <typename Tin, typename Tout, typename Token, int ALIGN>
-__global__ void __launch_bounds__(kWarps * 32)
+__global__ void __launch_bounds__(kWarps * 32, ALIGN ? 6 : 4)
 embedding_kernel(const Tin *table, uint64_t n_rows, uint64_t dim, uint64_t row_stride, const Token *tokens, uint64_t n_tokens,
-                 float scale, Tout *out, uint64_t out_stride, uint32_t tiles, uint32_t *status) {
-    const uint32_t lane = threadIdx.x & 31u;
+                 float scale, Tout *out, uint64_t out_stride, uint32_t tiles, uint32_t lanes, uint32_t *status) {
+    const uint32_t lane = threadIdx.x & (lanes - 1u), teams = kWarps * 32u / lanes;
     const uint64_t units = n_tokens * tiles;
-    for (uint64_t unit = (uint64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); unit < units;
-         unit += (uint64_t)gridDim.x * kWarps) {
-        const uint64_t t = unit / tiles;
-        const uint64_t c0 = (unit - t * tiles) * kTile;
+    for (uint64_t unit = (uint64_t)blockIdx.x * teams + threadIdx.x / lanes; unit < units; unit += (uint64_t)gridDim.x * teams) {
+        uint64_t t = unit, c0 = 0;
+        if (tiles > 1u) {
+            t = unit / tiles;
+            c0 = (unit - t * tiles) * kTile;
+        }
         const uint32_t cols = (uint32_t)(dim - c0 < kTile ? dim - c0 : kTile);
         const uint64_t row = (uint64_t)(int64_t)tokens[t];       // a negative token becomes a large number
         Tout *o = out + t * out_stride + c0;
         if (row < n_rows) {
             const Tin *in = table + row * row_stride + c0;
             auto scaled = [scale](float x) { return x * scale; };
-            if constexpr (ALIGN != 0) elem::map_aligned<Tin, Tout, ALIGN>(in, o, cols, lane, 32u, scaled);
-            else elem::map_any<Tin, Tout>(in, o, cols, lane, 32u, scaled);
+            if constexpr (ALIGN != 0) elem::map_aligned<Tin, Tout, ALIGN>(in, o, cols, lane, lanes, scaled);
+            else elem::map_any<Tin, Tout>(in, o, cols, lane, lanes, scaled);
         } else {
-            for (uint32_t i = lane; i < cols; i += 32u) o[i] = elem::from_float<Tout>(0.f);
+            for (uint32_t i = lane; i < cols; i += lanes) o[i] = elem::from_float<Tout>(0.f);
             if (lane == 0 && c0 == 0) atomicMax(status, (uint32_t)IVK_DEV_BOUNDS);
         }
     }
@@ -43,11 +46,14 @@ embedding_kernel(const Tin *table, uint64_t n_rows, uint64_t dim, uint64_t row_s
 template <typename Tin, typename Tout, typename Token, int ALIGN>
 cudaError_t launch_instance(const EmbeddingArgs &a, uint32_t *d_status, cudaStream_t stream) {
     const uint32_t tiles = (uint32_t)((a.dim + kTile - 1) / kTile);
-    const uint64_t blocks = (a.n_tokens * tiles + kWarps - 1) / kWarps;
+    const uint64_t vectors = a.dim / elem::MapShape<Tin, Tout>::V;
+    const uint32_t lanes = vectors <= 8u ? 8u : vectors <= 16u ? 16u : 32u;      // at least 8: single elements at a row's ends
+    const uint32_t teams = kWarps * 32u / lanes;
+    const uint64_t blocks = (a.n_tokens * tiles + teams - 1) / teams;
     const uint32_t grid = (uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30));
     embedding_kernel<Tin, Tout, Token, ALIGN><<<grid, kWarps * 32, 0, stream>>>(
         static_cast<const Tin *>(a.d_table), a.n_rows, a.dim, a.row_stride, static_cast<const Token *>(a.d_tokens), a.n_tokens,
-        a.scale, static_cast<Tout *>(a.d_out), a.out_stride, tiles, d_status);
+        a.scale, static_cast<Tout *>(a.d_out), a.out_stride, tiles, lanes, d_status);
     return cudaGetLastError();
 }
 

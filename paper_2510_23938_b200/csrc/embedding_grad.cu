@@ -438,7 +438,11 @@ __device__ __forceinline__ void load_cols(const T *p, uint32_t have, float (&v)[
 template <typename T, uint32_t V>
 __device__ __forceinline__ void store_cols(T *p, uint32_t have, const float (&v)[V]) {
     constexpr uint32_t W = 16 / sizeof(T) < V ? 16 / sizeof(T) : V;
-    if (have == V && (reinterpret_cast<uintptr_t>(p) & (W * sizeof(T) - 1u)) == 0u) {
+    if (V * sizeof(T) == 32 && have == V && (reinterpret_cast<uintptr_t>(p) & 31u) == 0u) {     // whole sectors at once
+        elem::Packed<T, (int)V> x;
+        x.pack(v);
+        elem::store_32_bytes(p, x.w);
+    } else if (have == V && (reinterpret_cast<uintptr_t>(p) & (W * sizeof(T) - 1u)) == 0u) {
 #pragma unroll
         for (uint32_t i = 0; i < V; i += W) {
             elem::Packed<T, (int)W> x;
