@@ -100,18 +100,21 @@ __device__ __forceinline__ void store_32_bytes(void *p, const uint32_t *w) {
 
 // V consecutive elements (a multiple of 16 bytes) with the aligned pieces of memory they lie in; load() only loads,
 // get() shifts the wanted bytes out, so that several loads can be in flight.  ALIGN: 16 or 8 bytes (tables of weight
-// files: their header is a multiple of 8), which need no shifting; 0 for any element alignment.
+// files: their header is a multiple of 8), which need no shifting; 0 for any other element alignment; kAny for all of
+// them (nothing of the last piece is wanted, and it is not touched, when the vector starts at a piece).
+constexpr int kAny = -1;
 template <typename T, int V, int ALIGN>
 struct Vector {
     static constexpr int W = Packed<T, V>::kWords;
     static constexpr int P = W % 4 == 0 ? 4 : 2;                          // words of an aligned piece: 16 bytes, or 8 of a vector of 8
-    static constexpr int kLoaded = ALIGN ? W : W + P;
+    static constexpr int kLoaded = ALIGN > 0 ? W : W + P;
     uint32_t w[kLoaded];
     __device__ __forceinline__ void load(const T *p, uint32_t off) {
-        const uint8_t *q = reinterpret_cast<const uint8_t *>(p) - (ALIGN ? 0u : off & (4u * P - 1u));
+        const uint8_t *q = reinterpret_cast<const uint8_t *>(p) - (ALIGN > 0 ? 0u : off & (4u * P - 1u));
         constexpr int kStep = ALIGN == 8 ? 2 : P;
 #pragma unroll
-        for (int i = 0; i < kLoaded; i += kStep) load_aligned<kStep>(q + 4 * i, w + i);
+        for (int i = 0; i < kLoaded; i += kStep)
+            if (i < W || ALIGN == 0 || off) load_aligned<kStep>(q + 4 * i, w + i);
     }
     __device__ __forceinline__ void zero() {
 #pragma unroll
@@ -120,7 +123,7 @@ struct Vector {
     // `off`: bytes from the 16-byte boundary, the same for all lanes that walk one tensor with a stride of whole vectors
     __device__ __forceinline__ Packed<T, V> get(uint32_t off) const {
         Packed<T, V> out;
-        if constexpr (ALIGN != 0) {
+        if constexpr (ALIGN > 0) {
 #pragma unroll
             for (int i = 0; i < W; ++i) out.w[i] = w[i];
         } else {
@@ -181,7 +184,10 @@ struct MapShape {
 template <typename Tin, typename Tout, int ALIGN, typename F>
 __device__ __forceinline__ void map_vectors(const Tin *in, Tout *out, uint32_t vecs, uint32_t lane, uint32_t lanes, F f) {
     constexpr int V = MapShape<Tin, Tout>::V;
-    constexpr int UNROLL = (ALIGN ? 64 : 32) / (V * (int)sizeof(Tin)); // 64 bytes in flight per thread; 32 where their neighbours come along
+    // bytes in flight per thread: 64, or 32 and their neighbours; one vector in the form for all alignments, where more
+    // warps serve better than more registers (65,536 rows of 4095 16-bit columns: 150 us with 32 registers, 215 with 64)
+    constexpr int kBytes = V * (int)sizeof(Tin), kFlight = ALIGN > 0 ? 64 : ALIGN == 0 ? 32 : 16;
+    constexpr int UNROLL = kBytes < kFlight ? kFlight / kBytes : 1;
     const uint32_t off = misalignment(in);
     for (uint32_t v0 = lane; v0 < vecs; v0 += lanes * UNROLL) {
         Vector<Tin, V, ALIGN> raw[UNROLL];
@@ -217,8 +223,9 @@ __device__ __forceinline__ void map_aligned(const Tin *in, Tout *out, uint32_t n
     map_vectors<Tin, Tout, ALIGN>(in, out, vecs, lane, lanes, f);
     if (lane < n - done) out[done + lane] = from_float<Tout>(f(to_float(in[done + lane])));
 }
-// The same at any element alignment: single elements up to the first 16-byte boundary of the output.
-template <typename Tin, typename Tout, typename F>
+// Both at any element alignment: single elements up to the first 16-byte boundary of the output.  BY_CLASS: one loop for
+// each class of alignment (few spans with their own alignment), else one for all.
+template <typename Tin, typename Tout, bool BY_CLASS, typename F>
 __device__ __forceinline__ void map_any(const Tin *in, Tout *out, uint32_t n, uint32_t lane, uint32_t lanes, F f) {
     uint32_t head = ((16u - misalignment(out)) & 15u) / (uint32_t)sizeof(Tout);
     if (head > n) head = n;
@@ -226,10 +233,14 @@ __device__ __forceinline__ void map_any(const Tin *in, Tout *out, uint32_t n, ui
     in += head;
     out += head;
     n -= head;
-    const uint32_t off = misalignment(in);
-    if (off == 0u) map_aligned<Tin, Tout, 16>(in, out, n, lane, lanes, f);
-    else if (off == 8u) map_aligned<Tin, Tout, 8>(in, out, n, lane, lanes, f);
-    else map_aligned<Tin, Tout, 0>(in, out, n, lane, lanes, f);
+    if constexpr (BY_CLASS) {
+        const uint32_t off = misalignment(in);
+        if (off == 0u) map_aligned<Tin, Tout, 16>(in, out, n, lane, lanes, f);
+        else if (off == 8u) map_aligned<Tin, Tout, 8>(in, out, n, lane, lanes, f);
+        else map_aligned<Tin, Tout, 0>(in, out, n, lane, lanes, f);
+    } else {
+        map_aligned<Tin, Tout, kAny>(in, out, n, lane, lanes, f);
+    }
 }
 
 }  // namespace elem

@@ -17,7 +17,7 @@ constexpr uint32_t kWarps = 8;
 // ALIGN: every row of the output starts at a 16-byte boundary and every row of the table at one of ALIGN (16 or 8) bytes;
 // 0: anywhere.
 template <typename Tin, typename Tout, typename Token, int ALIGN>
-__global__ void __launch_bounds__(kWarps * 32, ALIGN ? 6 : 4)
+__global__ void __launch_bounds__(kWarps * 32, ALIGN ? 6 : 8)
 embedding_kernel(const Tin *table, uint64_t n_rows, uint64_t dim, uint64_t row_stride, const Token *tokens, uint64_t n_tokens,
                  float scale, Tout *out, uint64_t out_stride, uint32_t tiles, uint32_t lanes, uint32_t *status) {
     const uint32_t lane = threadIdx.x & (lanes - 1u), teams = kWarps * 32u / lanes;
@@ -35,7 +35,7 @@ embedding_kernel(const Tin *table, uint64_t n_rows, uint64_t dim, uint64_t row_s
             const Tin *in = table + row * row_stride + c0;
             auto scaled = [scale](float x) { return x * scale; };
             if constexpr (ALIGN != 0) elem::map_aligned<Tin, Tout, ALIGN>(in, o, cols, lane, lanes, scaled);
-            else elem::map_any<Tin, Tout>(in, o, cols, lane, lanes, scaled);
+            else elem::map_any<Tin, Tout, false>(in, o, cols, lane, lanes, scaled);
         } else {
             for (uint32_t i = lane; i < cols; i += lanes) o[i] = elem::from_float<Tout>(0.f);
             if (lane == 0 && c0 == 0) atomicMax(status, (uint32_t)IVK_DEV_BOUNDS);

@@ -397,7 +397,7 @@ template <typename Tin, typename Tout>
 __device__ __forceinline__ void scale_piece(const uint8_t *in8, uint8_t *out8, uint64_t e0, uint32_t count, float scale) {
     const Tin *in = reinterpret_cast<const Tin *>(in8) + e0;
     Tout *out = reinterpret_cast<Tout *>(out8) + e0;
-    elem::map_any<Tin, Tout>(in, out, count, threadIdx.x, kThreads, [scale](float x) { return x * scale; });
+    elem::map_any<Tin, Tout, true>(in, out, count, threadIdx.x, kThreads, [scale](float x) { return x * scale; });
 }
 
 // Tin, Tout: the types of all tensors, void for a set of several types.
