@@ -416,11 +416,11 @@ template <typename T> struct Tile {
     static constexpr uint32_t kCols = kParts * 32 * V;            // columns per warp: 512 (16-bit types) or 256
 };
 
-// V columns of type T, `have` of them: the rest reads as zero and is not written.
+// V columns of type T of which from .. to - 1 are there: the rest reads as zero and is not written.
 template <typename T, uint32_t V>
-__device__ __forceinline__ void load_cols(const T *p, uint32_t have, float (&v)[V]) {
+__device__ __forceinline__ void load_cols(const T *p, uint32_t from, uint32_t to, float (&v)[V]) {
     constexpr uint32_t W = 16 / sizeof(T);                               // 16 bytes at a time
-    if (V % W == 0 && have == V) {
+    if (V % W == 0 && to - from == V) {
 #pragma unroll
         for (uint32_t i = 0; i + W <= V; i += W) {
             elem::Packed<T, (int)W> x;
@@ -432,17 +432,18 @@ __device__ __forceinline__ void load_cols(const T *p, uint32_t have, float (&v)[
         }
     } else {
 #pragma unroll
-        for (uint32_t i = 0; i < V; ++i) v[i] = i < have ? elem::to_float(p[i]) : 0.f;
+        for (uint32_t i = 0; i < V; ++i) v[i] = i >= from && i < to ? elem::to_float(p[i]) : 0.f;
     }
 }
 template <typename T, uint32_t V>
-__device__ __forceinline__ void store_cols(T *p, uint32_t have, const float (&v)[V]) {
+__device__ __forceinline__ void store_cols(T *p, uint32_t from, uint32_t to, const float (&v)[V]) {
     constexpr uint32_t W = 16 / sizeof(T) < V ? 16 / sizeof(T) : V;
-    if (V * sizeof(T) == 32 && have == V && (reinterpret_cast<uintptr_t>(p) & 31u) == 0u) {     // whole sectors at once
+    const bool whole = to - from == V;
+    if (V * sizeof(T) == 32 && whole && (reinterpret_cast<uintptr_t>(p) & 31u) == 0u) {         // whole sectors at once
         elem::Packed<T, (int)V> x;
         x.pack(v);
         elem::store_32_bytes(p, x.w);
-    } else if (have == V && (reinterpret_cast<uintptr_t>(p) & (W * sizeof(T) - 1u)) == 0u) {
+    } else if (whole && (reinterpret_cast<uintptr_t>(p) & (W * sizeof(T) - 1u)) == 0u) {
 #pragma unroll
         for (uint32_t i = 0; i < V; i += W) {
             elem::Packed<T, (int)W> x;
@@ -455,7 +456,7 @@ __device__ __forceinline__ void store_cols(T *p, uint32_t have, const float (&v)
     } else {
 #pragma unroll
         for (uint32_t i = 0; i < V; ++i)
-            if (i < have) p[i] = elem::from_float<T>(v[i]);
+            if (i >= from && i < to) p[i] = elem::from_float<T>(v[i]);
     }
 }
 
@@ -481,7 +482,6 @@ struct SumArgs {
     uint64_t out_stride;
     float scale;
     uint32_t tiles, tile_shift;
-    bool aligned;          // every row of grad_out starts at a multiple of 16 bytes
     int64_t *rows;         // compact form: row numbers and how many rows there is room for
     uint64_t cap;
 };
@@ -492,11 +492,15 @@ __device__ __forceinline__ uint32_t slot_of(uint32_t piece_begin, bool first_of_
     return 2u * (piece_begin / kPiece) + (first_of_row ? 1u : 0u);
 }
 
-template <typename Tin, typename Tout, bool COMPACT, bool ADD>
+// ALIGNED: every row of grad_out and of the output starts at a 16-byte boundary.  Otherwise a lane's columns are moved
+// back to where the output row has one, so that stores stay whole vectors, and the input is staged in its own
+// 16-byte pieces, from which a lane picks its bytes.
+template <typename Tin, typename Tout, bool COMPACT, bool ADD, bool ALIGNED>
 __global__ void __launch_bounds__(kSumWarps * 32, 6)
 sum_rows_kernel(SumArgs a, SortBuffers b) {
     constexpr uint32_t V = Tile<Tin>::V, kCols = Tile<Tin>::kCols;
-    __shared__ __align__(16) uint4 ring[kSumWarps][2][kStageRows][kParts][32];             // a lane reads back its own copies only
+    constexpr uint32_t kRowPieces = ALIGNED ? kParts * 32u : kParts * 32u + 4u;            // 16-byte pieces of a staged row
+    __shared__ __align__(16) uint4 ring[kSumWarps][2][kStageRows][kRowPieces];
     // a CTA's warps take consecutive tiles of one window, or, where a row has fewer tiles, several windows
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint32_t tile = (blockIdx.y << a.tile_shift) + (warp & ((1u << a.tile_shift) - 1u));
@@ -504,30 +508,36 @@ sum_rows_kernel(SumArgs a, SortBuffers b) {
     if (tile >= a.tiles) return;
     wait_for_previous_kernel();
     const uint32_t valid = *reinterpret_cast<const volatile uint32_t *>(b.totals);
-    // this lane's columns: V from col[q], have[q] of them there
-    uint32_t col[kParts], have[kParts];
-#pragma unroll
-    for (uint32_t q = 0; q < kParts; ++q) {
-        col[q] = tile * kCols + (q * 32u + lane) * V;
-        have[q] = col[q] < a.dim ? (a.dim - col[q] < V ? (uint32_t)(a.dim - col[q]) : V) : 0u;
-    }
     Tout *out = static_cast<Tout *>(a.out);
+
+    // this lane's columns in part q: V from col(q), of which [from(q), to(q)) are there; back: how far they are moved
+    constexpr uint32_t kUnit = V * sizeof(Tout) < 16u ? V * (uint32_t)sizeof(Tout) : 16u;  // bytes of an aligned store
+    uint32_t back = 0;
+    auto moved = [&](const Tout *row) { return ALIGNED ? 0u : ((uint32_t)reinterpret_cast<uintptr_t>(row) & (kUnit - 1u)) / (uint32_t)sizeof(Tout); };
+    auto col = [&](uint32_t q) { return (int32_t)(tile * kCols + (q * 32u + lane) * V) - (int32_t)back; };
+    auto from = [&](uint32_t q) { return !ALIGNED && col(q) < 0 ? (uint32_t)-col(q) : 0u; };
+    auto to = [&](uint32_t q) {
+        const int32_t left = (int32_t)a.dim - col(q);
+        return left >= (int32_t)V ? V : left > 0 ? (uint32_t)left : 0u;
+    };
 
     if (COMPACT) {                                      // what lies behind the last distinct row: number -1, gradient zero
         const float zero[V] = {};
         const uint64_t distinct = b.totals[1];
         for (uint64_t r = window * kWindow > distinct ? window * kWindow : distinct; r < (window + 1) * kWindow && r < a.cap; ++r) {
             if (tile == 0 && lane == 0) a.rows[r] = -1;
+            Tout *o = out + r * a.out_stride;
+            back = moved(o);
 #pragma unroll
             for (uint32_t q = 0; q < kParts; ++q)
-                if (have[q]) store_cols<Tout, V>(out + r * a.out_stride + col[q], have[q], zero);
+                if (to(q) > from(q)) store_cols<Tout, V>(o + col(q), from(q), to(q), zero);
         }
     }
     if (window * kWindow >= valid) return;
     const uint32_t w0 = (uint32_t)window * kWindow, w1 = valid - w0 < kWindow ? valid : w0 + kWindow;
     const Tin *g = static_cast<const Tin *>(a.grad_out);
 
-    uint4 *mine = &ring[warp][0][0][0][lane];
+    uint4 *stages = &ring[warp][0][0][0];
     float acc[kParts][V];
     bool open = false;                                  // a piece of ours is being added up
     uint32_t begin = 0, row_start = 0, row_number = 0, row = 0;
@@ -536,17 +546,17 @@ sum_rows_kernel(SumArgs a, SortBuffers b) {
         Tout *o = out + (uint64_t)(COMPACT ? row_number : row) * a.out_stride;
 #pragma unroll
         for (uint32_t q = 0; q < kParts; ++q) {
-            if (have[q] == 0u) continue;
+            if (to(q) <= from(q)) continue;
             float v[V];
             if (ADD) {
-                load_cols<Tout, V>(o + col[q], have[q], v);
+                load_cols<Tout, V>(o + col(q), from(q), to(q), v);
 #pragma unroll
                 for (uint32_t i = 0; i < V; ++i) v[i] = fmaf(a.scale, sum[q][i], v[i]);
             } else {
 #pragma unroll
                 for (uint32_t i = 0; i < V; ++i) v[i] = a.scale * sum[q][i];
             }
-            store_cols<Tout, V>(o + col[q], have[q], v);
+            store_cols<Tout, V>(o + col(q), from(q), to(q), v);
         }
     };
     auto partial = [&](uint32_t slot, uint32_t q) {
@@ -617,49 +627,49 @@ sum_rows_kernel(SumArgs a, SortBuffers b) {
         const uint32_t begins = __ballot_sync(0xffffffffu, (i - rec.y) % kPiece == 0u);
         const uint32_t row_begins = __ballot_sync(0xffffffffu, i == rec.y);
         // ours: from the first piece that begins in the window to the first that begins behind it
-        uint32_t from = 0, to = 32u;
+        uint32_t first = 0, last = 32u;
         if (!open) {
-            from = begins ? __ffs(begins) - 1u : 32u;
-            if (i0 + from >= w1) return;
+            first = begins ? __ffs(begins) - 1u : 32u;
+            if (i0 + first >= w1) return;
         }
         const uint32_t inside = w1 > i0 ? w1 - i0 : 0u;
         const uint32_t behind = inside < 32u ? begins >> inside << inside : 0u;
-        if (behind) to = __ffs(behind) - 1u;
+        if (behind) last = __ffs(behind) - 1u;
         // rows j .. j + kStageRows - 1 of them into a stage of the ring
         const uint64_t my_row = reinterpret_cast<uint64_t>(g) + (uint64_t)rec.x * a.grad_stride * sizeof(Tin);
         auto fetch = [&](uint32_t j, uint32_t stage) {
-            uint4 *dst = mine + stage * (kStageRows * kParts * 32u);
+            uint4 *dst = stages + stage * (kStageRows * kRowPieces) + lane;
+            if (!ALIGNED) __syncwarp();                 // everybody has read what lies there
 #pragma unroll
             for (uint32_t u = 0; u < kStageRows; ++u) {
-                const uint64_t src = __shfl_sync(0xffffffffu, my_row, (j + u) & 31u) + col[0] * sizeof(Tin);
-                if (j + u < to) {
-                    if (a.aligned) {
-                        const uint32_t shared = tma::smem_u32(dst + u * kParts * 32u);
-                        if (have[0]) copy_async16<0, 0>(shared, src, have[0] * (uint32_t)sizeof(Tin));
-                        if (have[1]) copy_async16<512, 512>(shared, src, have[1] * (uint32_t)sizeof(Tin));
+                const uint64_t src = __shfl_sync(0xffffffffu, my_row, (j + u) & 31u);
+                if (j + u < last) {
+                    const uint32_t shared = tma::smem_u32(dst + u * kRowPieces);
+                    if constexpr (ALIGNED) {
+                        if (to(0)) copy_async16<0, 0>(shared, src + col(0) * (int32_t)sizeof(Tin), to(0) * (uint32_t)sizeof(Tin));
+                        if (to(1)) copy_async16<512, 512>(shared, src + col(0) * (int32_t)sizeof(Tin), to(1) * (uint32_t)sizeof(Tin));
                     } else {
-#pragma unroll
-                        for (uint32_t q = 0; q < kParts; ++q) {
-                            float v[V] = {};
-                            if (have[q]) load_cols<Tin, V>(reinterpret_cast<const Tin *>(src) + q * 32u * V, have[q], v);
-                            elem::Packed<Tin, (int)V> x;
-                            x.pack(v);
-                            dst[(u * kParts + q) * 32u] = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
-                        }
+                        // pieces from the one before the tile's first on, as far as they hold something of the row
+                        const uint64_t row_end = src + a.dim * sizeof(Tin);
+                        const uint64_t piece = (src & ~15ull) + tile * 1024u + lane * 16u - 16u;
+                        if (piece + 16u > src && piece < row_end) copy_async16<0, 0>(shared, piece, 16u);
+                        if (piece + 528u > src && piece + 512u < row_end) copy_async16<512, 512>(shared, piece, 16u);
+                        if (lane < 4u && piece + 1024u < row_end) copy_async16<1024, 1024>(shared, piece, 16u);
                     }
                 }
             }
             copy_commit();
         };
         uint32_t stage = 0;
-        fetch(from, 0u);
-        for (uint32_t j0 = from; j0 < to; j0 += kStageRows) {
+        fetch(first, 0u);
+        for (uint32_t j0 = first; j0 < last; j0 += kStageRows) {
             fetch(j0 + kStageRows, stage ^ 1u);
             copy_wait<1>();
-            const uint4 *src = mine + stage * (kStageRows * kParts * 32u);
-            const uint32_t end = to < j0 + kStageRows ? to : j0 + kStageRows;
+            if (!ALIGNED) __syncwarp();                 // the other lanes' copies
+            const uint4 *src = stages + stage * (kStageRows * kRowPieces) + lane;
+            const uint32_t end = last < j0 + kStageRows ? last : j0 + kStageRows;
 #pragma unroll 1
-            for (uint32_t j = j0; j < end; ++j, src += kParts * 32u) {
+            for (uint32_t j = j0; j < end; ++j, src += kRowPieces) {
                 if (begins >> j & 1u) {
                     if (open) flush(row_begins >> j & 1u);
                     open = true;
@@ -667,16 +677,28 @@ sum_rows_kernel(SumArgs a, SortBuffers b) {
                     row_start = __shfl_sync(0xffffffffu, rec.y, j);
                     row_number = __shfl_sync(0xffffffffu, rec.z, j);
                     row = __shfl_sync(0xffffffffu, rec.w, j);
+                    back = moved(out + (uint64_t)(COMPACT ? row_number : row) * a.out_stride);
 #pragma unroll
                     for (uint32_t q = 0; q < kParts; ++q)
 #pragma unroll
                         for (uint32_t c = 0; c < V; ++c) acc[q][c] = 0.f;
                 }
+                // where this lane's first column lies behind the first staged piece
+                uint32_t at = 0;
+                if constexpr (!ALIGNED) at = (__shfl_sync(0xffffffffu, (uint32_t)my_row, j) & 15u) + 16u - back * (uint32_t)sizeof(Tin);
 #pragma unroll
                 for (uint32_t q = 0; q < kParts; ++q) {
-                    const uint4 x = src[q * 32u];
                     elem::Packed<Tin, (int)V> c;
-                    c.w[0] = x.x; c.w[1] = x.y; c.w[2] = x.z; c.w[3] = x.w;
+                    if constexpr (ALIGNED) {
+                        const uint4 x = src[q * 32u];
+                        c.w[0] = x.x; c.w[1] = x.y; c.w[2] = x.z; c.w[3] = x.w;
+                    } else {
+                        const uint4 x = src[q * 32u + (at >> 4)], y = src[q * 32u + (at >> 4) + 1u];
+                        elem::Vector<Tin, (int)V, 0> both;
+                        both.w[0] = x.x; both.w[1] = x.y; both.w[2] = x.z; both.w[3] = x.w;
+                        both.w[4] = y.x; both.w[5] = y.y; both.w[6] = y.z; both.w[7] = y.w;
+                        c = both.get(at & 15u);
+                    }
                     float v[V];
                     c.unpack(v);
 #pragma unroll
@@ -686,8 +708,8 @@ sum_rows_kernel(SumArgs a, SortBuffers b) {
             stage ^= 1u;
         }
         copy_wait<0>();                                 // nothing but empty groups is left
-        if (to < 32u) {
-            flush(row_begins >> to & 1u);
+        if (last < 32u) {
+            flush(row_begins >> last & 1u);
             return;
         }
     }
@@ -743,10 +765,14 @@ cudaError_t launch_sums(const EmbeddingGradArgs &a, const SortBuffers &b, cudaSt
     s.out = a.d_grad;
     s.out_stride = a.out_stride;
     s.scale = a.scale;
-    s.aligned = ((reinterpret_cast<uintptr_t>(a.d_grad_out) | (a.n_tokens > 1 ? a.grad_stride * sizeof(Tin) : 0u)) & 15u) == 0u;
     s.rows = a.d_rows;
     s.cap = a.cap;
-    s.tiles = a.dim ? (uint32_t)((a.dim + Tile<Tin>::kCols - 1) / Tile<Tin>::kCols) : 1u;     // without columns: the row numbers alone
+    const uint64_t out_rows = a.d_rows ? a.cap : a.n_rows;
+    const uintptr_t ends = reinterpret_cast<uintptr_t>(a.d_grad_out) | (a.n_tokens > 1 ? a.grad_stride * sizeof(Tin) : 0u) |
+                           reinterpret_cast<uintptr_t>(a.d_grad) | (out_rows > 1 ? a.out_stride * sizeof(Tout) : 0u);
+    const bool aligned = (ends & 15u) == 0u;
+    const uint64_t columns = a.dim + (aligned ? 0u : Tile<Tin>::V);               // columns that are moved back need more room
+    s.tiles = a.dim ? (uint32_t)((columns + Tile<Tin>::kCols - 1) / Tile<Tin>::kCols) : 1u;     // without columns: the row numbers alone
     const uint64_t positions = a.n_tokens > a.cap ? a.n_tokens : a.cap;
     s.tile_shift = s.tiles >= 4u ? 2u : s.tiles >= 2u ? 1u : 0u;
     const uint64_t windows = (positions + kWindow - 1) / kWindow;
@@ -756,10 +782,15 @@ cudaError_t launch_sums(const EmbeddingGradArgs &a, const SortBuffers &b, cudaSt
     if (blocks > 0x7fffffffull || groups > 65535u) return cudaErrorInvalidConfiguration;   // refused at the entry points
     ++*launches;
     const dim3 grid((uint32_t)blocks, (uint32_t)groups), block(kSumWarps * 32);
-    if (a.d_rows) return launch_overlapping(sum_rows_kernel<Tin, Tout, true, false>, grid, block, 0, stream, s, b);
-    if (a.accumulate) return launch_overlapping(sum_rows_kernel<Tin, Tout, false, true>, grid, block, 0, stream, s, b);
-    sum_rows_kernel<Tin, Tout, false, false><<<grid, block, 0, stream>>>(s, b);          // the fill needs the SMs meanwhile
-    return cudaGetLastError();
+    auto launch = [&](auto kernel, bool overlapping) {
+        if (overlapping) return launch_overlapping(kernel, grid, block, 0, stream, s, b);
+        kernel<<<grid, block, 0, stream>>>(s, b);
+        return cudaGetLastError();
+    };
+    if (a.d_rows) return aligned ? launch(sum_rows_kernel<Tin, Tout, true, false, true>, true) : launch(sum_rows_kernel<Tin, Tout, true, false, false>, true);
+    if (a.accumulate) return aligned ? launch(sum_rows_kernel<Tin, Tout, false, true, true>, true) : launch(sum_rows_kernel<Tin, Tout, false, true, false>, true);
+    // the fill needs the SMs meanwhile
+    return aligned ? launch(sum_rows_kernel<Tin, Tout, false, false, true>, false) : launch(sum_rows_kernel<Tin, Tout, false, false, false>, false);
 }
 
 }  // namespace
@@ -770,13 +801,13 @@ namespace {
 uint64_t round16(uint64_t x) { return (x + 15u) & ~15ull; }
 uint64_t slot_count(uint64_t n) { return 2u * (n / kPiece + 1u); }
 constexpr uint64_t kLeastCols = Tile<float>::kCols, kMostCols = Tile<__half>::kCols;
-uint64_t tile_count(uint64_t dim) { return (dim + kLeastCols - 1) / kLeastCols; }
+uint64_t tile_count(uint64_t dim) { return (dim + 8u + kLeastCols - 1) / kLeastCols; }
 }  // namespace
 
 uint64_t embedding_grad_sort_bytes(uint64_t n) { return 16u * (n + 1u) + 5u * round16(4u * (n + 1u)) + 64u; }
 uint64_t embedding_grad_arrival_bytes(uint64_t n, uint64_t dim) { return round16(8u * slot_count(n) * tile_count(dim)); }
 uint64_t embedding_grad_partial_bytes(uint64_t n, uint64_t dim) {
-    return n <= kPiece ? 16u : 4u * slot_count(n) * ((dim + kMostCols - 1) / kMostCols * kMostCols);     // one piece at most: no partial sums
+    return n <= kPiece ? 16u : 4u * slot_count(n) * ((dim + 8u + kMostCols - 1) / kMostCols * kMostCols);     // one piece at most: no partial sums
 }
 
 namespace {
