@@ -33,10 +33,10 @@ struct SortShared {
         uint2 sorted[kSortThreads * kMaxItems];            // afterwards: the tile's keys and indices by digit
     };
     uint2 incoming[kSortThreads * kMaxItems];              // one tile per CTA: the keys at this CTA's positions after the pass
-    uint16_t warp_bins[kSortWarps][kBins];                 // keys of each digit in a warp's part of the tile, then their prefix over half of the warps
+    uint16_t warp_bins[kSortWarps][kBins];                 // keys of each digit in a warp's part of the tile, then their prefix over a quarter of the warps
     uint32_t from[kMaxCluster][kBins];                     // keys of each digit in every CTA's share
     uint4 rows_from[kMaxCluster];                          // of every CTA's share: rows that begin, valid keys, 1 + the last place a row begins
-    uint32_t half_count[kBins];                            // keys of each digit in the first half of the warps
+    uint32_t quarter[4][kBins];                            // keys of each digit in every quarter of the warps, then before it
     uint32_t count[kBins];                                 // keys of each digit in this CTA's share
     uint32_t tile_first[kBins];                            // place of the first key of each digit in the current tile, sorted
     uint32_t base[kBins];                                  // where this CTA's next key of each digit goes
@@ -144,7 +144,16 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
         uint32_t *out_key = b.key[pass & 1], *out_idx = b.index[pass & 1];
         uint32_t key[ITEMS], idx[ITEMS], rank[ITEMS];
 
-        auto load_tile = [&](uint32_t t0) {
+        // counters of the warps that have keys to zero, while the tile's loads are under way
+        auto clear = [&](uint32_t t0) {
+            const uint32_t keys = hi - t0 < kTileKeys ? hi - t0 : kTileKeys;
+            const uint32_t warps = (keys + ITEMS * 32u - 1) / (ITEMS * 32u);
+            for (uint32_t i = threadIdx.x; i < warps * (kBins / 8); i += kSortThreads)
+                reinterpret_cast<uint4 *>(&s.warp_bins[0][0])[i] = make_uint4(0u, 0u, 0u, 0u);
+            for (uint32_t i = threadIdx.x; i < warps * (kBins / 4); i += kSortThreads)
+                reinterpret_cast<uint4 *>(&s.peers[0][0])[i] = make_uint4(0u, 0u, 0u, 0u);
+        };
+        auto load_tile = [&](uint32_t t0, bool clearing) {
             if (pass == 0) {
                 Token token[ITEMS];
 #pragma unroll
@@ -153,15 +162,19 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
                     token[j] = i < hi ? tokens[i] : Token(0);
                     idx[j] = i;
                 }
+                if (clearing) clear(t0);
 #pragma unroll
                 for (uint32_t j = 0; j < ITEMS; ++j) key[j] = idx[j] < hi ? to_key(token[j]) : 0u;
             } else if (one_tile) {
+                const uint2 *from = ranks > 1 ? s.incoming : s.sorted;
 #pragma unroll
                 for (uint32_t j = 0; j < ITEMS; ++j) {
-                    const uint2 k = t0 + mine + j * 32u < hi ? s.incoming[mine + j * 32u] : make_uint2(0u, 0u);
+                    const uint2 k = t0 + mine + j * 32u < hi ? from[mine + j * 32u] : make_uint2(0u, 0u);
                     key[j] = k.x;
                     idx[j] = k.y;
                 }
+                if (ranks == 1) __syncthreads();               // the counters lie where the sorted keys were
+                if (clearing) clear(t0);
             } else {
 #pragma unroll
                 for (uint32_t j = 0; j < ITEMS; ++j) {
@@ -169,17 +182,14 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
                     key[j] = i < hi ? in_key[i] : 0u;
                     idx[j] = i < hi ? in_idx[i] : 0u;
                 }
+                if (clearing) clear(t0);
             }
+            if (clearing) __syncthreads();
         };
         // The tile sorted by this pass's digit into s.sorted; returns the tile's keys of digit threadIdx.x.
         auto sort_tile = [&](uint32_t t0) {
             const uint32_t keys = hi - t0 < kTileKeys ? hi - t0 : kTileKeys;
             const uint32_t warps = (keys + ITEMS * 32u - 1) / (ITEMS * 32u);          // that have keys
-            for (uint32_t i = threadIdx.x; i < warps * (kBins / 8); i += kSortThreads)
-                reinterpret_cast<uint4 *>(&s.warp_bins[0][0])[i] = make_uint4(0u, 0u, 0u, 0u);
-            for (uint32_t i = threadIdx.x; i < warps * (kBins / 4); i += kSortThreads)
-                reinterpret_cast<uint4 *>(&s.peers[0][0])[i] = make_uint4(0u, 0u, 0u, 0u);
-            __syncthreads();
 #pragma unroll
             for (uint32_t j = 0; j < ITEMS; ++j) {
                 rank[j] = 0;
@@ -201,25 +211,30 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
                 }
             }
             __syncthreads();
-            // prefix over the warps, two digits (16 bits each) and half of the warps per thread
-            constexpr uint32_t kHalf = kSortWarps / 2;
-            if (threadIdx.x < kBins) {
-                const uint32_t pair = threadIdx.x % (kBins / 2), half = threadIdx.x / (kBins / 2);
-                const uint32_t from = half * kHalf, to = warps < from + kHalf ? warps : from + kHalf;
+            // prefix over the warps, two digits (16 bits each) and a quarter of the warps per thread
+            constexpr uint32_t kQuarter = kSortWarps / 4;
+            {
+                const uint32_t pair = threadIdx.x % (kBins / 2), part = threadIdx.x / (kBins / 2);
                 uint32_t run = 0;
-#pragma unroll 8
-                for (uint32_t w = from; w < to; ++w) {
+#pragma unroll
+                for (uint32_t w = part * kQuarter; w < (part + 1u) * kQuarter; ++w) {
                     uint32_t *p = reinterpret_cast<uint32_t *>(&s.warp_bins[w][0]) + pair;
-                    const uint32_t c = *p;
-                    *p = run;
+                    const uint32_t c = w < warps ? *p : 0u;
+                    if (w < warps) *p = run;
                     run += c;
                 }
-                uint32_t *total = half == 0 ? s.half_count : s.tile_first;             // tile_first: of the second half for now
-                total[2 * pair] = run & 0xffffu;
-                total[2 * pair + 1] = run >> 16;
+                reinterpret_cast<uint2 *>(&s.quarter[part][0])[pair] = make_uint2(run & 0xffffu, run >> 16);
             }
             __syncthreads();
-            const uint32_t total = threadIdx.x < kBins ? s.half_count[threadIdx.x] + s.tile_first[threadIdx.x] : 0u;
+            uint32_t total = 0;
+            if (threadIdx.x < kBins) {
+#pragma unroll
+                for (uint32_t part = 0; part < 4u; ++part) {
+                    const uint32_t c = s.quarter[part][threadIdx.x];
+                    s.quarter[part][threadIdx.x] = total;
+                    total += c;
+                }
+            }
             const uint32_t first = block_exclusive(total, s.scan);
             if (threadIdx.x < kBins) s.tile_first[threadIdx.x] = first;
             __syncthreads();
@@ -228,8 +243,7 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
             for (uint32_t j = 0; j < ITEMS; ++j) {
                 if (mine + j * 32u < keys) {
                     const uint32_t digit = (key[j] >> shift) & (kBins - 1);
-                    const uint32_t at = s.tile_first[digit] + (warp >= kHalf ? s.half_count[digit] : 0u) +
-                                        s.warp_bins[warp][digit] + rank[j];
+                    const uint32_t at = s.tile_first[digit] + s.quarter[warp / kQuarter][digit] + s.warp_bins[warp][digit] + rank[j];
                     s.sorted[at] = make_uint2(key[j], idx[j]);
                 }
             }
@@ -238,13 +252,17 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
 
         uint32_t digits = 0;                                   // of digit threadIdx.x: keys in the share
         if (one_tile) {
-            load_tile(lo);
+            load_tile(lo, true);
             digits = sort_tile(lo);
+            if (ranks == 1) {                                  // sorted by this digit as a whole
+                __syncthreads();
+                continue;
+            }
         } else {
             for (uint32_t i = threadIdx.x; i < kBins; i += kSortThreads) s.count[i] = 0;
             __syncthreads();
             for (uint32_t t0 = lo; t0 < hi; t0 += kTileKeys) {
-                load_tile(t0);
+                load_tile(t0, false);
 #pragma unroll
                 for (uint32_t j = 0; j < ITEMS; ++j)
                     if (t0 + mine + j * 32u < hi) atomicAdd(&s.count[(key[j] >> shift) & (kBins - 1)], 1u);
@@ -274,7 +292,7 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
         for (uint32_t t0 = lo; t0 < hi; t0 += kTileKeys) {
             uint32_t tile_count = 0;
             if (!one_tile) {
-                load_tile(t0);
+                load_tile(t0, true);
                 tile_count = sort_tile(t0);
                 __syncthreads();
             }
@@ -319,10 +337,11 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
             idx[j] = 0;
             if (i < hi) {
                 if (one_tile) {
-                    const uint2 x = s.incoming[i - lo];
+                    const uint2 *from = ranks > 1 ? s.incoming : s.sorted;
+                    const uint2 x = from[i - lo];
                     k[j] = x.x;
                     idx[j] = x.y;
-                    if (i > lo) prev[j] = s.incoming[i - lo - 1u].x;
+                    if (i > lo) prev[j] = from[i - lo - 1u].x;
                     else if (i) prev[j] = cluster.map_shared_rank(&s.incoming[share - 1u], me - 1u)->x;
                 } else {
                     k[j] = key[i];
@@ -496,15 +515,15 @@ __device__ __forceinline__ uint32_t slot_of(uint32_t piece_begin, bool first_of_
 // back to where the output row has one, so that stores stay whole vectors, and the input is staged in its own
 // 16-byte pieces, from which a lane picks its bytes.
 template <typename Tin, typename Tout, bool COMPACT, bool ADD, bool ALIGNED>
-__global__ void __launch_bounds__(kSumWarps * 32, 6)
+__global__ void __launch_bounds__(kSumWarps * 32, 5)
 sum_rows_kernel(SumArgs a, SortBuffers b) {
     constexpr uint32_t V = Tile<Tin>::V, kCols = Tile<Tin>::kCols;
     constexpr uint32_t kRowPieces = ALIGNED ? kParts * 32u : kParts * 32u + 4u;            // 16-byte pieces of a staged row
     __shared__ __align__(16) uint4 ring[kSumWarps][2][kStageRows][kRowPieces];
     // a CTA's warps take consecutive tiles of one window, or, where a row has fewer tiles, several windows
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    const uint32_t tile = (blockIdx.y << a.tile_shift) + (warp & ((1u << a.tile_shift) - 1u));
-    const uint64_t window = ((uint64_t)blockIdx.x * kSumWarps + warp) >> a.tile_shift;
+    const uint64_t unit = (uint64_t)blockIdx.x * kSumWarps + warp, window = unit >> a.tile_shift;
+    const uint32_t tile = (blockIdx.y << a.tile_shift) + ((uint32_t)unit & ((1u << a.tile_shift) - 1u));
     if (tile >= a.tiles) return;
     wait_for_previous_kernel();
     const uint32_t valid = *reinterpret_cast<const volatile uint32_t *>(b.totals);
