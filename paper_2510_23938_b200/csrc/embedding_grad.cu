@@ -606,15 +606,14 @@ sum_rows_kernel(SumArgs a, SortBuffers b) {
     };
     // true for the warp that arrives last of `members`; leaves the counter at zero for the next call
     auto arrive = [&](uint32_t *counter, uint32_t members) {
-        __threadfence();
         __syncwarp();
         uint32_t last = 0;
         if (lane == 0) {
-            last = atomicAdd(counter, 1u) + 1u == members ? 1u : 0u;
+            last = arrive_add(counter, 1u) + 1u == members ? 1u : 0u;
             if (last) *counter = 0u;
         }
         last = __shfl_sync(0xffffffffu, last, 0);
-        __threadfence();
+        __syncwarp();
         return last != 0u;
     };
     auto counter = [&](uint32_t slot, uint32_t level) { return b.arrivals + ((uint64_t)slot * a.tiles + tile) * 2u + level; };

@@ -331,12 +331,10 @@ norm_kernel(TensorSet set, PlanAt at, NormScratch scratch, bool clip, float max_
     if (range_begin == range_end) return;
     // pieces done of tensor k; true for the CTA whose pieces complete it (and likewise the set)
     auto arrive = [&](uint32_t *counter, uint32_t mine, uint32_t all) {
-        __threadfence();
         __syncthreads();
         if (threadIdx.x == 0) {
-            flag = atomicAdd(counter, mine) + mine == all ? 1u : 0u;
+            flag = arrive_add(counter, mine) + mine == all ? 1u : 0u;
             if (flag) *counter = 0u;
-            __threadfence();
         }
         __syncthreads();
         const bool last = flag != 0u;

@@ -54,6 +54,13 @@ inline cudaError_t launch_overlapping(void (*kernel)(Params...), dim3 grid, dim3
 }
 #ifdef __CUDACC__
 __device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;"); }
+// Adds to a counter; what this thread and, through a barrier before, its neighbours have written is visible to whoever
+// reads the counter's new value here, and what those who added before have written is visible afterwards.
+__device__ __forceinline__ uint32_t arrive_add(uint32_t *counter, uint32_t n) {
+    uint32_t old;
+    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], %2;" : "=r"(old) : "l"(counter), "r"(n) : "memory");
+    return old;
+}
 __device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 #endif
 
