@@ -795,8 +795,9 @@ def read_norm_result(result: torch.Tensor) -> dict:
 
 
 def tensor_ranges(tensors) -> tuple:
-    """(base, offsets, lengths, types) of tensors of their own, as grad_norm, grad_clip and hash_ragged take a set: the
-    first tensor and, per tensor, the bytes from it, the length in bytes (int64 device tensors) and the DTYPES code."""
+    """(base, offsets, lengths, types) of tensors of their own, as grad_norm, grad_clip and grad_scale take a set: the
+    first tensor and, per tensor, the bytes from it (modulo 2^64), the length in bytes (int64 device tensors) and the
+    DTYPES code.  The arrays hold addresses: they are for these tensors, not for others of the same shapes."""
     base = tensors[0]
     assert all(t.is_cuda and t.is_contiguous() for t in tensors), "device tensors must be contiguous CUDA tensors"
     signed = [(t.data_ptr() - base.data_ptr() + (1 << 63)) % (1 << 64) - (1 << 63) for t in tensors]

@@ -79,6 +79,36 @@ def sharded_root(ctx, local_leaves: torch.Tensor, plan: ShardPlan, rank: int, gr
     return ctx.merkle_root(all_nodes.contiguous())
 
 
+def sharded_grad_clip(ctx, base, offsets, lengths, max_norm: float, group=None, **kw):
+    """Clips gradients that are spread over several GPUs by their common norm, in place: `base`, `offsets`, `lengths` (and
+    `dtype`, `types`) are this rank's share as `ctx.grad_clip` takes it.  Returns (norm, scale, number of tensors with
+    an infinity or a NaN), each a one-element device tensor with the same value on every rank.
+
+    The exchange is 16 bytes per rank: the ranks' sums of squares (64 bits) are gathered and added in rank order, so
+    the norm does not depend on how a collective would have added them.  Collective: every rank of `group` calls it."""
+    result = torch.zeros(32, dtype=torch.uint8, device=offsets.device)
+    ctx.grad_norm(base, offsets, lengths, result, **kw)
+    mine = torch.stack([result.view(torch.float64)[2], result.view(torch.int32)[1].double()])   # sum of squares, bad tensors
+    world = dist.get_world_size(group) if dist.is_initialized() else 1
+    if world == 1:
+        gathered = [mine]
+    elif mine.is_cuda and dist.get_backend(group) == "gloo":
+        host = mine.cpu()
+        gathered = [torch.empty_like(host) for _ in range(world)]
+        dist.all_gather(gathered, host, group=group)
+        gathered = [g.to(mine.device) for g in gathered]
+    else:
+        gathered = [torch.empty_like(mine) for _ in range(world)]
+        dist.all_gather(gathered, mine, group=group)
+    total = gathered[0].clone()
+    for g in gathered[1:]:
+        total += g
+    norm = total[0].sqrt()
+    scale = torch.where(norm <= max_norm, torch.ones_like(norm), max_norm / norm).float()
+    ctx.grad_scale(base, offsets, lengths, scale.reshape(1), **kw)
+    return norm.float(), scale, total[1].to(torch.int64)
+
+
 def count_mismatches(local_count, device, group=None):
     """Total number of mismatching chunks over all ranks (an 8-byte all-reduce).
 
