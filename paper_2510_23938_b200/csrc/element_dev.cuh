@@ -114,7 +114,7 @@ struct Vector {
         constexpr int kStep = ALIGN == 8 ? 2 : P;
 #pragma unroll
         for (int i = 0; i < kLoaded; i += kStep)
-            if (i < W || ALIGN == 0 || off) load_aligned<kStep>(q + 4 * i, w + i);
+            if (i < W || ALIGN == 0 || (off & (4u * P - 1u))) load_aligned<kStep>(q + 4 * i, w + i);
     }
     __device__ __forceinline__ void zero() {
 #pragma unroll

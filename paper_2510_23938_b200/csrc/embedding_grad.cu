@@ -788,7 +788,7 @@ cudaError_t launch_sums(const EmbeddingGradArgs &a, const SortBuffers &b, cudaSt
     const uint64_t out_rows = a.d_rows ? a.cap : a.n_rows;
     const uintptr_t ends = reinterpret_cast<uintptr_t>(a.d_grad_out) | (a.n_tokens > 1 ? a.grad_stride * sizeof(Tin) : 0u) |
                            reinterpret_cast<uintptr_t>(a.d_grad) | (out_rows > 1 ? a.out_stride * sizeof(Tout) : 0u);
-    const bool aligned = (ends & 15u) == 0u;
+    const bool aligned = (ends & 15u) == 0u || a.dim == 0;                          // without columns no row is touched
     const uint64_t columns = a.dim + (aligned ? 0u : Tile<Tin>::V);               // columns that are moved back need more room
     s.tiles = a.dim ? (uint32_t)((columns + Tile<Tin>::kCols - 1) / Tile<Tin>::kCols) : 1u;     // without columns: the row numbers alone
     const uint64_t positions = a.n_tokens > a.cap ? a.n_tokens : a.cap;

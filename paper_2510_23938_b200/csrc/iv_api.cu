@@ -1009,7 +1009,6 @@ bool aligned_to(const void *p, uint64_t bytes) { return (reinterpret_cast<uintpt
 constexpr uint64_t kMaxTokens = 1ull << 30;
 constexpr uint64_t kMaxRows = 1ull << 31;
 constexpr uint64_t kMaxColumns = 1ull << 24;
-constexpr uint64_t kForkFillBytes = 8ull << 20;
 
 // Arguments that both forms of the gradient have in common, then scratch and launch.
 int embedding_grad(iv_ctx *ctx, const ivk::EmbeddingGradArgs &a, void *cuda_stream) {
@@ -1037,10 +1036,13 @@ int embedding_grad(iv_ctx *ctx, const ivk::EmbeddingGradArgs &a, void *cuda_stre
     const ivk::EmbeddingGradScratch scratch = {ctx->d_sort, ctx->d_arrivals, ctx->d_partial};
 
     const uint64_t fill_bytes = !a.d_rows && !a.accumulate ? a.n_rows * a.dim * dtype_bytes(a.out_type) : 0;
+    const bool sorts = a.d_rows || a.n_tokens;                       // also where it only finds rows that are not there
     const bool sums = a.d_rows || (a.n_tokens && a.dim && a.n_rows);
-    const bool fork = sums && fill_bytes >= kForkFillBytes;
+    // the fill beside the sort and the sums, also for small tables (1024 tokens of 1024 columns, 500 / 4000 / 64,000 rows:
+    // 19 / 21 / 30 us, one after the other 23 / 27 / 46)
+    const bool fork = sums && fill_bytes;
     if (fork && (rc = fork_tail_stream(ctx, stream)) != IV_OK) return rc;
-    if (sums) IV_TRY(ctx, ivk::launch_embedding_grad_sort(a, scratch, ctx->d_status, stream, &ctx->launches));
+    if (sorts) IV_TRY(ctx, ivk::launch_embedding_grad_sort(a, scratch, ctx->d_status, stream, &ctx->launches));
     if (fill_bytes) IV_TRY(ctx, ivk::launch_embedding_grad_fill(a, ctx->sm_count, fork ? ctx->tail_stream : stream, &ctx->launches));
     if (sums) IV_TRY(ctx, ivk::launch_embedding_grad_sums(a, scratch, stream, &ctx->launches));
     if (fork && (rc = join_tail_stream(ctx, stream)) != IV_OK) return rc;
