@@ -6,6 +6,18 @@
 //
 //   1. sort_tokens_kernel      stable radix sort of (token, t) by one cluster, then the list of distinct rows
 //   2. sum_rows_kernel         one warp per (8 sorted positions, tile of columns): adds up the pieces that begin there
+//   3. fill_rows_kernel        fresh table gradient: the rows without a token, beside the other two
+//
+// The sums are bound by memory (every gradient row read once, every row written once), the sort by latency: its passes
+// are chains of shared-memory steps and cluster barriers.  So the sort uses as many SMs as a cluster spans before it gives a
+// thread a second key, the sums' CTAs are in place when it ends, and what needs no order (the fill) runs beside it.
+// One warp adds up 1 KiB of a row: a row of 8 KiB is eight warps' work, which keeps rows with many tokens from
+// becoming the longest path; rows of more than kPiece tokens are cut, and the warp that completes a group of pieces
+// adds up their sums.
+//
+// On one B200, bf16 rows of 8 KiB: 65,536 tokens, whole table of 128,256 rows: 272 us, 5.8 TB/s (sort 26, sums 115, fill 145, the
+// last two sharing the memory); 16,384 tokens, compact: 61 us (sort 17, sums 40 at 5.1 TB/s of what has to move).
+// 8192 tokens of 4 KiB added to a 32-bit table gradient: 38 us (sort 15, sums 22); 509 tokens: 17 us.
 #include <cooperative_groups.h>
 
 #include "element_dev.cuh"
@@ -25,7 +37,7 @@ constexpr uint32_t kSortWarps = kSortThreads / 32;
 constexpr uint32_t kMaxItems = 8;                          // keys per thread and tile
 constexpr uint32_t kDigitBits = 9;                         // two passes for tables of up to 262,143 rows
 constexpr uint32_t kBins = 1u << kDigitBits;
-constexpr uint32_t kMaxCluster = 16;
+constexpr uint32_t kMaxCluster = 16;                       // 65,536 tokens: 26 us with 16 CTAs of four keys a thread, 41 with 8 of eight
 
 struct SortShared {
     union {
@@ -425,7 +437,7 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
 
 // ------------------------------------------------------------------------------------------------- sums
 
-constexpr uint32_t kWindow = 8;        // sorted positions per warp
+constexpr uint32_t kWindow = 8;        // sorted positions per warp (16: 48 us against 42 for 8192 tokens added)
 constexpr uint32_t kSumWarps = 4;
 constexpr uint32_t kParts = 2;         // a lane holds this many vectors of 16 bytes of a row, a warp 1 KiB
 constexpr uint32_t kStageRows = 4;     // rows per stage of the ring, two stages: eight rows in flight
@@ -501,6 +513,7 @@ struct SumArgs {
     uint64_t out_stride;
     float scale;
     uint32_t tiles, tile_shift;
+    uint64_t positions;    // records there are
     int64_t *rows;         // compact form: row numbers and how many rows there is room for
     uint64_t cap;
 };
@@ -511,11 +524,12 @@ __device__ __forceinline__ uint32_t slot_of(uint32_t piece_begin, bool first_of_
     return 2u * (piece_begin / kPiece) + (first_of_row ? 1u : 0u);
 }
 
-// ALIGNED: every row of grad_out and of the output starts at a 16-byte boundary.  Otherwise a lane's columns are moved
+// ALIGNED: every row of grad_out and of the output starts at a 16-byte boundary (16,384 rows of 4096 bf16 columns: 69 us;
+// of 4095 columns, through the other instance: 90, and 194 with single-element stores).  Otherwise a lane's columns are moved
 // back to where the output row has one, so that stores stay whole vectors, and the input is staged in its own
 // 16-byte pieces, from which a lane picks its bytes.
 template <typename Tin, typename Tout, bool COMPACT, bool ADD, bool ALIGNED>
-__global__ void __launch_bounds__(kSumWarps * 32, 5)
+__global__ void __launch_bounds__(kSumWarps * 32, 5)    // six CTAs per SM spill: 66 us against 62 for 16,384 tokens
 sum_rows_kernel(SumArgs a, SortBuffers b) {
     constexpr uint32_t V = Tile<Tin>::V, kCols = Tile<Tin>::kCols;
     constexpr uint32_t kRowPieces = ALIGNED ? kParts * 32u : kParts * 32u + 4u;            // 16-byte pieces of a staged row
@@ -526,7 +540,10 @@ sum_rows_kernel(SumArgs a, SortBuffers b) {
     const uint32_t tile = (blockIdx.y << a.tile_shift) + ((uint32_t)unit & ((1u << a.tile_shift) - 1u));
     if (tile >= a.tiles) return;
     wait_for_previous_kernel();
-    const uint32_t valid = *reinterpret_cast<const volatile uint32_t *>(b.totals);
+    const uint4 *records = b.record + window * kWindow + lane;
+    uint4 ahead = make_uint4(0u, 0u, 0u, 0u);           // the first record, before it is known whether there is one
+    if (window * kWindow + lane < a.positions) ahead = __ldcg(records);
+    const uint32_t valid = __ldcg(b.totals);
     Tout *out = static_cast<Tout *>(a.out);
 
     // this lane's columns in part q: V from col(q), of which [from(q), to(q)) are there; back: how far they are moved
@@ -641,7 +658,7 @@ sum_rows_kernel(SumArgs a, SortBuffers b) {
         // 32 sorted positions, one per lane; behind the last one everything begins anew
         const uint32_t i = i0 + lane;
         uint4 rec = make_uint4(0u, i, 0u, 0u);
-        if (i < valid) rec = b.record[i];
+        if (i < valid) rec = i0 == w0 ? ahead : __ldcg(b.record + i);
         const uint32_t begins = __ballot_sync(0xffffffffu, (i - rec.y) % kPiece == 0u);
         const uint32_t row_begins = __ballot_sync(0xffffffffu, i == rec.y);
         // ours: from the first piece that begins in the window to the first that begins behind it
@@ -767,6 +784,7 @@ template <typename Token>
 cudaError_t launch_sort_sized(const EmbeddingGradArgs &a, const SortBuffers &b, uint32_t passes, uint32_t *d_status,
                               cudaStream_t stream) {
     // first all CTAs of a cluster, then more keys per thread: what a pass costs is the keys of ONE multiprocessor
+    // (8192 tokens: 18 us with eight CTAs of one key a thread, 47 with one CTA of eight)
     const uint64_t row = (uint64_t)kMaxCluster * kSortThreads;
     if (a.n_tokens <= row) return launch_sort<Token, 1>(a, b, passes, d_status, stream);
     if (a.n_tokens <= 2 * row) return launch_sort<Token, 2>(a, b, passes, d_status, stream);
@@ -785,6 +803,7 @@ cudaError_t launch_sums(const EmbeddingGradArgs &a, const SortBuffers &b, cudaSt
     s.scale = a.scale;
     s.rows = a.d_rows;
     s.cap = a.cap;
+    s.positions = a.n_tokens;
     const uint64_t out_rows = a.d_rows ? a.cap : a.n_rows;
     const uintptr_t ends = reinterpret_cast<uintptr_t>(a.d_grad_out) | (a.n_tokens > 1 ? a.grad_stride * sizeof(Tin) : 0u) |
                            reinterpret_cast<uintptr_t>(a.d_grad) | (out_rows > 1 ? a.out_stride * sizeof(Tout) : 0u);

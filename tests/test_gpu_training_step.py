@@ -3,9 +3,9 @@
 Tolerances are derived, not tuned.  u = 2^-24 is the unit roundoff of 32-bit floats; an output of type T adds one
 rounding of at most ROUND[T] relative (or half the type's smallest number).  A lookup is one 32-bit product, so it must
 equal the same product bit for bit.  A 32-bit sum of m terms in any order is within (m - 1) u sum|terms| of the true
-one; scaling and adding to what is there are two more roundings.  A norm adds at most 64 squares in one 32-bit
-accumulator (each square one rounding) and everything above in 64 bits, the root halves the relative error, and the
-result is rounded once to 32 bits: 65 u / 2 + u.
+one; scaling and adding to what is there are two more roundings.  In a norm a square goes through
+at most 64 roundings of 32 bits (its own, and the additions of its share of a piece) and everything above is in 64 bits, the
+root halves the relative error, and the result is rounded once to 32 bits: 65 u / 2 + u.
 """
 import ctypes
 import math
