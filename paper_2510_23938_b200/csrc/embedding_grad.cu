@@ -32,11 +32,12 @@ namespace {
 
 // ------------------------------------------------------------------------------------------------- sorted tokens
 
-constexpr uint32_t kSortThreads = 1024;
+constexpr uint32_t kSortThreads = 512;                     // with 1024 the barriers of a pass cost more (8192 tokens added: 38.4 us, 36.1)
 constexpr uint32_t kSortWarps = kSortThreads / 32;
-constexpr uint32_t kMaxItems = 8;                          // keys per thread and tile
+constexpr uint32_t kMaxItems = 16;                         // keys per thread and tile
 constexpr uint32_t kDigitBits = 9;                         // two passes for tables of up to 262,143 rows
 constexpr uint32_t kBins = 1u << kDigitBits;
+constexpr uint32_t kWarpParts = kSortWarps / 8;            // the prefix over the warps is taken eight at a time
 constexpr uint32_t kMaxCluster = 16;                       // 65,536 tokens: 26 us with 16 CTAs of four keys a thread, 41 with 8 of eight
 
 struct SortShared {
@@ -45,10 +46,10 @@ struct SortShared {
         uint2 sorted[kSortThreads * kMaxItems];            // afterwards: the tile's keys and indices by digit
     };
     uint2 incoming[kSortThreads * kMaxItems];              // one tile per CTA: the keys at this CTA's positions after the pass
-    uint16_t warp_bins[kSortWarps][kBins];                 // keys of each digit in a warp's part of the tile, then their prefix over a quarter of the warps
+    uint16_t warp_bins[kSortWarps][kBins];                 // keys of each digit in a warp's part of the tile, then their prefix over eight warps
     uint32_t from[kMaxCluster][kBins];                     // keys of each digit in every CTA's share
     uint4 rows_from[kMaxCluster];                          // of every CTA's share: rows that begin, valid keys, 1 + the last place a row begins
-    uint32_t quarter[4][kBins];                            // keys of each digit in every quarter of the warps, then before it
+    uint32_t parts[kWarpParts][kBins];                     // keys of each digit in every part of the warps, then before it
     uint32_t count[kBins];                                 // keys of each digit in this CTA's share
     uint32_t tile_first[kBins];                            // place of the first key of each digit in the current tile, sorted
     uint32_t base[kBins];                                  // where this CTA's next key of each digit goes
@@ -223,27 +224,27 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
                 }
             }
             __syncthreads();
-            // prefix over the warps, two digits (16 bits each) and a quarter of the warps per thread
-            constexpr uint32_t kQuarter = kSortWarps / 4;
+            // prefix over the warps, two digits (16 bits each) and eight of the warps per thread
+            static_assert(kWarpParts * (kBins / 2) == kSortThreads, "a thread for every pair of digits and eight warps");
             {
                 const uint32_t pair = threadIdx.x % (kBins / 2), part = threadIdx.x / (kBins / 2);
                 uint32_t run = 0;
 #pragma unroll
-                for (uint32_t w = part * kQuarter; w < (part + 1u) * kQuarter; ++w) {
+                for (uint32_t w = part * 8u; w < (part + 1u) * 8u; ++w) {
                     uint32_t *p = reinterpret_cast<uint32_t *>(&s.warp_bins[w][0]) + pair;
                     const uint32_t c = w < warps ? *p : 0u;
                     if (w < warps) *p = run;
                     run += c;
                 }
-                reinterpret_cast<uint2 *>(&s.quarter[part][0])[pair] = make_uint2(run & 0xffffu, run >> 16);
+                reinterpret_cast<uint2 *>(&s.parts[part][0])[pair] = make_uint2(run & 0xffffu, run >> 16);
             }
             __syncthreads();
             uint32_t total = 0;
             if (threadIdx.x < kBins) {
 #pragma unroll
-                for (uint32_t part = 0; part < 4u; ++part) {
-                    const uint32_t c = s.quarter[part][threadIdx.x];
-                    s.quarter[part][threadIdx.x] = total;
+                for (uint32_t part = 0; part < kWarpParts; ++part) {
+                    const uint32_t c = s.parts[part][threadIdx.x];
+                    s.parts[part][threadIdx.x] = total;
                     total += c;
                 }
             }
@@ -255,7 +256,7 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
             for (uint32_t j = 0; j < ITEMS; ++j) {
                 if (mine + j * 32u < keys) {
                     const uint32_t digit = (key[j] >> shift) & (kBins - 1);
-                    const uint32_t at = s.tile_first[digit] + s.quarter[warp / kQuarter][digit] + s.warp_bins[warp][digit] + rank[j];
+                    const uint32_t at = s.tile_first[digit] + s.parts[warp / 8u][digit] + s.warp_bins[warp][digit] + rank[j];
                     s.sorted[at] = make_uint2(key[j], idx[j]);
                 }
             }
@@ -404,7 +405,7 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
             s.warp_last[warp] = my_last;
         }
         __syncthreads();
-        const uint32_t h = s.warp_heads[lane], p = s.warp_last[lane];
+        const uint32_t h = lane < kSortWarps ? s.warp_heads[lane] : 0u, p = lane < kSortWarps ? s.warp_last[lane] : 0u;
         uint32_t number = before + __reduce_add_sync(0xffffffffu, lane < warp ? h : 0u);
         uint32_t start = max(last, __reduce_max_sync(0xffffffffu, lane < warp ? p : 0u));
         before += __reduce_add_sync(0xffffffffu, h);
@@ -789,6 +790,7 @@ cudaError_t launch_sort_sized(const EmbeddingGradArgs &a, const SortBuffers &b, 
     if (a.n_tokens <= row) return launch_sort<Token, 1>(a, b, passes, d_status, stream);
     if (a.n_tokens <= 2 * row) return launch_sort<Token, 2>(a, b, passes, d_status, stream);
     if (a.n_tokens <= 4 * row) return launch_sort<Token, 4>(a, b, passes, d_status, stream);
+    if (a.n_tokens <= 8 * row) return launch_sort<Token, 8>(a, b, passes, d_status, stream);
     return launch_sort<Token, kMaxItems>(a, b, passes, d_status, stream);
 }
 

@@ -192,7 +192,9 @@ GRADS = [  # n, rows, dim, kind, grad skew, grad padding, out skew, out padding
     (511, 700, 2048, "distinct", 4, 0, 0, 0), (2047, 3, 72, "zipf", 0, 0, 0, 0), (2048, 1, 40, "same", 0, 0, 0, 0),
     (2049, 2, 40, "same", 0, 0, 0, 0), (4500, 1000, 96, "descending", 0, 5, 0, 3), (10_000, 128_256, 33, "zipf", 2, 0, 0, 0),
     (20_001, 262_200, 16, "zipf", 0, 0, 0, 0), (70_000, 300_000, 8, "zipf", 0, 0, 0, 0), (70_001, 2, 24, "same", 0, 0, 0, 0),
-    (3, 2_000_000_000, 8, "huge", 0, 0, 0, 0),
+    (3, 2_000_000_000, 8, "huge", 0, 0, 0, 0), (8_192, 50_257, 12, "zipf", 0, 0, 0, 0), (8_193, 513, 12, "zipf", 0, 0, 0, 0),
+    (33_000, 511, 9, "zipf", 0, 0, 0, 0), (131_072, 128_256, 8, "zipf", 0, 0, 0, 0), (131_073, 262_144, 8, "zipf", 0, 0, 0, 0),
+    (300_000, 140_000, 4, "descending", 0, 0, 0, 0), (257, 100_000, 515, "distinct", 1, 3, 2, 1),
 ]
 
 
@@ -307,6 +309,21 @@ def test_gradient_of_no_tokens(ctx):
     rows, g, count = ctx.embedding_grad_rows(grad, none, 5, rows=torch.zeros(4, dtype=torch.int64, device="cuda"),
                                              out=torch.ones(4, 16, device="cuda"))
     assert rows.tolist() == [-1] * 4 and not bool(g.any()) and int(count) == 0
+
+
+def test_gradient_without_columns_or_without_rows(ctx):
+    tokens = torch.tensor([3, 1, 3], device="cuda")
+    rows, g, count = ctx.embedding_grad_rows(torch.empty(3, 0, device="cuda"), tokens, 5)
+    assert rows.tolist() == [1, 3, -1] and g.shape == (3, 0) and int(count) == 2
+    odd = torch.zeros(8, dtype=torch.uint8, device="cuda")[2:6].view(torch.float16)[:0].view(3, 0)   # no columns at an odd place
+    rows, g, count = ctx.embedding_grad_rows(odd, tokens, 5)
+    assert rows.tolist() == [1, 3, -1] and int(count) == 2
+    assert ctx.embedding_grad(torch.empty(3, 0, device="cuda"), tokens, 5).shape == (5, 0) and ctx.device_status() == 0
+    # a table without rows: no token is in it
+    rows, g, count = ctx.embedding_grad_rows(torch.ones(3, 4, device="cuda"), tokens, 0)
+    assert rows.numel() == 0 and int(count) == 0 and ctx.device_status() == 2
+    assert ctx.embedding_grad(torch.ones(3, 4, device="cuda"), tokens, 0).shape == (0, 4) and ctx.device_status() == 2
+    assert not bool(ctx.embedding(torch.ones(0, 4, device="cuda"), tokens).any()) and ctx.device_status() == 2
 
 
 def test_gradient_passes_infinities_and_nan_to_their_rows_only(ctx):
