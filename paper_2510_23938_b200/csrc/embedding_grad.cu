@@ -15,9 +15,9 @@
 // becoming the longest path; rows of more than kPiece tokens are cut, and the warp that completes a group of pieces
 // adds up their sums.
 //
-// On one B200, bf16 rows of 8 KiB: 65,536 tokens, whole table of 128,256 rows: 272 us, 5.8 TB/s (sort 26, sums 115, fill 145, the
-// last two sharing the memory); 16,384 tokens, compact: 61 us (sort 17, sums 40 at 5.1 TB/s of what has to move).
-// 8192 tokens of 4 KiB added to a 32-bit table gradient: 38 us (sort 15, sums 22); 509 tokens: 17 us.
+// On one B200, bf16 rows of 8 KiB: 65,536 tokens, whole table of 128,256 rows: 264 us, 6.0 TB/s of what has to move (alone: sort
+// 27, sums 113, fill 160; the last two share the memory); 16,384 tokens, compact: 58 us (sort 15, sums 38 at 6 TB/s).
+// 8192 tokens of 4 KiB added to a 32-bit table gradient: 36 us (sort 13, sums 22); 509 tokens: 15 us.
 #include <cooperative_groups.h>
 
 #include "element_dev.cuh"
@@ -38,7 +38,7 @@ constexpr uint32_t kMaxItems = 16;                         // keys per thread an
 constexpr uint32_t kDigitBits = 9;                         // two passes for tables of up to 262,143 rows
 constexpr uint32_t kBins = 1u << kDigitBits;
 constexpr uint32_t kWarpParts = kSortWarps / 8;            // the prefix over the warps is taken eight at a time
-constexpr uint32_t kMaxCluster = 16;                       // 65,536 tokens: 26 us with 16 CTAs of four keys a thread, 41 with 8 of eight
+constexpr uint32_t kMaxCluster = 16;                       // 65,536 tokens, CTAs of 1024 threads: 26 us with 16 of them, 41 with 8
 
 struct SortShared {
     union {
