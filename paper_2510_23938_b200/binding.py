@@ -212,6 +212,8 @@ def n_chunks(nbytes: int, chunk_bytes: int) -> int:
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
     if stream is None:                # the current stream's handle, without a Stream object around it
+        if not torch.cuda.is_initialized():
+            torch.cuda.init()
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream
 

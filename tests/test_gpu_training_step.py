@@ -589,6 +589,75 @@ def test_large_sets(ctx):
     assert bool((big == big[0]).all()) and big[0] == np.float32(0.5) * np.float32(r["scale"])
 
 
+# ------------------------------------------------------------------------------------------------- streams and graphs
+
+def test_two_contexts_side_by_side():
+    """Two contexts on two streams, gradients and clipping under way at the same time, three times without waiting."""
+    work, results = [], []
+    for k in range(2):
+        g = _gen(100 + k)
+        grad = torch.randn(20_000, 512, generator=g, device="cuda")
+        tokens = _tokens(20_000, 30_000, 200 + k)
+        flat, starts, offsets, nbytes = _packed([300_000, 17, 70_000], torch.float32, 300 + k)
+        work.append((binding.Context(0), torch.cuda.Stream(), grad, tokens, flat, offsets, nbytes))
+        with binding.Context(0) as alone:
+            clipped, result = flat.clone(), binding.new_norm_result("cuda")
+            alone.grad_clip(clipped, offsets, nbytes, 0.5, result)
+            results.append((alone.embedding_grad(grad, tokens, 30_000), alone.embedding_grad_rows(grad, tokens, 30_000)[1], clipped))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = []
+        for ctx, stream, grad, tokens, flat, offsets, nbytes in work:
+            with torch.cuda.stream(stream):
+                clipped, result = flat.clone(), binding.new_norm_result("cuda")
+                dense = ctx.embedding_grad(grad, tokens, 30_000)
+                rows = ctx.embedding_grad_rows(grad, tokens, 30_000)[1]
+                ctx.grad_clip(clipped, offsets, nbytes, 0.5, result)
+                got.append((dense, rows, clipped))
+        torch.cuda.synchronize()
+        for a, b in zip(got, results):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+    for w in work:
+        assert w[0].device_status() == 0
+        w[0].close()
+
+
+def test_calls_in_a_graph(ctx):
+    """A step captured once and replayed on new inputs (after a first call has sized the scratch)."""
+    n, rows, dim = 3000, 5000, 264
+    tokens, grad = _tokens(n, rows, 1), torch.randn(n, dim, generator=_gen(2), device="cuda")
+    table = torch.randn(rows, dim, generator=_gen(3), device="cuda")
+    out, dense = torch.empty(n, dim, device="cuda"), torch.empty(rows, dim, device="cuda")
+    touched, d_rows, count = (torch.empty(n, dtype=torch.int64, device="cuda"), torch.empty(n, dim, device="cuda"),
+                              torch.empty(1, dtype=torch.int64, device="cuda"))
+    result = binding.new_norm_result("cuda")
+    zero, size = torch.zeros(1, dtype=torch.int64, device="cuda"), torch.tensor([4 * n * dim], device="cuda")
+
+    def step():
+        ctx.embedding(table, tokens, scale=2.0, out=out)
+        ctx.embedding_grad(grad, tokens, rows, out=dense)
+        ctx.embedding_grad_rows(grad, tokens, rows, rows=touched, out=d_rows, count=count)
+        ctx.grad_clip(d_rows, zero, size, 1.0, result)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in (10, 20):
+        tokens.copy_(_tokens(n, rows, seed))
+        grad.copy_(torch.randn(n, dim, generator=_gen(seed), device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (out, dense, touched, d_rows, count, result)]
+        step()
+        assert all(torch.equal(a, b) for a, b in zip(got, (out, dense, touched, d_rows, count, result)))
+        assert torch.equal(out, table[tokens] * 2.0)
+
+
 # ------------------------------------------------------------------------------------------------- refusals
 
 def test_refusals_of_the_binding(ctx):
