@@ -17,7 +17,7 @@
 //
 // On one B200, bf16 rows of 8 KiB: 65,536 tokens, whole table of 128,256 rows: 264 us, 6.0 TB/s of what has to move (alone: sort
 // 27, sums 113, fill 160; the last two share the memory); 16,384 tokens, compact: 58 us (sort 15, sums 38 at 6 TB/s).
-// 8192 tokens of 4 KiB added to a 32-bit table gradient: 36 us (sort 13, sums 22); 509 tokens: 15 us.
+// 8192 tokens of 4 KiB added to a 32-bit table gradient: 33 us (sort 13, sums 19); 509 tokens: 15 us.
 #include <cooperative_groups.h>
 
 #include "element_dev.cuh"
@@ -713,7 +713,13 @@ sum_rows_kernel(SumArgs a, SortBuffers b) {
                     row_start = __shfl_sync(0xffffffffu, rec.y, j);
                     row_number = __shfl_sync(0xffffffffu, rec.z, j);
                     row = __shfl_sync(0xffffffffu, rec.w, j);
-                    back = moved(out + (uint64_t)(COMPACT ? row_number : row) * a.out_stride);
+                    const Tout *o = out + (uint64_t)(COMPACT ? row_number : row) * a.out_stride;
+                    back = moved(o);
+                    if (ADD && begin == row_start) {    // the old row on its way while its terms are added up (36 us without)
+#pragma unroll
+                        for (uint32_t q = 0; q < kParts; ++q)
+                            if (to(q) > from(q)) asm volatile("prefetch.global.L2 [%0];" ::"l"(o + col(q) + from(q)));
+                    }
 #pragma unroll
                     for (uint32_t q = 0; q < kParts; ++q)
 #pragma unroll
