@@ -19,6 +19,7 @@
 // 27, sums 113, fill 160; the last two share the memory); 16,384 tokens, compact: 58 us (sort 15, sums 38 at 6 TB/s).
 // 8192 tokens of 4 KiB added to a 32-bit table gradient: 33 us (sort 13, sums 19); 509 tokens: 15 us.
 #include <cooperative_groups.h>
+#include <type_traits>
 
 #include "element_dev.cuh"
 #include "iv_internal.h"
@@ -440,12 +441,13 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
 
 constexpr uint32_t kWindow = 8;        // sorted positions per warp (16: 48 us against 42 for 8192 tokens added)
 constexpr uint32_t kSumWarps = 4;
-constexpr uint32_t kParts = 2;         // a lane holds this many vectors of 16 bytes of a row, a warp 1 KiB
-constexpr uint32_t kStageRows = 4;     // rows per stage of the ring, two stages: eight rows in flight
 
-template <typename T> struct Tile {
+// A lane holds PARTS vectors of 16 bytes of a row, a warp 512 * PARTS bytes of it: two for rows in general; one, and twice
+// the rows in flight, for rows that fit (131,072 tokens of 64 columns: 72 us, 80 with two).
+template <typename T, uint32_t PARTS> struct Tile {
     static constexpr uint32_t V = 16 / sizeof(T);                 // columns of a vector
-    static constexpr uint32_t kCols = kParts * 32 * V;            // columns per warp: 512 (16-bit types) or 256
+    static constexpr uint32_t kCols = PARTS * 32 * V;             // columns per warp
+    static constexpr uint32_t kStageRows = 8 / PARTS;             // rows per stage of the ring, which has two
 };
 
 // V columns of type T of which from .. to - 1 are there: the rest reads as zero and is not written.
@@ -529,10 +531,10 @@ __device__ __forceinline__ uint32_t slot_of(uint32_t piece_begin, bool first_of_
 // of 4095 columns, through the other instance: 90, and 194 with single-element stores).  Otherwise a lane's columns are moved
 // back to where the output row has one, so that stores stay whole vectors, and the input is staged in its own
 // 16-byte pieces, from which a lane picks its bytes.
-template <typename Tin, typename Tout, bool COMPACT, bool ADD, bool ALIGNED>
+template <typename Tin, typename Tout, bool COMPACT, bool ADD, bool ALIGNED, uint32_t PARTS>
 __global__ void __launch_bounds__(kSumWarps * 32, 5)    // six CTAs per SM spill: 66 us against 62 for 16,384 tokens
 sum_rows_kernel(SumArgs a, SortBuffers b) {
-    constexpr uint32_t V = Tile<Tin>::V, kCols = Tile<Tin>::kCols;
+    constexpr uint32_t V = Tile<Tin, PARTS>::V, kCols = Tile<Tin, PARTS>::kCols, kParts = PARTS, kStageRows = Tile<Tin, PARTS>::kStageRows;
     constexpr uint32_t kRowPieces = ALIGNED ? kParts * 32u : kParts * 32u + 4u;            // 16-byte pieces of a staged row
     __shared__ __align__(16) uint4 ring[kSumWarps][2][kStageRows][kRowPieces];
     // a CTA's warps take consecutive tiles of one window, or, where a row has fewer tiles, several windows
@@ -683,14 +685,14 @@ sum_rows_kernel(SumArgs a, SortBuffers b) {
                     const uint32_t shared = tma::smem_u32(dst + u * kRowPieces);
                     if constexpr (ALIGNED) {
                         if (to(0)) copy_async16<0, 0>(shared, src + col(0) * (int32_t)sizeof(Tin), to(0) * (uint32_t)sizeof(Tin));
-                        if (to(1)) copy_async16<512, 512>(shared, src + col(0) * (int32_t)sizeof(Tin), to(1) * (uint32_t)sizeof(Tin));
+                        if (kParts > 1 && to(1)) copy_async16<512, 512>(shared, src + col(0) * (int32_t)sizeof(Tin), to(1) * (uint32_t)sizeof(Tin));
                     } else {
                         // pieces from the one before the tile's first on, as far as they hold something of the row
                         const uint64_t row_end = src + a.dim * sizeof(Tin);
-                        const uint64_t piece = (src & ~15ull) + tile * 1024u + lane * 16u - 16u;
+                        const uint64_t piece = (src & ~15ull) + tile * (kParts * 512u) + lane * 16u - 16u;
                         if (piece + 16u > src && piece < row_end) copy_async16<0, 0>(shared, piece, 16u);
-                        if (piece + 528u > src && piece + 512u < row_end) copy_async16<512, 512>(shared, piece, 16u);
-                        if (lane < 4u && piece + 1024u < row_end) copy_async16<1024, 1024>(shared, piece, 16u);
+                        if (kParts > 1 && piece + 528u > src && piece + 512u < row_end) copy_async16<512, 512>(shared, piece, 16u);
+                        if (lane < 4u && piece + kParts * 512u < row_end) copy_async16<kParts * 512, kParts * 512>(shared, piece, 16u);
                     }
                 }
             }
@@ -816,8 +818,9 @@ cudaError_t launch_sums(const EmbeddingGradArgs &a, const SortBuffers &b, cudaSt
     const uintptr_t ends = reinterpret_cast<uintptr_t>(a.d_grad_out) | (a.n_tokens > 1 ? a.grad_stride * sizeof(Tin) : 0u) |
                            reinterpret_cast<uintptr_t>(a.d_grad) | (out_rows > 1 ? a.out_stride * sizeof(Tout) : 0u);
     const bool aligned = (ends & 15u) == 0u || a.dim == 0;                          // without columns no row is touched
-    const uint64_t columns = a.dim + (aligned ? 0u : Tile<Tin>::V);               // columns that are moved back need more room
-    s.tiles = a.dim ? (uint32_t)((columns + Tile<Tin>::kCols - 1) / Tile<Tin>::kCols) : 1u;     // without columns: the row numbers alone
+    const uint64_t columns = a.dim + (aligned ? 0u : Tile<Tin, 1>::V);               // columns that are moved back need more room
+    const bool narrow = columns <= Tile<Tin, 1>::kCols;
+    s.tiles = narrow ? 1u : (uint32_t)((columns + Tile<Tin, 2>::kCols - 1) / Tile<Tin, 2>::kCols);   // without columns: the row numbers alone
     const uint64_t positions = a.n_tokens > a.cap ? a.n_tokens : a.cap;
     s.tile_shift = s.tiles >= 4u ? 2u : s.tiles >= 2u ? 1u : 0u;
     const uint64_t windows = (positions + kWindow - 1) / kWindow;
@@ -832,10 +835,15 @@ cudaError_t launch_sums(const EmbeddingGradArgs &a, const SortBuffers &b, cudaSt
         kernel<<<grid, block, 0, stream>>>(s, b);
         return cudaGetLastError();
     };
-    if (a.d_rows) return aligned ? launch(sum_rows_kernel<Tin, Tout, true, false, true>, true) : launch(sum_rows_kernel<Tin, Tout, true, false, false>, true);
-    if (a.accumulate) return aligned ? launch(sum_rows_kernel<Tin, Tout, false, true, true>, true) : launch(sum_rows_kernel<Tin, Tout, false, true, false>, true);
-    // the fill needs the SMs meanwhile
-    return aligned ? launch(sum_rows_kernel<Tin, Tout, false, false, true>, false) : launch(sum_rows_kernel<Tin, Tout, false, false, false>, false);
+    auto pick = [&](auto compact, auto add, bool overlapping) {
+        constexpr bool C = decltype(compact)::value, A = decltype(add)::value;
+        if (narrow)
+            return aligned ? launch(sum_rows_kernel<Tin, Tout, C, A, true, 1>, overlapping) : launch(sum_rows_kernel<Tin, Tout, C, A, false, 1>, overlapping);
+        return aligned ? launch(sum_rows_kernel<Tin, Tout, C, A, true, 2>, overlapping) : launch(sum_rows_kernel<Tin, Tout, C, A, false, 2>, overlapping);
+    };
+    if (a.d_rows) return pick(std::true_type{}, std::false_type{}, true);
+    if (a.accumulate) return pick(std::false_type{}, std::true_type{}, true);
+    return pick(std::false_type{}, std::false_type{}, false);                            // the fill needs the SMs meanwhile
 }
 
 }  // namespace
@@ -845,7 +853,7 @@ cudaError_t launch_sums(const EmbeddingGradArgs &a, const SortBuffers &b, cudaSt
 namespace {
 uint64_t round16(uint64_t x) { return (x + 15u) & ~15ull; }
 uint64_t slot_count(uint64_t n) { return 2u * (n / kPiece + 1u); }
-constexpr uint64_t kLeastCols = Tile<float>::kCols, kMostCols = Tile<__half>::kCols;
+constexpr uint64_t kLeastCols = Tile<float, 2>::kCols, kMostCols = Tile<__half, 2>::kCols;
 uint64_t tile_count(uint64_t dim) { return (dim + 8u + kLeastCols - 1) / kLeastCols; }
 }  // namespace
 
