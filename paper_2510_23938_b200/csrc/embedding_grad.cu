@@ -133,6 +133,9 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
     allow_next_kernel();
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t ranks = cluster.num_blocks(), me = cluster.block_rank();
+    // another CTA's shared memory may be written only once that CTA has started: everybody says so here and waits for the
+    // others before the first such write, behind the first tile's loads and its sort
+    if (ranks > 1) cluster.barrier_arrive();
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint32_t share = ((n + ranks - 1) / ranks + 31u) & ~31u;
     const uint32_t lo = me * share < n ? me * share : n;
@@ -285,6 +288,7 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
             if (threadIdx.x < kBins) digits = s.count[threadIdx.x];
         }
         if (ranks > 1) {
+            if (pass == 0) cluster.barrier_wait();
             if (threadIdx.x < kBins)
                 for (uint32_t r = 0; r < ranks; ++r) *cluster.map_shared_rank(&s.from[me][threadIdx.x], r) = digits;
             cluster.sync();
