@@ -147,12 +147,12 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
         if (ranks > 1) cluster.sync();
         else __syncthreads();
     };
-    // padding and rows that are not there sort behind every row and are left out
+    // padding and rows that are not there sort behind every row and are left out; a padding row of -1 is none, not token -1
     auto to_key = [&](Token token) {
         const int64_t t = (int64_t)token;
-        const bool there = (uint64_t)t < n_rows;
-        bad |= !there && t != padding_row;
-        return there && t != padding_row ? (uint32_t)t : (uint32_t)n_rows;
+        const bool there = (uint64_t)t < n_rows, padding = t == padding_row && t >= 0;
+        bad |= !there && !padding;
+        return there && !padding ? (uint32_t)t : (uint32_t)n_rows;
     };
 
     for (uint32_t pass = 0; pass < passes; ++pass) {

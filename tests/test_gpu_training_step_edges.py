@@ -47,3 +47,32 @@ def test_sort_of_a_cluster_whose_blocks_have_very_different_shares(ctx, n):
         wrong += (c[0] != distinct.numel()) | (r[:distinct.numel()] != distinct).any() | (g[:distinct.numel()] != want).any()
     torch.cuda.current_stream().wait_stream(side)
     assert int(wrong) == 0
+
+
+# ------------------------------------------------------------------------------------------------- tokens outside the table
+
+@pytest.mark.parametrize("dtype", [torch.int32, torch.int64], ids=str)
+@pytest.mark.parametrize("padding", [None, 3])
+@pytest.mark.parametrize("form", ["table", "added", "rows"])
+def test_gradient_reports_token_minus_one(ctx, form, padding, dtype):
+    """-1 stands for "no padding row"; as a token it is a row that is not there, in the gradient as in the lookup."""
+    tokens = torch.tensor([2, -1, 0, 2], dtype=dtype, device="cuda")
+    grad = torch.ones(4, 5, device="cuda")
+    if form == "rows":
+        rows, got, count = ctx.embedding_grad_rows(grad, tokens, 6, padding_row=padding)
+        assert rows.tolist() == [0, 2, -1, -1] and int(count) == 2 and got[:, 0].tolist() == [1, 2, 0, 0]
+    else:
+        out = torch.full((6, 5), 10.0, device="cuda")
+        got = ctx.embedding_grad(grad, tokens, 6, padding_row=padding, out=out, accumulate=form == "added")
+        old = 10 if form == "added" else 0
+        assert got[:, 0].tolist() == [old + 1, old, old + 2, old, old, old]
+    assert ctx.device_status() == 2 and ctx.device_status() == 0
+
+
+def test_gradient_does_not_report_padding(ctx):
+    """A padding row inside the table or behind it gives no gradient and no complaint."""
+    grad = torch.ones(3, 5, device="cuda")
+    for padding in (0, 4, 2 ** 31):
+        tokens = torch.tensor([1, padding, 1], device="cuda")
+        assert ctx.embedding_grad(grad, tokens, 4, padding_row=padding)[:, 0].tolist() == [0, 2, 0, 0]
+        assert ctx.device_status() == 0
