@@ -797,13 +797,18 @@ def read_norm_result(result: torch.Tensor) -> dict:
 
 
 def tensor_ranges(tensors) -> tuple:
-    """(base, offsets, lengths, types) of tensors of their own, as grad_norm, grad_clip and grad_scale take a set: the
-    first tensor and, per tensor, the bytes from it (modulo 2^64), the length in bytes (int64 device tensors) and the
-    DTYPES code.  The arrays hold addresses: they are for these tensors, not for others of the same shapes."""
-    base = tensors[0]
+    """(base, offsets, lengths, types) of tensors of their own, as grad_norm, grad_clip and grad_scale take a set: a
+    tensor and, per tensor, the bytes from it (modulo 2^64), the length in bytes (int64 device tensors) and the
+    DTYPES code.  The arrays hold addresses: they are for these tensors, not for others of the same shapes.  Tensors
+    without elements may stand anywhere; they have no address, so the base is the first one that has (or, for a set of
+    nothing, an element of its own)."""
+    tensors = list(tensors)
     assert all(t.is_cuda and t.is_contiguous() for t in tensors), "device tensors must be contiguous CUDA tensors"
-    signed = [(t.data_ptr() - base.data_ptr() + (1 << 63)) % (1 << 64) - (1 << 63) for t in tensors]
-    device = base.device
+    device = tensors[0].device if tensors else "cuda"
+    base = next((t for t in tensors if t.numel()), None)
+    if base is None:
+        base = torch.zeros(1, device=device)
+    signed = [(t.data_ptr() - base.data_ptr() + (1 << 63)) % (1 << 64) - (1 << 63) if t.numel() else 0 for t in tensors]
     return (base, torch.tensor(signed, dtype=torch.int64, device=device),
             torch.tensor([_nbytes(t) for t in tensors], dtype=torch.int64, device=device),
             torch.tensor([DTYPES[t.dtype] for t in tensors], dtype=torch.uint8, device=device))

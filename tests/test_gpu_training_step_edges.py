@@ -76,3 +76,40 @@ def test_gradient_does_not_report_padding(ctx):
         tokens = torch.tensor([1, padding, 1], device="cuda")
         assert ctx.embedding_grad(grad, tokens, 4, padding_row=padding)[:, 0].tolist() == [0, 2, 0, 0]
         assert ctx.device_status() == 0
+
+
+# ------------------------------------------------------------------------------------------------- tensors of their own
+
+def _own(*shapes):
+    return [torch.randn(*s, generator=_gen(50 + i), device="cuda") for i, s in enumerate(shapes)]
+
+
+@pytest.mark.parametrize("shapes", [[(0, 8), (300,), (7,)], [(300,), (0,), (7,)], [(300,), (7,), (0, 8)],
+                                    [(0,), (0, 4), (5,)]], ids=str)
+def test_empty_tensors_anywhere_in_a_set(ctx, shapes):
+    """A step without tokens hands over a gradient of no rows."""
+    tensors = _own(*shapes)
+    before = [t.clone() for t in tensors]
+    base, offsets, lengths, types = binding.tensor_ranges(tensors)
+    result, norms = binding.new_norm_result("cuda"), torch.full((len(tensors),), 9.0, device="cuda")
+    ctx.grad_clip(base, offsets, lengths, 0.5, result, norms=norms, types=types)
+    r = binding.read_norm_result(result)
+    whole = torch.cat([b.reshape(-1) for b in before]).double()
+    assert r["status"] == 0 and r["n_elements"] == whole.numel()
+    assert abs(r["norm"] - float(whole.norm())) <= 34 * 2.0 ** -24 * float(whole.norm())     # 65 u / 2 + u
+    for t, b, norm in zip(tensors, before, norms.tolist()):
+        assert torch.equal(t, b * r["scale"]) and (norm == 0) == (t.numel() == 0)
+
+
+@pytest.mark.parametrize("tensors", [[], [(0,)], [(0, 3), (0,)]], ids=str)
+def test_sets_of_nothing(ctx, tensors):
+    base, offsets, lengths, types = binding.tensor_ranges(_own(*tensors))
+    assert offsets.numel() == lengths.numel() == types.numel() == len(tensors)
+    result, factor = binding.new_norm_result("cuda"), torch.ones(1, device="cuda")
+    nothing = {"status": 0, "n_nonfinite": 0, "norm": 0.0, "scale": 1.0, "sum_squares": 0.0, "n_elements": 0}
+    ctx.grad_norm(base, offsets, lengths, result, types=types)
+    assert binding.read_norm_result(result) == nothing
+    ctx.grad_clip(base, offsets, lengths, 1.0, result, types=types)
+    assert binding.read_norm_result(result) == nothing
+    ctx.grad_scale(base, offsets, lengths, factor, types=types)
+    assert ctx.device_status() == 0
