@@ -11,6 +11,7 @@ exchange (NCCL on GPUs; the tests run the same code over gloo).
 """
 from __future__ import annotations
 
+import contextlib
 from dataclasses import dataclass
 
 import torch
@@ -79,15 +80,22 @@ def sharded_root(ctx, local_leaves: torch.Tensor, plan: ShardPlan, rank: int, gr
     return ctx.merkle_root(all_nodes.contiguous())
 
 
-def sharded_grad_clip(ctx, base, offsets, lengths, max_norm: float, group=None, **kw):
-    """Clips gradients that are spread over several GPUs by their common norm, in place: `base`, `offsets`, `lengths` (and
-    `dtype`, `types`) are this rank's share as `ctx.grad_clip` takes it.  Returns (norm, scale, number of tensors with
+def sharded_grad_clip(ctx, base, offsets, lengths, max_norm: float, group=None, dtype=None, types=None, stream=None):
+    """Clips gradients that are spread over several GPUs by their common norm, in place: `base`, `offsets`, `lengths`,
+    `dtype` and `types` are this rank's share as `ctx.grad_clip` takes it.  Returns (norm, scale, number of tensors with
     an infinity or a NaN), each a one-element device tensor with the same value on every rank.
 
     The exchange is 16 bytes per rank: the ranks' sums of squares (64 bits) are gathered and added in rank order, so
-    the norm does not depend on how a collective would have added them.  Collective: every rank of `group` calls it."""
+    the norm does not depend on how a collective would have added them.  Collective: every rank of `group` calls it.
+    All of it is issued on `stream` (default: the current one), and what it returns is ready there."""
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+        return _sharded_grad_clip(ctx, base, offsets, lengths, max_norm, group, dtype, types)
+
+
+def _sharded_grad_clip(ctx, base, offsets, lengths, max_norm, group, dtype, types):
+    kinds = {key: value for key, value in (("dtype", dtype), ("types", types)) if value is not None}
     result = torch.zeros(32, dtype=torch.uint8, device=offsets.device)
-    ctx.grad_norm(base, offsets, lengths, result, **kw)
+    ctx.grad_norm(base, offsets, lengths, result, **kinds)
     mine = torch.stack([result.view(torch.float64)[2], result.view(torch.int32)[1].double()])   # sum of squares, bad tensors
     world = dist.get_world_size(group) if dist.is_initialized() else 1
     if world == 1:
@@ -105,7 +113,7 @@ def sharded_grad_clip(ctx, base, offsets, lengths, max_norm: float, group=None, 
         total += g
     norm = total[0].sqrt()
     scale = torch.where(norm <= max_norm, torch.ones_like(norm), max_norm / norm).float()
-    ctx.grad_scale(base, offsets, lengths, scale.reshape(1), **kw)
+    ctx.grad_scale(base, offsets, lengths, scale.reshape(1), **kinds)
     return norm.float(), scale, total[1].to(torch.int64)
 
 

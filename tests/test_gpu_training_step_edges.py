@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2510_23938_b200 import binding
+from paper_2510_23938_b200 import binding, sharded
 
 pytestmark = pytest.mark.gpu
 
@@ -113,3 +113,24 @@ def test_sets_of_nothing(ctx, tensors):
     assert binding.read_norm_result(result) == nothing
     ctx.grad_scale(base, offsets, lengths, factor, types=types)
     assert ctx.device_status() == 0
+
+
+# ------------------------------------------------------------------------------------------------- clipping over ranks
+
+def test_sharded_clipping_on_another_stream_with_work_in_front(ctx):
+    """The gradients are still being written on that stream when the call returns to the host."""
+    flat = torch.randn(70_001, generator=_gen(1), device="cuda")
+    offsets, lengths = torch.tensor([0, 40_000], device="cuda"), torch.tensor([40_000, 240_004], device="cuda")
+    side, front = torch.cuda.Stream(), torch.ones(8192, 8192, device="cuda")
+    want, result = flat.clone(), binding.new_norm_result("cuda")
+    ctx.grad_clip(want, offsets, lengths, 0.5, result)
+    r = binding.read_norm_result(result)
+    for _ in range(5):
+        late = torch.zeros_like(flat)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            front @ front
+            late.copy_(flat)
+        norm, scale, bad = sharded.sharded_grad_clip(ctx, late, offsets, lengths, 0.5, stream=side)
+        side.synchronize()
+        assert (float(norm), float(scale), int(bad)) == (r["norm"], r["scale"], 0) and torch.equal(late, want)

@@ -1,0 +1,86 @@
+"""Clipping over ranks: streams, refusals and what comes back, on the host with a context made of torch operations."""
+import contextlib
+import math
+import os
+import socket
+
+import pytest
+import torch
+import torch.distributed as dist
+import torch.multiprocessing as mp
+from torch.utils._python_dispatch import TorchDispatchMode
+
+from paper_2510_23938_b200 import sharded
+
+
+class HostSetOps:
+    """grad_norm and grad_scale of a context, for float32 tensors on the host; `seen` receives what was called."""
+
+    def __init__(self, seen=None):
+        self.seen = seen if seen is not None else []
+
+    @staticmethod
+    def _parts(base, offsets, lengths):
+        return [base[o // 4:(o + n) // 4] for o, n in zip(offsets.tolist(), lengths.tolist())]
+
+    def grad_norm(self, base, offsets, lengths, result, norms=None, dtype=None, types=None, stream=None):
+        self.seen.append(("grad_norm", stream))
+        parts = self._parts(base, offsets, lengths)
+        each = torch.stack([p.double().square().sum() for p in parts])
+        result.view(torch.float64)[2] = each.sum()
+        result.view(torch.int32)[1] = sum(int(not torch.isfinite(p).all()) for p in parts)
+        result.view(torch.int64)[3] = sum(p.numel() for p in parts)
+        if norms is not None:
+            norms.copy_(each.sqrt())
+
+    def grad_scale(self, base, offsets, lengths, scale, out=None, out_offsets=None, dtype=None, types=None, out_dtype=None,
+                   stream=None):
+        self.seen.append(("grad_scale", stream))
+        for p in self._parts(base, offsets, lengths):
+            p.mul_(scale)
+
+
+def _two_halves(flat):
+    half = flat.numel() // 2 * 4
+    return torch.tensor([0, half]), torch.tensor([half, flat.numel() * 4 - half])
+
+
+def _free_port():
+    with socket.socket() as s:
+        s.bind(("127.0.0.1", 0))
+        return s.getsockname()[1]
+
+
+def test_everything_runs_on_the_given_stream(monkeypatch):
+    """The two calls and every torch operation between them are issued with the caller's stream as the current one; nothing
+    is handed a stream of its own beside operations on another."""
+    seen, inside = [], []
+
+    @contextlib.contextmanager
+    def entered(stream):
+        inside.append(stream)
+        yield
+        inside.pop()
+
+    class Operations(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            outside_of.append(str(func)) if not inside else None
+            return func(*args, **(kwargs or {}))
+
+    class Ops(HostSetOps):
+        def grad_norm(self, *args, **kw):
+            seen.append(("grad_norm", kw.get("stream") or (inside and inside[-1])))
+            super().grad_norm(*args, **kw)
+
+        def grad_scale(self, *args, **kw):
+            seen.append(("grad_scale", kw.get("stream") or (inside and inside[-1])))
+            super().grad_scale(*args, **kw)
+
+    outside_of = []
+    monkeypatch.setattr(torch.cuda, "stream", entered)
+    flat = torch.tensor([3.0, 4.0, 0.0, 0.0])
+    offsets, lengths = _two_halves(flat)
+    with Operations():
+        norm, scale, bad = sharded.sharded_grad_clip(Ops(), flat, offsets, lengths, 1.0, stream="side")
+    assert seen == [("grad_norm", "side"), ("grad_scale", "side")] and outside_of == [] and inside == []
+    assert float(norm) == 5.0 and flat.tolist()[:2] == [pytest.approx(0.6), pytest.approx(0.8)]
