@@ -17,6 +17,8 @@ from dataclasses import dataclass
 import torch
 import torch.distributed as dist
 
+from .binding import IV_ERR_INVALID_ARG, IvError
+
 
 @dataclass(frozen=True)
 class ShardPlan:
@@ -82,12 +84,14 @@ def sharded_root(ctx, local_leaves: torch.Tensor, plan: ShardPlan, rank: int, gr
 
 def sharded_grad_clip(ctx, base, offsets, lengths, max_norm: float, group=None, dtype=None, types=None, stream=None):
     """Clips gradients that are spread over several GPUs by their common norm, in place: `base`, `offsets`, `lengths`,
-    `dtype` and `types` are this rank's share as `ctx.grad_clip` takes it.  Returns (norm, scale, number of tensors with
+    `dtype` and `types` are this rank's share as `ctx.grad_clip` takes it, `max_norm` (>= 0) is the same on every rank.  Returns (norm, scale, number of tensors with
     an infinity or a NaN), each a one-element device tensor with the same value on every rank.
 
     The exchange is 16 bytes per rank: the ranks' sums of squares (64 bits) are gathered and added in rank order, so
     the norm does not depend on how a collective would have added them.  Collective: every rank of `group` calls it.
     All of it is issued on `stream` (default: the current one), and what it returns is ready there."""
+    if not max_norm >= 0:             # also NaN; before the exchange, on every rank alike
+        raise IvError(IV_ERR_INVALID_ARG, "sharded_grad_clip")
     with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
         return _sharded_grad_clip(ctx, base, offsets, lengths, max_norm, group, dtype, types)
 

@@ -10,7 +10,7 @@ import torch.distributed as dist
 import torch.multiprocessing as mp
 from torch.utils._python_dispatch import TorchDispatchMode
 
-from paper_2510_23938_b200 import sharded
+from paper_2510_23938_b200 import binding, sharded
 
 
 class HostSetOps:
@@ -84,3 +84,20 @@ def test_everything_runs_on_the_given_stream(monkeypatch):
         norm, scale, bad = sharded.sharded_grad_clip(Ops(), flat, offsets, lengths, 1.0, stream="side")
     assert seen == [("grad_norm", "side"), ("grad_scale", "side")] and outside_of == [] and inside == []
     assert float(norm) == 5.0 and flat.tolist()[:2] == [pytest.approx(0.6), pytest.approx(0.8)]
+
+
+@pytest.mark.parametrize("limit", [-1.0, -1e-30, math.nan, -math.inf])
+def test_a_limit_that_is_none_is_refused_before_anything_runs(limit):
+    """As grad_clip refuses it; every rank has the same limit, so none is left waiting in the exchange."""
+    ops, flat = HostSetOps(), torch.tensor([3.0, 4.0])
+    offsets, lengths = _two_halves(flat)
+    with pytest.raises(binding.IvError) as err:
+        sharded.sharded_grad_clip(ops, flat, offsets, lengths, limit)
+    assert err.value.code == binding.IV_ERR_INVALID_ARG and ops.seen == [] and flat.tolist() == [3.0, 4.0]
+
+
+@pytest.mark.parametrize("limit", [0.0, -0.0, math.inf])
+def test_limits_at_the_ends_are_taken(limit):
+    flat = torch.tensor([3.0, 4.0])
+    norm, scale, bad = sharded.sharded_grad_clip(HostSetOps(), flat, *_two_halves(flat), limit)
+    assert float(norm) == 5.0 and float(scale) == (1.0 if limit else 0.0) and flat.tolist() == [3.0 * float(scale), 4.0 * float(scale)]
