@@ -12,6 +12,7 @@ exchange (NCCL on GPUs; the tests run the same code over gloo).
 from __future__ import annotations
 
 import contextlib
+import ctypes
 from dataclasses import dataclass
 
 import torch
@@ -90,6 +91,7 @@ def sharded_grad_clip(ctx, base, offsets, lengths, max_norm: float, group=None, 
     The exchange is 16 bytes per rank: the ranks' sums of squares (64 bits) are gathered and added in rank order, so
     the norm does not depend on how a collective would have added them.  Collective: every rank of `group` calls it.
     All of it is issued on `stream` (default: the current one), and what it returns is ready there."""
+    max_norm = ctypes.c_float(max_norm).value      # the 32-bit limit that grad_clip takes
     if not max_norm >= 0:             # also NaN; before the exchange, on every rank alike
         raise IvError(IV_ERR_INVALID_ARG, "sharded_grad_clip")
     with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):

@@ -134,3 +134,17 @@ def test_sharded_clipping_on_another_stream_with_work_in_front(ctx):
         norm, scale, bad = sharded.sharded_grad_clip(ctx, late, offsets, lengths, 0.5, stream=side)
         side.synchronize()
         assert (float(norm), float(scale), int(bad)) == (r["norm"], r["scale"], 0) and torch.equal(late, want)
+
+
+@pytest.mark.parametrize("limit", [0.1, 0.3, 1e-3])
+def test_sharded_clipping_on_one_rank_is_grad_clip_bit_for_bit(ctx, limit):
+    """Limits that 32 bits do not hold exactly, over several gradients."""
+    offsets, lengths = torch.tensor([0, 8000], device="cuda"), torch.tensor([8000, 12_000], device="cuda")
+    for seed in range(40):
+        flat = torch.randn(5000, generator=_gen(seed), device="cuda")
+        other, result = flat.clone(), binding.new_norm_result("cuda")
+        ctx.grad_clip(flat, offsets, lengths, limit, result)
+        norm, scale, bad = sharded.sharded_grad_clip(ctx, other, offsets, lengths, limit)
+        r = binding.read_norm_result(result)
+        assert (float(norm), float(scale), int(bad)) == (r["norm"], r["scale"], r["n_nonfinite"]), seed
+        assert torch.equal(flat, other), seed

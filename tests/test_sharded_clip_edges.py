@@ -4,6 +4,7 @@ import math
 import os
 import socket
 
+import numpy as np
 import pytest
 import torch
 import torch.distributed as dist
@@ -23,10 +24,14 @@ class HostSetOps:
     def _parts(base, offsets, lengths):
         return [base[o // 4:(o + n) // 4] for o, n in zip(offsets.tolist(), lengths.tolist())]
 
+    @classmethod
+    def _squares(cls, base, offsets, lengths):
+        return [p.double().square().sum() for p in cls._parts(base, offsets, lengths)]
+
     def grad_norm(self, base, offsets, lengths, result, norms=None, dtype=None, types=None, stream=None):
         self.seen.append(("grad_norm", stream))
         parts = self._parts(base, offsets, lengths)
-        each = torch.stack([p.double().square().sum() for p in parts])
+        each = torch.stack(self._squares(base, offsets, lengths))
         result.view(torch.float64)[2] = each.sum()
         result.view(torch.int32)[1] = sum(int(not torch.isfinite(p).all()) for p in parts)
         result.view(torch.int64)[3] = sum(p.numel() for p in parts)
@@ -101,3 +106,15 @@ def test_limits_at_the_ends_are_taken(limit):
     flat = torch.tensor([3.0, 4.0])
     norm, scale, bad = sharded.sharded_grad_clip(HostSetOps(), flat, *_two_halves(flat), limit)
     assert float(norm) == 5.0 and float(scale) == (1.0 if limit else 0.0) and flat.tolist() == [3.0 * float(scale), 4.0 * float(scale)]
+
+
+def test_the_limit_is_rounded_as_grad_clip_takes_it():
+    """grad_clip takes a 32-bit limit: scale = round(limit32 / norm), the quotient in 64 bits."""
+    limit, seen = float(np.float32(0.1)), set()
+    for seed in range(200):
+        flat = torch.randn(64, generator=torch.Generator().manual_seed(seed))
+        want = np.float32(limit / math.sqrt(sum(HostSetOps._squares(flat, *_two_halves(flat)))))
+        norm, scale, bad = sharded.sharded_grad_clip(HostSetOps(), flat, *_two_halves(flat), 0.1)
+        assert float(scale) == want, seed
+        seen.add(float(scale))
+    assert len(seen) > 100
