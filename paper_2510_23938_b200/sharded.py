@@ -83,10 +83,12 @@ def sharded_root(ctx, local_leaves: torch.Tensor, plan: ShardPlan, rank: int, gr
     return ctx.merkle_root(all_nodes.contiguous())
 
 
-def sharded_grad_clip(ctx, base, offsets, lengths, max_norm: float, group=None, dtype=None, types=None, stream=None):
+def sharded_grad_clip(ctx, base, offsets, lengths, max_norm: float, group=None, norms=None, dtype=None, types=None,
+                      stream=None):
     """Clips gradients that are spread over several GPUs by their common norm, in place: `base`, `offsets`, `lengths`,
-    `dtype` and `types` are this rank's share as `ctx.grad_clip` takes it, `max_norm` (>= 0) is the same on every rank.  Returns (norm, scale, number of tensors with
-    an infinity or a NaN), each a one-element device tensor with the same value on every rank.
+    `norms`, `dtype` and `types` are this rank's share as `ctx.grad_clip` takes it, `max_norm` (>= 0) is the same on
+    every rank.  Returns (norm, scale, number of tensors with an infinity or a NaN), each a one-element device tensor
+    with the same value on every rank.
 
     The exchange is 16 bytes per rank: the ranks' sums of squares (64 bits) are gathered and added in rank order, so
     the norm does not depend on how a collective would have added them.  Collective: every rank of `group` calls it.
@@ -95,13 +97,13 @@ def sharded_grad_clip(ctx, base, offsets, lengths, max_norm: float, group=None, 
     if not max_norm >= 0:             # also NaN; before the exchange, on every rank alike
         raise IvError(IV_ERR_INVALID_ARG, "sharded_grad_clip")
     with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-        return _sharded_grad_clip(ctx, base, offsets, lengths, max_norm, group, dtype, types)
+        return _sharded_grad_clip(ctx, base, offsets, lengths, max_norm, group, norms, dtype, types)
 
 
-def _sharded_grad_clip(ctx, base, offsets, lengths, max_norm, group, dtype, types):
+def _sharded_grad_clip(ctx, base, offsets, lengths, max_norm, group, norms, dtype, types):
     kinds = {key: value for key, value in (("dtype", dtype), ("types", types)) if value is not None}
     result = torch.zeros(32, dtype=torch.uint8, device=offsets.device)
-    ctx.grad_norm(base, offsets, lengths, result, **kinds)
+    ctx.grad_norm(base, offsets, lengths, result, **kinds, **({} if norms is None else {"norms": norms}))
     mine = torch.stack([result.view(torch.float64)[2], result.view(torch.int32)[1].double()])   # sum of squares, bad tensors
     world = dist.get_world_size(group) if dist.is_initialized() else 1
     if world == 1:

@@ -118,3 +118,9 @@ def test_the_limit_is_rounded_as_grad_clip_takes_it():
         assert float(scale) == want, seed
         seen.add(float(scale))
     assert len(seen) > 100
+
+
+def test_norms_of_this_ranks_tensors():
+    flat, norms = torch.tensor([3.0, 4.0, 6.0, 8.0]), torch.zeros(2)
+    norm, scale, bad = sharded.sharded_grad_clip(HostSetOps(), flat, *_two_halves(flat), 100.0, norms=norms)
+    assert norms.tolist() == [5.0, 10.0] and float(norm) == pytest.approx(math.sqrt(125))
