@@ -84,27 +84,30 @@ def sharded_root(ctx, local_leaves: torch.Tensor, plan: ShardPlan, rank: int, gr
 
 
 def sharded_grad_clip(ctx, base, offsets, lengths, max_norm: float, group=None, norms=None, dtype=None, types=None,
-                      stream=None):
+                      result=None, stream=None):
     """Clips gradients that are spread over several GPUs by their common norm, in place: `base`, `offsets`, `lengths`,
     `norms`, `dtype` and `types` are this rank's share as `ctx.grad_clip` takes it, `max_norm` (>= 0) is the same on
     every rank.  Returns (norm, scale, number of tensors with an infinity or a NaN), each a one-element device tensor
-    with the same value on every rank.
+    with the same value on every rank.  `result` (new_norm_result) receives the record that grad_clip would have written
+    for all ranks' tensors in one set: its status tells whether any rank has left an ill-formed tensor out.
 
-    The exchange is 16 bytes per rank: the ranks' sums of squares (64 bits) are gathered and added in rank order, so
+    The exchange is 32 bytes per rank: the ranks' sums of squares (64 bits) are gathered and added in rank order, so
     the norm does not depend on how a collective would have added them.  Collective: every rank of `group` calls it.
     All of it is issued on `stream` (default: the current one), and what it returns is ready there."""
     max_norm = ctypes.c_float(max_norm).value      # the 32-bit limit that grad_clip takes
     if not max_norm >= 0:             # also NaN; before the exchange, on every rank alike
         raise IvError(IV_ERR_INVALID_ARG, "sharded_grad_clip")
     with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-        return _sharded_grad_clip(ctx, base, offsets, lengths, max_norm, group, norms, dtype, types)
+        return _sharded_grad_clip(ctx, base, offsets, lengths, max_norm, group, norms, dtype, types, result)
 
 
-def _sharded_grad_clip(ctx, base, offsets, lengths, max_norm, group, norms, dtype, types):
+def _sharded_grad_clip(ctx, base, offsets, lengths, max_norm, group, norms, dtype, types, result):
     kinds = {key: value for key, value in (("dtype", dtype), ("types", types)) if value is not None}
-    result = torch.zeros(32, dtype=torch.uint8, device=offsets.device)
-    ctx.grad_norm(base, offsets, lengths, result, **kinds, **({} if norms is None else {"norms": norms}))
-    mine = torch.stack([result.view(torch.float64)[2], result.view(torch.int32)[1].double()])   # sum of squares, bad tensors
+    own = torch.zeros(32, dtype=torch.uint8, device=offsets.device)
+    ctx.grad_norm(base, offsets, lengths, own, **kinds, **({} if norms is None else {"norms": norms}))
+    words = own.view(torch.int32)
+    # sum of squares, elements, tensors with an infinity or a NaN, status: all exact in 64 bits
+    mine = torch.stack([own.view(torch.float64)[2], own.view(torch.int64)[3].double(), words[1].double(), words[0].double()])
     world = dist.get_world_size(group) if dist.is_initialized() else 1
     if world == 1:
         gathered = [mine]
@@ -118,11 +121,16 @@ def _sharded_grad_clip(ctx, base, offsets, lengths, max_norm, group, norms, dtyp
         dist.all_gather(gathered, mine, group=group)
     total = gathered[0].clone()
     for g in gathered[1:]:
-        total += g
+        total[:3] += g[:3]
+        total[3] = torch.maximum(total[3], g[3])
     norm = total[0].sqrt()
     scale = torch.where(norm <= max_norm, torch.ones_like(norm), max_norm / norm).float()
     ctx.grad_scale(base, offsets, lengths, scale.reshape(1), **kinds)
-    return norm.float(), scale, total[1].to(torch.int64)
+    if result is not None:
+        result.view(torch.int32)[0], result.view(torch.int32)[1] = total[3].int(), total[2].int()
+        result.view(torch.float32)[2], result.view(torch.float32)[3] = norm.float(), scale
+        result.view(torch.float64)[2], result.view(torch.int64)[3] = total[0], total[1].long()
+    return norm.float(), scale, total[2].to(torch.int64)
 
 
 def count_mismatches(local_count, device, group=None):

@@ -148,3 +148,15 @@ def test_sharded_clipping_on_one_rank_is_grad_clip_bit_for_bit(ctx, limit):
         r = binding.read_norm_result(result)
         assert (float(norm), float(scale), int(bad)) == (r["norm"], r["scale"], r["n_nonfinite"]), seed
         assert torch.equal(flat, other), seed
+
+
+def test_sharded_clipping_tells_of_an_ill_formed_tensor(ctx):
+    flat = torch.ones(100, device="cuda")
+    offsets, lengths = torch.tensor([0, 42], device="cuda"), torch.tensor([40, 40], device="cuda")
+    result, norms = binding.new_norm_result("cuda"), torch.full((2,), 9.0, device="cuda")
+    sharded.sharded_grad_clip(ctx, flat, offsets, lengths, 1.0, norms=norms, result=result)
+    got = result.clone()
+    assert ctx.device_status() == 2 and binding.read_norm_result(got)["status"] == 2
+    other = torch.ones(100, device="cuda")
+    ctx.grad_clip(other, offsets, lengths, 1.0, result)
+    assert ctx.device_status() == 2 and torch.equal(got, result) and torch.equal(flat, other) and float(norms[1]) == 0

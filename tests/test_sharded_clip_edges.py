@@ -124,3 +124,37 @@ def test_norms_of_this_ranks_tensors():
     flat, norms = torch.tensor([3.0, 4.0, 6.0, 8.0]), torch.zeros(2)
     norm, scale, bad = sharded.sharded_grad_clip(HostSetOps(), flat, *_two_halves(flat), 100.0, norms=norms)
     assert norms.tolist() == [5.0, 10.0] and float(norm) == pytest.approx(math.sqrt(125))
+
+
+class IllFormedOnOneRank(HostSetOps):
+    """Rank 1 has left a tensor out (status 2), as the kernels do with an offset that no element starts at."""
+
+    def grad_norm(self, base, offsets, lengths, result, **kw):
+        super().grad_norm(base, offsets, lengths, result, **kw)
+        result.view(torch.int32)[0] = 2 if dist.get_rank() == 1 else 0
+
+
+def _rank(rank, world, port, out):
+    os.environ.update(MASTER_ADDR="127.0.0.1", MASTER_PORT=str(port), RANK=str(rank), WORLD_SIZE=str(world))
+    dist.init_process_group("gloo", rank=rank, world_size=world)
+    flat = torch.arange(1.0, 5.0 + rank)
+    result = torch.zeros(32, dtype=torch.uint8)
+    norm, scale, bad = sharded.sharded_grad_clip(IllFormedOnOneRank(), flat, *_two_halves(flat), 1.0, result=result)
+    torch.save((float(norm), float(scale), binding.read_norm_result(result)), f"{out}/{rank}.pt")
+    dist.destroy_process_group()
+
+
+def test_every_rank_gets_the_record_of_all_ranks(tmp_path):
+    mp.spawn(_rank, args=(2, _free_port(), str(tmp_path)), nprocs=2)
+    got = [torch.load(tmp_path / f"{r}.pt") for r in range(2)]
+    assert got[0] == got[1]
+    norm, scale, record = got[0]
+    assert record == {"status": 2, "n_nonfinite": 0, "norm": norm, "scale": scale, "sum_squares": 30.0 + 55.0, "n_elements": 9}
+    assert norm == np.float32(math.sqrt(85.0)) and scale == np.float32(1.0 / math.sqrt(85.0))
+
+
+def test_the_record_of_one_rank():
+    flat, result = torch.tensor([3.0, 4.0, math.inf]), torch.full((32,), 255, dtype=torch.uint8)
+    sharded.sharded_grad_clip(HostSetOps(), flat, torch.tensor([0, 8]), torch.tensor([8, 4]), 1.0, result=result)
+    assert binding.read_norm_result(result) == {"status": 0, "n_nonfinite": 1, "norm": math.inf, "scale": 0.0,
+                                                "sum_squares": math.inf, "n_elements": 3}
