@@ -275,7 +275,8 @@ def _out_args(out, out_offsets, out_dtype, types, n):
     if out is None:
         assert out_offsets is None and out_dtype is None, "in place needs no output arguments"
         return None, None, -1
-    assert out_offsets.dtype == torch.int64 and out_offsets.numel() == n
+    assert out_offsets is not None and out_offsets.dtype == torch.int64 and out_offsets.numel() == n, \
+        "out needs out_offsets: one int64 byte offset per tensor"
     code = DTYPES[out_dtype] if out_dtype is not None else (DTYPES[out.dtype] if types is None else -1)
     return _ptr(out), _dev_ptr(out_offsets), code
 
