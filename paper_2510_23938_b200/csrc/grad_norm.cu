@@ -3,7 +3,7 @@
 //     out_k = round(scale * tensor_k)
 //
 // Both passes are bound by memory: two (four) operations per element read.  Tensors of very different sizes are cut
-// into pieces of one size, a power of two that the total size (and whether all are of a 16-bit type) decides.  A CTA adds
+// into pieces of one size, a power of two that the number of elements (and whether all are of 16-bit types) decides.  A CTA adds
 // up a piece, each of its eight warps every eighth run of 32 vectors, without waiting for the others; the warps' sums are
 // collected in shared memory and written for up to 256 pieces at a time.  So the order of every sum is a function of
 // the lengths and not of the launch, the alignment or the GPU: the same gradients give the same norm bit for bit.
@@ -79,8 +79,9 @@ __device__ __forceinline__ uint64_t block_exclusive64(uint64_t v, uint64_t *scan
     return before + x - v;
 }
 
-__device__ __forceinline__ uint32_t shift_for(const TensorSet &set, uint64_t elements) {
-    uint32_t shift = kMinShift + (!set.d_types && set.type != IV_F32 ? 1u : 0u);
+// wide: a tensor with elements is of 32 bits.  However the set is described, the same tensors are cut alike.
+__device__ __forceinline__ uint32_t shift_for(bool wide, uint64_t elements) {
+    uint32_t shift = kMinShift + (wide ? 0u : 1u);
     while (shift < kMaxShift && (elements >> shift) > kPieceTarget) ++shift;
     return shift;
 }
@@ -92,20 +93,26 @@ struct Plan {
 };
 
 // The set laid out by one CTA: first[k] = number of pieces before tensor k, first[n] = all.  A thread takes consecutive
-// tensors; every thread gets the plan.
-template <uint32_t THREADS>
+// tensors; every thread gets the plan.  T: the tensors' type, void where the set says it.
+template <uint32_t THREADS, typename T>
 __device__ __forceinline__ Plan lay_out(const TensorSet &set, uint32_t *first, uint64_t *scan, uint32_t *live_shared, uint32_t *status) {
     const uint64_t per = (set.n + THREADS - 1) / THREADS;
     const uint64_t begin = threadIdx.x * per < set.n ? threadIdx.x * per : set.n;
     const uint64_t end = begin + per < set.n ? begin + per : set.n;
     if (threadIdx.x == 0) *live_shared = 0u;
-    bool bad = false;
+    bool bad = false, wide = false;
     uint64_t elements = 0;
 #pragma unroll 4
-    for (uint64_t k = begin; k < end; ++k) elements += elements_of(set, k, bad);
+    for (uint64_t k = begin; k < end; ++k) {
+        const uint64_t here = elements_of(set, k, bad);
+        elements += here;
+        if (std::is_void_v<T> && set.d_types) wide |= here && type_of(set, k) == IV_F32;
+    }
     Plan plan;
     block_exclusive64<THREADS>(elements, scan, plan.elements);
-    plan.shift = shift_for(set, plan.elements);
+    if constexpr (std::is_void_v<T>) wide = set.d_types ? __syncthreads_or(wide) != 0 : set.type == IV_F32;
+    else wide = sizeof(T) == 4;
+    plan.shift = shift_for(wide, plan.elements);
     auto pieces_of = [&](uint64_t k) { return (elements_of(set, k, bad) + (1ull << plan.shift) - 1) >> plan.shift; };
     uint64_t pieces = 0;
     uint32_t live = 0;
@@ -134,7 +141,7 @@ __global__ void __launch_bounds__(kPlanThreads)
 plan_kernel(TensorSet set, Plan *header, uint32_t *first, uint32_t *status) {
     __shared__ uint64_t scan[kPlanThreads / 32];
     __shared__ uint32_t live;
-    const Plan plan = lay_out<kPlanThreads>(set, first, scan, &live, status);
+    const Plan plan = lay_out<kPlanThreads, void>(set, first, scan, &live, status);
     if (threadIdx.x == 0) *header = plan;
 }
 
@@ -163,13 +170,14 @@ __device__ __forceinline__ uint64_t tensor_of(const uint32_t *first, uint64_t n,
     return lo;
 }
 
+template <typename T>
 __device__ __forceinline__ Walk start_walk(const TensorSet &set, const PlanAt &at, uint32_t *shared_first, uint64_t *scan, uint32_t *live, uint32_t *status) {
     Walk w;
     if (at.header) {
         w.plan = *at.header;
         w.first = at.first;
     } else {
-        w.plan = lay_out<kThreads>(set, shared_first, scan, live, status);
+        w.plan = lay_out<kThreads, T>(set, shared_first, scan, live, status);
         w.first = shared_first;
     }
     return w;
@@ -275,7 +283,7 @@ norm_kernel(TensorSet set, PlanAt at, NormScratch scratch, bool clip, float max_
     __shared__ double pending[kPending][kWarps];     // of pieces this CTA has added up and not written yet
     __shared__ uint32_t flag;
     allow_next_kernel();                                 // the scale kernel may lay out its set
-    const Walk w = start_walk(set, at, shared_first, scan, &live, status);
+    const Walk w = start_walk<T>(set, at, shared_first, scan, &live, status);
     const uint32_t *first = w.first;
     auto finish_set = [&]() {
         double total = 0.0;
@@ -386,7 +394,7 @@ scale_kernel(TensorSet set, PlanAt at, const float *scale_at, uint8_t *out_base,
     extern __shared__ uint32_t shared_first[];
     __shared__ uint64_t scan[kWarps];
     __shared__ uint32_t live;
-    const Walk w = start_walk(set, at, shared_first, scan, &live, status);
+    const Walk w = start_walk<Tin>(set, at, shared_first, scan, &live, status);
     wait_for_previous_kernel();
     const float scale = *reinterpret_cast<const volatile float *>(scale_at);
     if (scale == 1.f && out_base == set.d_base && out_offsets == set.d_offsets) return;   // in place, nothing to change

@@ -160,3 +160,30 @@ def test_sharded_clipping_tells_of_an_ill_formed_tensor(ctx):
     other = torch.ones(100, device="cuda")
     ctx.grad_clip(other, offsets, lengths, 1.0, result)
     assert ctx.device_status() == 2 and torch.equal(got, result) and torch.equal(flat, other) and float(norms[1]) == 0
+
+
+# ------------------------------------------------------------------------------------------------- two descriptions of a set
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32], ids=str)
+@pytest.mark.parametrize("lengths", [[100_003, 7, 0, 40_000], [8193], [20_000] * 1100 + [300_000], [5_000_000, 3]],
+                         ids=lambda s: f"{len(s)}x{sum(s)}")
+def test_bits_do_not_depend_on_how_the_set_is_described(ctx, dtype, lengths):
+    """One type for all tensors, or the same type tensor by tensor, with a tensor of another type and no elements too."""
+    size = torch.empty(0, dtype=dtype).element_size()
+    flat = (torch.randn(sum(lengths), generator=_gen(4), device="cuda") * torch.rand(sum(lengths), generator=_gen(5), device="cuda")).to(dtype)
+    nbytes = torch.tensor(lengths, dtype=torch.int64, device="cuda") * size
+    offsets = torch.cumsum(nbytes, 0) - nbytes
+    code, n = binding.DTYPES[dtype], len(lengths)
+    types = torch.full((n,), code, dtype=torch.uint8, device="cuda")
+    zero = torch.zeros(1, dtype=torch.int64, device="cuda")
+    sets = [(offsets, nbytes, None), (offsets, nbytes, types)]
+    sets += [(torch.cat([zero, offsets]), torch.cat([zero, nbytes]), torch.cat([torch.full_like(types[:1], other), types]))
+             for other in (0, 1)]
+    got = []
+    for where, sizes, kinds in sets:
+        clipped, result, norms = flat.clone(), binding.new_norm_result("cuda"), torch.empty(where.numel(), device="cuda")
+        ctx.grad_clip(clipped, where, sizes, 1.0, result, norms=norms, types=kinds)
+        r = binding.read_norm_result(result)
+        got.append((r, norms[-n:].tolist(), clipped))
+    for r, norms, clipped in got[1:]:
+        assert r == got[0][0] and norms == got[0][1] and torch.equal(clipped, got[0][2])
