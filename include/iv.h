@@ -450,6 +450,14 @@ int iv_merkle_root_noalloc(const uint8_t *d_leaves, uint64_t n_leaves, uint8_t *
  * input and an output type may be the same, or one of them IV_F32.  Tensors may
  * start at any multiple of their element size (a tensor inside a weight file
  * rarely starts at a multiple of 16 bytes); sizes and strides are in elements.
+ *
+ * The calls may be captured into a CUDA graph once the context has made a call
+ * of the same kind and at least that size outside a capture.  A call under
+ * capture that would have to enlarge the context's scratch is refused with
+ * IV_ERR_CUDA (iv_last_cuda_error: cudaErrorStreamCaptureUnsupported) before
+ * anything is recorded.  Scratch that a captured call uses stays until
+ * iv_destroy, also when later calls need more and get their own: replay such
+ * graphs only while the context lives, and not beside its other calls.
  */
 typedef enum iv_dtype { IV_F32 = 0, IV_F16 = 1, IV_BF16 = 2 } iv_dtype;
 

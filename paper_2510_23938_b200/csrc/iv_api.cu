@@ -8,6 +8,12 @@
 
 #include "iv_internal.h"
 
+// A buffer that a growing context has replaced but may not free: a captured graph still points to it.
+struct RetiredBuffer {
+    void *p;
+    RetiredBuffer *next;
+};
+
 struct iv_ctx {
     int device = 0;
     int sm_count = 0;
@@ -59,6 +65,9 @@ struct iv_ctx {
     uint64_t plan_cap = 0;                    // bytes
     uint32_t *d_norm_arrivals = nullptr;      // its arrival counters, zero between calls
     uint64_t norm_arrivals_cap = 0;           // bytes
+
+    bool captured = false;                    // a training-step call has been recorded into a graph
+    RetiredBuffer *retired = nullptr;         // freed with the context
 
     // streaming windows
     uint8_t *d_digests384 = nullptr;          // chunk digests of iv_verify_manifest_sha384 / _sha512, then the root
@@ -116,8 +125,14 @@ template <typename T>
 int grow(iv_ctx *ctx, T **buf, uint64_t *cap_items, uint64_t need_items, uint64_t item_bytes) {
     if (need_items <= *cap_items) return IV_OK;
     if (*buf) {
-        IV_TRY(ctx, cudaDeviceSynchronize());
-        IV_TRY(ctx, cudaFree(*buf));
+        if (ctx->captured) {
+            RetiredBuffer *kept = new (std::nothrow) RetiredBuffer{*buf, ctx->retired};
+            if (!kept) return IV_ERR_NOMEM;
+            ctx->retired = kept;
+        } else {
+            IV_TRY(ctx, cudaDeviceSynchronize());
+            IV_TRY(ctx, cudaFree(*buf));
+        }
         *buf = nullptr;
         *cap_items = 0;
     }
@@ -128,6 +143,37 @@ int grow(iv_ctx *ctx, T **buf, uint64_t *cap_items, uint64_t need_items, uint64_
     *cap_items = items;
     return IV_OK;
 }
+
+// Scratch of the training-step calls.  A call under capture may only use what is there: memory allocated and counters
+// zeroed now would not be so when the graph runs, so growth is then refused (and the capture left as it was).
+struct StepScratch {
+    iv_ctx *ctx;
+    cudaStream_t stream;
+    bool capturing = false;
+
+    int begin() {
+        cudaStreamCaptureStatus status;
+        IV_TRY(ctx, cudaStreamIsCapturing(stream, &status));
+        capturing = status != cudaStreamCaptureStatusNone;
+        ctx->captured |= capturing;
+        return IV_OK;
+    }
+    template <typename T>
+    int ensure(T **buf, uint64_t *cap, uint64_t bytes) {
+        if (capturing && bytes > *cap) return fail_cuda(ctx, cudaErrorStreamCaptureUnsupported);
+        return grow(ctx, buf, cap, bytes, 1);
+    }
+    // Counters that are zero between calls.
+    int ensure_zeroed(uint32_t **buf, uint64_t *cap, uint64_t bytes) {
+        const uint64_t before = *cap;
+        int rc = ensure(buf, cap, bytes);
+        if (rc != IV_OK || *cap == before) return rc;
+        const cudaError_t e = cudaMemsetAsync(*buf, 0, *cap, stream);
+        if (e != cudaSuccess) *cap = 0;          // not zero: the next call begins with another buffer
+        IV_TRY(ctx, e);
+        return IV_OK;
+    }
+};
 
 int ensure_merkle_scratch(iv_ctx *ctx, uint64_t n_leaves) {
     const uint64_t need = (n_leaves + ivk::kMerkleRun - 1) / ivk::kMerkleRun + 1;
@@ -422,6 +468,12 @@ int iv_destroy(iv_ctx *ctx) {
     cudaFree(ctx->d_partial);
     cudaFree(ctx->d_plan);
     cudaFree(ctx->d_norm_arrivals);
+    while (ctx->retired) {
+        RetiredBuffer *kept = ctx->retired;
+        ctx->retired = kept->next;
+        cudaFree(kept->p);
+        delete kept;
+    }
     cudaFree(ctx->d_tree384[0]);
     cudaFree(ctx->d_tree384[1]);
     cudaFree(ctx->d_window[0]);
@@ -1025,14 +1077,12 @@ int embedding_grad(iv_ctx *ctx, const ivk::EmbeddingGradArgs &a, void *cuda_stre
     if (out_rows && a.dim && (!a.d_grad || !aligned_to(a.d_grad, dtype_bytes(a.out_type)))) return IV_ERR_INVALID_ARG;
     DeviceGuard guard(ctx->device);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    int rc = grow(ctx, &ctx->d_sort, &ctx->sort_cap, ivk::embedding_grad_sort_bytes(a.n_tokens), 1);
+    StepScratch step = {ctx, stream};
+    int rc = step.begin();
+    if (rc == IV_OK) rc = step.ensure(&ctx->d_sort, &ctx->sort_cap, ivk::embedding_grad_sort_bytes(a.n_tokens));
+    if (rc == IV_OK) rc = step.ensure(&ctx->d_partial, &ctx->partial_cap, ivk::embedding_grad_partial_bytes(a.n_tokens, a.dim));
+    if (rc == IV_OK) rc = step.ensure_zeroed(&ctx->d_arrivals, &ctx->arrivals_cap, ivk::embedding_grad_arrival_bytes(a.n_tokens, a.dim));
     if (rc != IV_OK) return rc;
-    rc = grow(ctx, &ctx->d_partial, &ctx->partial_cap, ivk::embedding_grad_partial_bytes(a.n_tokens, a.dim), 1);
-    if (rc != IV_OK) return rc;
-    const uint64_t before = ctx->arrivals_cap;
-    rc = grow(ctx, &ctx->d_arrivals, &ctx->arrivals_cap, ivk::embedding_grad_arrival_bytes(a.n_tokens, a.dim), 1);
-    if (rc != IV_OK) return rc;
-    if (ctx->arrivals_cap != before) IV_TRY(ctx, cudaMemsetAsync(ctx->d_arrivals, 0, ctx->arrivals_cap, stream));
     const ivk::EmbeddingGradScratch scratch = {ctx->d_sort, ctx->d_arrivals, ctx->d_partial};
 
     const uint64_t fill_bytes = !a.d_rows && !a.accumulate ? a.n_rows * a.dim * dtype_bytes(a.out_type) : 0;
@@ -1051,13 +1101,11 @@ int embedding_grad(iv_ctx *ctx, const ivk::EmbeddingGradArgs &a, void *cuda_stre
 
 // Scratch of the norm over n tensors.
 int ensure_norm_scratch(iv_ctx *ctx, uint64_t n, cudaStream_t stream) {
-    int rc = grow(ctx, &ctx->d_plan, &ctx->plan_cap, ivk::grad_norm_scratch_bytes(n), 1);
-    if (rc != IV_OK) return rc;
-    const uint64_t before = ctx->norm_arrivals_cap;
-    rc = grow(ctx, &ctx->d_norm_arrivals, &ctx->norm_arrivals_cap, ivk::grad_norm_arrival_bytes(n), 1);
-    if (rc != IV_OK) return rc;
-    if (ctx->norm_arrivals_cap != before) IV_TRY(ctx, cudaMemsetAsync(ctx->d_norm_arrivals, 0, ctx->norm_arrivals_cap, stream));
-    return IV_OK;
+    StepScratch step = {ctx, stream};
+    int rc = step.begin();
+    if (rc == IV_OK) rc = step.ensure(&ctx->d_plan, &ctx->plan_cap, ivk::grad_norm_scratch_bytes(n));
+    if (rc == IV_OK) rc = step.ensure_zeroed(&ctx->d_norm_arrivals, &ctx->norm_arrivals_cap, ivk::grad_norm_arrival_bytes(n));
+    return rc;
 }
 
 // The set as the kernels take it.
@@ -1164,10 +1212,13 @@ int iv_grad_scale(iv_ctx *ctx, void *d_base, const uint64_t *d_offsets, const ui
     if (rc == IV_OK) rc = check_scaled_output(d_out, d_out_offsets, out_type, d_types, type, n);
     if (rc != IV_OK) return rc;
     DeviceGuard guard(ctx->device);
-    if ((rc = grow(ctx, &ctx->d_plan, &ctx->plan_cap, ivk::grad_norm_scratch_bytes(n), 1)) != IV_OK) return rc;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    StepScratch step = {ctx, stream};
+    if ((rc = step.begin()) != IV_OK) return rc;
+    if ((rc = step.ensure(&ctx->d_plan, &ctx->plan_cap, ivk::grad_norm_scratch_bytes(n))) != IV_OK) return rc;
     IV_TRY(ctx, ivk::launch_grad_scale(set, false, d_scale, d_out ? static_cast<uint8_t *>(d_out) : set.d_base,
                                        d_out ? d_out_offsets : d_offsets, out_type, ctx->d_plan, ctx->d_status, ctx->sm_count,
-                                       static_cast<cudaStream_t>(cuda_stream), &ctx->launches));
+                                       stream, &ctx->launches));
     return IV_OK;
 }
 

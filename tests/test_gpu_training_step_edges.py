@@ -187,3 +187,86 @@ def test_bits_do_not_depend_on_how_the_set_is_described(ctx, dtype, lengths):
         got.append((r, norms[-n:].tolist(), clipped))
     for r, norms, clipped in got[1:]:
         assert r == got[0][0] and norms == got[0][1] and torch.equal(clipped, got[0][2])
+
+
+# ------------------------------------------------------------------------------------------------- captured calls and scratch
+
+def _step(ctx, n, rows, dim, tensors):
+    """Inputs and outputs of a gradient of either form, a clip and a scale, and the calls."""
+    tokens = torch.randint(0, rows, (n,), generator=_gen(n), device="cuda")
+    grad = torch.randn(n, dim, generator=_gen(n + 1), device="cuda")
+    flat = torch.randn(tensors * 100, generator=_gen(tensors), device="cuda")
+    lengths = torch.full((tensors,), 400, dtype=torch.int64, device="cuda")
+    offsets = torch.cumsum(lengths, 0) - lengths
+    result, factor = binding.new_norm_result("cuda"), torch.full((1,), 0.5, device="cuda")
+    cap = min(n, rows)
+    out = [torch.zeros(rows, dim, device="cuda"), torch.zeros(cap, dtype=torch.int64, device="cuda"), torch.zeros(cap, dim, device="cuda"),
+           torch.zeros(1, dtype=torch.int64, device="cuda"), torch.zeros_like(flat), torch.zeros_like(flat), result]
+    calls = {
+        "embedding_grad": lambda: ctx.embedding_grad(grad, tokens, rows, out=out[0]),
+        "embedding_grad_rows": lambda: ctx.embedding_grad_rows(grad, tokens, rows, rows=out[1], out=out[2], count=out[3]),
+        "grad_clip": lambda: ctx.grad_clip(flat, offsets, lengths, 1.0, result, out=out[4], out_offsets=offsets),
+        "grad_norm": lambda: ctx.grad_norm(flat, offsets, lengths, result),
+        "grad_scale": lambda: ctx.grad_scale(flat, offsets, lengths, factor, out=out[5], out_offsets=offsets),
+    }
+    return out, calls
+
+
+def test_a_graph_outlives_the_growth_of_its_context():
+    """Captured on small inputs, replayed after larger calls have enlarged the scratch, and between them."""
+    with binding.Context(0) as ctx:
+        out, calls = _step(ctx, 3000, 40, 264, 1100)
+        for call in calls.values():
+            call()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in out]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for call in calls.values():
+                call()
+        for size in (2, 7, 20):
+            large, larger_calls = _step(ctx, 3000 * size, 50, 264 + 8 * size, 1100 * size)
+            for call in larger_calls.values():
+                call()
+            kept = [t.clone() for t in large]
+            for t in out:
+                t.zero_()
+            graph.replay()
+            filler = torch.full((1 << 24,), 7, dtype=torch.int32, device="cuda")      # takes freed memory, if there is any
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(out, want))
+            for call in larger_calls.values():
+                call()
+            assert all(torch.equal(a, b) for a, b in zip(large, kept))
+            del filler
+        assert ctx.device_status() == 0
+        del graph
+
+
+@pytest.mark.parametrize("name", ["embedding_grad", "embedding_grad_rows", "grad_clip", "grad_norm", "grad_scale"])
+@pytest.mark.parametrize("mode", ["global", "thread_local", "relaxed"])
+def test_growth_under_capture_is_refused(name, mode):
+    """With an error and nothing else: the capture goes on, and the call works afterwards."""
+    with binding.Context(0) as ctx:
+        out, calls = _step(ctx, 2000, 300, 40, 50)
+        launched, mark = ctx.kernel_launches, torch.zeros(1, device="cuda")
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, capture_error_mode=mode):
+            mark.add_(1)
+            with pytest.raises(binding.IvError) as err:
+                calls[name]()
+        assert err.value.code == binding.IV_ERR_CUDA and err.value.cuda_error == 900 and ctx.kernel_launches == launched
+        graph.replay()
+        calls[name]()
+        torch.cuda.synchronize()
+        assert float(mark) == 1 and ctx.device_status() == 0
+        first, again = [t.clone() for t in out], torch.cuda.CUDAGraph()
+        with torch.cuda.graph(again, capture_error_mode=mode):
+            calls[name]()
+        for t in out:
+            t.zero_()
+        again.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, first)) and any(bool(t.any()) for t in out)
+        del graph, again
