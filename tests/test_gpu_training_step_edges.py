@@ -270,3 +270,185 @@ def test_growth_under_capture_is_refused(name, mode):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, first)) and any(bool(t.any()) for t in out)
         del graph, again
+
+
+# ------------------------------------------------------------------------------------------------- types the first tests leave out
+
+U = 2.0 ** -24
+ROUND = {t: torch.finfo(t).eps / 2 for t in (torch.float32, torch.float16, torch.bfloat16)}      # unit roundoff
+TINY = {torch.float32: 2.0 ** -150, torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134}      # half the smallest number
+
+
+@pytest.mark.parametrize("pair", [(torch.bfloat16, torch.float32), (torch.float16, torch.float16), (torch.float32, torch.float16)],
+                         ids=lambda p: f"{p[0]}-{p[1]}".replace("torch.", ""))
+@pytest.mark.parametrize("shape", [(1, 3, 1, 0, 0), (129, 300, 257, 3, 1), (511, 700, 2048, 0, 0), (2049, 2, 40, 1, 2), (9000, 4, 515, 0, 0),
+                                   (20_001, 5000, 129, 1, 0)], ids=str)
+def test_gradient_of_the_other_type_pairs(ctx, shape, pair):
+    """n, rows, dim, elements before the first and between the rows.  m terms: (m - 1) u of their magnitudes, one u each for the
+    scale's own rounding, the product and (added) the sum with the old value, one rounding to the output's type."""
+    n, rows, dim, skew, gap = shape
+    kind, out_kind = pair
+    def strided(r, values, dtype):
+        flat = torch.zeros(skew + r * (dim + gap), dtype=dtype, device="cuda")
+        view = flat[skew:].view(r, dim + gap)[:, :dim]
+        return view.copy_(values) if values is not None else view
+    grad = strided(n, torch.randn(n, dim, generator=_gen(n), device="cuda") * 0.05, kind)
+    tokens = torch.randint(0, rows, (n,), generator=_gen(n + 1), device="cuda")
+    old = (torch.randn(rows, dim, generator=_gen(2), device="cuda") * 0.05).to(out_kind)
+    scale = 1.5
+    true = torch.zeros(rows, dim, dtype=torch.float64, device="cuda").index_add_(0, tokens, grad.double()) * scale
+    size = torch.zeros_like(true).index_add_(0, tokens, grad.double().abs()) * scale
+    terms = torch.bincount(tokens, minlength=rows)[:, None].double()
+
+    def close(got, want, extra):
+        limit = ((terms + 3.0) * U * size + extra) * (1 + 1e-6)
+        limit = limit + ROUND[out_kind] * (want.abs() + limit) + TINY[out_kind]
+        return bool(((got.double() - want).abs() <= limit).all())
+
+    dense = ctx.embedding_grad(grad, tokens, rows, scale=scale, out=strided(rows, None, out_kind))
+    assert close(dense, true, 0.0)
+    cap = min(n, rows)
+    touched, packed, count = ctx.embedding_grad_rows(grad, tokens, rows, scale=scale, out=strided(cap, None, out_kind))
+    distinct = torch.unique(tokens)
+    assert int(count) == distinct.numel() and torch.equal(touched[:int(count)], distinct)
+    assert torch.equal(packed[:int(count)], dense[distinct]) and not bool(packed[int(count):].any())
+    added = ctx.embedding_grad(grad, tokens, rows, scale=scale, out=strided(rows, old, out_kind), accumulate=True)
+    assert close(added, true + old.double(), U * (old.double().abs() + size))
+
+
+@pytest.mark.parametrize("cap", [5, 6, 40, 1000])
+def test_compact_gradient_with_more_room_than_tokens(ctx, cap):
+    tokens = torch.tensor([7, 2, 7, 9, 2], device="cuda")
+    grad = torch.arange(1, 6, device="cuda").float()[:, None].expand(5, 300).contiguous()
+    rows = torch.full((cap,), 55, device="cuda")
+    r, g, c = ctx.embedding_grad_rows(grad, tokens, 10, rows=rows, out=torch.full((cap, 300), 7.0, device="cuda"))
+    assert r.tolist() == [2, 7, 9] + [-1] * (cap - 3) and int(c) == 3
+    assert bool((g == torch.tensor([7.0, 4.0, 4.0] + [0.0] * (cap - 3), device="cuda")[:, None]).all())
+
+
+def test_outputs_of_more_than_32_bits_of_bytes(ctx):
+    """Lookup and table gradient whose last rows lie behind 2^32 bytes."""
+    n, dim, rows = 530_000, 4096, 1000                       # 4.3 GB of 16-bit rows
+    table = torch.randn(rows, dim, generator=_gen(1), device="cuda").to(torch.bfloat16)
+    tokens = torch.randint(0, rows, (n,), generator=_gen(2), device="cuda")
+    got = ctx.embedding(table, tokens)
+    for at in range(0, n, 53_000):
+        assert torch.equal(got[at:at + 53_000], table[tokens[at:at + 53_000]])
+    del got
+    torch.cuda.empty_cache()
+    few = torch.tensor([0, n - 1, 524_287, 524_288, n - 1], device="cuda")
+    grad = torch.arange(1, 6, device="cuda").to(torch.bfloat16)[:, None].expand(5, dim).contiguous()
+    out = torch.full((n, dim), 3.0, dtype=torch.bfloat16, device="cuda")
+    ctx.embedding_grad(grad, few, n, out=out)
+    want = {0: 1.0, n - 1: 7.0, 524_287: 3.0, 524_288: 4.0}
+    for row, value in want.items():
+        assert bool((out[row] == value).all()), row
+        out[row] = 0
+    assert not bool(out.view(torch.int64).any())
+
+
+# ------------------------------------------------------------------------------------------------- sets of several types
+
+def _mixed(seed=0):
+    """Tensors of three types in one byte buffer, some at odd multiples of their element, one of several blocks' pieces."""
+    kinds = [torch.float32, torch.bfloat16, torch.float16, torch.bfloat16, torch.float32, torch.float16]
+    counts = [1_000_003, 2_500_001, 7, 0, 12_345, 700_000]
+    places, at = [], 4
+    for kind, count in zip(kinds, counts):
+        size = torch.empty(0, dtype=kind).element_size()
+        at = -(-at // size) * size
+        places.append(at)
+        at += count * size + 2
+    raw = torch.zeros(at + 16, dtype=torch.uint8, device="cuda")
+    views = [raw[p:p + c * torch.empty(0, dtype=k).element_size()].view(k) for k, c, p in zip(kinds, counts, places)]
+    for i, v in enumerate(views):
+        v.copy_(torch.randn(v.numel(), generator=_gen(seed + i), device="cuda") * 0.01)
+    offsets = torch.tensor(places, dtype=torch.int64, device="cuda")
+    lengths = torch.tensor([v.numel() * v.element_size() for v in views], dtype=torch.int64, device="cuda")
+    types = torch.tensor([binding.DTYPES[k] for k in kinds], dtype=torch.uint8, device="cuda")
+    return raw, views, offsets, lengths, types
+
+
+def test_mixed_set_norm_and_clip_in_place(ctx):
+    raw, views, offsets, lengths, types = _mixed()
+    before, untouched = [v.clone() for v in views], raw.clone()
+    want = torch.stack([v.double().square().sum() for v in views])
+    result, norms = binding.new_norm_result("cuda"), torch.empty(len(views), device="cuda")
+    ctx.grad_clip(raw, offsets, lengths, 0.25, result, norms=norms, types=types)
+    r = binding.read_norm_result(result)
+    tolerance = 65 * U / 2 + U
+    assert r["status"] == 0 and r["n_elements"] == sum(v.numel() for v in views)
+    assert abs(r["norm"] - float(want.sum().sqrt())) <= tolerance * r["norm"]
+    assert bool(((norms.double() - want.sqrt()).abs() <= tolerance * want.sqrt()).all())
+    for v, b in zip(views, before):
+        assert torch.equal(v, (b.float() * r["scale"]).to(b.dtype))
+        v.copy_(b)
+    assert r["scale"] < 1 and torch.equal(raw, untouched)            # and nothing between the tensors
+
+
+@pytest.mark.parametrize("out_dtype", [None, torch.float32], ids=str)
+@pytest.mark.parametrize("call", ["grad_clip", "grad_scale"])
+def test_mixed_set_into_another_buffer(ctx, call, out_dtype):
+    raw, views, offsets, lengths, types = _mixed(10)
+    kept = raw.clone()
+    kinds = [out_dtype or v.dtype for v in views]
+    places, at = [], 8
+    for v, k in zip(views, kinds):
+        size = torch.empty(0, dtype=k).element_size()
+        at = -(-at // size) * size
+        places.append(at)
+        at += v.numel() * size + 6
+    out = torch.full((at + 16,), 0xA5, dtype=torch.uint8, device="cuda")
+    where = torch.tensor(places, dtype=torch.int64, device="cuda")
+    result, factor = binding.new_norm_result("cuda"), torch.full((1,), 0.3, device="cuda")
+    if call == "grad_clip":
+        ctx.grad_clip(raw, offsets, lengths, 0.25, result, out=out, out_offsets=where, types=types, out_dtype=out_dtype)
+        scale = binding.read_norm_result(result)["scale"]
+    else:
+        ctx.grad_scale(raw, offsets, lengths, factor, out=out, out_offsets=where, types=types, out_dtype=out_dtype)
+        scale = float(factor)
+    want = torch.full_like(out, 0xA5)
+    for v, k, p in zip(views, kinds, places):
+        values = (v.float() * scale).to(k)
+        want[p:p + values.numel() * values.element_size()] = values.view(torch.uint8)
+    assert torch.equal(out, want) and torch.equal(raw, kept) and ctx.device_status() == 0
+
+
+def test_mixed_set_with_outputs_that_cannot_be(ctx):
+    """An output type that a tensor's type is not rounded to, and an output that no element starts at: status 2, and that
+    tensor's output stays as it was; the others are written."""
+    tensors = [torch.full((300,), 2.0, device="cuda"), torch.full((300,), 2.0, device="cuda").half(),
+               torch.full((300,), 2.0, device="cuda").bfloat16()]
+    base, offsets, lengths, types = binding.tensor_ranges(tensors)
+    factor, where = torch.full((1,), 0.5, device="cuda"), torch.tensor([0, 600, 1200], device="cuda")
+    out = torch.full((900,), 7.0, dtype=torch.bfloat16, device="cuda")
+    ctx.grad_scale(base, offsets, lengths, factor, out=out, out_offsets=where, types=types, out_dtype=torch.bfloat16)
+    assert ctx.device_status() == 2
+    assert out.view(3, 300).float().tolist() == [[1.0] * 300, [7.0] * 300, [1.0] * 300]
+    out = torch.full((1204,), 7.0, device="cuda")
+    ctx.grad_scale(base, offsets, lengths, factor, out=out, out_offsets=torch.tensor([0, 1202, 2404], device="cuda"), types=types,
+                   out_dtype=torch.float32)
+    assert ctx.device_status() == 2
+    assert bool((out[:300] == 1).all()) and bool((out[300:601] == 7).all()) and bool((out[601:901] == 1).all()) and bool((out[901:] == 7).all())
+
+
+def test_more_pieces_of_one_tensor_in_a_block_than_it_keeps(ctx):
+    """160,000 small tensors beside a large one: the set is cut into pieces of 8,192 elements, of which one block has over 256
+    of the large tensor in a row."""
+    small, large = 160_000, 40_000_000
+    flat = torch.randn(small * 3 + large, generator=_gen(1), device="cuda")
+    lengths = torch.cat([torch.full((small // 2,), 12, device="cuda"), torch.tensor([large * 4], device="cuda"),
+                         torch.full((small // 2,), 12, device="cuda")])
+    offsets = torch.cumsum(lengths, 0) - lengths
+    result, norms = binding.new_norm_result("cuda"), torch.empty(small + 1, device="cuda")
+    ctx.grad_norm(flat, offsets, lengths, result, norms=norms)
+    r = binding.read_norm_result(result)
+    first = small // 2 * 3
+    want = torch.cat([flat[:first].view(-1, 3).double().square().sum(1), flat[first:first + large].double().square().sum()[None],
+                      flat[first + large:].view(-1, 3).double().square().sum(1)])
+    assert r["status"] == 0 and r["n_elements"] == flat.numel()
+    assert abs(r["sum_squares"] - float(want.sum())) <= 65 * U * r["sum_squares"]
+    assert bool(((norms.double() - want.sqrt()).abs() <= (65 * U / 2 + U) * want.sqrt()).all())
+    again = binding.new_norm_result("cuda")
+    ctx.grad_norm(flat, offsets, lengths, again)
+    assert torch.equal(again, result)
