@@ -134,8 +134,9 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t ranks = cluster.num_blocks(), me = cluster.block_rank();
     // another CTA's shared memory may be written only once that CTA has started: everybody says so here and waits for the
-    // others before the first such write, behind the first tile's loads and its sort
-    if (ranks > 1) cluster.barrier_arrive();
+    // others before the first such write, behind the first tile's loads and its sort (relaxed: nothing has been written yet
+    // that they could read; an arrival that publishes writes costs 0.7 us)
+    if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint32_t share = ((n + ranks - 1) / ranks + 31u) & ~31u;
     const uint32_t lo = me * share < n ? me * share : n;
