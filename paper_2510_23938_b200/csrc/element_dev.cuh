@@ -174,7 +174,7 @@ __device__ __forceinline__ void load_any(const T *p, Packed<T, V> &out) {
 }
 
 // Elements per vector of a map.  Widening: 8 bytes in, 16 out, so that a warp's stores are contiguous (two 16-byte stores
-// 32 bytes apart from lane to lane write half sectors: 284 against 240 us for 65,536 rows of 4096); narrowing: 32 in, 16 out (loads that
+// 32 bytes apart from lane to lane write half sectors: 284 against 207 us for 65,536 rows of 4096); narrowing: 32 in, 16 out (loads that
 // share sectors meet in L1).
 template <typename Tin, typename Tout>
 struct MapShape {

@@ -15,9 +15,10 @@
 // becoming the longest path; rows of more than kPiece tokens are cut, and the warp that completes a group of pieces
 // adds up their sums.
 //
-// On one B200, bf16 rows of 8 KiB: 65,536 tokens, whole table of 128,256 rows: 264 us, 6.0 TB/s of what has to move (alone: sort
-// 27, sums 113, fill 160; the last two share the memory); 16,384 tokens, compact: 58 us (sort 15, sums 38 at 6 TB/s).
-// 8192 tokens of 4 KiB added to a 32-bit table gradient: 33 us (sort 13, sums 19); 509 tokens: 15 us.
+// On one B200, bf16 rows of 8 KiB: 65,536 tokens, whole table of 128,256 rows: 264 to 272 us, 5.9 TB/s of what has to move
+// (alone: sort 27, sums 112, fill 145; the last two share the memory); 16,384 tokens, compact: 58 us (sort 15, sums 38 at
+// 6 TB/s).  8192 tokens of 4 KiB added to a 32-bit table gradient: 33 us (sort 13, sums 20); 509 tokens: 14 us.  Narrow
+// rows wait for the sort and for one latency per row: 131,072 tokens of 64 columns 70 us, where their bytes need 4.
 #include <cooperative_groups.h>
 #include <type_traits>
 
@@ -33,13 +34,13 @@ namespace {
 
 // ------------------------------------------------------------------------------------------------- sorted tokens
 
-constexpr uint32_t kSortThreads = 512;                     // with 1024 the barriers of a pass cost more (8192 tokens added: 38.4 us, 36.1)
+constexpr uint32_t kSortThreads = 512;                     // with 1024 the barriers of a pass cost more (8192 tokens added: 35.5 us, 33.6; compact 16,384: 61.3, 58.3)
 constexpr uint32_t kSortWarps = kSortThreads / 32;
 constexpr uint32_t kMaxItems = 16;                         // keys per thread and tile
 constexpr uint32_t kDigitBits = 9;                         // two passes for tables of up to 262,143 rows
 constexpr uint32_t kBins = 1u << kDigitBits;
 constexpr uint32_t kWarpParts = kSortWarps / 8;            // the prefix over the warps is taken eight at a time
-constexpr uint32_t kMaxCluster = 16;                       // 65,536 tokens, CTAs of 1024 threads: 26 us with 16 of them, 41 with 8
+constexpr uint32_t kMaxCluster = 16;                       // 16,384 tokens, compact: 58.5 us with 16, 60.0 with 8 (8192 added: 33.9, 33.1)
 
 struct SortShared {
     union {
@@ -444,7 +445,7 @@ sort_tokens_kernel(const Token *tokens, uint32_t n, uint64_t n_rows, int64_t pad
 
 // ------------------------------------------------------------------------------------------------- sums
 
-constexpr uint32_t kWindow = 8;        // sorted positions per warp (16: 48 us against 42 for 8192 tokens added)
+constexpr uint32_t kWindow = 8;        // sorted positions per warp (8192 tokens added / whole table of 65,536: 4 33.0 / 284 us, 8 33.9 / 266, 16 39.2 / 266)
 constexpr uint32_t kSumWarps = 4;
 
 // A lane holds PARTS vectors of 16 bytes of a row, a warp 512 * PARTS bytes of it: two for rows in general; one, and twice
@@ -532,12 +533,14 @@ __device__ __forceinline__ uint32_t slot_of(uint32_t piece_begin, bool first_of_
     return 2u * (piece_begin / kPiece) + (first_of_row ? 1u : 0u);
 }
 
-// ALIGNED: every row of grad_out and of the output starts at a 16-byte boundary (16,384 rows of 4096 bf16 columns: 69 us;
-// of 4095 columns, through the other instance: 90, and 194 with single-element stores).  Otherwise a lane's columns are moved
+// ALIGNED: every row of grad_out and of the output starts at a 16-byte boundary (16,384 rows of 4096 bf16 columns: 64 us;
+// of 4095 columns, through the other instance: 83).  Otherwise a lane's columns are moved
 // back to where the output row has one, so that stores stay whole vectors, and the input is staged in its own
 // 16-byte pieces, from which a lane picks its bytes.
 template <typename Tin, typename Tout, bool COMPACT, bool ADD, bool ALIGNED, uint32_t PARTS>
-__global__ void __launch_bounds__(kSumWarps * 32, 5)    // six CTAs per SM spill: 66 us against 62 for 16,384 tokens
+// Five CTAs per SM: the instances with two vectors of 16-bit columns a lane keep 16 bytes in local memory.  8192 tokens added /
+// 16,384 compact / whole table of 65,536: four CTAs 35.0 / 57.0 / 278 us, five 33.9 / 58.5 / 266, six 41.9 / 62.0 / 274.
+__global__ void __launch_bounds__(kSumWarps * 32, 5)
 sum_rows_kernel(SumArgs a, SortBuffers b) {
     constexpr uint32_t V = Tile<Tin, PARTS>::V, kCols = Tile<Tin, PARTS>::kCols, kParts = PARTS, kStageRows = Tile<Tin, PARTS>::kStageRows;
     constexpr uint32_t kRowPieces = ALIGNED ? kParts * 32u : kParts * 32u + 4u;            // 16-byte pieces of a staged row
@@ -798,7 +801,7 @@ template <typename Token>
 cudaError_t launch_sort_sized(const EmbeddingGradArgs &a, const SortBuffers &b, uint32_t passes, uint32_t *d_status,
                               cudaStream_t stream) {
     // first all CTAs of a cluster, then more keys per thread: what a pass costs is the keys of ONE multiprocessor
-    // (8192 tokens: 18 us with eight CTAs of one key a thread, 47 with one CTA of eight)
+    // (8192 tokens added: 33.8 us with sixteen CTAs of one key a thread, 42.0 with one CTA of sixteen)
     const uint64_t row = (uint64_t)kMaxCluster * kSortThreads;
     if (a.n_tokens <= row) return launch_sort<Token, 1>(a, b, passes, d_status, stream);
     if (a.n_tokens <= 2 * row) return launch_sort<Token, 2>(a, b, passes, d_status, stream);

@@ -271,7 +271,7 @@ struct NormScratch {
     uint32_t *arrived, *arrived_set;
 };
 
-// T: the tensors' type, void for a set of several types.
+// T: the tensors' type, void for a set described by d_types (194 bf16 tensors of 2.6 GB: 455 us against 376).
 template <typename T>
 __global__ void __launch_bounds__(kThreads, std::is_void_v<T> ? 2 : 4)
 norm_kernel(TensorSet set, PlanAt at, NormScratch scratch, bool clip, float max_norm, float *norms, iv_norm_result *result,
@@ -385,8 +385,10 @@ __device__ __forceinline__ void scale_piece(const uint8_t *in8, uint8_t *out8, u
     elem::map_any<Tin, Tout, true>(in, out, count, threadIdx.x, kThreads, [scale](float x) { return x * scale; });
 }
 
-// Tin, Tout: the types of all tensors, void for a set of several types.  Four CTAs per SM: with three the largest sets
-// gain 3 %, sets of 120 MB lose 8 %.
+// Tin, Tout: the types of all tensors, void for a set described by d_types.  Four CTAs per SM: with three the largest sets
+// gain 3 %, sets of 120 MB lose 8 %.  The instance for d_types holds the loops of all seven pairs of types and keeps 1.3 KiB a
+// thread in local memory at two CTAs per SM: clip of 1000 float32 tensors into bf16 3.7 to 3.9 ms against 2.7, of 200
+// packed bf16 tensors 102 us against 81.
 template <typename Tin, typename Tout>
 __global__ void __launch_bounds__(kThreads, std::is_void_v<Tin> ? 2 : 4)
 scale_kernel(TensorSet set, PlanAt at, const float *scale_at, uint8_t *out_base, const uint64_t *out_offsets, int out_type,
