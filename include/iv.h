@@ -440,7 +440,8 @@ int iv_merkle_root_noalloc(const uint8_t *d_leaves, uint64_t n_leaves, uint8_t *
  * between the steps of a training pipeline and, after an update that "touches
  * some chunks", re-verifies only those (iv_tree_update).  The calls below are
  * the parts of such a step that touch few rows or all gradients at once: the
- * embedding lookup, its gradient, the global gradient norm and clipping.
+ * embedding lookup, its gradient, the global gradient norm and clipping; the
+ * norms in front of its products with their gradient; and the update itself.
  * Results are functions of the inputs alone, bit for bit: no floating-point
  * atomics, every sum in an order fixed by the data, so replicas that make the
  * same step keep the same digests and root.
@@ -549,6 +550,94 @@ int iv_grad_clip(iv_ctx *ctx, void *d_base, const uint64_t *d_offsets, const uin
 int iv_grad_scale(iv_ctx *ctx, void *d_base, const uint64_t *d_offsets, const uint64_t *d_lengths, const uint8_t *d_types,
                   int type, uint64_t n, const float *d_scale, void *d_out, const uint64_t *d_out_offsets, int out_type,
                   void *cuda_stream);
+
+/* Layer norm of rows:  y[r, :] = round((x[r, :] - mu) * s * weight + bias),
+ *   mu = mean of x[r, :],  s = 1 / sqrt(mean of (x[r, :] - mu)^2 + eps);
+ * with rms != 0 the root-mean-square form, mu = 0.
+ *   d_x        n_rows rows of dim elements, x_stride apart
+ *   d_weight   dim elements of param_type (any of the three), NULL: ones;
+ *   d_bias     the same, NULL: zeros
+ *   d_y        n_rows rows, y_stride apart; must not overlap the inputs
+ *   d_mean, d_rstd   optional: n_rows floats each, mu and s (for the gradient)
+ *   eps        >= 0, not NaN
+ * A row's result does not depend on the other rows, nor on strides or
+ * alignment.  Sums of squares are taken in 32 bits: a row whose squares leave
+ * that range has s = 0.  IV_ERR_TOO_LARGE for n_rows > 2^30, dim > 2^24. */
+int iv_layer_norm(iv_ctx *ctx, const void *d_x, int x_type, uint64_t x_stride, uint64_t n_rows, uint64_t dim,
+                  const void *d_weight, const void *d_bias, int param_type, float eps, int rms, void *d_y, int y_type,
+                  uint64_t y_stride, float *d_mean, float *d_rstd, void *cuda_stream);
+
+/* Its gradient, from d_dy (of the result's type), the inputs and the stored mu and s:  with h = (x - mu) s and
+ * p = dy * weight,
+ *   dx[r, :] = round(s (p - mean(p) - h mean(p h)))     (rms: without mean(p))
+ *   d_weight_grad = round(old + sum over rows of dy h),  d_bias_grad = round(old + sum over rows of dy)
+ * old being what is there when accumulate != 0 and 0 otherwise.  The sums over
+ * rows are taken in 32 bits in an order that n_rows, dim and the types alone decide.
+ *   x_type, y_type  as in the forward call: dx is of x_type
+ *   d_mean          not read when rms != 0
+ *   d_weight_grad, d_bias_grad   dim elements of sum_type (any), NULL: not wanted
+ * Without rows dx is empty and both sums are 0 (or old).  Outputs must not
+ * overlap inputs or each other. */
+int iv_layer_norm_grad(iv_ctx *ctx, const void *d_dy, int y_type, uint64_t dy_stride, const void *d_x, int x_type,
+                       uint64_t x_stride, uint64_t n_rows, uint64_t dim, const void *d_weight, int param_type,
+                       const float *d_mean, const float *d_rstd, int rms, void *d_dx, uint64_t dx_stride,
+                       void *d_weight_grad, void *d_bias_grad, int sum_type, int accumulate, void *cuda_stream);
+
+/* One AdamW step over a ragged tensor set, t being the number of this step (*d_step + 1):
+ *   g = c * gradient,   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
+ *   w = w (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps),
+ * in 32 bits, w rounded once.  The weights are given as for iv_grad_norm, all
+ * of one type, and updated in place (in the bytes of a weight file: the chunks
+ * they lie in are then dirty).
+ *   d_grads, d_grad_offsets   tensor k's gradient, as many elements of
+ *                    grad_type, starts at d_grads + d_grad_offsets[k] (bytes,
+ *                    modulo 2^64).  The types are equal or one of them is IV_F32
+ *   d_state_offsets  n places in the state, in ELEMENTS, ascending multiples of
+ *                    IV_ADAMW_BLOCK: element i of tensor k has its moments at
+ *                    d_state_offsets[k] + i
+ *   state_size       elements of the state, a multiple of IV_ADAMW_BLOCK
+ *   state_bits       32: d_m, d_v are state_size floats, 32-byte aligned.
+ *                    8: d_m, d_v are state_size codes (e4m3: sign, four bits of
+ *                    exponent with bias 7, three digits; 0x7f is NaN), 8-byte
+ *                    aligned, and d_m_scales, d_v_scales one float for each
+ *                    block: m = code * scale, sqrt(v) = code * scale.  All
+ *                    zero: no moments yet.  What lies between tensors is left alone
+ *   d_master         optional, for 16-bit weights: state_size floats, 32-byte
+ *                    aligned, the weights in 32 bits; they are updated, and
+ *                    the weights receive them rounded
+ *   d_lr             optional: the learning rate in device memory, instead of lr
+ *   d_norm           optional: the record of iv_grad_norm over all gradients;
+ *                    c = norm <= max_norm ? 1 : max_norm / norm (c = 1 without a
+ *                    record).  When its n_nonfinite is not 0 the call
+ *                    changes nothing, the number of steps included
+ *   d_step           the number of steps taken, counted up by the call
+ * stochastic != 0 rounds 16-bit weights up with the probability that the lost
+ * bits give (to nearest otherwise); 8-bit moments are always rounded so, a
+ * root that is not 0 to no less than the smallest code.  The random words are
+ * a function of (seed, t, place in the state):  with
+ *   mix(x): x ^= x >> 16; x *= 0x6A09E667; x ^= x >> 15; x *= 0xBB67AE85; x ^= x >> 16,
+ *   K0 = mix(mix(mix(low(seed) + G) + high(seed)) + low(t)),  K1 = mix(K0 + high(t) + G),
+ *   G = 0x9E3779B9,  q = place / 8,  b = mix(q ^ K0),  a = mix(b + K1)
+ * word k is b + (k + 1) a, and k = place % 8 rounds m, 8 + place % 8 the root, 16 +
+ * place % 8 the weight, each by the word's upper bits, as many as are lost (16 at
+ * most for weights, 20 for codes).
+ * A block's scale is its largest finite magnitude / 447.9995; an infinite or NaN
+ * moment becomes a NaN code and leaves the other elements of its block alone.
+ * A tensor that is ill-formed (a length, address or place at no multiple of its
+ * unit, no room before the next tensor's place) is left out and sets the device status
+ * to 2.  IV_ERR_TOO_LARGE for n > 2^30 or state_size > 2^34. */
+#define IV_ADAMW_BLOCK 256
+typedef struct iv_adamw_options {
+    double lr, beta1, beta2, eps, weight_decay; /* all >= 0 and finite, the betas < 1 */
+    float max_norm;                             /* >= 0; read with d_norm only */
+    uint32_t stochastic;
+    uint64_t seed;
+} iv_adamw_options;
+int iv_adamw_step(iv_ctx *ctx, void *d_base, const uint64_t *d_offsets, const uint64_t *d_lengths, int type, uint64_t n,
+                  const void *d_grads, const uint64_t *d_grad_offsets, int grad_type, const uint64_t *d_state_offsets,
+                  uint64_t state_size, int state_bits, void *d_m, void *d_v, float *d_m_scales, float *d_v_scales,
+                  float *d_master, const iv_adamw_options *h_options, const float *d_lr, const iv_norm_result *d_norm,
+                  uint64_t *d_step, void *cuda_stream);
 
 /* ---------------------------------------------------------------------------
  * Roofline probe (a measurement aid; the paper has no counterpart).  Runs a

@@ -35,7 +35,10 @@ EXPORTS = (
     "iv_hash_chunks_sha512", "iv_merkle_root_sha512", "iv_verify_manifest_sha512",
     "iv_hash_chunks_rfc6962", "iv_merkle_root_rfc6962", "iv_verify_manifest_rfc6962",
     "iv_embedding", "iv_embedding_grad", "iv_embedding_grad_rows", "iv_grad_norm", "iv_grad_clip", "iv_grad_scale",
+    "iv_layer_norm", "iv_layer_norm_grad", "iv_adamw_step",
 )
+
+ADAMW_BLOCK = 256          # IV_ADAMW_BLOCK
 
 # iv_dtype of the training-step operators
 DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
@@ -92,6 +95,13 @@ class NormResult(ctypes.Structure):
     """iv_norm_result as laid out in device memory (32 bytes)."""
     _fields_ = [("status", ctypes.c_uint32), ("n_nonfinite", ctypes.c_uint32), ("norm", ctypes.c_float),
                 ("scale", ctypes.c_float), ("sum_squares", ctypes.c_double), ("n_elements", ctypes.c_uint64)]
+
+
+class AdamwOptions(ctypes.Structure):
+    """iv_adamw_options: host struct."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("max_norm", ctypes.c_float), ("stochastic", ctypes.c_uint32),
+                ("seed", ctypes.c_uint64)]
 
 
 _lib = None
@@ -195,6 +205,14 @@ def load_library() -> ctypes.CDLL:
     lib.iv_grad_clip.restype = i32
     lib.iv_grad_scale.argtypes = [vp, vp, vp, vp, vp, i32, u64, vp, vp, vp, i32, vp]
     lib.iv_grad_scale.restype = i32
+    lib.iv_layer_norm.argtypes = [vp, vp, i32, u64, u64, u64, vp, vp, i32, f32, i32, vp, i32, u64, vp, vp, vp]
+    lib.iv_layer_norm.restype = i32
+    lib.iv_layer_norm_grad.argtypes = [vp, vp, i32, u64, vp, i32, u64, u64, u64, vp, i32, vp, vp, i32, vp, u64, vp, vp, i32,
+                                       i32, vp]
+    lib.iv_layer_norm_grad.restype = i32
+    lib.iv_adamw_step.argtypes = [vp, vp, vp, vp, i32, u64, vp, vp, i32, vp, u64, i32, vp, vp, vp, vp, vp,
+                                  ctypes.POINTER(AdamwOptions), vp, vp, vp, vp]
+    lib.iv_adamw_step.restype = i32
     _lib = lib
     return lib
 
@@ -256,6 +274,16 @@ def _rows_of(t: torch.Tensor, n: int, dim: int) -> tuple:
         return ptr, stride
     assert t.is_cuda and t.is_contiguous() and t.numel() == n * dim and t.shape[-1] == dim, "wrong number of rows or columns"
     return t.data_ptr(), dim
+
+
+def _vector_ptr(t: Optional[torch.Tensor], n: int, dtype: Optional[torch.dtype] = None) -> Optional[int]:
+    """Device pointer of n contiguous elements (of `dtype`), None for no tensor."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.is_contiguous(), "device tensors must be contiguous CUDA tensors"
+    assert t.numel() == n, "wrong number of elements"
+    assert dtype is None or t.dtype == dtype, f"must be {dtype}"
+    return t.data_ptr()
 
 
 def _token_bytes(tokens: torch.Tensor) -> int:
@@ -750,6 +778,93 @@ class Context:
                                      *_out_args(out, out_offsets, out_dtype, types, args[-1]), _stream_ptr(stream))
         self._check(rc, "iv_grad_scale")
 
+    def layer_norm(self, x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                   eps: float = 1e-5, rms: bool = False, out: torch.Tensor | None = None,
+                   out_dtype: torch.dtype | None = None, mean: torch.Tensor | None = None,
+                   rstd: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+        """iv_layer_norm over the last dimension of `x` (a matrix with contiguous rows, or a contiguous tensor of more
+        dimensions): (x - mean) * rstd * weight + bias, rounded once to `out_dtype` (default: x's); `rms`: without the
+        mean.  `mean` and `rstd` (float32, one per row) receive what `layer_norm_grad` wants."""
+        dim = x.shape[-1]
+        n = x.numel() // dim if dim else 0
+        x_ptr, x_stride = _rows_of(x, n, dim)
+        if out is None:
+            out = _empty(x.shape, out_dtype or x.dtype, x.device, stream)
+        out_ptr, out_stride = _rows_of(out, n, dim)
+        assert weight is None or bias is None or weight.dtype == bias.dtype, "weight and bias are of one type"
+        param = weight if weight is not None else bias
+        rc = self._lib.iv_layer_norm(self._h, x_ptr, DTYPES[x.dtype], x_stride, n, dim, _vector_ptr(weight, dim),
+                                     _vector_ptr(bias, dim), 0 if param is None else DTYPES[param.dtype], eps, rms, out_ptr,
+                                     DTYPES[out.dtype], out_stride, _vector_ptr(mean, n, torch.float32),
+                                     _vector_ptr(rstd, n, torch.float32), _stream_ptr(stream))
+        if rc:
+            self._check(rc, "iv_layer_norm")
+        return out
+
+    def layer_norm_grad(self, grad_out: torch.Tensor, x: torch.Tensor, mean: torch.Tensor | None, rstd: torch.Tensor,
+                        weight: torch.Tensor | None = None, rms: bool = False, out: torch.Tensor | None = None,
+                        weight_grad: torch.Tensor | None = None, bias_grad: torch.Tensor | None = None,
+                        accumulate: bool = False, stream=None) -> torch.Tensor:
+        """iv_layer_norm_grad: the gradient of `layer_norm`'s x (of x's type), `grad_out` being that of its result;
+        `weight_grad` and `bias_grad` (of one type), where given, receive the sums over the rows, or with `accumulate`
+        have them added.  `mean` is not read with `rms` and may then be None."""
+        dim = x.shape[-1]
+        n = x.numel() // dim if dim else 0
+        x_ptr, x_stride = _rows_of(x, n, dim)
+        grad_ptr, grad_stride = _rows_of(grad_out, n, dim)
+        if out is None:
+            out = _empty(x.shape, x.dtype, x.device, stream)
+        assert out.dtype == x.dtype, "the gradient is of x's type"
+        out_ptr, out_stride = _rows_of(out, n, dim)
+        assert weight_grad is None or bias_grad is None or weight_grad.dtype == bias_grad.dtype, "sums are of one type"
+        sums = weight_grad if weight_grad is not None else bias_grad
+        rc = self._lib.iv_layer_norm_grad(self._h, grad_ptr, DTYPES[grad_out.dtype], grad_stride, x_ptr, DTYPES[x.dtype], x_stride,
+                                          n, dim, _vector_ptr(weight, dim), 0 if weight is None else DTYPES[weight.dtype],
+                                          None if rms else _vector_ptr(mean, n, torch.float32),
+                                          _vector_ptr(rstd, n, torch.float32), rms, out_ptr, out_stride,
+                                          _vector_ptr(weight_grad, dim), _vector_ptr(bias_grad, dim),
+                                          0 if sums is None else DTYPES[sums.dtype], accumulate, _stream_ptr(stream))
+        if rc:
+            self._check(rc, "iv_layer_norm_grad")
+        return out
+
+    def adamw_step(self, base: torch.Tensor, offsets: torch.Tensor, lengths: torch.Tensor, grads: torch.Tensor,
+                   grad_offsets: torch.Tensor, state_offsets: torch.Tensor, m: torch.Tensor, v: torch.Tensor,
+                   step: torch.Tensor, m_scales: torch.Tensor | None = None, v_scales: torch.Tensor | None = None,
+                   master: torch.Tensor | None = None, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
+                   weight_decay: float = 1e-2, norm: torch.Tensor | None = None, max_norm: float | None = None,
+                   stochastic: bool = False, seed: int = 0, dtype: torch.dtype | None = None,
+                   grad_dtype: torch.dtype | None = None, stream=None) -> None:
+        """iv_adamw_step (asynchronous), in place: `base`, `offsets`, `lengths` (bytes) give the weights as for grad_norm,
+        `grads`, `grad_offsets` (bytes) the gradients; `state_offsets` to `master` are the state as adamw_state makes it
+        (`**state`), its moments float32 or float8_e4m3fn.  `lr` is a number or a one-element float32 device tensor, read
+        when the step runs.  `norm` is the record of grad_norm over the gradients: they are clipped to `max_norm` on the
+        way (None: not clipped), and where one is not finite nothing changes.  `seed` sets the random words that round
+        8-bit moments and, with `stochastic`, 16-bit weights.  Types default to those of `base` and `grads`."""
+        n = offsets.numel()
+        for t in (offsets, lengths, grad_offsets, state_offsets):
+            assert t.numel() == n and t.dtype == torch.int64, "offsets, lengths and places: one int64 per tensor"
+        size = m.numel()
+        assert m.dtype in (torch.float32, torch.float8_e4m3fn), "moments are float32 or float8_e4m3fn"
+        bits = 32 if m.dtype == torch.float32 else 8
+        assert bits == 32 or (m_scales is not None and v_scales is not None), "8-bit moments need their scales"
+        assert step.is_cuda and step.dtype == torch.int64 and step.numel() == 1, "step: one int64 on the device"
+        blocks = size // ADAMW_BLOCK
+        lr_ptr = None
+        if isinstance(lr, torch.Tensor):
+            assert lr.is_cuda and lr.dtype == torch.float32 and lr.numel() == 1, "lr: a number or one float32 on the device"
+            lr_ptr, lr = lr.data_ptr(), 0.0
+        options = AdamwOptions(lr, betas[0], betas[1], eps, weight_decay, float("inf") if max_norm is None else max_norm,
+                               stochastic, seed & 0xffffffffffffffff)
+        rc = self._lib.iv_adamw_step(
+            self._h, _ptr(base), _dev_ptr(offsets), _dev_ptr(lengths), DTYPES[dtype or base.dtype], n, _ptr(grads),
+            _dev_ptr(grad_offsets), DTYPES[grad_dtype or grads.dtype], _dev_ptr(state_offsets), size, bits,
+            _vector_ptr(m, size), _vector_ptr(v, size, m.dtype), _vector_ptr(m_scales, blocks, torch.float32) if bits == 8 else None,
+            _vector_ptr(v_scales, blocks, torch.float32) if bits == 8 else None, _vector_ptr(master, size, torch.float32),
+            options, lr_ptr, None if norm is None else _result_ptr(norm), step.data_ptr(), _stream_ptr(stream))
+        if rc:
+            self._check(rc, "iv_adamw_step")
+
     def last_digests(self, n: int) -> torch.Tensor:
         """Copy of the chunk digests the last verification on this context computed."""
         ptr = self._lib.iv_ctx_digests(self._h)
@@ -818,6 +933,28 @@ def tensor_ranges(tensors) -> tuple:
     return (base, torch.tensor(signed, dtype=torch.int64, device=device),
             torch.tensor([_nbytes(t) for t in tensors], dtype=torch.int64, device=device),
             torch.tensor([DTYPES[t.dtype] for t in tensors], dtype=torch.uint8, device=device))
+
+
+def adamw_state(elements, device, bits: int = 32, master: bool = False) -> dict:
+    """The state of adamw_step for tensors of `elements` elements each (a list of numbers), before the first step: places
+    (multiples of ADAMW_BLOCK), moments in 32 or 8 bits, the number of steps and, with `master`, room for the weights in
+    32 bits, which the caller fills (grad_scale by 1 into `master` at 4 * state_offsets does)."""
+    assert bits in (8, 32), "moments are held in 8 or 32 bits"
+    places, size = [], 0
+    for n in elements:
+        places.append(size)
+        size += -(-int(n) // ADAMW_BLOCK) * ADAMW_BLOCK
+    state = {"state_offsets": torch.tensor(places, dtype=torch.int64, device=device),
+             "step": torch.zeros(1, dtype=torch.int64, device=device)}
+    for name in ("m", "v"):
+        if bits == 32:
+            state[name] = torch.zeros(size, device=device)
+        else:
+            state[name] = torch.zeros(size, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+            state[name + "_scales"] = torch.zeros(size // ADAMW_BLOCK, device=device)
+    if master:
+        state["master"] = torch.zeros(size, device=device)
+    return state
 
 
 def read_results(results: torch.Tensor) -> list:

@@ -1,5 +1,6 @@
 // C ABI of libiv (see include/iv.h): argument checks, scratch management,
 // stream plumbing.  All arithmetic of the path runs in the kernels.
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
 #include <new>
@@ -65,6 +66,10 @@ struct iv_ctx {
     uint64_t plan_cap = 0;                    // bytes
     uint32_t *d_norm_arrivals = nullptr;      // its arrival counters, zero between calls
     uint64_t norm_arrivals_cap = 0;           // bytes
+    float *d_norm_partial = nullptr;          // runs' sums of iv_layer_norm_grad
+    uint64_t norm_partial_cap = 0;            // bytes
+    uint32_t *d_adamw_arrivals = nullptr;     // arrival counter of iv_adamw_step, zero between calls
+    uint64_t adamw_arrivals_cap = 0;          // bytes
 
     bool captured = false;                    // a training-step call has been recorded into a graph
     RetiredBuffer *retired = nullptr;         // freed with the context
@@ -468,6 +473,8 @@ int iv_destroy(iv_ctx *ctx) {
     cudaFree(ctx->d_partial);
     cudaFree(ctx->d_plan);
     cudaFree(ctx->d_norm_arrivals);
+    cudaFree(ctx->d_norm_partial);
+    cudaFree(ctx->d_adamw_arrivals);
     while (ctx->retired) {
         RetiredBuffer *kept = ctx->retired;
         ctx->retired = kept->next;
@@ -1061,6 +1068,7 @@ bool aligned_to(const void *p, uint64_t bytes) { return (reinterpret_cast<uintpt
 constexpr uint64_t kMaxTokens = 1ull << 30;
 constexpr uint64_t kMaxRows = 1ull << 31;
 constexpr uint64_t kMaxColumns = 1ull << 24;
+constexpr uint64_t kMaxState = 1ull << 34;
 
 // Arguments that both forms of the gradient have in common, then scratch and launch.
 int embedding_grad(iv_ctx *ctx, const ivk::EmbeddingGradArgs &a, void *cuda_stream) {
@@ -1219,6 +1227,88 @@ int iv_grad_scale(iv_ctx *ctx, void *d_base, const uint64_t *d_offsets, const ui
     IV_TRY(ctx, ivk::launch_grad_scale(set, false, d_scale, d_out ? static_cast<uint8_t *>(d_out) : set.d_base,
                                        d_out ? d_out_offsets : d_offsets, out_type, ctx->d_plan, ctx->d_status, ctx->sm_count,
                                        stream, &ctx->launches));
+    return IV_OK;
+}
+
+int iv_layer_norm(iv_ctx *ctx, const void *d_x, int x_type, uint64_t x_stride, uint64_t n_rows, uint64_t dim,
+                  const void *d_weight, const void *d_bias, int param_type, float eps, int rms, void *d_y, int y_type,
+                  uint64_t y_stride, float *d_mean, float *d_rstd, void *cuda_stream) {
+    if (!ctx || !type_pair_ok(x_type, y_type) || !is_dtype(param_type) || !(eps >= 0.f)) return IV_ERR_INVALID_ARG;
+    if (n_rows > kMaxTokens || dim > kMaxColumns) return IV_ERR_TOO_LARGE;
+    if (n_rows == 0 || dim == 0) return IV_OK;
+    if (!d_x || !d_y || (n_rows > 1 && (x_stride < dim || y_stride < dim))) return IV_ERR_INVALID_ARG;
+    if (!aligned_to(d_x, dtype_bytes(x_type)) || !aligned_to(d_y, dtype_bytes(y_type)) ||
+        !aligned_to(d_weight, dtype_bytes(param_type)) || !aligned_to(d_bias, dtype_bytes(param_type)) ||
+        !aligned_to(d_mean, 4) || !aligned_to(d_rstd, 4))
+        return IV_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    const ivk::LayerNormArgs a = {d_x, x_type, x_stride, n_rows, dim, d_weight, d_bias, param_type, eps, rms != 0,
+                                  d_y, y_type, y_stride, d_mean, d_rstd};
+    IV_TRY(ctx, ivk::launch_layer_norm(a, ctx->sm_count, static_cast<cudaStream_t>(cuda_stream), &ctx->launches));
+    return IV_OK;
+}
+
+int iv_layer_norm_grad(iv_ctx *ctx, const void *d_dy, int y_type, uint64_t dy_stride, const void *d_x, int x_type,
+                       uint64_t x_stride, uint64_t n_rows, uint64_t dim, const void *d_weight, int param_type,
+                       const float *d_mean, const float *d_rstd, int rms, void *d_dx, uint64_t dx_stride,
+                       void *d_weight_grad, void *d_bias_grad, int sum_type, int accumulate, void *cuda_stream) {
+    if (!ctx || !type_pair_ok(x_type, y_type) || !is_dtype(param_type) || !is_dtype(sum_type)) return IV_ERR_INVALID_ARG;
+    if (n_rows > kMaxTokens || dim > kMaxColumns) return IV_ERR_TOO_LARGE;
+    if (dim == 0) return IV_OK;
+    if (n_rows && (!d_dy || !d_x || !d_dx || !d_rstd || (!rms && !d_mean))) return IV_ERR_INVALID_ARG;
+    if (n_rows > 1 && (dy_stride < dim || x_stride < dim || dx_stride < dim)) return IV_ERR_INVALID_ARG;
+    if (!aligned_to(d_dy, dtype_bytes(y_type)) || !aligned_to(d_x, dtype_bytes(x_type)) || !aligned_to(d_dx, dtype_bytes(x_type)) ||
+        !aligned_to(d_weight, dtype_bytes(param_type)) || !aligned_to(d_mean, 4) || !aligned_to(d_rstd, 4) ||
+        !aligned_to(d_weight_grad, dtype_bytes(sum_type)) || !aligned_to(d_bias_grad, dtype_bytes(sum_type)))
+        return IV_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    StepScratch step = {ctx, stream};
+    int rc = step.begin();
+    if (rc == IV_OK && n_rows)
+        rc = step.ensure(&ctx->d_norm_partial, &ctx->norm_partial_cap, ivk::layer_norm_grad_scratch_bytes(n_rows, dim));
+    if (rc != IV_OK) return rc;
+    const ivk::LayerNormGradArgs a = {d_dy, y_type, dy_stride, d_x, x_type, x_stride, n_rows, dim, d_weight, param_type,
+                                      rms ? nullptr : d_mean, d_rstd, rms != 0, d_dx, dx_stride, d_weight_grad, d_bias_grad,
+                                      sum_type, accumulate != 0};
+    IV_TRY(ctx, ivk::launch_layer_norm_grad(a, ctx->d_norm_partial, ctx->sm_count, stream, &ctx->launches));
+    return IV_OK;
+}
+
+int iv_adamw_step(iv_ctx *ctx, void *d_base, const uint64_t *d_offsets, const uint64_t *d_lengths, int type, uint64_t n,
+                  const void *d_grads, const uint64_t *d_grad_offsets, int grad_type, const uint64_t *d_state_offsets,
+                  uint64_t state_size, int state_bits, void *d_m, void *d_v, float *d_m_scales, float *d_v_scales,
+                  float *d_master, const iv_adamw_options *h_options, const float *d_lr, const iv_norm_result *d_norm,
+                  uint64_t *d_step, void *cuda_stream) {
+    if (!ctx || !h_options || !d_step || !aligned_to(d_step, 8) || !type_pair_ok(type, grad_type)) return IV_ERR_INVALID_ARG;
+    const iv_adamw_options &o = *h_options;
+    for (double x : {o.lr, o.beta1, o.beta2, o.eps, o.weight_decay})
+        if (!(x >= 0.0 && x < HUGE_VAL)) return IV_ERR_INVALID_ARG;
+    if (o.beta1 >= 1.0 || o.beta2 >= 1.0 || (d_norm && !(o.max_norm >= 0.f))) return IV_ERR_INVALID_ARG;
+    if (!aligned_to(d_norm, 8) || !aligned_to(d_lr, 4)) return IV_ERR_INVALID_ARG;
+    ivk::TensorSet set;
+    int rc = tensor_set(ctx, d_base, d_offsets, d_lengths, nullptr, type, n, &set);
+    if (rc != IV_OK) return rc;
+    if (n && (!d_grads || !d_grad_offsets || !d_state_offsets)) return IV_ERR_INVALID_ARG;
+    if (!aligned_to(d_grad_offsets, 8) || !aligned_to(d_state_offsets, 8)) return IV_ERR_INVALID_ARG;
+    if (state_size > kMaxState) return IV_ERR_TOO_LARGE;
+    if (state_size % IV_ADAMW_BLOCK || (state_bits != 8 && state_bits != 32)) return IV_ERR_INVALID_ARG;
+    if (d_master && type == IV_F32) return IV_ERR_INVALID_ARG;
+    if (state_size && (!d_m || !d_v || (state_bits == 8 && (!d_m_scales || !d_v_scales)))) return IV_ERR_INVALID_ARG;
+    const uint64_t unit = state_bits == 8 ? 8 : 32;
+    if (!aligned_to(d_m, unit) || !aligned_to(d_v, unit) || !aligned_to(d_master, 32) || !aligned_to(d_m_scales, 4) ||
+        !aligned_to(d_v_scales, 4))
+        return IV_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    StepScratch step = {ctx, stream};
+    if ((rc = step.begin()) != IV_OK) return rc;
+    if ((rc = step.ensure_zeroed(&ctx->d_adamw_arrivals, &ctx->adamw_arrivals_cap, 4)) != IV_OK) return rc;
+    const ivk::AdamwArgs a = {set, static_cast<const uint8_t *>(d_grads), d_grad_offsets, grad_type, d_state_offsets, state_size,
+                              state_bits, d_m, d_v, d_m_scales, d_v_scales, d_master, o.lr, o.weight_decay, std::log(o.beta1),
+                              std::log(o.beta2), (float)o.beta1, (float)(1.0 - o.beta1), (float)o.beta2, (float)(1.0 - o.beta2),
+                              (float)o.eps, o.max_norm, o.stochastic != 0, o.seed, d_lr, d_norm, d_step};
+    IV_TRY(ctx, ivk::launch_adamw(a, ctx->d_adamw_arrivals, ctx->d_status, ctx->sm_count, stream, &ctx->launches));
     return IV_OK;
 }
 

@@ -314,6 +314,67 @@ cudaError_t launch_grad_scale(const TensorSet &set, bool planned, const float *d
                               const uint64_t *d_out_offsets, int out_type, void *d_scratch, uint32_t *d_status, int sm_count,
                               cudaStream_t stream, uint64_t *launches);
 
+// layer_norm.cu --------------------------------------------------------------
+// Arguments as in iv.h (checked there); strides in elements.
+struct LayerNormArgs {
+    const void *d_x;
+    int x_type;
+    uint64_t x_stride, n, dim;
+    const void *d_weight, *d_bias;   // NULL: none
+    int param_type;
+    float eps;
+    bool rms;
+    void *d_y;
+    int y_type;
+    uint64_t y_stride;
+    float *d_mean, *d_rstd;          // NULL: not wanted
+};
+cudaError_t launch_layer_norm(const LayerNormArgs &a, int sm_count, cudaStream_t stream, uint64_t *launches);
+
+// layer_norm_grad.cu ---------------------------------------------------------
+struct LayerNormGradArgs {
+    const void *d_dy;
+    int y_type;
+    uint64_t dy_stride;
+    const void *d_x;
+    int x_type;
+    uint64_t x_stride, n, dim;
+    const void *d_weight;            // NULL: ones
+    int param_type;
+    const float *d_mean, *d_rstd;    // mean: NULL for zeros
+    bool rms;
+    void *d_dx;                      // of x_type
+    uint64_t dx_stride;
+    void *d_dw, *d_db;               // NULL: not wanted
+    int dw_type;
+    bool accumulate;
+};
+uint64_t layer_norm_grad_scratch_bytes(uint64_t n, uint64_t dim);
+cudaError_t launch_layer_norm_grad(const LayerNormGradArgs &a, float *d_partial, int sm_count, cudaStream_t stream, uint64_t *launches);
+
+// adamw.cu -------------------------------------------------------------------
+struct AdamwArgs {
+    TensorSet set;                   // the weights; all of set.type
+    const uint8_t *d_grads;
+    const uint64_t *d_grad_offsets;  // bytes
+    int grad_type;
+    const uint64_t *d_state_offsets; // elements
+    uint64_t size;                   // elements of the state, a multiple of IV_ADAMW_BLOCK
+    int bits;
+    void *d_m, *d_v;
+    float *d_m_scales, *d_v_scales;  // 8 bits only
+    float *d_master;                 // NULL: none
+    double lr, weight_decay, log_beta1, log_beta2;
+    float beta1, rest1, beta2, rest2, eps, max_norm;
+    bool stochastic;
+    uint64_t seed;
+    const float *d_lr;               // NULL: lr
+    const iv_norm_result *d_norm;    // NULL: no clipping
+    uint64_t *d_step;
+};
+// d_arrived: a word that is zero between calls.
+cudaError_t launch_adamw(const AdamwArgs &a, uint32_t *d_arrived, uint32_t *d_status, int sm_count, cudaStream_t stream, uint64_t *launches);
+
 // selftest.cu --------------------------------------------------------------
 // One warp waits (bounded by limit_cycles SM clocks) on a barrier nobody arrives at, then sets *d_status to
 // IVK_DEV_TIMEOUT and returns; *d_waited (may be NULL) receives the clocks it waited.
