@@ -13,10 +13,14 @@
 // random words that are a hash of (seed, step, element): the same call gives the same bits.
 #include "element_dev.cuh"
 #include "iv_internal.h"
+#include "row_dev.cuh"
 
 namespace ivk {
 
 namespace {
+
+using elem::Pair;
+using elem::unpack8;
 
 constexpr uint32_t kBlock = IV_ADAMW_BLOCK;
 constexpr uint32_t kWarps = 8;
@@ -73,33 +77,48 @@ struct Words {
     __device__ __forceinline__ uint32_t word(uint32_t k) const { return b + (k + 1u) * a; }
 };
 
-__device__ __forceinline__ float root_approx(float x) {
-    float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
+// Root and reciprocal to 2^-22 or better.  The reciprocal takes what is below 2^-126 for 0.
+__device__ __forceinline__ Pair root_approx(Pair x) {
+    float lo, hi;
+    x.get(lo, hi);
+    asm("sqrt.approx.f32 %0, %0;" : "+f"(lo));
+    asm("sqrt.approx.f32 %0, %0;" : "+f"(hi));
+    return Pair(lo, hi);
+}
+__device__ __forceinline__ Pair reciprocal_approx(Pair x) {
+    float lo, hi;
+    x.get(lo, hi);
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(lo));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(hi));
+    return Pair(lo, hi);
 }
 
-// A 32-bit value rounded to a 16-bit type by random bits in the place of those that go; infinities and NaN as they are.
-template <typename T> __device__ __forceinline__ T round_random(float x, uint32_t word);
-template <> __device__ __forceinline__ float round_random<float>(float x, uint32_t) { return x; }
-template <> __device__ __forceinline__ __nv_bfloat16 round_random<__nv_bfloat16>(float x, uint32_t word) {
-    const uint32_t bits = __float_as_uint(x);
-    if ((bits & 0x7f800000u) == 0x7f800000u) return __float2bfloat16_rn(x);
-    return __ushort_as_bfloat16((uint16_t)((bits + (word >> 16)) >> 16));
+// Bits of a 32-bit value with random bits added in the place of those that a 16-bit type does not have; infinities stay, NaN too.
+template <typename T> __device__ __forceinline__ uint32_t round_random(float x, uint32_t word);
+template <> __device__ __forceinline__ uint32_t round_random<__nv_bfloat16>(float x, uint32_t word) {
+    // the bits of a NaN that an operation gives, 0x7fffffff, would carry into the sign
+    return ((uint32_t)min((int32_t)__float_as_uint(x), 0x7fff0000) + (word >> 16)) >> 16;
 }
-template <> __device__ __forceinline__ __half round_random<__half>(float x, uint32_t word) {
-    if (!(fabsf(x) < 65536.f)) return __float2half_rn(x);
+template <> __device__ __forceinline__ uint32_t round_random<__half>(float x, uint32_t word) {
+    if (!(fabsf(x) < 65536.f)) return __half_as_ushort(__float2half_rn(x));
     // times 2^-112 a half's exponent and digits, small ones too, are the upper bits of the float's
-    const uint32_t code = (__float_as_uint(fabsf(x) * 0x1p-112f) + (word >> 19)) >> 13;
-    return __ushort_as_half((uint16_t)(code | (__float_as_uint(x) >> 31 << 15)));
+    return (__float_as_uint(fabsf(x) * 0x1p-112f) + (word >> 19)) >> 13 | __float_as_uint(x) >> 31 << 15;
 }
 
-// Four codes of a word as 32-bit values.
-__device__ __forceinline__ void decode4(uint32_t w, float *out) {
-    uint32_t lo, hi;
-    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
-    elem::unpack2<__half>(lo, out[0], out[1]);
-    elem::unpack2<__half>(hi, out[2], out[3]);
+// Eight codes as 32-bit values times a scale.
+__device__ __forceinline__ void decode8(uint2 codes, float scale, Pair (&out)[4]) {
+    const Pair by(scale);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint32_t lo, hi;
+        asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+            : "=r"(lo), "=r"(hi) : "r"(i ? codes.y : codes.x));
+        float a, b;
+        elem::unpack2<__half>(lo, a, b);
+        out[2 * i] = Pair(a, b) * by;
+        elem::unpack2<__half>(hi, a, b);
+        out[2 * i + 1] = Pair(a, b) * by;
+    }
 }
 
 // What a block's values are multiplied by on their way to codes, and its scale.  kTop lies just below the largest code, 448, so
@@ -115,219 +134,243 @@ __device__ __forceinline__ BlockScale block_scale(float top, bool bad) {
     return {top > 0.f ? __fmul_rn(__frcp_rn(safe), kTop) : 0.f, top > 0.f ? safe * (float)(1.0 / 447.9995) : 0.f, bad};
 }
 
-// The largest of a warp's values, which are not negative or are looked at without their sign; infinities and NaN left out.
-__device__ __forceinline__ float block_top(const float (&x)[8], bool &bad) {
-    uint32_t top = 0u;
+// The largest magnitude of a warp's values; infinities and NaN left out.
+__device__ __forceinline__ float block_top(const Pair (&x)[4], bool &bad) {
+    float top = 0.f, lo, hi;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-    top = __reduce_max_sync(0xffffffffu, top);
-    bad = top >= 0x7f800000u;
-    if (bad) {
-        top = 0u;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t bits = __float_as_uint(x[i]) & 0x7fffffffu;
-            top = max(top, bits < 0x7f800000u ? bits : 0u);
-        }
-        top = __reduce_max_sync(0xffffffffu, top);
+    for (int i = 0; i < 4; ++i) {
+        x[i].get(lo, hi);
+        asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(lo), "f"(hi));
     }
-    return __uint_as_float(top);
+    uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
+    bad = bits >= 0x7f800000u;
+    if (bad) {
+        bits = 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i].get(lo, hi);
+            if (isfinite(lo)) bits = max(bits, __float_as_uint(fabsf(lo)));
+            if (isfinite(hi)) bits = max(bits, __float_as_uint(fabsf(hi)));
+        }
+        bits = __reduce_max_sync(0xffffffffu, bits);
+    }
+    return __uint_as_float(bits);
+}
+
+// Codes.  Times 2^-120 a value's exponent and digits, small ones too, are the upper bits of the float's, and 20 random bits are
+// added to the 20 that go; four bits further up the code is the upper byte.
+__device__ __forceinline__ uint32_t upper_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+}
+__device__ __forceinline__ uint2 upper_bytes(const uint32_t (&x)[8]) {
+    return make_uint2(upper_bytes(x[0], x[1], x[2], x[3]), upper_bytes(x[4], x[5], x[6], x[7]));
+}
+__device__ __forceinline__ bool has_zero_byte(uint32_t w) { return ((w - 0x01010101u) & ~w & 0x80808080u) != 0u; }
+constexpr uint32_t kNanCode = 0x7f000000u;
+
+__device__ __forceinline__ uint2 encode_first(const Pair (&m)[4], const BlockScale &s, const Words &words) {
+    uint32_t code[8];
+    const Pair inverse(s.inverse), shift(0x1p-120f);
+#pragma unroll
+    for (uint32_t i = 0; i < 4u; ++i) {
+        float y[2];
+        (m[i] * inverse * shift).get(y[0], y[1]);
+#pragma unroll
+        for (uint32_t k = 0; k < 2u; ++k) {
+            const uint32_t sum = __float_as_uint(y[k]) + (words.word(2u * i + k) >> 12);       // the sign stays where it is
+            code[2 * i + k] = sum * 16u | (sum & 0x80000000u);
+        }
+    }
+    if (s.bad) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; ++i) {
+            float x[2];
+            m[i / 2].get(x[0], x[1]);
+            if (!isfinite(x[i & 1])) code[i] = kNanCode;
+        }
+    }
+    return upper_bytes(code);
+}
+// Of the roots r, which stay above zero once they are.  `top` is the exact root of the block's largest finite v: the elements that
+// have it get the code that the exact root has.
+__device__ __forceinline__ uint2 encode_second(const Pair (&v)[4], const Pair (&r)[4], float v_top, float top, const BlockScale &s, const Words &words) {
+    uint32_t code[8];
+    const Pair inverse(s.inverse), shift(0x1p-120f);
+#pragma unroll
+    for (uint32_t i = 0; i < 4u; ++i) {
+        float x[2], z[2], y[2];
+        v[i].get(x[0], x[1]);
+        r[i].get(z[0], z[1]);
+        (Pair(x[0] == v_top ? top : z[0], x[1] == v_top ? top : z[1]) * inverse * shift).get(y[0], y[1]);
+#pragma unroll
+        for (uint32_t k = 0; k < 2u; ++k) code[2 * i + k] = (__float_as_uint(y[k]) + (words.word(8u + 2u * i + k) >> 12)) * 16u;
+    }
+    if (s.bad) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; ++i) {
+            float x[2];
+            v[i / 2].get(x[0], x[1]);
+            if (!isfinite(x[i & 1])) code[i] = kNanCode;
+        }
+    }
+    uint2 out = upper_bytes(code);
+    if (has_zero_byte(out.x) || has_zero_byte(out.y)) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; ++i) {
+            float x[2];
+            v[i / 2].get(x[0], x[1]);
+            if (x[i & 1] > 0.f) code[i] = max(code[i], 1u << 24);
+        }
+        out = upper_bytes(code);
+    }
+    return out;
 }
 
 // A lane's eight elements of a block.
-template <typename Tw, typename Tg, int BITS, bool MASTER>
+template <int BITS>
 struct Lane {
-    float w[8], g[8], m[8], r[8];              // r: second moments (32 bits) or their roots (8 bits)
+    Pair w[4], g[4], m[4], v[4], r[4];         // before update(), 8 bits: v holds the roots
 
-    // New moments and weights; r becomes the roots.  The moments' products and sums are rounded one by one, so that elementary
-    // operations give the same bits; the root and the quotient are approximate to 2^-22 of an update, which is small against the
-    // weight that it changes.
-    __device__ __forceinline__ void update(const Coefficients &c, float (&v)[8]) {
+    // New moments, roots r and weights.  The moments' products and sums are rounded one by one, so that elementary operations
+    // give the same bits; root and reciprocal are approximate, small against the weight that an update changes.
+    __device__ __forceinline__ void update(const Coefficients &c) {
+        const Pair factor(c.factor), beta1(c.beta1), rest1(c.rest1), beta2(c.beta2), rest2(c.rest2), root(c.root), eps(c.eps), step(-c.step), keep(c.keep);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float g1 = __fmul_rn(g[i], c.factor), square = BITS == 32 ? r[i] : __fmul_rn(r[i], r[i]);
-            m[i] = __fadd_rn(__fmul_rn(m[i], c.beta1), __fmul_rn(g1, c.rest1));
-            v[i] = __fadd_rn(__fmul_rn(square, c.beta2), __fmul_rn(__fmul_rn(g1, g1), c.rest2));
+        for (int i = 0; i < 4; ++i) {
+            const Pair g1 = g[i] * factor, square = BITS == 32 ? v[i] : v[i] * v[i];
+            m[i] = m[i] * beta1 + g1 * rest1;
+            v[i] = square * beta2 + g1 * g1 * rest2;
             r[i] = root_approx(v[i]);
-            w[i] = fmaf(w[i], c.keep, -__fdividef(m[i] * c.step, fmaf(r[i], c.root, c.eps)));
+            w[i] = fma2(w[i], keep, m[i] * step * reciprocal_approx(fma2(r[i], root, eps)));
+        }
+    }
+    // The new moments' codes and scales.
+    __device__ __forceinline__ void encode(const Words &words, uint2 &m_codes, uint2 &v_codes, float &m_scale, float &v_scale) const {
+        bool bad;
+        const float m_top = block_top(m, bad);
+        const BlockScale first = block_scale(m_top, bad);
+        const float v_top = block_top(v, bad), root_top = __fsqrt_rn(v_top);
+        const BlockScale second = block_scale(root_top, bad);
+        m_codes = encode_first(m, first, words);
+        v_codes = encode_second(v, r, v_top, root_top, second, words);
+        m_scale = first.scale;
+        v_scale = second.scale;
+    }
+    // The weights as elements of type T.
+    template <typename T>
+    __device__ __forceinline__ elem::Packed<T, 8> rounded(bool stochastic, const Words &words) const {
+        elem::Packed<T, 8> out;
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i].get(x[2 * i], x[2 * i + 1]);
+        if constexpr (sizeof(T) == 2) {
+            if (stochastic) {
+#pragma unroll
+                for (uint32_t i = 0; i < 8u; i += 2u)
+                    out.w[i / 2] = __byte_perm(round_random<T>(x[i], words.word(16u + i)), round_random<T>(x[i + 1], words.word(17u + i)), 0x5410);
+                return out;
+            }
+        }
+        out.pack(x);
+        return out;
+    }
+};
+
+__device__ __forceinline__ void load8(const float *p, Pair (&x)[4]) {
+    asm volatile("ld.global.v4.b64 {%0, %1, %2, %3}, [%4];" : "=l"(x[0].bits), "=l"(x[1].bits), "=l"(x[2].bits), "=l"(x[3].bits) : "l"(p));
+}
+__device__ __forceinline__ void store8(float *p, const Pair (&x)[4]) {
+    asm volatile("st.global.v4.b64 [%0], {%1, %2, %3, %4};" ::"l"(p), "l"(x[0].bits), "l"(x[1].bits), "l"(x[2].bits), "l"(x[3].bits) : "memory");
+}
+// A warp's 256 consecutive elements.  WALIGN: 16 or 8 where the elements start at such a boundary.
+template <typename T, int WALIGN>
+__device__ __forceinline__ void store_warp(T *p, const elem::Packed<T, 8> &own) {
+    constexpr int kStep = WALIGN == 8 ? 2 : 4;
+    if (WALIGN > 0 || elem::misalignment(p) == 0u) {
+#pragma unroll
+        for (int i = 0; i < elem::Packed<T, 8>::kWords; i += kStep) elem::store_aligned<kStep>(reinterpret_cast<uint32_t *>(p) + i, own.w + i);
+    } else {
+        rows::store_pieces<T>(p, own, 8u, 32u);
+    }
+}
+
+// A lane's share of a block as it lies in memory.
+template <typename Tw, typename Tg, int BITS, bool MASTER, int WALIGN, int GALIGN>
+struct Raw {
+    elem::Vector<Tg, 8, GALIGN> g;
+    elem::Vector<Tw, 8, MASTER ? 16 : WALIGN> w;         // not with MASTER
+    Pair master[4], m[4], v[4];                          // with MASTER; 32 bits
+    uint2 m8, v8;                                        // 8 bits
+    float m_scale, v_scale;
+    __device__ __forceinline__ void load(const AdamwArgs &a, uint64_t at, const Tw *pw, const Tg *pg) {
+        g.load(pg, elem::misalignment(pg));
+        if constexpr (MASTER) load8(a.d_master + at, master);
+        else w.load(pw, elem::misalignment(pw));
+        if constexpr (BITS == 32) {
+            load8(static_cast<const float *>(a.d_m) + at, m);
+            load8(static_cast<const float *>(a.d_v) + at, v);
+        } else {
+            m8 = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(a.d_m) + at);
+            v8 = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(a.d_v) + at);
+            m_scale = a.d_m_scales[at / kBlock];
+            v_scale = a.d_v_scales[at / kBlock];
+        }
+    }
+    __device__ __forceinline__ void get(const Tw *pw, const Tg *pg, Lane<BITS> &e) const {
+        unpack8(g.get(elem::misalignment(pg)), e.g);
+        if constexpr (!MASTER) unpack8(w.get(elem::misalignment(pw)), e.w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (MASTER) e.w[i] = master[i];
+            if constexpr (BITS == 32) {
+                e.m[i] = m[i];
+                e.v[i] = v[i];
+            }
+        }
+        if constexpr (BITS == 8) {
+            decode8(m8, m_scale, e.m);
+            decode8(v8, v_scale, e.v);
         }
     }
 };
 
-__device__ __forceinline__ void load8(const float *p, float (&x)[8]) {
-    uint32_t b[8];
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]), "=r"(b[4]),
-                 "=r"(b[5]), "=r"(b[6]), "=r"(b[7]) : "l"(p));
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(b[i]);
-}
-__device__ __forceinline__ void store8(float *p, const float (&x)[8]) {
-    uint32_t b[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(x[i]);
-    elem::store_32_bytes(p, b);
-}
-
-// A warp's 256 consecutive elements at any element alignment: every lane but the last stores the aligned pieces that begin in its
-// elements, with its neighbour's first bytes behind its own; what lies before the first and behind the last goes one by one.
-template <typename T>
-__device__ __forceinline__ void store_warp(T *p, const elem::Packed<T, 8> &own) {
-    constexpr int W = elem::Packed<T, 8>::kWords;
-    const uint32_t lane = threadIdx.x & 31u, off = elem::misalignment(p);
-    if (off == 0u) {
-#pragma unroll
-        for (int i = 0; i < W; i += 4) elem::store_aligned<4>(reinterpret_cast<uint32_t *>(p) + i, own.w + i);
-        return;
-    }
-    if (off == 8u) {
-#pragma unroll
-        for (int i = 0; i < W; i += 2) elem::store_aligned<2>(reinterpret_cast<uint32_t *>(p) + i, own.w + i);
-        return;
-    }
-    uint32_t x[W + 4];
-#pragma unroll
-    for (int i = 0; i < W; ++i) x[i] = own.w[i];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[W + i] = __shfl_down_sync(0xffffffffu, own.w[i], 1);
-    const uint32_t skip = 16u - off;                     // bytes of this lane before its first piece
-    if (skip & 8u) {
-#pragma unroll
-        for (int i = 0; i < W + 2; ++i) x[i] = x[i + 2];
-    }
-    if (skip & 4u) {
-#pragma unroll
-        for (int i = 0; i < W + 1; ++i) x[i] = x[i + 1];
-    }
-    if constexpr (sizeof(T) == 2) {
-#pragma unroll
-        for (int i = 0; i < W; ++i) x[i] = __funnelshift_r(x[i], x[i + 1], (skip & 2u) * 8u);
-    }
-    uint32_t *pieces = reinterpret_cast<uint32_t *>(reinterpret_cast<uint8_t *>(p) + skip);
-#pragma unroll
-    for (int i = 0; i < W; i += 4)
-        if (lane < 31u || i + 4 < W) elem::store_aligned<4>(pieces + i, x + i);
-    // the first lane's elements before its first piece, the last one's behind its last whole piece
-    const uint32_t head = skip / (uint32_t)sizeof(T), tail = (uint32_t)(sizeof(T) * 8u - off) / (uint32_t)sizeof(T);
-#pragma unroll
-    for (uint32_t i = 0; i < 8u; ++i)
-        if ((lane == 0u && i < head) || (lane == 31u && i >= tail)) {
-            if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t *>(p)[i] = own.w[i];
-            else reinterpret_cast<uint16_t *>(p)[i] = (uint16_t)(own.w[i / 2] >> (16u * (i & 1u)));
-        }
-}
-
-// Codes of eight values into two words.  Times 2^-120 a value's exponent and digits, small ones too, are the upper bits of the
-// float's, and 20 random bits are added to the 20 that go.  Infinities and NaN give 0x7f, NaN.
-__device__ __forceinline__ uint32_t pack_codes(const uint32_t *c) { return c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24; }
-__device__ __forceinline__ uint32_t code_of(uint32_t bits, uint32_t word) { return (bits + (word >> 12)) >> 20; }
-__device__ __forceinline__ uint2 encode_first(const float (&m)[8], const BlockScale &s, const Words &words) {
-    uint32_t code[8];
-#pragma unroll
-    for (uint32_t i = 0; i < 8u; ++i) {
-        code[i] = code_of(__float_as_uint(fabsf(m[i]) * s.inverse * 0x1p-120f), words.word(i));
-        if (s.bad && !isfinite(m[i])) code[i] = 0x7fu;
-        code[i] |= __float_as_uint(m[i]) >> 24 & 0x80u;
-    }
-    return make_uint2(pack_codes(code), pack_codes(code + 4));
-}
-// Of the roots, which stay above zero once they are.  `top` is the exact root of the block's largest finite v: the element that has it
-// gets the code that the exact root has (the approximate ones are taken 2^-21 larger and no larger than it).
-__device__ __forceinline__ uint2 encode_second(const float (&r)[8], float top, const BlockScale &s, const Words &words) {
-    uint32_t code[8];
-    const float inverse = s.inverse * (1.f + 0x1p-21f);
-    const uint32_t cap = __float_as_uint(top * s.inverse * 0x1p-120f);
-#pragma unroll
-    for (uint32_t i = 0; i < 8u; ++i) {
-        code[i] = code_of(min(__float_as_uint(r[i] * inverse * 0x1p-120f), cap), words.word(8u + i));
-        code[i] = max(code[i], min(__float_as_uint(r[i]), 1u));
-        if (s.bad && !isfinite(r[i])) code[i] = 0x7fu;
-    }
-    return make_uint2(pack_codes(code), pack_codes(code + 4));
-}
-
-// The new moments' codes and scales; r: the approximate roots of v.
-__device__ __forceinline__ void encode_block(const float (&m)[8], const float (&v)[8], const float (&r)[8], const Words &words, uint2 &m_codes,
-                                             uint2 &v_codes, float &m_scale, float &v_scale) {
-    bool bad;
-    const float m_top = block_top(m, bad);
-    const BlockScale first = block_scale(m_top, bad);
-    const float v_top = __fsqrt_rn(block_top(v, bad));
-    const BlockScale second = block_scale(v_top, bad);
-    m_codes = encode_first(m, first, words);
-    v_codes = encode_second(r, v_top, second, words);
-    m_scale = first.scale;
-    v_scale = second.scale;
-}
-
-// One block: state elements s .. s + 255, of which `left` belong to the tensor whose weights and gradients are at w and g.
+// `count` whole blocks from state element s on, of the tensor whose weights and gradients are at w and g.  8 bits: the next block is
+// on its way while one is worked on.
 template <typename Tw, typename Tg, int BITS, bool MASTER, int WALIGN, int GALIGN>
-__device__ __forceinline__ void whole_block(const AdamwArgs &a, const Coefficients &c, uint64_t s, Tw *w, const Tg *g) {
+__device__ __forceinline__ void whole_blocks(const AdamwArgs &a, const Coefficients &c, uint64_t s, uint32_t count, Tw *w, const Tg *g) {
     const uint32_t lane = threadIdx.x & 31u;
-    const uint64_t at = s + lane * 8u;
-    Lane<Tw, Tg, BITS, MASTER> e;
+    uint64_t at = s + lane * 8u;
     w += lane * 8u;
     g += lane * 8u;
-    elem::Vector<Tw, 8, WALIGN> raw_w;
-    elem::Vector<Tg, 8, GALIGN> raw_g;
-    const uint32_t w_off = elem::misalignment(w), g_off = elem::misalignment(g);
-    uint2 m8, v8;
-    float m_scale = 1.f, v_scale = 1.f;
-    raw_g.load(g, g_off);
-    if constexpr (BITS == 32) {
-        load8(static_cast<const float *>(a.d_m) + at, e.m);
-        load8(static_cast<const float *>(a.d_v) + at, e.r);
-    } else {
-        m8 = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(a.d_m) + at);
-        v8 = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(a.d_v) + at);
-        m_scale = a.d_m_scales[s / kBlock];
-        v_scale = a.d_v_scales[s / kBlock];
-    }
-    if constexpr (MASTER) load8(a.d_master + at, e.w);
-    else {
-        raw_w.load(w, w_off);
-        raw_w.get(w_off).unpack(e.w);
-    }
-    raw_g.get(g_off).unpack(e.g);
-    if constexpr (BITS == 8) {
-        decode4(m8.x, e.m);
-        decode4(m8.y, e.m + 4);
-        decode4(v8.x, e.r);
-        decode4(v8.y, e.r + 4);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            e.m[i] *= m_scale;
-            e.r[i] *= v_scale;
+    Raw<Tw, Tg, BITS, MASTER, WALIGN, GALIGN> raw, next;
+    if (BITS == 8) next.load(a, at, w, g);
+#pragma unroll 1
+    for (uint32_t b = 0; b < count; ++b, at += kBlock, w += kBlock, g += kBlock) {
+        if (BITS == 8) {
+            raw = next;
+            if (b + 1u < count) next.load(a, at + kBlock, w + kBlock, g + kBlock);
+        } else {
+            raw.load(a, at, w, g);
         }
-    }
-    float v[8];
-    e.update(c, v);
-    const Words words((uint32_t)(at / 8u), c);
-    if constexpr (MASTER) store8(a.d_master + at, e.w);
-    elem::Packed<Tw, 8> out;
-    if (sizeof(Tw) == 2 && a.stochastic) {
-        if constexpr (sizeof(Tw) == 2) {
-#pragma unroll
-            for (uint32_t i = 0; i < 8u; i += 2u) {
-                const Tw lo = round_random<Tw>(e.w[i], words.word(16u + i)), hi = round_random<Tw>(e.w[i + 1], words.word(17u + i));
-                out.w[i / 2] = (uint32_t)*reinterpret_cast<const uint16_t *>(&lo) | (uint32_t)*reinterpret_cast<const uint16_t *>(&hi) << 16;
+        Lane<BITS> e;
+        raw.get(w, g, e);
+        e.update(c);
+        const Words words((uint32_t)(at / 8u), c);
+        store_warp<Tw, WALIGN>(w, e.template rounded<Tw>(a.stochastic, words));
+        if constexpr (MASTER) store8(a.d_master + at, e.w);
+        if constexpr (BITS == 32) {
+            store8(static_cast<float *>(a.d_m) + at, e.m);
+            store8(static_cast<float *>(a.d_v) + at, e.v);
+        } else {
+            uint2 m_codes, v_codes;
+            float m_scale, v_scale;
+            e.encode(words, m_codes, v_codes, m_scale, v_scale);
+            *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(a.d_m) + at) = m_codes;
+            *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(a.d_v) + at) = v_codes;
+            if (lane == 0u) {
+                a.d_m_scales[at / kBlock] = m_scale;
+                a.d_v_scales[at / kBlock] = v_scale;
             }
-        }
-    } else {
-        out.pack(e.w);
-    }
-    store_warp<Tw>(w, out);
-    if constexpr (BITS == 32) {
-        store8(static_cast<float *>(a.d_m) + at, e.m);
-        store8(static_cast<float *>(a.d_v) + at, v);
-    } else {
-        uint2 m_codes, v_codes;
-        float new_m, new_v;
-        encode_block(e.m, v, e.r, words, m_codes, v_codes, new_m, new_v);
-        *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(a.d_m) + at) = m_codes;
-        *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(a.d_v) + at) = v_codes;
-        if (lane == 0u) {
-            a.d_m_scales[s / kBlock] = new_m;
-            a.d_v_scales[s / kBlock] = new_v;
         }
     }
 }
@@ -338,59 +381,77 @@ __device__ __noinline__ void part_block(const AdamwArgs &a, const Coefficients &
     const uint32_t lane = threadIdx.x & 31u;
     const uint64_t at = s + lane * 8u;
     const uint32_t count = left > lane * 8u ? (left - lane * 8u < 8u ? left - lane * 8u : 8u) : 0u;
-    Lane<Tw, Tg, BITS, MASTER> e;
+    Lane<BITS> e;
     w += lane * 8u;
     g += lane * 8u;
-    uint2 m8 = make_uint2(0u, 0u), v8 = m8;
-    float m_scale = 1.f, v_scale = 1.f;
+    float x[4][8];                                       // weights, gradients, moments
     if constexpr (BITS == 8) {
-        m8 = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(a.d_m) + at);
-        v8 = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(a.d_v) + at);
-        m_scale = a.d_m_scales[s / kBlock];
-        v_scale = a.d_v_scales[s / kBlock];
-        decode4(m8.x, e.m);
-        decode4(m8.y, e.m + 4);
-        decode4(v8.x, e.r);
-        decode4(v8.y, e.r + 4);
+        decode8(*reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(a.d_m) + at), a.d_m_scales[s / kBlock], e.m);
+        decode8(*reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(a.d_v) + at), a.d_v_scales[s / kBlock], e.v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            e.m[i].get(x[2][2 * i], x[2][2 * i + 1]);
+            e.v[i].get(x[3][2 * i], x[3][2 * i + 1]);
+        }
         __syncwarp();                                    // every lane has the scales
     }
 #pragma unroll
     for (uint32_t i = 0; i < 8u; ++i) {
         const bool there = i < count;
-        e.g[i] = there ? elem::to_float(g[i]) : 0.f;
-        if constexpr (MASTER) e.w[i] = there ? a.d_master[at + i] : 0.f;
-        else e.w[i] = there ? elem::to_float(w[i]) : 0.f;
+        if constexpr (MASTER) x[0][i] = there ? a.d_master[at + i] : 0.f;
+        else x[0][i] = there ? elem::to_float(w[i]) : 0.f;
+        x[1][i] = there ? elem::to_float(g[i]) : 0.f;
         if constexpr (BITS == 32) {
-            e.m[i] = there ? static_cast<const float *>(a.d_m)[at + i] : 0.f;
-            e.r[i] = there ? static_cast<const float *>(a.d_v)[at + i] : 0.f;
+            x[2][i] = there ? static_cast<const float *>(a.d_m)[at + i] : 0.f;
+            x[3][i] = there ? static_cast<const float *>(a.d_v)[at + i] : 0.f;
         } else {
-            e.m[i] = there ? e.m[i] * m_scale : 0.f;
-            e.r[i] = there ? e.r[i] * v_scale : 0.f;
+            x[2][i] = there ? x[2][i] : 0.f;
+            x[3][i] = there ? x[3][i] : 0.f;
         }
     }
-    float v[8];
-    e.update(c, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        e.w[i] = Pair(x[0][2 * i], x[0][2 * i + 1]);
+        e.g[i] = Pair(x[1][2 * i], x[1][2 * i + 1]);
+        e.m[i] = Pair(x[2][2 * i], x[2][2 * i + 1]);
+        e.v[i] = Pair(x[3][2 * i], x[3][2 * i + 1]);
+    }
+    e.update(c);
+#pragma unroll
+    for (uint32_t i = 0; i < 8u; ++i) {
+        float y[2];
+        e.m[i / 2].get(y[0], y[1]);
+        x[2][i] = i < count ? y[i & 1] : 0.f;            // 0 * infinity, if the gradients' factor is that
+        e.v[i / 2].get(y[0], y[1]);
+        x[3][i] = i < count ? y[i & 1] : 0.f;
+        e.w[i / 2].get(y[0], y[1]);
+        x[0][i] = y[i & 1];
+    }
     const Words words((uint32_t)(at / 8u), c);
     uint2 m_codes, v_codes;
     if constexpr (BITS == 8) {
 #pragma unroll
-        for (uint32_t i = 0; i < 8u; ++i)
-            if (i >= count) e.m[i] = e.r[i] = v[i] = 0.f;       // 0 * infinity, if the gradients' factor is that
-        float new_m, new_v;
-        encode_block(e.m, v, e.r, words, m_codes, v_codes, new_m, new_v);
+        for (int i = 0; i < 4; ++i) {
+            e.m[i] = Pair(x[2][2 * i], x[2][2 * i + 1]);
+            e.v[i] = Pair(x[3][2 * i], x[3][2 * i + 1]);
+        }
+        float m_scale, v_scale;
+        e.encode(words, m_codes, v_codes, m_scale, v_scale);
         if (lane == 0u) {
-            a.d_m_scales[s / kBlock] = new_m;
-            a.d_v_scales[s / kBlock] = new_v;
+            a.d_m_scales[s / kBlock] = m_scale;
+            a.d_v_scales[s / kBlock] = v_scale;
         }
     }
+    const elem::Packed<Tw, 8> out = e.template rounded<Tw>(a.stochastic, words);
 #pragma unroll
     for (uint32_t i = 0; i < 8u; ++i) {
         if (i >= count) continue;
-        w[i] = a.stochastic ? round_random<Tw>(e.w[i], words.word(16u + i)) : elem::from_float<Tw>(e.w[i]);
-        if constexpr (MASTER) a.d_master[at + i] = e.w[i];
+        if constexpr (sizeof(Tw) == 4) reinterpret_cast<uint32_t *>(w)[i] = out.w[i];
+        else reinterpret_cast<uint16_t *>(w)[i] = (uint16_t)(out.w[i / 2] >> (16u * (i & 1u)));
+        if constexpr (MASTER) a.d_master[at + i] = x[0][i];
         if constexpr (BITS == 32) {
-            static_cast<float *>(a.d_m)[at + i] = e.m[i];
-            static_cast<float *>(a.d_v)[at + i] = v[i];
+            static_cast<float *>(a.d_m)[at + i] = x[2][i];
+            static_cast<float *>(a.d_v)[at + i] = x[3][i];
         } else {
             static_cast<uint8_t *>(a.d_m)[at + i] = (uint8_t)((i < 4u ? m_codes.x : m_codes.y) >> (8u * (i & 3u)));
             static_cast<uint8_t *>(a.d_v)[at + i] = (uint8_t)((i < 4u ? v_codes.x : v_codes.y) >> (8u * (i & 3u)));
@@ -434,15 +495,14 @@ struct Tensor {
 };
 
 template <typename Tw, typename Tg, int BITS, bool MASTER>
-__global__ void __launch_bounds__(kWarps * 32, 3)
+__global__ void __launch_bounds__(kWarps * 32, 2)
 adamw_kernel(const __grid_constant__ AdamwArgs a, uint32_t run, uint32_t *arrived, uint32_t *status) {
     __shared__ Coefficients shared;
     if (threadIdx.x == 0) make_coefficients(a, shared);
     __syncthreads();
-    const Coefficients c = shared;
     for (uint64_t k = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; k < a.set.n; k += (uint64_t)gridDim.x * blockDim.x)
         if (!Tensor<Tw, Tg>(a, k).good) atomicMax(status, (uint32_t)IVK_DEV_BOUNDS);
-    if (c.skip) return;
+    if (shared.skip) return;
     const uint64_t blocks = a.set.n ? a.size / kBlock : 0u, warps = (uint64_t)gridDim.x * kWarps;
     uint64_t from = 1, to = 0;                           // the blocks' elements of the tensor at hand
     Tw *w = nullptr;
@@ -450,7 +510,7 @@ adamw_kernel(const __grid_constant__ AdamwArgs a, uint32_t run, uint32_t *arrive
     uint64_t elements_end = 0;
     for (uint64_t first = ((uint64_t)blockIdx.x * kWarps + (threadIdx.x >> 5)) * run; first < blocks; first += warps * run) {
         const uint64_t last = first + run < blocks ? first + run : blocks;
-        for (uint64_t b = first; b < last; ++b) {
+        for (uint64_t b = first; b < last;) {
             const uint64_t s = b * kBlock;
             if (s < from || s >= to) {
                 const uint64_t k = tensor_at(a.d_state_offsets, a.set.n, s);
@@ -461,17 +521,23 @@ adamw_kernel(const __grid_constant__ AdamwArgs a, uint32_t run, uint32_t *arrive
                 w = tensor.w;
                 g = tensor.g;
             }
-            if (s < from || s >= elements_end) continue;
-            Tw *wb = w + (s - from);
-            const Tg *gb = g + (s - from);
-            if (elements_end - s < kBlock) {
-                part_block<Tw, Tg, BITS, MASTER>(a, shared, s, (uint32_t)(elements_end - s), wb, gb);
+            if (s < from || s >= elements_end) {
+                ++b;
                 continue;
             }
-            const uint32_t w_off = elem::misalignment(wb), g_off = elem::misalignment(gb);
-            if (g_off == 0u && w_off == 0u) whole_block<Tw, Tg, BITS, MASTER, 16, 16>(a, c, s, wb, gb);
-            else if (g_off == 0u && w_off == 8u) whole_block<Tw, Tg, BITS, MASTER, 8, 16>(a, c, s, wb, gb);
-            else whole_block<Tw, Tg, BITS, MASTER, elem::kAny, elem::kAny>(a, c, s, wb, gb);
+            Tw *wb = w + (s - from);
+            const Tg *gb = g + (s - from);
+            const uint64_t whole = (elements_end - s) / kBlock;
+            if (whole == 0u) {
+                part_block<Tw, Tg, BITS, MASTER>(a, shared, s, (uint32_t)(elements_end - s), wb, gb);
+                ++b;
+                continue;
+            }
+            const uint32_t count = (uint32_t)(whole < last - b ? whole : last - b), w_off = elem::misalignment(wb), g_off = elem::misalignment(gb);
+            if (g_off == 0u && w_off == 0u) whole_blocks<Tw, Tg, BITS, MASTER, 16, 16>(a, shared, s, count, wb, gb);
+            else if (g_off == 0u && w_off == 8u) whole_blocks<Tw, Tg, BITS, MASTER, 8, 16>(a, shared, s, count, wb, gb);
+            else whole_blocks<Tw, Tg, BITS, MASTER, elem::kAny, elem::kAny>(a, shared, s, count, wb, gb);
+            b += count;
         }
     }
     __syncthreads();
@@ -483,7 +549,7 @@ adamw_kernel(const __grid_constant__ AdamwArgs a, uint32_t run, uint32_t *arrive
 
 template <typename Tw, typename Tg, int BITS, bool MASTER>
 cudaError_t launch_instance(const AdamwArgs &a, uint32_t *arrived, uint32_t *d_status, int sm_count, cudaStream_t stream) {
-    const uint64_t blocks = a.size / kBlock, ctas = (blocks + kWarps - 1) / kWarps, most = (uint64_t)sm_count * 3u;
+    const uint64_t blocks = a.size / kBlock, ctas = (blocks + kWarps - 1) / kWarps, most = (uint64_t)sm_count * 2u;
     const uint32_t grid = (uint32_t)(ctas < most ? (ctas ? ctas : 1u) : most);
     const uint64_t share = blocks / ((uint64_t)grid * kWarps);
     const uint32_t run = (uint32_t)(share < 1u ? 1u : share < 16u ? share : 16u);

@@ -150,6 +150,48 @@ struct Vector {
     }
 };
 
+// Two 32-bit floats that one instruction works on, each rounded by itself.
+struct Pair {
+    uint64_t bits;
+    __device__ __forceinline__ Pair() {}
+    __device__ __forceinline__ Pair(float lo, float hi) { asm("mov.b64 %0, {%1, %2};" : "=l"(bits) : "f"(lo), "f"(hi)); }
+    __device__ __forceinline__ explicit Pair(float both) : Pair(both, both) {}
+    __device__ __forceinline__ float sum() const {
+        float lo, hi;
+        get(lo, hi);
+        return lo + hi;
+    }
+    __device__ __forceinline__ void get(float &lo, float &hi) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(bits)); }
+};
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
+    return r;
+}
+__device__ __forceinline__ Pair operator+(Pair a, Pair b) {
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
+    return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits), "l"(c.bits));
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void unpack8(const Packed<T, 8> &packed, Pair (&x)[4]) {
+    float e[8];
+    packed.unpack(e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = Pair(e[2 * i], e[2 * i + 1]);
+}
+
+__device__ __forceinline__ void unpair(const Pair (&x)[4], float (&e)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i].get(e[2 * i], e[2 * i + 1]);
+}
+
 // (a0, a1) += (x0^2, x1^2), each rounded as a multiply-add of its own.
 __device__ __forceinline__ void add_squares2(float &a0, float &a1, float x0, float x1) {
     asm("{\n\t.reg .b64 a, x;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 x, {%2, %3};\n\tfma.rn.f32x2 a, x, x, a;\n\tmov.b64 {%0, %1}, a;\n\t}"

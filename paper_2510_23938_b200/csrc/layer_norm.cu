@@ -14,13 +14,14 @@ namespace ivk {
 namespace {
 
 using namespace rows;
+using elem::Pair;
 
 constexpr uint32_t kThreads = 512;
 
-// Aligned rows: the next row is on its way while this one is worked on.
+// Aligned rows: the next row is on its way while one is worked on.
 template <typename Tx, typename Ty, uint32_t T, int NV, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads, NV * sizeof(Tx) > 8 ? 1 : 2)
-layer_norm_kernel(LayerNormArgs a) {
+layer_norm_kernel(const __grid_constant__ LayerNormArgs a) {
     constexpr uint32_t kGroups = kThreads / T;
     extern __shared__ float4 params[];                   // weight, then bias: two planes each
     __shared__ float slots[2][kThreads / 32];
@@ -28,16 +29,16 @@ layer_norm_kernel(LayerNormArgs a) {
     const uint32_t dim = (uint32_t)a.dim, vectors = (dim + 7u) / 8u;
     const Tx *x = static_cast<const Tx *>(a.d_x);
     Ty *y = static_cast<Ty *>(a.d_y);
-    RowVector<Tx, ALIGNED> raw[NV], next[NV];
+    RowVector<Tx, ALIGNED> next[NV];
     const uint64_t step = (uint64_t)gridDim.x * kGroups;
     // a row that is not there is a row without elements: all groups of a warp stay together
-    auto fetch = [&](RowVector<Tx, ALIGNED> (&to)[NV], uint64_t row) {
+    auto fetch = [&](uint64_t row) {
         const Tx *p = x + (row < a.n ? row * a.x_stride : 0u);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) to[j].load(p, t + j * T, row < a.n ? dim : 0u);
+        for (int j = 0; j < NV; ++j) next[j].load(p, t + j * T, row < a.n ? dim : 0u);
     };
     uint64_t base = (uint64_t)blockIdx.x * kGroups;
-    if (ALIGNED) fetch(next, base + group);
+    if (ALIGNED) fetch(base + group);
     if (a.d_weight) widen_params(a.d_weight, a.param_type, dim, params);
     float4 *bias = params + (a.d_weight ? 2u * vectors : 0u);
     if (a.d_bias) widen_params(a.d_bias, a.param_type, dim, bias);
@@ -46,63 +47,68 @@ layer_norm_kernel(LayerNormArgs a) {
     for (; base < a.n; base += step) {
         const uint64_t row = base + group;
         const bool live = row < a.n;
-        if (ALIGNED) {
+        elem::Packed<Tx, 8> raw[NV];
+        if (!ALIGNED) fetch(row);
+        const uint32_t off = ALIGNED ? 0u : elem::misalignment(x + (live ? row * a.x_stride : 0u));
 #pragma unroll
-            for (int j = 0; j < NV; ++j) raw[j] = next[j];
-            if (base + step < a.n) fetch(next, row + step);
-        } else {
-            fetch(raw, row);
-        }
-        const uint32_t off = elem::misalignment(x + (live ? row * a.x_stride : 0u));
+        for (int j = 0; j < NV; ++j) raw[j] = next[j].get(off, t + j * T, live ? dim : 0u);
+        if (ALIGNED && base + step < a.n) fetch(row + step);
         float mean = 0.f;
         if (!a.rms) {
             float sum[NV];
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                float v[8];
-                raw[j].get(off, v);
-                sum[j] = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+                Pair v[4];
+                elem::unpack8(raw[j], v);
+                sum[j] = ((v[0] + v[1]) + (v[2] + v[3])).sum();
             }
             mean = group_sum<T>(sum_of<NV>(sum), slots[0]) * scale;
         }
+        const Pair shift(-mean);
         float squares[NV];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            float v[8];
-            raw[j].get(off, v);
+            Pair v[4], s(0.f);
+            elem::unpack8(raw[j], v);
             const uint32_t left = left_of(t + j * T, dim);
-            float s0 = 0.f, s1 = 0.f;
+            if (!ALIGNED && left < 8u && left) {             // zeros behind the row's end that are not the mean away from it
 #pragma unroll
-            for (uint32_t i = 0; i < 8u; i += 2u) {
-                const float d0 = i < left ? v[i] - mean : 0.f, d1 = i + 1u < left ? v[i + 1] - mean : 0.f;
-                elem::add_squares2(s0, s1, d0, d1);
+                for (uint32_t i = 0; i < 4u; ++i) {
+                    float lo, hi;
+                    v[i].get(lo, hi);
+                    v[i] = Pair(2u * i < left ? lo : mean, 2u * i + 1u < left ? hi : mean);
+                }
             }
-            squares[j] = s0 + s1;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const Pair d = v[i] + shift;
+                s = fma2(d, d, s);
+            }
+            squares[j] = left ? s.sum() : 0.f;
         }
         const float rstd = 1.f / sqrtf(group_sum<T>(sum_of<NV>(squares), slots[1]) * scale + a.eps);
-        if (!live) continue;
-        Ty *out = y + row * a.y_stride;
+        Ty *out = y + (live ? row * a.y_stride : 0u);
+        const Pair by(rstd);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const uint32_t v = t + j * T;
-            if (v >= vectors) break;
-            float e[8], w[8];
-            raw[j].get(off, e);
+            const uint32_t v = t + j * T, at = v < vectors ? v : 0u;
+            Pair e[4], w[4];
+            elem::unpack8(raw[j], e);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = (e[i] - mean) * rstd;
+            for (int i = 0; i < 4; ++i) e[i] = (e[i] + shift) * by;
             if (a.d_weight) {
-                read_params(params, v, vectors, w);
+                read_params(params, at, vectors, w);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) e[i] *= w[i];
+                for (int i = 0; i < 4; ++i) e[i] = e[i] * w[i];
             }
             if (a.d_bias) {
-                read_params(bias, v, vectors, w);
+                read_params(bias, at, vectors, w);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) e[i] += w[i];
+                for (int i = 0; i < 4; ++i) e[i] = e[i] + w[i];
             }
-            store_row_vector<Ty, ALIGNED>(out, v, dim, e);
+            store_row_vector<Ty, ALIGNED, T>(out, v, live ? dim : 0u, e);
         }
-        if (t == 0u) {
+        if (live && t == 0u) {
             if (a.d_mean) a.d_mean[row] = mean;
             if (a.d_rstd) a.d_rstd[row] = rstd;
         }
@@ -122,35 +128,43 @@ layer_norm_wide_kernel(LayerNormArgs a) {
         Ty *out = static_cast<Ty *>(a.d_y) + row * a.y_stride;
         const uint32_t off = elem::misalignment(in);
         auto each = [&](auto f) {
-            for (uint32_t v = threadIdx.x; v < vectors; v += kWideThreads) {
+            for (uint32_t base = 0; base < vectors; base += kWideThreads) {      // whole warps
+                const uint32_t v = base + threadIdx.x;
                 RowVector<Tx, false> raw;
-                float e[8];
+                Pair e[4];
                 raw.load(in, v, dim);
-                raw.get(off, e);
+                elem::unpack8(raw.get(off, v, dim), e);
                 f(v, e);
             }
         };
         float mean = 0.f, sum = 0.f;
         if (!a.rms) {
-            each([&](uint32_t, float (&e)[8]) { sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])); });
+            each([&](uint32_t, Pair (&e)[4]) { sum += ((e[0] + e[1]) + (e[2] + e[3])).sum(); });
             mean = group_sum<kWideThreads>(sum, slots[0]) * scale;
         }
         sum = 0.f;
-        each([&](uint32_t v, float (&e)[8]) {
+        each([&](uint32_t v, Pair (&p)[4]) {
             const uint32_t left = left_of(v, dim);
-            float part = 0.f;
-            for (int i = 0; i < 8; ++i) part = i < left ? fmaf(e[i] - mean, e[i] - mean, part) : part;
+            float e[8], part = 0.f;
+            unpair(p, e);
+#pragma unroll
+            for (uint32_t i = 0; i < 8u; ++i) part = i < left ? fmaf(e[i] - mean, e[i] - mean, part) : part;
             sum += part;
         });
         const float rstd = 1.f / sqrtf(group_sum<kWideThreads>(sum, slots[1]) * scale + a.eps);
-        each([&](uint32_t v, float (&e)[8]) {
+        each([&](uint32_t v, Pair (&p)[4]) {
             const uint32_t left = left_of(v, dim);
+            float e[8];
+            unpair(p, e);
+#pragma unroll
             for (uint32_t i = 0; i < 8u; ++i) {
                 e[i] = (e[i] - mean) * rstd;
                 if (i < left && a.d_weight) e[i] *= param_at(a.d_weight, a.param_type, v * 8u + i);
                 if (i < left && a.d_bias) e[i] += param_at(a.d_bias, a.param_type, v * 8u + i);
             }
-            store_row_vector<Ty, false>(out, v, dim, e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = Pair(e[2 * i], e[2 * i + 1]);
+            store_row_vector<Ty, false, kWideThreads>(out, v, dim, p);
         });
         if (threadIdx.x == 0) {
             if (a.d_mean) a.d_mean[row] = mean;
@@ -204,7 +218,7 @@ cudaError_t launch_layer_norm(const LayerNormArgs &a, int sm_count, cudaStream_t
             layer_norm_wide_kernel<Tx, Ty><<<(uint32_t)(a.n < most ? a.n : most), kWideThreads, 0, stream>>>(a);
             return cudaGetLastError();
         }
-        return rows_aligned<Tx>(a.d_x, a.x_stride, a.n) && rows_aligned<Ty>(a.d_y, a.y_stride, a.n)
+        return rows_aligned<Tx>(a.d_x, a.x_stride, a.n, a.dim) && rows_aligned<Ty>(a.d_y, a.y_stride, a.n, a.dim)
                    ? launch_width<Tx, Ty, true>(a, sm_count, stream)
                    : launch_width<Tx, Ty, false>(a, sm_count, stream);
     });

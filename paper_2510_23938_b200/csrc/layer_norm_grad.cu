@@ -16,6 +16,7 @@ namespace ivk {
 namespace {
 
 using namespace rows;
+using elem::Pair;
 
 constexpr uint32_t kThreads = 512;
 constexpr uint64_t kMostParts = 296;      // runs of rows: two for each of a B200's SMs, whatever GPU it is (the sums' order goes by it)
@@ -71,26 +72,41 @@ struct Slot {
     static constexpr int kPieces = (int)sizeof(T) / 2 + (ALIGNED ? 0 : 1);
     // pieces[i * kThreads]: this thread's piece i
     static __device__ __forceinline__ void fetch(uint4 *pieces, const T *row, uint32_t v, uint32_t dim) {
-        const uint32_t left = left_of(v, dim);
         const T *p = row + v * 8u;
-        const uint32_t off = elem::misalignment(p), wanted = off + left * (uint32_t)sizeof(T);
-        const uint8_t *q = reinterpret_cast<const uint8_t *>(p) - off;
+        if constexpr (ALIGNED) {
+            if (v * 8u < dim) {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i)
-            if (left && 16u * i < wanted) copy_async16(pieces + i * kThreads, q + 16 * i);
+                for (int i = 0; i < kPieces; ++i) copy_async16(pieces + i * kThreads, reinterpret_cast<const uint8_t *>(p) + 16 * i);
+            }
+        } else {
+            const uint32_t left = left_of(v, dim), off = elem::misalignment(p), wanted = left ? off + left * (uint32_t)sizeof(T) : 0u;
+            const uint8_t *q = reinterpret_cast<const uint8_t *>(p) - off;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                if (16u * i < wanted) copy_async16(pieces + i * kThreads, q + 16 * i);
+        }
     }
     // zeros behind the row's end
-    static __device__ __forceinline__ void get(const uint4 *pieces, uint32_t row_off, uint32_t left, float (&e)[8]) {
+    static __device__ __forceinline__ void get(const uint4 *pieces, uint32_t row_off, uint32_t v, uint32_t dim, Pair (&e)[4]) {
         elem::Vector<T, 8, ALIGNED ? 16 : elem::kAny> raw;
+        if (v * 8u < dim) {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const uint4 x = pieces[i * kThreads];
-            raw.w[4 * i] = x.x; raw.w[4 * i + 1] = x.y; raw.w[4 * i + 2] = x.z; raw.w[4 * i + 3] = x.w;
+            for (int i = 0; i < kPieces; ++i) {
+                const uint4 x = pieces[i * kThreads];
+                raw.w[4 * i] = x.x; raw.w[4 * i + 1] = x.y; raw.w[4 * i + 2] = x.z; raw.w[4 * i + 3] = x.w;
+            }
+        } else {
+            raw.zero();
         }
-        raw.get(ALIGNED ? 0u : row_off).unpack(e);
-        if (left < 8u) {
+        elem::unpack8(raw.get(ALIGNED ? 0u : row_off), e);
+        if constexpr (!ALIGNED) {
+            const uint32_t left = left_of(v, dim);
+            if (left < 8u) {
+                float x[8];
+                unpair(e, x);
 #pragma unroll
-            for (uint32_t i = 0; i < 8u; ++i) e[i] = i < left ? e[i] : 0.f;
+                for (uint32_t i = 0; i < 4u; ++i) e[i] = Pair(2u * i < left ? x[2 * i] : 0.f, 2u * i + 1u < left ? x[2 * i + 1] : 0.f);
+            }
         }
     }
 };
@@ -106,7 +122,7 @@ __host__ __device__ constexpr int stages_of() {
 
 template <typename Tx, typename Ty, uint32_t T, int NV, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads, NV > 1 ? 1 : 2)
-norm_grad_kernel(LayerNormGradArgs a, float *partial) {
+norm_grad_kernel(const __grid_constant__ LayerNormGradArgs a, float *partial) {
     constexpr uint32_t kGroups = kThreads / T;
     constexpr int kStages = stages_of<Tx, Ty, ALIGNED, NV>();
     constexpr int kX = Slot<Tx, ALIGNED>::kPieces, kY = Slot<Ty, ALIGNED>::kPieces;
@@ -133,14 +149,15 @@ norm_grad_kernel(LayerNormGradArgs a, float *partial) {
     };
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) fetch(begin + s * kGroups, s);
-    float w[NV][8], dw[NV][8], db[NV][8];
+    Pair w[NV][4], dw[NV][4], db[NV][4];
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (uint32_t i = 0; i < 8u; ++i) {
-            const uint32_t c = (t + j * T) * 8u + i;
-            w[j][i] = c >= dim ? 0.f : a.d_weight ? param_at(a.d_weight, a.param_type, c) : 1.f;
-            dw[j][i] = db[j][i] = 0.f;
+        for (uint32_t i = 0; i < 4u; ++i) {
+            const uint32_t c = (t + j * T) * 8u + 2u * i;
+            auto weight = [&](uint32_t at) { return at >= dim ? 0.f : a.d_weight ? param_at(a.d_weight, a.param_type, at) : 1.f; };
+            w[j][i] = Pair(weight(c), weight(c + 1u));
+            dw[j][i] = db[j][i] = Pair(0.f);
         }
     const float scale = 1.f / (float)dim;
     int stage = 0;
@@ -152,33 +169,32 @@ norm_grad_kernel(LayerNormGradArgs a, float *partial) {
         const bool live = row < end;
         const float rstd = live ? a.d_rstd[row] : 0.f, mean = live && a.d_mean ? a.d_mean[row] : 0.f;
         const uint32_t x_off = elem::misalignment(x + (live ? row * a.x_stride : 0u)), y_off = elem::misalignment(dy + (live ? row * a.dy_stride : 0u));
-        float h[NV][8], p[NV][8], s = 0.f, sh = 0.f;
+        const Pair shift(-mean), by(rstd);
+        Pair h[NV][4], p[NV][4], s2(0.f), sh2(0.f);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const uint32_t left = live ? left_of(t + j * T, dim) : 0u;
-            float e[8];
-            Slot<Tx, ALIGNED>::get(slot(stage, j), x_off, left, h[j]);
-            Slot<Ty, ALIGNED>::get(slot(stage, j) + kX * kThreads, y_off, left, e);
+            Pair e[4];
+            Slot<Tx, ALIGNED>::get(slot(stage, j), x_off, t + j * T, live ? dim : 0u, h[j]);
+            Slot<Ty, ALIGNED>::get(slot(stage, j) + kX * kThreads, y_off, t + j * T, live ? dim : 0u, e);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                h[j][i] = (h[j][i] - mean) * rstd;
+            for (int i = 0; i < 4; ++i) {
+                h[j][i] = (h[j][i] + shift) * by;
                 p[j][i] = e[i] * w[j][i];
-                db[j][i] += e[i];
-                dw[j][i] = fmaf(e[i], h[j][i], dw[j][i]);
-                s += p[j][i];
-                sh = fmaf(p[j][i], h[j][i], sh);
+                db[j][i] = db[j][i] + e[i];
+                dw[j][i] = fma2(e[i], h[j][i], dw[j][i]);
+                s2 = s2 + p[j][i];
+                sh2 = fma2(p[j][i], h[j][i], sh2);
             }
         }
+        float s = s2.sum(), sh = sh2.sum();
         group_sum2<T>(s, sh, sums);
-        const float mp = a.rms ? 0.f : s * scale, mh = sh * scale;
-        if (live) {
-            Tx *out = dx + row * a.dx_stride;
+        const Pair mp(a.rms ? 0.f : -s * scale), mh(-sh * scale);
+        Tx *out = dx + (live ? row * a.dx_stride : 0u);
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
+        for (int j = 0; j < NV; ++j) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) h[j][i] = rstd * (p[j][i] - mp - h[j][i] * mh);
-                store_row_vector<Tx, ALIGNED>(out, t + j * T, dim, h[j]);
-            }
+            for (int i = 0; i < 4; ++i) h[j][i] = (fma2(h[j][i], mh, p[j][i]) + mp) * by;
+            store_row_vector<Tx, ALIGNED, T>(out, t + j * T, live ? dim : 0u, h[j]);
         }
         float *swap = sums;
         sums = other;
@@ -195,9 +211,10 @@ norm_grad_kernel(LayerNormGradArgs a, float *partial) {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                all[((2 * j) * 8 + i) * kThreads + threadIdx.x] = dw[j][i];
-                all[((2 * j + 1) * 8 + i) * kThreads + threadIdx.x] = db[j][i];
+            for (int i = 0; i < 4; ++i) {
+                float *to = all + ((2 * j) * 8 + 2 * i) * kThreads + threadIdx.x;
+                dw[j][i].get(to[0], to[kThreads]);
+                db[j][i].get(to[8 * kThreads], to[9 * kThreads]);
             }
         __syncthreads();
         for (uint32_t q = threadIdx.x; q < 16u * NV * T; q += kThreads) {
@@ -211,12 +228,17 @@ norm_grad_kernel(LayerNormGradArgs a, float *partial) {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (uint32_t i = 0; i < 8u; ++i) {
-                const uint32_t c = (t + j * T) * 8u + i;
-                if (c < dim) {
-                    out[c] = dw[j][i];
-                    out[dim + c] = db[j][i];
-                }
+            for (uint32_t i = 0; i < 4u; ++i) {
+                const uint32_t c = (t + j * T) * 8u + 2u * i;
+                float x[2], y[2];
+                dw[j][i].get(x[0], x[1]);
+                db[j][i].get(y[0], y[1]);
+#pragma unroll
+                for (uint32_t k = 0; k < 2u; ++k)
+                    if (c + k < dim) {
+                        out[c + k] = x[k];
+                        out[dim + c + k] = y[k];
+                    }
             }
     }
 }
@@ -236,13 +258,18 @@ norm_grad_wide_rows_kernel(LayerNormGradArgs a, float2 *row_sums) {
         for (uint32_t v = threadIdx.x; v < vectors; v += kThreads) {
             RowVector<Tx, false> rx;
             RowVector<Ty, false> ry;
+            Pair pairs[4];
             float h[8], p[8];
             rx.load(x, v, dim);
             ry.load(dy, v, dim);
-            rx.get(elem::misalignment(x), h);
-            ry.get(elem::misalignment(dy), p);
+            elem::unpack8(rx.get(elem::misalignment(x), v, dim), pairs);
+            unpair(pairs, h);
+            elem::unpack8(ry.get(elem::misalignment(dy), v, dim), pairs);
+            unpair(pairs, p);
             const uint32_t left = left_of(v, dim);
-            for (uint32_t i = 0; i < left; ++i) {
+#pragma unroll
+            for (uint32_t i = 0; i < 8u; ++i) {
+                if (i >= left) break;
                 const float q = a.d_weight ? p[i] * param_at(a.d_weight, a.param_type, v * 8u + i) : p[i];
                 s += q;
                 sh = fmaf(q, (h[i] - mean) * rstd, sh);
@@ -278,9 +305,12 @@ norm_grad_wide_kernel(LayerNormGradArgs a, const float2 *row_sums, float *partia
         const float rstd = a.d_rstd[row], mean = a.d_mean ? a.d_mean[row] : 0.f;
         const float2 sums = row_sums[row];
         const float mp = a.rms ? 0.f : sums.x * scale, mh = sums.y * scale;
+        Pair pairs[4];
         float h[8], e[8];
-        rx.get(elem::misalignment(x), h);
-        ry.get(elem::misalignment(dy), e);
+        elem::unpack8(rx.get(elem::misalignment(x), v, dim), pairs);
+        unpair(pairs, h);
+        elem::unpack8(ry.get(elem::misalignment(dy), v, dim), pairs);
+        unpair(pairs, e);
 #pragma unroll
         for (uint32_t i = 0; i < 8u; ++i) {
             h[i] = (h[i] - mean) * rstd;
@@ -288,7 +318,9 @@ norm_grad_wide_kernel(LayerNormGradArgs a, const float2 *row_sums, float *partia
             dw[i] = fmaf(e[i], h[i], dw[i]);
             h[i] = rstd * (e[i] * w[i] - mp - h[i] * mh);
         }
-        store_row_vector<Tx, false>(static_cast<Tx *>(a.d_dx) + row * a.dx_stride, v, dim, h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pairs[i] = Pair(h[2 * i], h[2 * i + 1]);
+        store_row_vector<Tx, false, 32>(static_cast<Tx *>(a.d_dx) + row * a.dx_stride, v, dim, pairs);
     }
     if (!a.d_dw && !a.d_db) return;
 #pragma unroll
@@ -399,8 +431,8 @@ cudaError_t launch_layer_norm_grad(const LayerNormGradArgs &a, float *d_partial,
             using Tx = typename decltype(in)::type;
             using Ty = typename decltype(out)::type;
             if (a.dim > kWidest) return launch_wide<Tx, Ty>(a, d_partial, parts, sm_count, stream);
-            return rows_aligned<Tx>(a.d_x, a.x_stride, a.n) && rows_aligned<Ty>(a.d_dy, a.dy_stride, a.n) &&
-                           rows_aligned<Tx>(a.d_dx, a.dx_stride, a.n)
+            return rows_aligned<Tx>(a.d_x, a.x_stride, a.n, a.dim) && rows_aligned<Ty>(a.d_dy, a.dy_stride, a.n, a.dim) &&
+                           rows_aligned<Tx>(a.d_dx, a.dx_stride, a.n, a.dim)
                        ? launch_width<Tx, Ty, true>(a, d_partial, parts, stream)
                        : launch_width<Tx, Ty, false>(a, d_partial, parts, stream);
         });
