@@ -2,9 +2,12 @@
 //     mu = mean(x) (rms: 0),  r = 1 / sqrt(mean((x - mu)^2) + eps),  y = round((x - mu) r w + b)
 //
 // Bound by memory: a row is read once, held in registers for both sums (the mean first, then the squares of what is left,
-// so nothing cancels) and written once.  the threads of a row, 8 to 512 with one to four
-// vectors of eight elements each, follow from its width and type alone, and so does the order of its sums: a row's bits do not depend on the other rows, on the
-// launch or on the alignment.  Weight and bias are widened into shared memory once per CTA.
+// so nothing cancels) and written once.  The threads of a row, 8 to 512 with one, two or four vectors of eight elements each,
+// follow from its width alone, and so does the order of its sums: a row's bits do not depend on the other rows, on the
+// launch or on the alignment.  Rows come through a ring in shared memory that each warp fills for itself with asynchronous copies,
+// several rows ahead; a group of threads works on four (or two) at a time, so that their sums cross threads together.
+#include <type_traits>
+
 #include "element_dev.cuh"
 #include "iv_internal.h"
 #include "row_dev.cuh"
@@ -18,101 +21,153 @@ using elem::Pair;
 
 constexpr uint32_t kThreads = 512;
 
-// Aligned rows: the next row is on its way while one is worked on.
-template <typename Tx, typename Ty, uint32_t T, int NV, bool ALIGNED>
-__global__ void __launch_bounds__(kThreads, NV * sizeof(Tx) > 8 ? 1 : 2)
+// The ring: 16-byte pieces in a row of every group, rows that a group works on at a time, and steps.  One CTA takes an SM's shared
+// memory, but for aligned 16-bit rows of 2049 to 4096 columns two share it (131072 x 4096: 342 us, 370 with one; 262144 x 1024 181
+// with two, 166 with one; float32 rows to 16 bits, 65536 x 4096: 279 and 240).
+template <typename Tx, uint32_t T, int NV, int MODE>
+struct Ring {
+    static constexpr uint32_t kWidth = T < 32u ? T : 32u, kSegments = kThreads / kWidth;
+    using X = Segment<Tx, kWidth, MODE>;
+    static constexpr uint32_t kX = kSegments * X::kPieces, kRow = NV * kX;
+    static constexpr int kCtas = NV == 1 && T == kThreads && sizeof(Tx) == 2 && MODE != kAnyRows ? 2 : 1;
+    static constexpr uint32_t kRoom = kCtas == 2 ? 6144 : 12288;     // pieces: 96 or 192 KiB
+    static constexpr int kRows = 12u * kRow <= kRoom ? 4 : 6u * kRow <= kRoom ? 2 : 1;
+    static constexpr int kStages = (int)(kRoom / (kRow * kRows));
+    static_assert(kStages >= 2, "a step in flight");
+};
+
+template <typename Tx, typename Ty, uint32_t T, int NV, int MODE>
+__global__ void __launch_bounds__(kThreads, Ring<Tx, T, NV, MODE>::kCtas)
 layer_norm_kernel(const __grid_constant__ LayerNormArgs a) {
-    constexpr uint32_t kGroups = kThreads / T;
-    extern __shared__ float4 params[];                   // weight, then bias: two planes each
-    __shared__ float slots[2][kThreads / 32];
-    const uint32_t t = threadIdx.x % T, group = threadIdx.x / T;
-    const uint32_t dim = (uint32_t)a.dim, vectors = (dim + 7u) / 8u;
+    using Rows = Ring<Tx, T, NV, MODE>;
+    using X = typename Rows::X;
+    constexpr uint32_t kGroups = kThreads / T, kWidth = Rows::kWidth, kRow = Rows::kRow;
+    constexpr int kStages = Rows::kStages, R = Rows::kRows;
+    extern __shared__ uint4 ring[];                      // steps x rows x vectors
+    __shared__ float slots[2][R * 16];
+    const uint32_t t = threadIdx.x % T, group = threadIdx.x / T, lane = threadIdx.x % kWidth;
+    const uint32_t dim = (uint32_t)a.dim;
+    constexpr uint32_t kStep = R * kGroups;              // rows of a step: row i of the group is number i * kGroups + group of them
+    const uint64_t begin = (uint64_t)blockIdx.x * kStep, end = a.n, stride = (uint64_t)gridDim.x * kStep;
     const Tx *x = static_cast<const Tx *>(a.d_x);
     Ty *y = static_cast<Ty *>(a.d_y);
-    RowVector<Tx, ALIGNED> next[NV];
-    const uint64_t step = (uint64_t)gridDim.x * kGroups;
-    // a row that is not there is a row without elements: all groups of a warp stay together
-    auto fetch = [&](uint64_t row) {
-        const Tx *p = x + (row < a.n ? row * a.x_stride : 0u);
+    uint4 *const own = ring + threadIdx.x / kWidth * X::kPieces;
+    // this thread's next row to fetch and to work on, and from one row of a step to the next; a CTA takes every gridDim.x-th step, so
+    // that all of them read and write in one region of memory (131072 x 4096: 342 us, 387 with a run of rows each)
+    const uint64_t row_x = kGroups * a.x_stride, row_y = kGroups * a.y_stride;
+    const Tx *fetch_x = x + (begin + group) * a.x_stride, *work_x = fetch_x;
+    Ty *work_y = y + (begin + group) * a.y_stride;
+    auto fetch = [&](uint64_t base, uint32_t at) {       // at: the step's place in the ring
 #pragma unroll
-        for (int j = 0; j < NV; ++j) next[j].load(p, t + j * T, row < a.n ? dim : 0u);
+        for (int i = 0; i < R; ++i) {
+            if (base + i * kGroups + group >= end) break;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) X::fetch(own + at + (i * NV + j) * Rows::kX, fetch_x + i * row_x, t + j * T, lane, dim);
+        }
+        commit_copies();
+        fetch_x += gridDim.x * R * row_x;
     };
-    uint64_t base = (uint64_t)blockIdx.x * kGroups;
-    if (ALIGNED) fetch(base + group);
-    if (a.d_weight) widen_params(a.d_weight, a.param_type, dim, params);
-    float4 *bias = params + (a.d_weight ? 2u * vectors : 0u);
-    if (a.d_bias) widen_params(a.d_bias, a.param_type, dim, bias);
-    __syncthreads();
-    const float scale = 1.f / (float)dim;
-    for (; base < a.n; base += step) {
-        const uint64_t row = base + group;
-        const bool live = row < a.n;
-        elem::Packed<Tx, 8> raw[NV];
-        if (!ALIGNED) fetch(row);
-        const uint32_t off = ALIGNED ? 0u : elem::misalignment(x + (live ? row * a.x_stride : 0u));
 #pragma unroll
-        for (int j = 0; j < NV; ++j) raw[j] = next[j].get(off, t + j * T, live ? dim : 0u);
-        if (ALIGNED && base + step < a.n) fetch(row + step);
-        float mean = 0.f;
+    for (int s = 0; s < kStages - 1; ++s) fetch(begin + s * stride, s * R * kRow);
+    Pair w[NV][4], b[NV][4];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        params_of(a.d_weight, a.param_type, t + j * T, dim, 1.f, w[j]);
+        params_of(a.d_bias, a.param_type, t + j * T, dim, 0.f, b[j]);
+    }
+    const float scale = 1.f / (float)dim;
+    uint32_t now = 0, last = (kStages - 1) * R * kRow;
+    float *sums = slots[0], *other = slots[1];
+    auto turn = [&]() {
+        float *used = sums;
+        sums = other;
+        other = used;
+    };
+    // `whole`: all rows of the step are there
+    auto work = [&](uint64_t base, auto whole) {
+        fetch(base + (kStages - 1) * stride, last);
+        last = now;
+        wait_copies<kStages - 1>();
+        __syncwarp();
+        elem::Packed<Tx, 8> raw[R][NV];
+        float mean[R], rstd[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const bool live = decltype(whole)::value || base + i * kGroups + group < end;
+            const uint32_t off = elem::misalignment(work_x + i * row_x);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) raw[i][j] = X::get(own + now + (i * NV + j) * Rows::kX, off, t + j * T, lane, dim, live);
+            mean[i] = 0.f;
+        }
         if (!a.rms) {
-            float sum[NV];
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                Pair sum(0.f);
+#pragma unroll
+                for (int j = 0; j < NV; ++j) {
+                    Pair v[4];
+                    elem::unpack8(raw[i][j], v);
+                    sum = sum + ((v[0] + v[1]) + (v[2] + v[3]));
+                }
+                mean[i] = sum.sum();
+            }
+            group_sums<T, R>(mean, sums, [scale](float sum) { return sum * scale; });
+            turn();
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const Pair shift(-mean[i]);
+            Pair squares(0.f);
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
+                const uint32_t left = left_of(t + j * T, dim);
                 Pair v[4];
-                elem::unpack8(raw[j], v);
-                sum[j] = ((v[0] + v[1]) + (v[2] + v[3])).sum();
-            }
-            mean = group_sum<T>(sum_of<NV>(sum), slots[0]) * scale;
-        }
-        const Pair shift(-mean);
-        float squares[NV];
+                elem::unpack8(raw[i][j], v);
+                if (MODE == kAnyRows && left < 8u) {        // zeros behind the row's end are not the mean away from it
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            Pair v[4], s(0.f);
-            elem::unpack8(raw[j], v);
-            const uint32_t left = left_of(t + j * T, dim);
-            if (!ALIGNED && left < 8u && left) {             // zeros behind the row's end that are not the mean away from it
+                    for (uint32_t k = 0; k < 4u; ++k) {
+                        float lo, hi;
+                        v[k].get(lo, hi);
+                        v[k] = Pair(2u * k < left ? lo : mean[i], 2u * k + 1u < left ? hi : mean[i]);
+                    }
+                }
+                if (MODE != kAlignedRows || left) {
 #pragma unroll
-                for (uint32_t i = 0; i < 4u; ++i) {
-                    float lo, hi;
-                    v[i].get(lo, hi);
-                    v[i] = Pair(2u * i < left ? lo : mean, 2u * i + 1u < left ? hi : mean);
+                    for (int k = 0; k < 4; ++k) {
+                        const Pair d = v[k] + shift;
+                        squares = fma2(d, d, squares);
+                    }
                 }
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const Pair d = v[i] + shift;
-                s = fma2(d, d, s);
-            }
-            squares[j] = left ? s.sum() : 0.f;
+            rstd[i] = squares.sum();
         }
-        const float rstd = 1.f / sqrtf(group_sum<T>(sum_of<NV>(squares), slots[1]) * scale + a.eps);
-        Ty *out = y + (live ? row * a.y_stride : 0u);
-        const Pair by(rstd);
+        group_sums<T, R>(rstd, sums, [&](float sum) { return 1.f / sqrtf(sum * scale + a.eps); });
+        turn();
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const uint32_t v = t + j * T, at = v < vectors ? v : 0u;
-            Pair e[4], w[4];
-            elem::unpack8(raw[j], e);
+        for (int i = 0; i < R; ++i) {
+            const uint64_t row = base + i * kGroups + group;
+            const bool live = decltype(whole)::value || row < end;
+            const Pair shift(-mean[i]), by(rstd[i]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = (e[i] + shift) * by;
-            if (a.d_weight) {
-                read_params(params, at, vectors, w);
+            for (int j = 0; j < NV; ++j) {
+                Pair e[4];
+                elem::unpack8(raw[i][j], e);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] = e[i] * w[i];
+                for (int k = 0; k < 4; ++k) e[k] = fma2((e[k] + shift) * by, w[j][k], b[j][k]);
+                store_row_vector<Ty, MODE, T>(work_y + i * row_y, t + j * T, dim, live, e);
             }
-            if (a.d_bias) {
-                read_params(bias, at, vectors, w);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] = e[i] + w[i];
+            if (live && t == 0u) {
+                if (a.d_mean) a.d_mean[row] = mean[i];
+                if (a.d_rstd) a.d_rstd[row] = rstd[i];
             }
-            store_row_vector<Ty, ALIGNED, T>(out, v, live ? dim : 0u, e);
         }
-        if (live && t == 0u) {
-            if (a.d_mean) a.d_mean[row] = mean;
-            if (a.d_rstd) a.d_rstd[row] = rstd;
-        }
-    }
+        now = now + R * kRow == kStages * R * kRow ? 0u : now + R * kRow;
+        work_x += gridDim.x * R * row_x;
+        work_y += gridDim.x * R * row_y;
+    };
+    uint64_t base = begin;
+    for (; base + kStep <= end; base += stride) work(base, std::true_type());
+    if (base < end) work(base, std::false_type());
 }
 
 // Rows too wide for that: one CTA per row, which reads it three times (from the L2 cache the second and third time).
@@ -123,6 +178,7 @@ layer_norm_wide_kernel(LayerNormArgs a) {
     __shared__ float slots[2][kWideThreads / 32];
     const uint32_t dim = (uint32_t)a.dim, vectors = (dim + 7u) / 8u;
     const float scale = 1.f / (float)dim;
+    uint32_t turn = 0;
     for (uint64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const Tx *in = static_cast<const Tx *>(a.d_x) + row * a.x_stride;
         Ty *out = static_cast<Ty *>(a.d_y) + row * a.y_stride;
@@ -140,7 +196,10 @@ layer_norm_wide_kernel(LayerNormArgs a) {
         float mean = 0.f, sum = 0.f;
         if (!a.rms) {
             each([&](uint32_t, Pair (&e)[4]) { sum += ((e[0] + e[1]) + (e[2] + e[3])).sum(); });
-            mean = group_sum<kWideThreads>(sum, slots[0]) * scale;
+            float all[1] = {sum};
+            group_sums<kWideThreads, 1>(all, slots[turn], [scale](float s) { return s * scale; });
+            turn ^= 1u;
+            mean = all[0];
         }
         sum = 0.f;
         each([&](uint32_t v, Pair (&p)[4]) {
@@ -151,7 +210,10 @@ layer_norm_wide_kernel(LayerNormArgs a) {
             for (uint32_t i = 0; i < 8u; ++i) part = i < left ? fmaf(e[i] - mean, e[i] - mean, part) : part;
             sum += part;
         });
-        const float rstd = 1.f / sqrtf(group_sum<kWideThreads>(sum, slots[1]) * scale + a.eps);
+        float all[1] = {sum};
+        group_sums<kWideThreads, 1>(all, slots[turn], [&](float s) { return 1.f / sqrtf(s * scale + a.eps); });
+        turn ^= 1u;
+        const float rstd = all[0];
         each([&](uint32_t v, Pair (&p)[4]) {
             const uint32_t left = left_of(v, dim);
             float e[8];
@@ -164,7 +226,7 @@ layer_norm_wide_kernel(LayerNormArgs a) {
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) p[i] = Pair(e[2 * i], e[2 * i + 1]);
-            store_row_vector<Ty, false, kWideThreads>(out, v, dim, p);
+            store_row_vector<Ty, kAnyRows, kWideThreads>(out, v, dim, true, p);
         });
         if (threadIdx.x == 0) {
             if (a.d_mean) a.d_mean[row] = mean;
@@ -173,36 +235,38 @@ layer_norm_wide_kernel(LayerNormArgs a) {
     }
 }
 
-template <typename Tx, typename Ty, uint32_t T, int NV, bool ALIGNED>
+template <typename Tx, typename Ty, uint32_t T, int NV, int MODE>
 cudaError_t launch_instance(const LayerNormArgs &a, int sm_count, cudaStream_t stream) {
-    auto kernel = layer_norm_kernel<Tx, Ty, T, NV, ALIGNED>;
-    const uint64_t vectors = (a.dim + 7u) / 8u;
-    const size_t shared = 32u * vectors * ((a.d_weight ? 1u : 0u) + (a.d_bias ? 1u : 0u));
+    using Rows = Ring<Tx, T, NV, MODE>;
+    auto kernel = layer_norm_kernel<Tx, Ty, T, NV, MODE>;
+    constexpr uint32_t shared = 16u * Rows::kRow * Rows::kRows * Rows::kStages;
     static bool done[kMaxDevices] = {};
-    if (shared > 47u << 10) {                               // with the sums' slots beyond what a kernel has without asking
-        cudaError_t e = ensure_dynamic_smem(kernel, 2u * 32u * T * NV, done);
-        if (e != cudaSuccess) return e;
-    }
-    const uint64_t blocks = (a.n + kThreads / T - 1) / (kThreads / T), most = (uint64_t)sm_count * 2u;
+    cudaError_t e = ensure_dynamic_smem(kernel, shared, done);
+    if (e != cudaSuccess) return e;
+    const uint64_t blocks = (a.n + kThreads / T * Rows::kRows - 1) / (kThreads / T * Rows::kRows), most = (uint64_t)sm_count * Rows::kCtas;
     kernel<<<(uint32_t)(blocks < most ? blocks : most), kThreads, shared, stream>>>(a);
     return cudaGetLastError();
 }
 
-template <typename Tx, typename Ty, bool ALIGNED>
+template <typename Tx, typename Ty, uint32_t T, int NV>
+cudaError_t launch_mode(const LayerNormArgs &a, int sm_count, cudaStream_t stream) {
+    if (!rows_aligned<Tx>(a.d_x, a.x_stride, a.n, a.dim) || !rows_aligned<Ty>(a.d_y, a.y_stride, a.n, a.dim))
+        return launch_instance<Tx, Ty, T, NV, kAnyRows>(a, sm_count, stream);
+    return a.dim == 8u * T * NV ? launch_instance<Tx, Ty, T, NV, kExactRows>(a, sm_count, stream)
+                                : launch_instance<Tx, Ty, T, NV, kAlignedRows>(a, sm_count, stream);
+}
+template <typename Tx, typename Ty>
 cudaError_t launch_width(const LayerNormArgs &a, int sm_count, cudaStream_t stream) {
     const uint64_t v = (a.dim + 7u) / 8u;
-    if (v <= 8u) return launch_instance<Tx, Ty, 8, 1, ALIGNED>(a, sm_count, stream);
-    if (v <= 16u) return launch_instance<Tx, Ty, 16, 1, ALIGNED>(a, sm_count, stream);
-    if (v <= 32u) return launch_instance<Tx, Ty, 32, 1, ALIGNED>(a, sm_count, stream);
-    if (v <= 64u) return launch_instance<Tx, Ty, 32, 2, ALIGNED>(a, sm_count, stream);
-    // 64 bytes of a row per thread, or 128 where the row needs them
-    constexpr int NV = 8 / (int)sizeof(Tx);
-    if (v <= 32u * NV) return launch_instance<Tx, Ty, 32, NV, ALIGNED>(a, sm_count, stream);
-    if (v <= 64u * NV) return launch_instance<Tx, Ty, 64, NV, ALIGNED>(a, sm_count, stream);
-    if (v <= 128u * NV) return launch_instance<Tx, Ty, 128, NV, ALIGNED>(a, sm_count, stream);
-    if (v <= 256u * NV) return launch_instance<Tx, Ty, 256, NV, ALIGNED>(a, sm_count, stream);
-    if (v <= 512u * NV) return launch_instance<Tx, Ty, 512, NV, ALIGNED>(a, sm_count, stream);
-    return launch_instance<Tx, Ty, 512, 4, ALIGNED>(a, sm_count, stream);
+    if (v <= 8u) return launch_mode<Tx, Ty, 8, 1>(a, sm_count, stream);
+    if (v <= 16u) return launch_mode<Tx, Ty, 16, 1>(a, sm_count, stream);
+    if (v <= 32u) return launch_mode<Tx, Ty, 32, 1>(a, sm_count, stream);
+    if (v <= 64u) return launch_mode<Tx, Ty, 64, 1>(a, sm_count, stream);
+    if (v <= 128u) return launch_mode<Tx, Ty, 128, 1>(a, sm_count, stream);
+    if (v <= 256u) return launch_mode<Tx, Ty, 256, 1>(a, sm_count, stream);
+    if (v <= 512u) return launch_mode<Tx, Ty, 512, 1>(a, sm_count, stream);
+    if (v <= 1024u) return launch_mode<Tx, Ty, 512, 2>(a, sm_count, stream);
+    return launch_mode<Tx, Ty, 512, 4>(a, sm_count, stream);
 }
 
 }  // namespace
@@ -218,9 +282,7 @@ cudaError_t launch_layer_norm(const LayerNormArgs &a, int sm_count, cudaStream_t
             layer_norm_wide_kernel<Tx, Ty><<<(uint32_t)(a.n < most ? a.n : most), kWideThreads, 0, stream>>>(a);
             return cudaGetLastError();
         }
-        return rows_aligned<Tx>(a.d_x, a.x_stride, a.n, a.dim) && rows_aligned<Ty>(a.d_y, a.y_stride, a.n, a.dim)
-                   ? launch_width<Tx, Ty, true>(a, sm_count, stream)
-                   : launch_width<Tx, Ty, false>(a, sm_count, stream);
+        return launch_width<Tx, Ty>(a, sm_count, stream);
     });
 }
 

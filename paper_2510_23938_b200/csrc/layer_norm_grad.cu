@@ -3,10 +3,12 @@
 //
 // Bound by memory: x and dy are read once and dx is written once.  A CTA takes a run of consecutive rows; a thread owns
 // eight (or sixteen) columns of every T threads' row, so the sums over rows stay in its registers, and only the row's two sums
-// cross threads.  Rows come through a ring in shared memory that each thread fills for itself with asynchronous copies of
-// 16 bytes (of the aligned pieces its elements lie in), several rows ahead, and reads without any barrier.  At the end each
+// cross threads, those of four (or two) rows at a time.  Rows come through a ring in shared memory that each warp fills for itself
+// with asynchronous copies of 16 bytes (of the aligned pieces its elements lie in), several rows ahead.  At the end each
 // CTA leaves its sums over rows in global memory, and norm_grad_columns_kernel adds them up.
 // The order of every sum is a function of the number of rows, their width and type alone.
+#include <type_traits>
+
 #include "element_dev.cuh"
 #include "iv_internal.h"
 #include "row_dev.cuh"
@@ -19,8 +21,8 @@ using namespace rows;
 using elem::Pair;
 
 constexpr uint32_t kThreads = 512;
-constexpr uint64_t kMostParts = 296;      // runs of rows: two for each of a B200's SMs, whatever GPU it is (the sums' order goes by it)
-constexpr uint32_t kPartRows = 4;         // and no fewer rows than this per group of threads, if there are that many
+constexpr uint64_t kMostParts = 148;      // runs of rows: one for each of a B200's SMs, whatever GPU it is (the sums' order goes by it)
+constexpr uint32_t kPartRows = 2;         // and no fewer rows than this per group of threads, if there are that many
 
 // Runs of rows of a gradient over n rows, for groups of T threads.
 uint64_t part_count(uint64_t n, uint32_t groups) {
@@ -28,179 +30,137 @@ uint64_t part_count(uint64_t n, uint32_t groups) {
     return parts < kMostParts ? (parts ? parts : 1u) : kMostParts;
 }
 
-__device__ __forceinline__ void copy_async16(void *shared, const void *global) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(shared)), "l"(global) : "memory");
-}
-__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
-// Sums of two values over a group of T threads, in a fixed order; every thread gets both.  `slots`: as group_sum, 32 floats per
-// group of 512 threads (two values for each of 16 warps).
-template <uint32_t T>
-__device__ __forceinline__ void group_sum2(float &a, float &b, float *slots) {
-    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    if constexpr (T <= 16u) {
-#pragma unroll
-        for (uint32_t d = T / 2u; d; d >>= 1) {
-            a += __shfl_xor_sync(0xffffffffu, a, d);
-            b += __shfl_xor_sync(0xffffffffu, b, d);
-        }
-    } else {
-        // the lower half-warp adds up a, the upper b
-        const bool upper = lane & 16u;
-        float x = upper ? b : a;
-        x += __shfl_xor_sync(0xffffffffu, upper ? a : b, 16);
-#pragma unroll
-        for (uint32_t d = 8u; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-        if constexpr (T > 32u) {
-            constexpr uint32_t kWarps = T / 32u;
-            if ((lane & 15u) == 0u) slots[(upper ? kThreads / 32u : 0u) + warp] = x;
-            group_barrier<T>();
-            x = slots[(upper ? kThreads / 32u : 0u) + (warp & ~(kWarps - 1u)) + (lane & (kWarps - 1u))];
-#pragma unroll
-            for (uint32_t d = kWarps / 2u; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-        }
-        a = __shfl_sync(0xffffffffu, x, 0);
-        b = __shfl_sync(0xffffffffu, x, 16);
-    }
-}
-
-// A thread's vector of a row in the ring: the aligned 16-byte pieces it lies in.
-template <typename T, bool ALIGNED>
-struct Slot {
-    static constexpr int kPieces = (int)sizeof(T) / 2 + (ALIGNED ? 0 : 1);
-    // pieces[i * kThreads]: this thread's piece i
-    static __device__ __forceinline__ void fetch(uint4 *pieces, const T *row, uint32_t v, uint32_t dim) {
-        const T *p = row + v * 8u;
-        if constexpr (ALIGNED) {
-            if (v * 8u < dim) {
-#pragma unroll
-                for (int i = 0; i < kPieces; ++i) copy_async16(pieces + i * kThreads, reinterpret_cast<const uint8_t *>(p) + 16 * i);
-            }
-        } else {
-            const uint32_t left = left_of(v, dim), off = elem::misalignment(p), wanted = left ? off + left * (uint32_t)sizeof(T) : 0u;
-            const uint8_t *q = reinterpret_cast<const uint8_t *>(p) - off;
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i)
-                if (16u * i < wanted) copy_async16(pieces + i * kThreads, q + 16 * i);
-        }
-    }
-    // zeros behind the row's end
-    static __device__ __forceinline__ void get(const uint4 *pieces, uint32_t row_off, uint32_t v, uint32_t dim, Pair (&e)[4]) {
-        elem::Vector<T, 8, ALIGNED ? 16 : elem::kAny> raw;
-        if (v * 8u < dim) {
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                const uint4 x = pieces[i * kThreads];
-                raw.w[4 * i] = x.x; raw.w[4 * i + 1] = x.y; raw.w[4 * i + 2] = x.z; raw.w[4 * i + 3] = x.w;
-            }
-        } else {
-            raw.zero();
-        }
-        elem::unpack8(raw.get(ALIGNED ? 0u : row_off), e);
-        if constexpr (!ALIGNED) {
-            const uint32_t left = left_of(v, dim);
-            if (left < 8u) {
-                float x[8];
-                unpair(e, x);
-#pragma unroll
-                for (uint32_t i = 0; i < 4u; ++i) e[i] = Pair(2u * i < left ? x[2 * i] : 0.f, 2u * i + 1u < left ? x[2 * i + 1] : 0.f);
-            }
-        }
-    }
+// The ring: 16-byte pieces of x and of dy in a row of every group, rows that a group works on at a time (as many as leave room for
+// three such steps; two with fewer threads to a row, where four spill registers: 131072 x 1024 143 us, 209 with four), and steps.
+template <typename Tx, typename Ty, uint32_t T, int NV, int MODE>
+struct Ring {
+    static constexpr uint32_t kWidth = T < 32u ? T : 32u, kSegments = kThreads / kWidth;
+    using X = Segment<Tx, kWidth, MODE>;
+    using Y = Segment<Ty, kWidth, MODE>;
+    static constexpr uint32_t kX = kSegments * X::kPieces, kY = kSegments * Y::kPieces, kRow = NV * (kX + kY);
+    static constexpr uint32_t kRoom = 12288;             // pieces: 192 KiB
+    static constexpr int kRows = NV > 1 ? 1 : T == kThreads && 12u * kRow <= kRoom ? 4 : 2;
+    static constexpr int kStages = (int)(kRoom / (kRow * kRows));
+    static_assert(kStages >= 2 && 2u * kRows <= kWidth, "a step in flight; a lane for each of a step's statistics");
 };
 
-template <typename Tx, typename Ty, bool ALIGNED, int NV>
-__host__ __device__ constexpr uint32_t row_bytes() { return 16u * kThreads * NV * (Slot<Tx, ALIGNED>::kPieces + Slot<Ty, ALIGNED>::kPieces); }
-// Rows in the ring: what two CTAs can hold in an SM's shared memory, at most eight.
-template <typename Tx, typename Ty, bool ALIGNED, int NV>
-__host__ __device__ constexpr int stages_of() {
-    constexpr uint32_t fit = (96u << 10) / row_bytes<Tx, Ty, ALIGNED, NV>();
-    return fit > 8u ? 8 : fit < 2u ? 2 : (int)fit;
-}
-
-template <typename Tx, typename Ty, uint32_t T, int NV, bool ALIGNED>
-__global__ void __launch_bounds__(kThreads, NV > 1 ? 1 : 2)
+// One CTA per SM.
+template <typename Tx, typename Ty, uint32_t T, int NV, int MODE>
+__global__ void __launch_bounds__(kThreads, 1)
 norm_grad_kernel(const __grid_constant__ LayerNormGradArgs a, float *partial) {
-    constexpr uint32_t kGroups = kThreads / T;
-    constexpr int kStages = stages_of<Tx, Ty, ALIGNED, NV>();
-    constexpr int kX = Slot<Tx, ALIGNED>::kPieces, kY = Slot<Ty, ALIGNED>::kPieces;
-    extern __shared__ uint4 ring[];                      // kStages x (x, dy) x NV x pieces x kThreads
-    __shared__ float slots[2][kThreads / 16];
+    using Rows = Ring<Tx, Ty, T, NV, MODE>;
+    using X = typename Rows::X;
+    using Y = typename Rows::Y;
+    constexpr uint32_t kGroups = kThreads / T, kWidth = Rows::kWidth, kRow = Rows::kRow;
+    constexpr int kStages = Rows::kStages, R = Rows::kRows;
+    extern __shared__ uint4 ring[];                      // steps x rows x vectors x (x, dy)
+    __shared__ float slots[2][2 * R * 16];
     allow_next_kernel();
-    const uint32_t t = threadIdx.x % T, group = threadIdx.x / T;
+    const uint32_t t = threadIdx.x % T, group = threadIdx.x / T, lane = threadIdx.x % kWidth, segment = threadIdx.x / kWidth;
     const uint32_t dim = (uint32_t)a.dim;
     const uint64_t begin = a.n * blockIdx.x / gridDim.x, end = a.n * (blockIdx.x + 1u) / gridDim.x;
+    constexpr uint32_t kStep = R * kGroups;              // rows of a step: row i of the group is number i * kGroups + group of them
     const Tx *x = static_cast<const Tx *>(a.d_x);
     const Ty *dy = static_cast<const Ty *>(a.d_dy);
     Tx *dx = static_cast<Tx *>(a.d_dx);
-    auto slot = [&](int stage, int j) { return ring + (stage * NV + j) * (kX + kY) * kThreads + threadIdx.x; };
-    auto fetch = [&](uint64_t base, int stage) {         // the group's row of those from `base` on
-        const uint64_t row = base + group;
-        if (row < end) {
+    uint4 *const own_x = ring + segment * X::kPieces, *const own_y = ring + Rows::kX + segment * Y::kPieces;
+    // this thread's next row to fetch and to work on, and from one row of a step, or one step, to the next
+    const uint64_t row_x = kGroups * a.x_stride, row_dy = kGroups * a.dy_stride, row_dx = kGroups * a.dx_stride;
+    const Tx *fetch_x = x + (begin + group) * a.x_stride, *work_x = fetch_x;
+    const Ty *fetch_dy = dy + (begin + group) * a.dy_stride, *work_dy = fetch_dy;
+    Tx *work_dx = dx + (begin + group) * a.dx_stride;
+    auto fetch = [&](uint64_t base, uint32_t at) {       // at: the step's place in the ring
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            if (base + i * kGroups + group >= end) break;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                Slot<Tx, ALIGNED>::fetch(slot(stage, j), x + row * a.x_stride, t + j * T, dim);
-                Slot<Ty, ALIGNED>::fetch(slot(stage, j) + kX * kThreads, dy + row * a.dy_stride, t + j * T, dim);
+                const uint32_t place = at + (i * NV + j) * (Rows::kX + Rows::kY);
+                X::fetch(own_x + place, fetch_x + i * row_x, t + j * T, lane, dim);
+                Y::fetch(own_y + place, fetch_dy + i * row_dy, t + j * T, lane, dim);
             }
         }
         commit_copies();
+        fetch_x += R * row_x;
+        fetch_dy += R * row_dy;
+    };
+    // lane i of the group has 1 / deviation of its row i, lane R + i its mean
+    auto statistic = [&](uint64_t base) {
+        const uint64_t row = base + (lane & (R - 1u)) * kGroups + group;
+        const float *from = lane < R ? a.d_rstd : lane < 2u * R ? a.d_mean : nullptr;
+        return from && row < end ? from[row] : 0.f;
     };
 #pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) fetch(begin + s * kGroups, s);
+    for (int s = 0; s < kStages - 1; ++s) fetch(begin + s * kStep, s * R * kRow);
+    float next_statistic = statistic(begin);
     Pair w[NV][4], dw[NV][4], db[NV][4];
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) {
+        params_of(a.d_weight, a.param_type, t + j * T, dim, 1.f, w[j]);
 #pragma unroll
-        for (uint32_t i = 0; i < 4u; ++i) {
-            const uint32_t c = (t + j * T) * 8u + 2u * i;
-            auto weight = [&](uint32_t at) { return at >= dim ? 0.f : a.d_weight ? param_at(a.d_weight, a.param_type, at) : 1.f; };
-            w[j][i] = Pair(weight(c), weight(c + 1u));
-            dw[j][i] = db[j][i] = Pair(0.f);
-        }
+        for (int i = 0; i < 4; ++i) dw[j][i] = db[j][i] = Pair(0.f);
+    }
     const float scale = 1.f / (float)dim;
-    int stage = 0;
+    uint32_t now = 0, last = (kStages - 1) * R * kRow;
     float *sums = slots[0], *other = slots[1];
-    for (uint64_t base = begin; base < end; base += kGroups) {
-        fetch(base + (uint64_t)(kStages - 1) * kGroups, stage == 0 ? kStages - 1 : stage - 1);
+    // `whole`: all rows of the step are there
+    auto work = [&](uint64_t base, auto whole) {
+        fetch(base + (uint64_t)(kStages - 1) * kStep, last);
+        last = now;
+        const float statistics = next_statistic;
+        next_statistic = statistic(base + kStep);
         wait_copies<kStages - 1>();
-        const uint64_t row = base + group;
-        const bool live = row < end;
-        const float rstd = live ? a.d_rstd[row] : 0.f, mean = live && a.d_mean ? a.d_mean[row] : 0.f;
-        const uint32_t x_off = elem::misalignment(x + (live ? row * a.x_stride : 0u)), y_off = elem::misalignment(dy + (live ? row * a.dy_stride : 0u));
-        const Pair shift(-mean), by(rstd);
-        Pair h[NV][4], p[NV][4], s2(0.f), sh2(0.f);
+        __syncwarp();
+        Pair h[R][NV][4], p[R][NV][4];
+        float s[2 * R];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            Pair e[4];
-            Slot<Tx, ALIGNED>::get(slot(stage, j), x_off, t + j * T, live ? dim : 0u, h[j]);
-            Slot<Ty, ALIGNED>::get(slot(stage, j) + kX * kThreads, y_off, t + j * T, live ? dim : 0u, e);
+        for (int i = 0; i < R; ++i) {
+            const bool live = decltype(whole)::value || base + i * kGroups + group < end;
+            const uint32_t x_off = elem::misalignment(work_x + i * row_x), y_off = elem::misalignment(work_dy + i * row_dy);
+            const Pair by(__shfl_sync(0xffffffffu, statistics, i, kWidth)), shift(-__shfl_sync(0xffffffffu, statistics, R + i, kWidth));
+            Pair s2(0.f), sh2(0.f);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                h[j][i] = (h[j][i] + shift) * by;
-                p[j][i] = e[i] * w[j][i];
-                db[j][i] = db[j][i] + e[i];
-                dw[j][i] = fma2(e[i], h[j][i], dw[j][i]);
-                s2 = s2 + p[j][i];
-                sh2 = fma2(p[j][i], h[j][i], sh2);
+            for (int j = 0; j < NV; ++j) {
+                Pair e[4];
+                const uint32_t place = now + (i * NV + j) * (Rows::kX + Rows::kY);
+                elem::unpack8(X::get(own_x + place, x_off, t + j * T, lane, dim, live), h[i][j]);
+                elem::unpack8(Y::get(own_y + place, y_off, t + j * T, lane, dim, live), e);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    h[i][j][k] = (h[i][j][k] + shift) * by;
+                    p[i][j][k] = e[k] * w[j][k];
+                    db[j][k] = db[j][k] + e[k];
+                    dw[j][k] = fma2(e[k], h[i][j][k], dw[j][k]);
+                    s2 = s2 + p[i][j][k];
+                    sh2 = fma2(p[i][j][k], h[i][j][k], sh2);
+                }
             }
+            s[2 * i] = s2.sum();
+            s[2 * i + 1] = sh2.sum();
         }
-        float s = s2.sum(), sh = sh2.sum();
-        group_sum2<T>(s, sh, sums);
-        const Pair mp(a.rms ? 0.f : -s * scale), mh(-sh * scale);
-        Tx *out = dx + (live ? row * a.dx_stride : 0u);
+        group_sums<T, 2 * R>(s, sums, [scale](float sum) { return -sum * scale; });
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
+        for (int i = 0; i < R; ++i) {
+            const bool live = decltype(whole)::value || base + i * kGroups + group < end;
+            const Pair by(__shfl_sync(0xffffffffu, statistics, i, kWidth)), mp(a.rms ? 0.f : s[2 * i]), mh(s[2 * i + 1]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) h[j][i] = (fma2(h[j][i], mh, p[j][i]) + mp) * by;
-            store_row_vector<Tx, ALIGNED, T>(out, t + j * T, live ? dim : 0u, h[j]);
+            for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) h[i][j][k] = (fma2(h[i][j][k], mh, p[i][j][k]) + mp) * by;
+                store_row_vector<Tx, MODE, T>(work_dx + i * row_dx, t + j * T, dim, live, h[i][j]);
+            }
         }
         float *swap = sums;
         sums = other;
         other = swap;
-        stage = stage + 1 == kStages ? 0 : stage + 1;
-    }
+        now = now + R * kRow == kStages * R * kRow ? 0u : now + R * kRow;
+        work_x += R * row_x;
+        work_dy += R * row_dy;
+        work_dx += R * row_dx;
+    };
+    uint64_t base = begin;
+    for (; base + kStep <= end; base += kStep) work(base, std::true_type());
+    if (base < end) work(base, std::false_type());
     if (!a.d_dw && !a.d_db) return;
     // the groups' sums, first to last
     wait_copies<0>();
@@ -248,13 +208,13 @@ norm_grad_kernel(const __grid_constant__ LayerNormGradArgs a, float *partial) {
 template <typename Tx, typename Ty>
 __global__ void __launch_bounds__(kThreads)
 norm_grad_wide_rows_kernel(LayerNormGradArgs a, float2 *row_sums) {
-    __shared__ float slots[kThreads / 16];
+    __shared__ float slots[2 * 16];
     const uint32_t dim = (uint32_t)a.dim, vectors = (dim + 7u) / 8u;
     for (uint64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const Tx *x = static_cast<const Tx *>(a.d_x) + row * a.x_stride;
         const Ty *dy = static_cast<const Ty *>(a.d_dy) + row * a.dy_stride;
         const float rstd = a.d_rstd[row], mean = a.d_mean ? a.d_mean[row] : 0.f;
-        float s = 0.f, sh = 0.f;
+        float sums[2] = {0.f, 0.f};
         for (uint32_t v = threadIdx.x; v < vectors; v += kThreads) {
             RowVector<Tx, false> rx;
             RowVector<Ty, false> ry;
@@ -271,12 +231,12 @@ norm_grad_wide_rows_kernel(LayerNormGradArgs a, float2 *row_sums) {
             for (uint32_t i = 0; i < 8u; ++i) {
                 if (i >= left) break;
                 const float q = a.d_weight ? p[i] * param_at(a.d_weight, a.param_type, v * 8u + i) : p[i];
-                s += q;
-                sh = fmaf(q, (h[i] - mean) * rstd, sh);
+                sums[0] += q;
+                sums[1] = fmaf(q, (h[i] - mean) * rstd, sums[1]);
             }
         }
-        group_sum2<kThreads>(s, sh, slots);
-        if (threadIdx.x == 0) row_sums[row] = make_float2(s, sh);
+        group_sums<kThreads, 2>(sums, slots, [](float sum) { return sum; });
+        if (threadIdx.x == 0) row_sums[row] = make_float2(sums[0], sums[1]);
         __syncthreads();                                 // before the slots are written again
     }
 }
@@ -320,7 +280,7 @@ norm_grad_wide_kernel(LayerNormGradArgs a, const float2 *row_sums, float *partia
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) pairs[i] = Pair(h[2 * i], h[2 * i + 1]);
-        store_row_vector<Tx, false, 32>(static_cast<Tx *>(a.d_dx) + row * a.dx_stride, v, dim, pairs);
+        store_row_vector<Tx, kAnyRows, 32>(static_cast<Tx *>(a.d_dx) + row * a.dx_stride, v, dim, true, pairs);
     }
     if (!a.d_dw && !a.d_db) return;
 #pragma unroll
@@ -365,10 +325,11 @@ norm_grad_columns_kernel(const float *partial, uint32_t parts, uint32_t dim, voi
     else static_cast<__nv_bfloat16 *>(out)[i] = elem::from_float<__nv_bfloat16>(sum);
 }
 
-template <typename Tx, typename Ty, uint32_t T, int NV, bool ALIGNED>
+template <typename Tx, typename Ty, uint32_t T, int NV, int MODE>
 cudaError_t launch_instance(const LayerNormGradArgs &a, float *partial, uint32_t parts, cudaStream_t stream) {
-    auto kernel = norm_grad_kernel<Tx, Ty, T, NV, ALIGNED>;
-    constexpr uint32_t rows = row_bytes<Tx, Ty, ALIGNED, NV>() * stages_of<Tx, Ty, ALIGNED, NV>(), sums = 64u * NV * kThreads;
+    auto kernel = norm_grad_kernel<Tx, Ty, T, NV, MODE>;
+    using Rows = Ring<Tx, Ty, T, NV, MODE>;
+    constexpr uint32_t rows = 16u * Rows::kRow * Rows::kRows * Rows::kStages, sums = 64u * NV * kThreads;
     constexpr uint32_t shared = rows > sums ? rows : sums;
     static bool done[kMaxDevices] = {};
     cudaError_t e = ensure_dynamic_smem(kernel, shared, done);
@@ -391,17 +352,25 @@ uint64_t parts_for(uint64_t n, uint64_t dim) {
     return parts < most ? parts : most;                  // 16 CTAs for each of a B200's SMs, all tiles together
 }
 
-template <typename Tx, typename Ty, bool ALIGNED>
+template <typename Tx, typename Ty, uint32_t T, int NV>
+cudaError_t launch_mode(const LayerNormGradArgs &a, float *partial, uint32_t parts, cudaStream_t stream) {
+    if (!rows_aligned<Tx>(a.d_x, a.x_stride, a.n, a.dim) || !rows_aligned<Ty>(a.d_dy, a.dy_stride, a.n, a.dim) ||
+        !rows_aligned<Tx>(a.d_dx, a.dx_stride, a.n, a.dim))
+        return launch_instance<Tx, Ty, T, NV, kAnyRows>(a, partial, parts, stream);
+    return a.dim == 8u * T * NV ? launch_instance<Tx, Ty, T, NV, kExactRows>(a, partial, parts, stream)
+                                : launch_instance<Tx, Ty, T, NV, kAlignedRows>(a, partial, parts, stream);
+}
+template <typename Tx, typename Ty>
 cudaError_t launch_width(const LayerNormGradArgs &a, float *partial, uint32_t parts, cudaStream_t stream) {
-    if (a.dim > 8u * kThreads) return launch_instance<Tx, Ty, kThreads, 2, ALIGNED>(a, partial, parts, stream);
+    if (a.dim > 8u * kThreads) return launch_mode<Tx, Ty, kThreads, 2>(a, partial, parts, stream);
     switch (threads_for(a.dim)) {
-        case 8: return launch_instance<Tx, Ty, 8, 1, ALIGNED>(a, partial, parts, stream);
-        case 16: return launch_instance<Tx, Ty, 16, 1, ALIGNED>(a, partial, parts, stream);
-        case 32: return launch_instance<Tx, Ty, 32, 1, ALIGNED>(a, partial, parts, stream);
-        case 64: return launch_instance<Tx, Ty, 64, 1, ALIGNED>(a, partial, parts, stream);
-        case 128: return launch_instance<Tx, Ty, 128, 1, ALIGNED>(a, partial, parts, stream);
-        case 256: return launch_instance<Tx, Ty, 256, 1, ALIGNED>(a, partial, parts, stream);
-        default: return launch_instance<Tx, Ty, 512, 1, ALIGNED>(a, partial, parts, stream);
+        case 8: return launch_mode<Tx, Ty, 8, 1>(a, partial, parts, stream);
+        case 16: return launch_mode<Tx, Ty, 16, 1>(a, partial, parts, stream);
+        case 32: return launch_mode<Tx, Ty, 32, 1>(a, partial, parts, stream);
+        case 64: return launch_mode<Tx, Ty, 64, 1>(a, partial, parts, stream);
+        case 128: return launch_mode<Tx, Ty, 128, 1>(a, partial, parts, stream);
+        case 256: return launch_mode<Tx, Ty, 256, 1>(a, partial, parts, stream);
+        default: return launch_mode<Tx, Ty, 512, 1>(a, partial, parts, stream);
     }
 }
 
@@ -431,10 +400,7 @@ cudaError_t launch_layer_norm_grad(const LayerNormGradArgs &a, float *d_partial,
             using Tx = typename decltype(in)::type;
             using Ty = typename decltype(out)::type;
             if (a.dim > kWidest) return launch_wide<Tx, Ty>(a, d_partial, parts, sm_count, stream);
-            return rows_aligned<Tx>(a.d_x, a.x_stride, a.n, a.dim) && rows_aligned<Ty>(a.d_dy, a.dy_stride, a.n, a.dim) &&
-                           rows_aligned<Tx>(a.d_dx, a.dx_stride, a.n, a.dim)
-                       ? launch_width<Tx, Ty, true>(a, d_partial, parts, stream)
-                       : launch_width<Tx, Ty, false>(a, d_partial, parts, stream);
+            return launch_width<Tx, Ty>(a, d_partial, parts, stream);
         });
         if (e != cudaSuccess) return e;
         *launches += a.dim > kWidest ? 2u : 1u;

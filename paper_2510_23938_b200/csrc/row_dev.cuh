@@ -9,6 +9,10 @@ namespace rows {
 using elem::Pair;
 using elem::unpair;
 
+// How rows lie: anywhere; at 16-byte boundaries and in whole vectors of eight elements; and so that all threads of a row's group
+// have the same number of vectors too.
+enum Rows { kAnyRows = 0, kAlignedRows = 1, kExactRows = 2 };
+
 // Elements of vector v that are in a row of `dim`.
 __device__ __forceinline__ uint32_t left_of(uint32_t v, uint32_t dim) { return v * 8u < dim ? (dim - v * 8u < 8u ? dim - v * 8u : 8u) : 0u; }
 
@@ -84,21 +88,24 @@ __device__ __forceinline__ void store_pieces(T *p, const elem::Packed<T, 8> &own
         }
 }
 
-// A lane's vector v of a row; T threads to a row, by whole warps; `dim` is 0 for a row that is not there.
-template <typename T, bool ALIGNED, uint32_t THREADS>
-__device__ __forceinline__ void store_row_vector(T *row, uint32_t v, uint32_t dim, const Pair (&pairs)[4]) {
+// A lane's vector v of a row; T threads to a row, by whole warps; `live`: the row is there.
+template <typename T, int MODE, uint32_t THREADS>
+__device__ __forceinline__ void store_row_vector(T *row, uint32_t v, uint32_t dim, bool live, const Pair (&pairs)[4]) {
     float e[8];
     unpair(pairs, e);
     elem::Packed<T, 8> out;
     out.pack(e);
     T *p = row + v * 8u;
-    if constexpr (ALIGNED) {
-        if (v * 8u < dim) {
+    if constexpr (MODE != kAnyRows) {
+        if (live && (MODE == kExactRows || v * 8u < dim)) {
+            if (sizeof(T) == 4 && (reinterpret_cast<uintptr_t>(row) & 16u) == 0u) elem::store_32_bytes(p, out.w);
+            else {
 #pragma unroll
-            for (int i = 0; i < elem::Packed<T, 8>::kWords; i += 4) elem::store_aligned<4>(reinterpret_cast<uint32_t *>(p) + i, out.w + i);
+                for (int i = 0; i < elem::Packed<T, 8>::kWords; i += 4) elem::store_aligned<4>(reinterpret_cast<uint32_t *>(p) + i, out.w + i);
+            }
         }
     } else {
-        store_pieces<T>(p, out, left_of(v, dim), THREADS < 32u ? THREADS : 32u);
+        store_pieces<T>(p, out, live ? left_of(v, dim) : 0u, THREADS < 32u ? THREADS : 32u);
     }
 }
 
@@ -117,44 +124,116 @@ __device__ __forceinline__ void group_barrier() {
     asm volatile("bar.sync %0, %1;" ::"r"(threadIdx.x / T + 1u), "n"(T) : "memory");
 }
 
-// Sum over a group of T threads, in a fixed order; every thread gets it.  `slots`: one float per warp of the CTA, which the
-// group may write again once it has met at another barrier of its own (two alternating arrays need no other).
-template <uint32_t T>
-__device__ __forceinline__ float group_sum(float x, float *slots) {
-#pragma unroll
-    for (uint32_t d = (T < 32u ? T : 32u) / 2u; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    if constexpr (T > 32u) {
-        constexpr uint32_t kWarps = T / 32u;
-        const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
-        if (lane == 0u) slots[warp] = x;
-        group_barrier<T>();
-        x = slots[(warp & ~(kWarps - 1u)) + (lane & (kWarps - 1u))];
-#pragma unroll
-        for (uint32_t d = kWarps / 2u; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    }
-    return x;
-}
-
 __device__ __forceinline__ float param_at(const void *p, int type, uint32_t i) {
     if (type == IV_F32) return static_cast<const float *>(p)[i];
     if (type == IV_F16) return elem::to_float(static_cast<const __half *>(p)[i]);
     return elem::to_float(static_cast<const __nv_bfloat16 *>(p)[i]);
 }
 
-// `dim` weights in 32 bits, by the whole CTA: the first halves of all vectors of eight, then the second halves, so that a
-// warp's 16-byte reads of consecutive vectors touch every bank once.
-__device__ __forceinline__ void widen_params(const void *p, int type, uint32_t dim, float4 *out) {
-    const uint32_t vectors = (dim + 7u) / 8u;
-    float *o = reinterpret_cast<float *>(out);
-    for (uint32_t i = threadIdx.x; i < vectors * 8u; i += blockDim.x)
-        o[((i >> 2 & 1u) * vectors + (i >> 3)) * 4u + (i & 3u)] = i < dim ? param_at(p, type, i) : 0.f;
+__device__ __forceinline__ void copy_async16(void *shared, const void *global) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(shared)), "l"(global) : "memory");
 }
-__device__ __forceinline__ void read_params(const float4 *params, uint32_t v, uint32_t vectors, Pair (&w)[4]) {
-    const float4 lo = params[v], hi = params[vectors + v];
-    w[0] = Pair(lo.x, lo.y);
-    w[1] = Pair(lo.z, lo.w);
-    w[2] = Pair(hi.x, hi.y);
-    w[3] = Pair(hi.z, hi.w);
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// f of the sums of N values (a power of two, at most 8) over a group of T threads; every thread gets all.  The order is that of a
+// tree over the threads' numbers, upper bits first, whatever N.  Lanes halve the values among them before they halve themselves,
+// so that eight values take nine exchanges.  `slots`: a float per value and warp; a call writes them while others may still read
+// those of the call before, so calls alternate between two arrays.
+template <uint32_t T, int N, typename F>
+__device__ __forceinline__ void group_sums(float (&v)[N], float *slots, F f) {
+    constexpr uint32_t kWidth = T < 32u ? T : 32u, L = kWidth / N;      // L lanes end up with one value
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    uint32_t d = kWidth / 2u;
+#pragma unroll
+    for (int n = N; n > 1; n /= 2, d /= 2u) {
+        const bool upper = lane & d;
+#pragma unroll
+        for (int i = 0; i < n / 2; ++i) {
+            const float send = upper ? v[i] : v[i + n / 2], keep = upper ? v[i + n / 2] : v[i];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, send, d);
+        }
+    }
+    float x = v[0];
+#pragma unroll
+    for (; d; d /= 2u) x += __shfl_xor_sync(0xffffffffu, x, d);
+    if constexpr (T > 32u) {
+        constexpr uint32_t kWarps = T / 32u, kEach = kWarps > L ? kWarps / L : 1u, kLanes = kWarps > L ? L : kWarps;
+        const uint32_t value = lane / L, q = lane & (kLanes - 1u);
+        constexpr uint32_t kAll = T > 512u ? 32u : 16u;                 // warps of a CTA
+        if (lane % L == 0u) slots[value * kAll + warp] = x;
+        group_barrier<T>();
+        float part[kEach];
+#pragma unroll
+        for (uint32_t e = 0; e < kEach; ++e) part[e] = slots[value * kAll + (warp & ~(kWarps - 1u)) + q + e * kLanes];
+        x = sum_of<(int)kEach>(part);
+#pragma unroll
+        for (uint32_t k = kLanes / 2u; k; k /= 2u) x += __shfl_xor_sync(0xffffffffu, x, k);
+    }
+    x = f(x);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, x, i * L, kWidth);
+}
+
+// The vectors of WIDTH consecutive lanes in a row, as the lanes bring them into shared memory with asynchronous copies of 16 bytes,
+// each the pieces in its turn: every piece of the row comes once, whatever its alignment.  The lanes read them after
+// wait_copies and a __syncwarp.
+template <typename T, uint32_t WIDTH, int MODE>
+struct Segment {
+    static constexpr bool kAligned = MODE != kAnyRows;
+    static constexpr uint32_t kEach = sizeof(T) / 2u, kPieces = WIDTH * kEach + (kAligned ? 0u : 1u);
+    // v: this lane's vector, `lane` its number among the WIDTH
+    static __device__ __forceinline__ void fetch(uint4 *to, const T *row, uint32_t v, uint32_t lane, uint32_t dim) {
+        const uint32_t first = (v - lane) * 8u;
+        const uint8_t *p = reinterpret_cast<const uint8_t *>(row + first);
+        if constexpr (MODE == kExactRows) {
+#pragma unroll
+            for (uint32_t i = 0; i < kEach; ++i) copy_async16(to + i * WIDTH + lane, p + 16u * (i * WIDTH + lane));
+        } else {
+            if (first >= dim) return;
+            const uint32_t off = kAligned ? 0u : elem::misalignment(p), bytes = off + (dim - first) * (uint32_t)sizeof(T);
+            p -= off;
+#pragma unroll
+            for (uint32_t i = 0; i < kEach; ++i) {
+                const uint32_t c = i * WIDTH + lane;
+                if (16u * c < bytes) copy_async16(to + c, p + 16u * c);
+            }
+            if constexpr (!kAligned)
+                if (lane == 0u && off && 16u * WIDTH * kEach < bytes) copy_async16(to + WIDTH * kEach, p + 16u * WIDTH * kEach);
+        }
+    }
+    // This lane's elements, zeros behind the row's end or if it is not there.  row_off: the row's bytes from a 16-byte boundary.
+    static __device__ __forceinline__ elem::Packed<T, 8> get(const uint4 *from, uint32_t row_off, uint32_t v, uint32_t lane, uint32_t dim, bool live) {
+        elem::Vector<T, 8, kAligned ? 16 : elem::kAny> raw;
+        const bool some = live && (MODE == kExactRows || v * 8u < dim);
+#pragma unroll
+        for (uint32_t i = 0; i < kEach + (kAligned ? 0u : 1u); ++i) {
+            const uint4 x = some ? from[lane * kEach + i] : make_uint4(0u, 0u, 0u, 0u);
+            raw.w[4 * i] = x.x; raw.w[4 * i + 1] = x.y; raw.w[4 * i + 2] = x.z; raw.w[4 * i + 3] = x.w;
+        }
+        elem::Packed<T, 8> out = raw.get(kAligned ? 0u : row_off);
+        if constexpr (!kAligned) {
+            const uint32_t left = left_of(v, dim);
+            if (left < 8u) {
+#pragma unroll
+                for (uint32_t i = 0; i < elem::Packed<T, 8>::kWords; ++i) {
+                    const uint32_t bytes = left * (uint32_t)sizeof(T);
+                    out.w[i] = 4u * i + 4u <= bytes ? out.w[i] : 4u * i < bytes ? out.w[i] & 0xffffu : 0u;
+                }
+            }
+        }
+        return out;
+    }
+};
+
+// Eight weights of a row's vector v, `otherwise` where there is none; zeros behind the row's end.
+__device__ __forceinline__ void params_of(const void *p, int type, uint32_t v, uint32_t dim, float otherwise, Pair (&w)[4]) {
+    float e[8];
+#pragma unroll
+    for (uint32_t i = 0; i < 8u; ++i) e[i] = v * 8u + i >= dim ? 0.f : p ? param_at(p, type, v * 8u + i) : otherwise;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = Pair(e[2 * i], e[2 * i + 1]);
 }
 
 }  // namespace rows
