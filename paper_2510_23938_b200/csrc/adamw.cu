@@ -39,6 +39,7 @@ struct Coefficients {
     float beta1, rest1, beta2, rest2;          // rest = 1 - beta
     float factor;                              // of the gradients
     float step, root, eps, keep;               // lr / (1 - b1^t), 1 / sqrt(1 - b2^t), eps, 1 - lr decay
+    float nothing;                             // -0: a product plus this is the product rounded, which no later addition takes in
     uint32_t key0, key1;
     bool skip;
 };
@@ -62,6 +63,7 @@ __device__ __forceinline__ void make_coefficients(const AdamwArgs &a, Coefficien
     c.step = (float)(lr / -expm1((double)t * a.log_beta1));
     c.root = (float)(1.0 / sqrt(-expm1((double)t * a.log_beta2)));
     c.eps = a.eps;
+    c.nothing = -0.f;
     c.keep = (float)(1.0 - lr * a.weight_decay);
     c.key0 = mix(mix(mix((uint32_t)a.seed + kGolden) + (uint32_t)(a.seed >> 32)) + (uint32_t)t);
     c.key1 = mix(c.key0 + (uint32_t)(t >> 32) + kGolden);
@@ -234,12 +236,13 @@ struct Lane {
     // New moments, roots r and weights.  The moments' products and sums are rounded one by one, so that elementary operations
     // give the same bits; root and reciprocal are approximate, small against the weight that an update changes.
     __device__ __forceinline__ void update(const Coefficients &c) {
-        const Pair factor(c.factor), beta1(c.beta1), rest1(c.rest1), beta2(c.beta2), rest2(c.rest2), root(c.root), eps(c.eps), step(-c.step), keep(c.keep);
+        const Pair factor(c.factor), beta1(c.beta1), rest1(c.rest1), beta2(c.beta2), rest2(c.rest2), root(c.root), eps(c.eps), step(-c.step), keep(c.keep),
+            nothing(c.nothing);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const Pair g1 = g[i] * factor, square = BITS == 32 ? v[i] : v[i] * v[i];
-            m[i] = m[i] * beta1 + g1 * rest1;
-            v[i] = square * beta2 + g1 * g1 * rest2;
+            m[i] = fma2(m[i], beta1, nothing) + fma2(g1, rest1, nothing);
+            v[i] = fma2(square, beta2, nothing) + fma2(g1 * g1, rest2, nothing);
             r[i] = root_approx(v[i]);
             w[i] = fma2(w[i], keep, m[i] * step * reciprocal_approx(fma2(r[i], root, eps)));
         }

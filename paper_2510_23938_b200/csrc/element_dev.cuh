@@ -150,7 +150,7 @@ struct Vector {
     }
 };
 
-// Two 32-bit floats that one instruction works on, each rounded by itself.
+// Two 32-bit floats that one instruction works on, each rounded by itself (but a product that is added may become one multiply-add).
 struct Pair {
     uint64_t bits;
     __device__ __forceinline__ Pair() {}
