@@ -39,6 +39,7 @@ EXPORTS = (
 )
 
 ADAMW_BLOCK = 256          # IV_ADAMW_BLOCK
+_INFINITY = float("inf")
 
 # iv_dtype of the training-step operators
 DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
@@ -280,9 +281,17 @@ def _vector_ptr(t: Optional[torch.Tensor], n: int, dtype: Optional[torch.dtype] 
     """Device pointer of n contiguous elements (of `dtype`), None for no tensor."""
     if t is None:
         return None
+    assert t.is_cuda and t.is_contiguous() and t.numel() == n, "must be a contiguous CUDA tensor of one element per place"
+    assert dtype is None or t.dtype is dtype, "wrong type of elements"
+    return t.data_ptr()
+
+
+def _int64_ptr(t: torch.Tensor, n: int) -> Optional[int]:
+    """Device pointer of n int64 numbers, None if n is 0."""
+    assert t.dtype is torch.int64 and t.numel() == n, "offsets, lengths and places: one int64 per tensor"
+    if n == 0:
+        return None
     assert t.is_cuda and t.is_contiguous(), "device tensors must be contiguous CUDA tensors"
-    assert t.numel() == n, "wrong number of elements"
-    assert dtype is None or t.dtype == dtype, f"must be {dtype}"
     return t.data_ptr()
 
 
@@ -791,12 +800,16 @@ class Context:
         if out is None:
             out = _empty(x.shape, out_dtype or x.dtype, x.device, stream)
         out_ptr, out_stride = _rows_of(out, n, dim)
-        assert weight is None or bias is None or weight.dtype == bias.dtype, "weight and bias are of one type"
-        param = weight if weight is not None else bias
-        rc = self._lib.iv_layer_norm(self._h, x_ptr, DTYPES[x.dtype], x_stride, n, dim, _vector_ptr(weight, dim),
-                                     _vector_ptr(bias, dim), 0 if param is None else DTYPES[param.dtype], eps, rms, out_ptr,
-                                     DTYPES[out.dtype], out_stride, _vector_ptr(mean, n, torch.float32),
-                                     _vector_ptr(rstd, n, torch.float32), _stream_ptr(stream))
+        param, weight_ptr, bias_ptr = 0, None, None
+        if bias is not None:
+            assert weight is None or weight.dtype is bias.dtype, "weight and bias are of one type"
+            param, bias_ptr = DTYPES[bias.dtype], _vector_ptr(bias, dim)
+        if weight is not None:
+            param, weight_ptr = DTYPES[weight.dtype], _vector_ptr(weight, dim)
+        rc = self._lib.iv_layer_norm(self._h, x_ptr, DTYPES[x.dtype], x_stride, n, dim, weight_ptr, bias_ptr, param, eps, rms, out_ptr,
+                                     DTYPES[out.dtype], out_stride,
+                                     None if mean is None else _vector_ptr(mean, n, torch.float32),
+                                     None if rstd is None else _vector_ptr(rstd, n, torch.float32), _stream_ptr(stream))
         if rc:
             self._check(rc, "iv_layer_norm")
         return out
@@ -816,14 +829,17 @@ class Context:
             out = _empty(x.shape, x.dtype, x.device, stream)
         assert out.dtype == x.dtype, "the gradient is of x's type"
         out_ptr, out_stride = _rows_of(out, n, dim)
-        assert weight_grad is None or bias_grad is None or weight_grad.dtype == bias_grad.dtype, "sums are of one type"
-        sums = weight_grad if weight_grad is not None else bias_grad
+        sums, weight_grad_ptr, bias_grad_ptr = 0, None, None
+        if bias_grad is not None:
+            assert weight_grad is None or weight_grad.dtype is bias_grad.dtype, "sums are of one type"
+            sums, bias_grad_ptr = DTYPES[bias_grad.dtype], _vector_ptr(bias_grad, dim)
+        if weight_grad is not None:
+            sums, weight_grad_ptr = DTYPES[weight_grad.dtype], _vector_ptr(weight_grad, dim)
         rc = self._lib.iv_layer_norm_grad(self._h, grad_ptr, DTYPES[grad_out.dtype], grad_stride, x_ptr, DTYPES[x.dtype], x_stride,
                                           n, dim, _vector_ptr(weight, dim), 0 if weight is None else DTYPES[weight.dtype],
                                           None if rms else _vector_ptr(mean, n, torch.float32),
-                                          _vector_ptr(rstd, n, torch.float32), rms, out_ptr, out_stride,
-                                          _vector_ptr(weight_grad, dim), _vector_ptr(bias_grad, dim),
-                                          0 if sums is None else DTYPES[sums.dtype], accumulate, _stream_ptr(stream))
+                                          _vector_ptr(rstd, n, torch.float32), rms, out_ptr, out_stride, weight_grad_ptr,
+                                          bias_grad_ptr, sums, accumulate, _stream_ptr(stream))
         if rc:
             self._check(rc, "iv_layer_norm_grad")
         return out
@@ -841,27 +857,29 @@ class Context:
         when the step runs.  `norm` is the record of grad_norm over the gradients: they are clipped to `max_norm` on the
         way (None: not clipped), and where one is not finite nothing changes.  `seed` sets the random words that round
         8-bit moments and, with `stochastic`, 16-bit weights.  Types default to those of `base` and `grads`."""
-        n = offsets.numel()
-        for t in (offsets, lengths, grad_offsets, state_offsets):
-            assert t.numel() == n and t.dtype == torch.int64, "offsets, lengths and places: one int64 per tensor"
-        size = m.numel()
-        assert m.dtype in (torch.float32, torch.float8_e4m3fn), "moments are float32 or float8_e4m3fn"
-        bits = 32 if m.dtype == torch.float32 else 8
-        assert bits == 32 or (m_scales is not None and v_scales is not None), "8-bit moments need their scales"
-        assert step.is_cuda and step.dtype == torch.int64 and step.numel() == 1, "step: one int64 on the device"
-        blocks = size // ADAMW_BLOCK
+        n, size, kind = offsets.numel(), m.numel(), m.dtype
+        tensors = (_int64_ptr(offsets, n), _int64_ptr(lengths, n), _int64_ptr(grad_offsets, n), _int64_ptr(state_offsets, n))
+        if kind is torch.float32:
+            bits, m_scales_ptr, v_scales_ptr = 32, None, None
+        else:
+            assert kind is torch.float8_e4m3fn, "moments are float32 or float8_e4m3fn"
+            assert m_scales is not None and v_scales is not None, "8-bit moments need their scales"
+            bits, blocks = 8, size // ADAMW_BLOCK
+            m_scales_ptr = _vector_ptr(m_scales, blocks, torch.float32)
+            v_scales_ptr = _vector_ptr(v_scales, blocks, torch.float32)
+        assert step.is_cuda and step.dtype is torch.int64 and step.numel() == 1, "step: one int64 on the device"
         lr_ptr = None
         if isinstance(lr, torch.Tensor):
-            assert lr.is_cuda and lr.dtype == torch.float32 and lr.numel() == 1, "lr: a number or one float32 on the device"
+            assert lr.is_cuda and lr.dtype is torch.float32 and lr.numel() == 1, "lr: a number or one float32 on the device"
             lr_ptr, lr = lr.data_ptr(), 0.0
-        options = AdamwOptions(lr, betas[0], betas[1], eps, weight_decay, float("inf") if max_norm is None else max_norm,
-                               stochastic, seed & 0xffffffffffffffff)
+        assert base.is_cuda and grads.is_cuda, "device tensors must be CUDA tensors"
+        options = AdamwOptions(lr, betas[0], betas[1], eps, weight_decay, _INFINITY if max_norm is None else max_norm, stochastic,
+                               seed & 0xffffffffffffffff)
         rc = self._lib.iv_adamw_step(
-            self._h, _ptr(base), _dev_ptr(offsets), _dev_ptr(lengths), DTYPES[dtype or base.dtype], n, _ptr(grads),
-            _dev_ptr(grad_offsets), DTYPES[grad_dtype or grads.dtype], _dev_ptr(state_offsets), size, bits,
-            _vector_ptr(m, size), _vector_ptr(v, size, m.dtype), _vector_ptr(m_scales, blocks, torch.float32) if bits == 8 else None,
-            _vector_ptr(v_scales, blocks, torch.float32) if bits == 8 else None, _vector_ptr(master, size, torch.float32),
-            options, lr_ptr, None if norm is None else _result_ptr(norm), step.data_ptr(), _stream_ptr(stream))
+            self._h, base.data_ptr(), tensors[0], tensors[1], DTYPES[dtype or base.dtype], n, grads.data_ptr(), tensors[2],
+            DTYPES[grad_dtype or grads.dtype], tensors[3], size, bits, _vector_ptr(m, size), _vector_ptr(v, size, kind),
+            m_scales_ptr, v_scales_ptr, None if master is None else _vector_ptr(master, size, torch.float32), options, lr_ptr,
+            None if norm is None else _result_ptr(norm), step.data_ptr(), _stream_ptr(stream))
         if rc:
             self._check(rc, "iv_adamw_step")
 
