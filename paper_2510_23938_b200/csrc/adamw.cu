@@ -127,36 +127,62 @@ __device__ __forceinline__ void decode8(uint2 codes, float scale, Pair (&out)[4]
 // that no rounding reaches the code behind it, which is NaN; the largest value is taken as 2^-110 at least, so that neither
 // factor leaves the range of 32 bits.
 constexpr float kTop = 447.9995f;
-struct BlockScale {
-    float inverse, scale;
-    bool bad;                                  // an infinity or a NaN in the block; the scale is the others'
-};
-__device__ __forceinline__ BlockScale block_scale(float top, bool bad) {
-    const float safe = fmaxf(top, 0x1p-110f);
-    return {top > 0.f ? __fmul_rn(__frcp_rn(safe), kTop) : 0.f, top > 0.f ? safe * (float)(1.0 / 447.9995) : 0.f, bad};
-}
 
-// The largest magnitude of a warp's values; infinities and NaN left out.
-__device__ __forceinline__ float block_top(const Pair (&x)[4], bool &bad) {
-    float top = 0.f, lo, hi;
+// Largest magnitude of eight values and `top`; NaN if there is one.
+__device__ __forceinline__ float largest(const Pair (&x)[4], float top) {
+    float lo, hi;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         x[i].get(lo, hi);
         asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(lo), "f"(hi));
     }
-    uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
-    bad = bits >= 0x7f800000u;
-    if (bad) {
-        bits = 0u;
+    return top;
+}
+// The same over what is finite.
+__device__ __forceinline__ float largest_finite(const Pair (&x)[4], float top) {
+    float lo, hi;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[i].get(lo, hi);
-            if (isfinite(lo)) bits = max(bits, __float_as_uint(fabsf(lo)));
-            if (isfinite(hi)) bits = max(bits, __float_as_uint(fabsf(hi)));
-        }
-        bits = __reduce_max_sync(0xffffffffu, bits);
+    for (int i = 0; i < 4; ++i) {
+        x[i].get(lo, hi);
+        if (isfinite(lo)) top = fmaxf(top, fabsf(lo));
+        if (isfinite(hi)) top = fmaxf(top, fabsf(hi));
     }
-    return __uint_as_float(bits);
+    return top;
+}
+
+// A block's tops, the exact root of the second one's, factors and scales, from its lanes' largest magnitudes m and v.  WIDTH lanes
+// hold a block: half of them work out the first moments', half the second's.
+struct Tops {
+    float v, root, m_inverse, v_inverse, scale;          // scale: of the first moments in the block's lower lanes, of the roots in the upper ones
+    bool bad;                                            // an infinity or a NaN in a block of the warp
+};
+template <uint32_t WIDTH, typename F>
+__device__ __forceinline__ Tops block_tops(float m, float v, F finite) {
+    const bool second = threadIdx.x & (WIDTH / 2u);
+    auto reduce = [&](float a, float b) {
+        float x = second ? b : a, y = __shfl_xor_sync(0xffffffffu, second ? a : b, WIDTH / 2u);
+#pragma unroll
+        for (uint32_t d = WIDTH / 4u;; d /= 2u) {
+            asm("max.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(y));
+            if (d == 0u) return x;
+            y = __shfl_xor_sync(0xffffffffu, x, d);
+        }
+    };
+    Tops t;
+    float top = reduce(m, v);
+    t.bad = __any_sync(0xffffffffu, !(top < __uint_as_float(0x7f800000u)));
+    if (t.bad) {
+        finite(m, v);
+        top = reduce(m, v);
+    }
+    const float root = __fsqrt_rn(top), x = second ? root : top, safe = fmaxf(x, 0x1p-110f);
+    const float inverse = x > 0.f ? __fmul_rn(__frcp_rn(safe), kTop) : 0.f;
+    t.scale = x > 0.f ? safe * (float)(1.0 / 447.9995) : 0.f;
+    t.v = __shfl_sync(0xffffffffu, top, WIDTH / 2u, WIDTH);
+    t.root = __shfl_sync(0xffffffffu, root, WIDTH / 2u, WIDTH);
+    t.m_inverse = __shfl_sync(0xffffffffu, inverse, 0, WIDTH);
+    t.v_inverse = __shfl_sync(0xffffffffu, inverse, WIDTH / 2u, WIDTH);
+    return t;
 }
 
 // Codes.  Times 2^-120 a value's exponent and digits, small ones too, are the upper bits of the float's, and 20 random bits are
@@ -170,9 +196,9 @@ __device__ __forceinline__ uint2 upper_bytes(const uint32_t (&x)[8]) {
 __device__ __forceinline__ bool has_zero_byte(uint32_t w) { return ((w - 0x01010101u) & ~w & 0x80808080u) != 0u; }
 constexpr uint32_t kNanCode = 0x7f000000u;
 
-__device__ __forceinline__ uint2 encode_first(const Pair (&m)[4], const BlockScale &s, const Words &words) {
+__device__ __forceinline__ uint2 encode_first(const Pair (&m)[4], const Tops &s, const Words &words) {
     uint32_t code[8];
-    const Pair inverse(s.inverse), shift(0x1p-120f);
+    const Pair inverse(s.m_inverse), shift(0x1p-120f);
 #pragma unroll
     for (uint32_t i = 0; i < 4u; ++i) {
         float y[2];
@@ -193,17 +219,17 @@ __device__ __forceinline__ uint2 encode_first(const Pair (&m)[4], const BlockSca
     }
     return upper_bytes(code);
 }
-// Of the roots r, which stay above zero once they are.  `top` is the exact root of the block's largest finite v: the elements that
-// have it get the code that the exact root has.
-__device__ __forceinline__ uint2 encode_second(const Pair (&v)[4], const Pair (&r)[4], float v_top, float top, const BlockScale &s, const Words &words) {
+// Of the approximate roots r, which stay above zero once they are; the elements that have the block's largest finite v get the code
+// that its exact root has.
+__device__ __forceinline__ uint2 encode_second(const Pair (&v)[4], const Pair (&r)[4], const Tops &s, const Words &words) {
     uint32_t code[8];
-    const Pair inverse(s.inverse), shift(0x1p-120f);
+    const Pair inverse(s.v_inverse), shift(0x1p-120f);
 #pragma unroll
     for (uint32_t i = 0; i < 4u; ++i) {
         float x[2], z[2], y[2];
         v[i].get(x[0], x[1]);
         r[i].get(z[0], z[1]);
-        (Pair(x[0] == v_top ? top : z[0], x[1] == v_top ? top : z[1]) * inverse * shift).get(y[0], y[1]);
+        (Pair(x[0] == s.v ? s.root : z[0], x[1] == s.v ? s.root : z[1]) * inverse * shift).get(y[0], y[1]);
 #pragma unroll
         for (uint32_t k = 0; k < 2u; ++k) code[2 * i + k] = (__float_as_uint(y[k]) + (words.word(8u + 2u * i + k) >> 12)) * 16u;
     }
@@ -228,7 +254,7 @@ __device__ __forceinline__ uint2 encode_second(const Pair (&v)[4], const Pair (&
     return out;
 }
 
-// A lane's eight elements of a block.
+// A lane's eight elements.
 template <int BITS>
 struct Lane {
     Pair w[4], g[4], m[4], v[4], r[4];         // before update(), 8 bits: v holds the roots
@@ -246,18 +272,6 @@ struct Lane {
             r[i] = root_approx(v[i]);
             w[i] = fma2(w[i], keep, m[i] * step * reciprocal_approx(fma2(r[i], root, eps)));
         }
-    }
-    // The new moments' codes and scales.
-    __device__ __forceinline__ void encode(const Words &words, uint2 &m_codes, uint2 &v_codes, float &m_scale, float &v_scale) const {
-        bool bad;
-        const float m_top = block_top(m, bad);
-        const BlockScale first = block_scale(m_top, bad);
-        const float v_top = block_top(v, bad), root_top = __fsqrt_rn(v_top);
-        const BlockScale second = block_scale(root_top, bad);
-        m_codes = encode_first(m, first, words);
-        v_codes = encode_second(v, r, v_top, root_top, second, words);
-        m_scale = first.scale;
-        v_scale = second.scale;
     }
     // The weights as elements of type T.
     template <typename T>
@@ -285,15 +299,18 @@ __device__ __forceinline__ void load8(const float *p, Pair (&x)[4]) {
 __device__ __forceinline__ void store8(float *p, const Pair (&x)[4]) {
     asm volatile("st.global.v4.b64 [%0], {%1, %2, %3, %4};" ::"l"(p), "l"(x[0].bits), "l"(x[1].bits), "l"(x[2].bits), "l"(x[3].bits) : "memory");
 }
-// A warp's 256 consecutive elements.  WALIGN: 16 or 8 where the elements start at such a boundary.
+// Vectors of consecutive lanes, `width` lanes to a run of elements.  WALIGN: 16 or 8 where they start at such a boundary.  `count` is 8, or 0 to
+// store nothing.
 template <typename T, int WALIGN>
-__device__ __forceinline__ void store_warp(T *p, const elem::Packed<T, 8> &own) {
+__device__ __forceinline__ void store_lanes(T *p, const elem::Packed<T, 8> &own, uint32_t count, uint32_t width) {
     constexpr int kStep = WALIGN == 8 ? 2 : 4;
     if (WALIGN > 0 || elem::misalignment(p) == 0u) {
+        if (count) {
 #pragma unroll
-        for (int i = 0; i < elem::Packed<T, 8>::kWords; i += kStep) elem::store_aligned<kStep>(reinterpret_cast<uint32_t *>(p) + i, own.w + i);
+            for (int i = 0; i < elem::Packed<T, 8>::kWords; i += kStep) elem::store_aligned<kStep>(reinterpret_cast<uint32_t *>(p) + i, own.w + i);
+        }
     } else {
-        rows::store_pieces<T>(p, own, 8u, 32u);
+        rows::store_pieces<T>(p, own, count, width);
     }
 }
 
@@ -337,45 +354,75 @@ struct Raw {
     }
 };
 
-// `count` whole blocks from state element s on, of the tensor whose weights and gradients are at w and g.  8 bits: the next block is
-// on its way while one is worked on.
-template <typename Tw, typename Tg, int BITS, bool MASTER, int WALIGN, int GALIGN>
-__device__ __forceinline__ void whole_blocks(const AdamwArgs &a, const Coefficients &c, uint64_t s, uint32_t count, Tw *w, const Tg *g) {
+// `count` whole blocks from state element s on, of the tensor whose weights and gradients are at w and g: a block by the warp.
+template <typename Tw, typename Tg, bool MASTER, int WALIGN, int GALIGN>
+__device__ __forceinline__ void whole_blocks32(const AdamwArgs &a, const Coefficients &c, uint64_t s, uint32_t count, Tw *w, const Tg *g) {
     const uint32_t lane = threadIdx.x & 31u;
     uint64_t at = s + lane * 8u;
     w += lane * 8u;
     g += lane * 8u;
-    Raw<Tw, Tg, BITS, MASTER, WALIGN, GALIGN> raw, next;
-    if (BITS == 8) next.load(a, at, w, g);
 #pragma unroll 1
     for (uint32_t b = 0; b < count; ++b, at += kBlock, w += kBlock, g += kBlock) {
-        if (BITS == 8) {
-            raw = next;
-            if (b + 1u < count) next.load(a, at + kBlock, w + kBlock, g + kBlock);
-        } else {
-            raw.load(a, at, w, g);
-        }
-        Lane<BITS> e;
+        Raw<Tw, Tg, 32, MASTER, WALIGN, GALIGN> raw;
+        Lane<32> e;
+        raw.load(a, at, w, g);
         raw.get(w, g, e);
         e.update(c);
-        const Words words((uint32_t)(at / 8u), c);
-        store_warp<Tw, WALIGN>(w, e.template rounded<Tw>(a.stochastic, words));
+        store_lanes<Tw, WALIGN>(w, e.template rounded<Tw>(a.stochastic, Words((uint32_t)(at / 8u), c)), 8u, 32u);
         if constexpr (MASTER) store8(a.d_master + at, e.w);
-        if constexpr (BITS == 32) {
-            store8(static_cast<float *>(a.d_m) + at, e.m);
-            store8(static_cast<float *>(a.d_v) + at, e.v);
-        } else {
-            uint2 m_codes, v_codes;
-            float m_scale, v_scale;
-            e.encode(words, m_codes, v_codes, m_scale, v_scale);
-            *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(a.d_m) + at) = m_codes;
-            *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(a.d_v) + at) = v_codes;
-            if (lane == 0u) {
-                a.d_m_scales[at / kBlock] = m_scale;
-                a.d_v_scales[at / kBlock] = v_scale;
+        store8(static_cast<float *>(a.d_m) + at, e.m);
+        store8(static_cast<float *>(a.d_v) + at, e.v);
+    }
+}
+// With 8-bit moments half a warp takes a block, sixteen elements a lane in two vectors half a block apart: what a block costs
+// beside its elements (tops, scales, addresses) is shared by twice as many.
+template <typename Tw, typename Tg, bool MASTER, int WALIGN, int GALIGN>
+__device__ __forceinline__ void whole_blocks8(const AdamwArgs &a, const Coefficients &c, uint64_t s, uint32_t count, Tw *w, const Tg *g) {
+    constexpr uint32_t kHalf = kBlock / 2u;
+    const uint32_t lane = threadIdx.x & 15u, half = threadIdx.x >> 4 & 1u;
+#pragma unroll 1
+    for (uint32_t b = 0; b < count; b += 2u) {
+        const bool live = b + half < count;              // an odd block out: the other half does it too, and stores nothing
+        const uint32_t first = (b + (live ? half : 0u)) * kBlock + lane * 8u;
+        const uint64_t at = s + first;
+        Tw *const pw = w + first;
+        const Tg *const pg = g + first;
+        Raw<Tw, Tg, 8, MASTER, WALIGN, GALIGN> raw[2];
+#pragma unroll
+        for (uint32_t j = 0; j < 2u; ++j) raw[j].load(a, at + j * kHalf, pw + j * kHalf, pg + j * kHalf);
+        Lane<8> e[2];
+        float m_top = 0.f, v_top = 0.f;
+#pragma unroll
+        for (uint32_t j = 0; j < 2u; ++j) {
+            raw[j].get(pw + j * kHalf, pg + j * kHalf, e[j]);
+            e[j].update(c);
+            m_top = largest(e[j].m, m_top);
+            v_top = largest(e[j].v, v_top);
+            store_lanes<Tw, WALIGN>(pw + j * kHalf, e[j].template rounded<Tw>(a.stochastic, Words((uint32_t)(at / 8u) + j * (kHalf / 8u), c)),
+                                    live ? 8u : 0u, 16u);
+            if constexpr (MASTER)
+                if (live) store8(a.d_master + at + j * kHalf, e[j].w);
+        }
+        const Tops tops = block_tops<16>(m_top, v_top, [&](float &m, float &v) {
+            m = largest_finite(e[1].m, largest_finite(e[0].m, 0.f));
+            v = largest_finite(e[1].v, largest_finite(e[0].v, 0.f));
+        });
+#pragma unroll
+        for (uint32_t j = 0; j < 2u; ++j) {
+            const Words words((uint32_t)(at / 8u) + j * (kHalf / 8u), c);
+            const uint2 m = encode_first(e[j].m, tops, words), v = encode_second(e[j].v, e[j].r, tops, words);
+            if (live) {
+                *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(a.d_m) + at + j * kHalf) = m;
+                *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(a.d_v) + at + j * kHalf) = v;
             }
         }
+        if (live && (lane & 7u) == 0u) (lane ? a.d_v_scales : a.d_m_scales)[at / kBlock] = tops.scale;
     }
+}
+template <typename Tw, typename Tg, int BITS, bool MASTER, int WALIGN, int GALIGN>
+__device__ __forceinline__ void whole_blocks(const AdamwArgs &a, const Coefficients &c, uint64_t s, uint32_t count, Tw *w, const Tg *g) {
+    if constexpr (BITS == 32) whole_blocks32<Tw, Tg, MASTER, WALIGN, GALIGN>(a, c, s, count, w, g);
+    else whole_blocks8<Tw, Tg, MASTER, WALIGN, GALIGN>(a, c, s, count, w, g);
 }
 
 // A tensor's last block: one element at a time; what lies behind the tensor stays as it is.
@@ -438,12 +485,13 @@ __device__ __noinline__ void part_block(const AdamwArgs &a, const Coefficients &
             e.m[i] = Pair(x[2][2 * i], x[2][2 * i + 1]);
             e.v[i] = Pair(x[3][2 * i], x[3][2 * i + 1]);
         }
-        float m_scale, v_scale;
-        e.encode(words, m_codes, v_codes, m_scale, v_scale);
-        if (lane == 0u) {
-            a.d_m_scales[s / kBlock] = m_scale;
-            a.d_v_scales[s / kBlock] = v_scale;
-        }
+        const Tops tops = block_tops<32>(largest(e.m, 0.f), largest(e.v, 0.f), [&](float &m, float &v) {
+            m = largest_finite(e.m, 0.f);
+            v = largest_finite(e.v, 0.f);
+        });
+        m_codes = encode_first(e.m, tops, words);
+        v_codes = encode_second(e.v, e.r, tops, words);
+        if ((lane & 15u) == 0u) (lane ? a.d_v_scales : a.d_m_scales)[s / kBlock] = tops.scale;
     }
     const elem::Packed<Tw, 8> out = e.template rounded<Tw>(a.stochastic, words);
 #pragma unroll
