@@ -314,42 +314,27 @@ __device__ __forceinline__ void store_lanes(T *p, const elem::Packed<T, 8> &own,
     }
 }
 
-// A lane's share of a block as it lies in memory.
-template <typename Tw, typename Tg, int BITS, bool MASTER, int WALIGN, int GALIGN>
+// A lane's share of a block with 32-bit moments as it lies in memory.
+template <typename Tw, typename Tg, bool MASTER, int WALIGN, int GALIGN>
 struct Raw {
     elem::Vector<Tg, 8, GALIGN> g;
     elem::Vector<Tw, 8, MASTER ? 16 : WALIGN> w;         // not with MASTER
-    Pair master[4], m[4], v[4];                          // with MASTER; 32 bits
-    uint2 m8, v8;                                        // 8 bits
-    float m_scale, v_scale;
+    Pair master[4], m[4], v[4];
     __device__ __forceinline__ void load(const AdamwArgs &a, uint64_t at, const Tw *pw, const Tg *pg) {
         g.load(pg, elem::misalignment(pg));
         if constexpr (MASTER) load8(a.d_master + at, master);
         else w.load(pw, elem::misalignment(pw));
-        if constexpr (BITS == 32) {
-            load8(static_cast<const float *>(a.d_m) + at, m);
-            load8(static_cast<const float *>(a.d_v) + at, v);
-        } else {
-            m8 = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(a.d_m) + at);
-            v8 = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(a.d_v) + at);
-            m_scale = a.d_m_scales[at / kBlock];
-            v_scale = a.d_v_scales[at / kBlock];
-        }
+        load8(static_cast<const float *>(a.d_m) + at, m);
+        load8(static_cast<const float *>(a.d_v) + at, v);
     }
-    __device__ __forceinline__ void get(const Tw *pw, const Tg *pg, Lane<BITS> &e) const {
+    __device__ __forceinline__ void get(const Tw *pw, const Tg *pg, Lane<32> &e) const {
         unpack8(g.get(elem::misalignment(pg)), e.g);
         if constexpr (!MASTER) unpack8(w.get(elem::misalignment(pw)), e.w);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if constexpr (MASTER) e.w[i] = master[i];
-            if constexpr (BITS == 32) {
-                e.m[i] = m[i];
-                e.v[i] = v[i];
-            }
-        }
-        if constexpr (BITS == 8) {
-            decode8(m8, m_scale, e.m);
-            decode8(v8, v_scale, e.v);
+            e.m[i] = m[i];
+            e.v[i] = v[i];
         }
     }
 };
@@ -363,7 +348,7 @@ __device__ __forceinline__ void whole_blocks32(const AdamwArgs &a, const Coeffic
     g += lane * 8u;
 #pragma unroll 1
     for (uint32_t b = 0; b < count; ++b, at += kBlock, w += kBlock, g += kBlock) {
-        Raw<Tw, Tg, 32, MASTER, WALIGN, GALIGN> raw;
+        Raw<Tw, Tg, MASTER, WALIGN, GALIGN> raw;
         Lane<32> e;
         raw.load(a, at, w, g);
         raw.get(w, g, e);
@@ -375,31 +360,84 @@ __device__ __forceinline__ void whole_blocks32(const AdamwArgs &a, const Coeffic
     }
 }
 // With 8-bit moments half a warp takes a block, sixteen elements a lane in two vectors half a block apart: what a block costs
-// beside its elements (tops, scales, addresses) is shared by twice as many.
+// beside its elements (tops, scales, addresses) is shared by twice as many.  Two blocks of a warp come through a ring in shared
+// memory that the warp fills with asynchronous copies, up to three steps ahead.
+template <typename Tw, typename Tg, bool MASTER>
+struct Ring {
+    // 16-byte pieces of half a block, at any alignment: weights, gradients, the 32-bit weights, the two moments' codes
+    static constexpr uint32_t kW = MASTER ? 0u : 8u * sizeof(Tw) + 1u, kG = 8u * sizeof(Tg) + 1u, kMaster = MASTER ? 32u : 0u;
+    static constexpr uint32_t kAtG = kW, kAtMaster = kAtG + kG, kAtM = kAtMaster + kMaster, kAtV = kAtM + 8u, kHalf = kAtV + 8u;
+    static constexpr uint32_t kStep = 4u * kHalf + 1u;   // two halves of two blocks, and their four scales
+    static constexpr int kStages = 3u * 16u * kStep * kWarps <= (108u << 10) ? 3 : 2;
+    static constexpr uint32_t kBytes = 16u * kStep * kStages * kWarps;
+    static_assert(2u * kBytes <= 220u << 10, "two CTAs per SM");
+};
+template <int BYTES>
+__device__ __forceinline__ void copy_async_small(void *shared, const void *global) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((uint32_t)__cvta_generic_to_shared(shared)), "l"(global), "n"(BYTES) : "memory");
+}
+
 template <typename Tw, typename Tg, bool MASTER, int WALIGN, int GALIGN>
-__device__ __forceinline__ void whole_blocks8(const AdamwArgs &a, const Coefficients &c, uint64_t s, uint32_t count, Tw *w, const Tg *g) {
+__device__ __forceinline__ void whole_blocks8(const AdamwArgs &a, const Coefficients &c, uint4 *ring, uint64_t s, uint32_t count, Tw *w, const Tg *g) {
+    using R = Ring<Tw, Tg, MASTER>;
+    using W = rows::Segment<Tw, 16, WALIGN == 16 ? rows::kExactRows : rows::kAnyRows>;
+    using G = rows::Segment<Tg, 16, GALIGN == 16 ? rows::kExactRows : rows::kAnyRows>;
+    using M = rows::Segment<float, 16, rows::kExactRows>;
     constexpr uint32_t kHalf = kBlock / 2u;
+    constexpr int kStages = R::kStages;
     const uint32_t lane = threadIdx.x & 15u, half = threadIdx.x >> 4 & 1u;
-#pragma unroll 1
-    for (uint32_t b = 0; b < count; b += 2u) {
-        const bool live = b + half < count;              // an odd block out: the other half does it too, and stores nothing
-        const uint32_t first = (b + (live ? half : 0u)) * kBlock + lane * 8u;
+    // this half warp's block in step i; where there is none the other half's, of which it stores nothing
+    auto block_of = [&](uint32_t i) { return 2u * i + half < count ? 2u * i + half : 2u * i; };
+    auto fetch = [&](uint32_t i, uint4 *to) {
+        const uint32_t first = block_of(i) * kBlock;
         const uint64_t at = s + first;
-        Tw *const pw = w + first;
-        const Tg *const pg = g + first;
-        Raw<Tw, Tg, 8, MASTER, WALIGN, GALIGN> raw[2];
 #pragma unroll
-        for (uint32_t j = 0; j < 2u; ++j) raw[j].load(a, at + j * kHalf, pw + j * kHalf, pg + j * kHalf);
+        for (uint32_t j = 0; j < 2u; ++j) {
+            uint4 *const here = to + (half * 2u + j) * R::kHalf;
+            const uint32_t e = first + j * kHalf;
+            if constexpr (MASTER) M::fetch(here + R::kAtMaster, a.d_master + s + e, lane, lane, kHalf);
+            else W::fetch(here, w + e, lane, lane, kHalf);
+            G::fetch(here + R::kAtG, g + e, lane, lane, kHalf);
+            copy_async_small<8>(reinterpret_cast<uint2 *>(here + R::kAtM) + lane, static_cast<const uint8_t *>(a.d_m) + s + e + lane * 8u);
+            copy_async_small<8>(reinterpret_cast<uint2 *>(here + R::kAtV) + lane, static_cast<const uint8_t *>(a.d_v) + s + e + lane * 8u);
+        }
+        if ((lane & 7u) == 0u)
+            copy_async_small<4>(reinterpret_cast<float *>(to + 4u * R::kHalf) + half * 2u + lane / 8u, (lane ? a.d_v_scales : a.d_m_scales) + at / kBlock);
+    };
+    const uint32_t steps = (count + 1u) / 2u;
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) {
+        if ((uint32_t)i < steps) fetch(i, ring + i * R::kStep);
+        rows::commit_copies();
+    }
+    uint32_t now = 0, last = (kStages - 1) * R::kStep;
+#pragma unroll 1
+    for (uint32_t i = 0; i < steps; ++i) {
+        if (i + kStages - 1u < steps) fetch(i + kStages - 1u, ring + last);
+        rows::commit_copies();
+        rows::wait_copies<kStages - 1>();
+        __syncwarp();
+        const uint4 *const from = ring + now;
+        const bool live = 2u * i + half < count;
+        const uint32_t first = block_of(i) * kBlock + lane * 8u;
+        const uint64_t at = s + first;
+        const float2 scales = *(reinterpret_cast<const float2 *>(from + 4u * R::kHalf) + half);
         Lane<8> e[2];
         float m_top = 0.f, v_top = 0.f;
 #pragma unroll
         for (uint32_t j = 0; j < 2u; ++j) {
-            raw[j].get(pw + j * kHalf, pg + j * kHalf, e[j]);
+            const uint4 *const here = from + (half * 2u + j) * R::kHalf;
+            Tw *const pw = w + first + j * kHalf;
+            const Tg *const pg = g + first + j * kHalf;
+            if constexpr (MASTER) unpack8(M::get(here + R::kAtMaster, 0u, lane, lane, kHalf, true), e[j].w);
+            else unpack8(W::get(here, WALIGN == 8 ? 8u : elem::misalignment(pw), lane, lane, kHalf, true), e[j].w);
+            unpack8(G::get(here + R::kAtG, elem::misalignment(pg), lane, lane, kHalf, true), e[j].g);
+            decode8(reinterpret_cast<const uint2 *>(here + R::kAtM)[lane], scales.x, e[j].m);
+            decode8(reinterpret_cast<const uint2 *>(here + R::kAtV)[lane], scales.y, e[j].v);
             e[j].update(c);
             m_top = largest(e[j].m, m_top);
             v_top = largest(e[j].v, v_top);
-            store_lanes<Tw, WALIGN>(pw + j * kHalf, e[j].template rounded<Tw>(a.stochastic, Words((uint32_t)(at / 8u) + j * (kHalf / 8u), c)),
-                                    live ? 8u : 0u, 16u);
+            store_lanes<Tw, WALIGN>(pw, e[j].template rounded<Tw>(a.stochastic, Words((uint32_t)(at / 8u) + j * (kHalf / 8u), c)), live ? 8u : 0u, 16u);
             if constexpr (MASTER)
                 if (live) store8(a.d_master + at + j * kHalf, e[j].w);
         }
@@ -417,12 +455,14 @@ __device__ __forceinline__ void whole_blocks8(const AdamwArgs &a, const Coeffici
             }
         }
         if (live && (lane & 7u) == 0u) (lane ? a.d_v_scales : a.d_m_scales)[at / kBlock] = tops.scale;
+        last = now;
+        now = now + R::kStep == kStages * R::kStep ? 0u : now + R::kStep;
     }
 }
 template <typename Tw, typename Tg, int BITS, bool MASTER, int WALIGN, int GALIGN>
-__device__ __forceinline__ void whole_blocks(const AdamwArgs &a, const Coefficients &c, uint64_t s, uint32_t count, Tw *w, const Tg *g) {
+__device__ __forceinline__ void whole_blocks(const AdamwArgs &a, const Coefficients &c, uint4 *ring, uint64_t s, uint32_t count, Tw *w, const Tg *g) {
     if constexpr (BITS == 32) whole_blocks32<Tw, Tg, MASTER, WALIGN, GALIGN>(a, c, s, count, w, g);
-    else whole_blocks8<Tw, Tg, MASTER, WALIGN, GALIGN>(a, c, s, count, w, g);
+    else whole_blocks8<Tw, Tg, MASTER, WALIGN, GALIGN>(a, c, ring, s, count, w, g);
 }
 
 // A tensor's last block: one element at a time; what lies behind the tensor stays as it is.
@@ -549,6 +589,9 @@ template <typename Tw, typename Tg, int BITS, bool MASTER>
 __global__ void __launch_bounds__(kWarps * 32, 2)
 adamw_kernel(const __grid_constant__ AdamwArgs a, uint32_t run, uint32_t *arrived, uint32_t *status) {
     __shared__ Coefficients shared;
+    extern __shared__ uint4 rings[];                     // 8 bits only
+    uint4 *ring = nullptr;
+    if constexpr (BITS == 8) ring = rings + (threadIdx.x >> 5) * (Ring<Tw, Tg, MASTER>::kStep * Ring<Tw, Tg, MASTER>::kStages);
     if (threadIdx.x == 0) make_coefficients(a, shared);
     __syncthreads();
     for (uint64_t k = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; k < a.set.n; k += (uint64_t)gridDim.x * blockDim.x)
@@ -585,9 +628,9 @@ adamw_kernel(const __grid_constant__ AdamwArgs a, uint32_t run, uint32_t *arrive
                 continue;
             }
             const uint32_t count = (uint32_t)(whole < last - b ? whole : last - b), w_off = elem::misalignment(wb), g_off = elem::misalignment(gb);
-            if (g_off == 0u && w_off == 0u) whole_blocks<Tw, Tg, BITS, MASTER, 16, 16>(a, shared, s, count, wb, gb);
-            else if (g_off == 0u && w_off == 8u) whole_blocks<Tw, Tg, BITS, MASTER, 8, 16>(a, shared, s, count, wb, gb);
-            else whole_blocks<Tw, Tg, BITS, MASTER, elem::kAny, elem::kAny>(a, shared, s, count, wb, gb);
+            if (g_off == 0u && w_off == 0u) whole_blocks<Tw, Tg, BITS, MASTER, 16, 16>(a, shared, ring, s, count, wb, gb);
+            else if (g_off == 0u && w_off == 8u) whole_blocks<Tw, Tg, BITS, MASTER, 8, 16>(a, shared, ring, s, count, wb, gb);
+            else whole_blocks<Tw, Tg, BITS, MASTER, elem::kAny, elem::kAny>(a, shared, ring, s, count, wb, gb);
             b += count;
         }
     }
@@ -603,8 +646,17 @@ cudaError_t launch_instance(const AdamwArgs &a, uint32_t *arrived, uint32_t *d_s
     const uint64_t blocks = a.size / kBlock, ctas = (blocks + kWarps - 1) / kWarps, most = (uint64_t)sm_count * 2u;
     const uint32_t grid = (uint32_t)(ctas < most ? (ctas ? ctas : 1u) : most);
     const uint64_t share = blocks / ((uint64_t)grid * kWarps);
-    const uint32_t run = (uint32_t)(share < 1u ? 1u : share < 16u ? share : 16u);
-    adamw_kernel<Tw, Tg, BITS, MASTER><<<grid, kWarps * 32, 0, stream>>>(a, run, arrived, d_status);
+    constexpr uint64_t kRun = BITS == 8 ? 32 : 16;
+    const uint32_t run = (uint32_t)(share < 1u ? 1u : share < kRun ? share : kRun);
+    auto kernel = adamw_kernel<Tw, Tg, BITS, MASTER>;
+    uint32_t bytes = 0;
+    if constexpr (BITS == 8) {
+        bytes = Ring<Tw, Tg, MASTER>::kBytes;
+        static bool done[kMaxDevices] = {};
+        cudaError_t e = ensure_dynamic_smem(kernel, bytes, done);
+        if (e != cudaSuccess) return e;
+    }
+    kernel<<<grid, kWarps * 32, bytes, stream>>>(a, run, arrived, d_status);
     return cudaGetLastError();
 }
 
