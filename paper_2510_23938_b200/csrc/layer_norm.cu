@@ -172,7 +172,7 @@ layer_norm_kernel(const __grid_constant__ LayerNormArgs a) {
 
 // Rows too wide for that: one CTA per row, which reads it three times (from the L2 cache the second and third time).
 constexpr uint32_t kWideThreads = 1024;
-template <typename Tx, typename Ty>
+template <typename Tx, typename Ty, bool ALIGNED>
 __global__ void __launch_bounds__(kWideThreads)
 layer_norm_wide_kernel(LayerNormArgs a) {
     __shared__ float slots[2][kWideThreads / 32];
@@ -186,7 +186,7 @@ layer_norm_wide_kernel(LayerNormArgs a) {
         auto each = [&](auto f) {
             for (uint32_t base = 0; base < vectors; base += kWideThreads) {      // whole warps
                 const uint32_t v = base + threadIdx.x;
-                RowVector<Tx, false> raw;
+                RowVector<Tx, ALIGNED> raw;
                 Pair e[4];
                 raw.load(in, v, dim);
                 elem::unpack8(raw.get(off, v, dim), e);
@@ -226,7 +226,7 @@ layer_norm_wide_kernel(LayerNormArgs a) {
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) p[i] = Pair(e[2 * i], e[2 * i + 1]);
-            store_row_vector<Ty, kAnyRows, kWideThreads>(out, v, dim, true, p);
+            store_row_vector<Ty, ALIGNED ? kAlignedRows : kAnyRows, kWideThreads>(out, v, dim, true, p);
         });
         if (threadIdx.x == 0) {
             if (a.d_mean) a.d_mean[row] = mean;
@@ -279,7 +279,9 @@ cudaError_t launch_layer_norm(const LayerNormArgs &a, int sm_count, cudaStream_t
         using Ty = typename decltype(out)::type;
         if (a.dim > 8u * kThreads * 4u) {
             const uint64_t most = (uint64_t)sm_count * 2u;
-            layer_norm_wide_kernel<Tx, Ty><<<(uint32_t)(a.n < most ? a.n : most), kWideThreads, 0, stream>>>(a);
+            const bool aligned = rows_aligned<Tx>(a.d_x, a.x_stride, a.n, a.dim) && rows_aligned<Ty>(a.d_y, a.y_stride, a.n, a.dim);
+            auto kernel = aligned ? layer_norm_wide_kernel<Tx, Ty, true> : layer_norm_wide_kernel<Tx, Ty, false>;
+            kernel<<<(uint32_t)(a.n < most ? a.n : most), kWideThreads, 0, stream>>>(a);
             return cudaGetLastError();
         }
         return launch_width<Tx, Ty>(a, sm_count, stream);

@@ -205,7 +205,7 @@ norm_grad_kernel(const __grid_constant__ LayerNormGradArgs a, float *partial) {
 
 // Rows too wide for that.  First the two sums of every row, a CTA each; then tiles of 256 columns by runs of rows, a warp
 // per row with every lane's eight columns in registers.  The second pass reads x and dy again.
-template <typename Tx, typename Ty>
+template <typename Tx, typename Ty, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads)
 norm_grad_wide_rows_kernel(LayerNormGradArgs a, float2 *row_sums) {
     __shared__ float slots[2 * 16];
@@ -216,8 +216,8 @@ norm_grad_wide_rows_kernel(LayerNormGradArgs a, float2 *row_sums) {
         const float rstd = a.d_rstd[row], mean = a.d_mean ? a.d_mean[row] : 0.f;
         float sums[2] = {0.f, 0.f};
         for (uint32_t v = threadIdx.x; v < vectors; v += kThreads) {
-            RowVector<Tx, false> rx;
-            RowVector<Ty, false> ry;
+            RowVector<Tx, ALIGNED> rx;
+            RowVector<Ty, ALIGNED> ry;
             Pair pairs[4];
             float h[8], p[8];
             rx.load(x, v, dim);
@@ -242,7 +242,7 @@ norm_grad_wide_rows_kernel(LayerNormGradArgs a, float2 *row_sums) {
 }
 
 constexpr uint32_t kWideWarps = 8;
-template <typename Tx, typename Ty>
+template <typename Tx, typename Ty, bool ALIGNED>
 __global__ void __launch_bounds__(kWideWarps * 32)
 norm_grad_wide_kernel(LayerNormGradArgs a, const float2 *row_sums, float *partial, uint32_t parts) {
     __shared__ float all[16][kWideWarps][32];
@@ -258,8 +258,8 @@ norm_grad_wide_kernel(LayerNormGradArgs a, const float2 *row_sums, float *partia
     for (uint64_t row = begin + warp; row < end; row += kWideWarps) {
         const Tx *x = static_cast<const Tx *>(a.d_x) + row * a.x_stride;
         const Ty *dy = static_cast<const Ty *>(a.d_dy) + row * a.dy_stride;
-        RowVector<Tx, false> rx;
-        RowVector<Ty, false> ry;
+        RowVector<Tx, ALIGNED> rx;
+        RowVector<Ty, ALIGNED> ry;
         rx.load(x, v, dim);
         ry.load(dy, v, dim);
         const float rstd = a.d_rstd[row], mean = a.d_mean ? a.d_mean[row] : 0.f;
@@ -280,7 +280,7 @@ norm_grad_wide_kernel(LayerNormGradArgs a, const float2 *row_sums, float *partia
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) pairs[i] = Pair(h[2 * i], h[2 * i + 1]);
-        store_row_vector<Tx, kAnyRows, 32>(static_cast<Tx *>(a.d_dx) + row * a.dx_stride, v, dim, true, pairs);
+        store_row_vector<Tx, ALIGNED ? kAlignedRows : kAnyRows, 32>(static_cast<Tx *>(a.d_dx) + row * a.dx_stride, v, dim, true, pairs);
     }
     if (!a.d_dw && !a.d_db) return;
 #pragma unroll
@@ -352,10 +352,14 @@ uint64_t parts_for(uint64_t n, uint64_t dim) {
     return parts < most ? parts : most;                  // 16 CTAs for each of a B200's SMs, all tiles together
 }
 
+template <typename Tx, typename Ty>
+bool all_aligned(const LayerNormGradArgs &a) {
+    return rows_aligned<Tx>(a.d_x, a.x_stride, a.n, a.dim) && rows_aligned<Ty>(a.d_dy, a.dy_stride, a.n, a.dim) &&
+           rows_aligned<Tx>(a.d_dx, a.dx_stride, a.n, a.dim);
+}
 template <typename Tx, typename Ty, uint32_t T, int NV>
 cudaError_t launch_mode(const LayerNormGradArgs &a, float *partial, uint32_t parts, cudaStream_t stream) {
-    if (!rows_aligned<Tx>(a.d_x, a.x_stride, a.n, a.dim) || !rows_aligned<Ty>(a.d_dy, a.dy_stride, a.n, a.dim) ||
-        !rows_aligned<Tx>(a.d_dx, a.dx_stride, a.n, a.dim))
+    if (!all_aligned<Tx, Ty>(a))
         return launch_instance<Tx, Ty, T, NV, kAnyRows>(a, partial, parts, stream);
     return a.dim == 8u * T * NV ? launch_instance<Tx, Ty, T, NV, kExactRows>(a, partial, parts, stream)
                                 : launch_instance<Tx, Ty, T, NV, kAlignedRows>(a, partial, parts, stream);
@@ -374,15 +378,15 @@ cudaError_t launch_width(const LayerNormGradArgs &a, float *partial, uint32_t pa
     }
 }
 
-template <typename Tx, typename Ty>
+template <typename Tx, typename Ty, bool ALIGNED>
 cudaError_t launch_wide(const LayerNormGradArgs &a, float *partial, uint32_t parts, int sm_count, cudaStream_t stream) {
     float2 *row_sums = reinterpret_cast<float2 *>(partial + (uint64_t)parts * 2u * a.dim);
     const uint64_t most = (uint64_t)sm_count * 4u;
-    norm_grad_wide_rows_kernel<Tx, Ty><<<(uint32_t)(a.n < most ? a.n : most), kThreads, 0, stream>>>(a, row_sums);
+    norm_grad_wide_rows_kernel<Tx, Ty, ALIGNED><<<(uint32_t)(a.n < most ? a.n : most), kThreads, 0, stream>>>(a, row_sums);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const uint32_t tiles = (uint32_t)((a.dim + 255u) / 256u);
-    norm_grad_wide_kernel<Tx, Ty><<<tiles * parts, kWideWarps * 32, 0, stream>>>(a, row_sums, partial, parts);
+    norm_grad_wide_kernel<Tx, Ty, ALIGNED><<<tiles * parts, kWideWarps * 32, 0, stream>>>(a, row_sums, partial, parts);
     return cudaGetLastError();
 }
 
@@ -399,7 +403,9 @@ cudaError_t launch_layer_norm_grad(const LayerNormGradArgs &a, float *d_partial,
         cudaError_t e = by_types(a.x_type, a.y_type, [&](auto in, auto out) {
             using Tx = typename decltype(in)::type;
             using Ty = typename decltype(out)::type;
-            if (a.dim > kWidest) return launch_wide<Tx, Ty>(a, d_partial, parts, sm_count, stream);
+            if (a.dim > kWidest)
+                return all_aligned<Tx, Ty>(a) ? launch_wide<Tx, Ty, true>(a, d_partial, parts, sm_count, stream)
+                                              : launch_wide<Tx, Ty, false>(a, d_partial, parts, sm_count, stream);
             return launch_width<Tx, Ty>(a, d_partial, parts, stream);
         });
         if (e != cudaSuccess) return e;

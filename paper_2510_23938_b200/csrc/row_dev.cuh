@@ -47,7 +47,7 @@ struct RowVector {
 
 // Vectors of eight elements by consecutive lanes, `width` lanes to a row, to consecutive places at any element alignment: a lane
 // stores the aligned pieces that begin in its elements, with its neighbour's first bytes behind its own, and what no lane's piece
-// covers (a row's first and last elements, those between two warps) goes one by one.  `count`: how many of the lane's elements
+// covers (a row's first and last elements, those between two warps) goes in smaller ones.  `count`: how many of the lane's elements
 // there are; by whole warps.
 template <typename T>
 __device__ __forceinline__ void store_pieces(T *p, const elem::Packed<T, 8> &own, uint32_t count, uint32_t width) {
@@ -77,15 +77,31 @@ __device__ __forceinline__ void store_pieces(T *p, const elem::Packed<T, 8> &own
 #pragma unroll
     for (int i = 0; i < W; i += 4)
         if (count == 8u && (i + 4 < W || last)) elem::store_aligned<4>(pieces + i, x + i);
-    const uint32_t head = count < 8u ? count : lane == 0u ? skip / (uint32_t)sizeof(T) : 0u;
-    const uint32_t tail = count < 8u || last ? 8u : (uint32_t)(sizeof(T) * 8u - off) / (uint32_t)sizeof(T);
-    if (head == 0u && tail == 8u) return;
-#pragma unroll
-    for (uint32_t i = 0; i < 8u; ++i)
-        if (i < head || i >= tail) {
-            if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t *>(p)[i] = own.w[i];
-            else reinterpret_cast<uint16_t *>(p)[i] = (uint16_t)(own.w[i / 2] >> (16u * (i & 1u)));
+    uint8_t *bytes = reinterpret_cast<uint8_t *>(p);
+    if (count == 8u && lane == 0u && skip) {             // the elements before the first piece: 2, 4 and 8 bytes of them
+        if (sizeof(T) == 2 && (skip & 2u)) *reinterpret_cast<uint16_t *>(bytes) = (uint16_t)own.w[0];
+        if (skip & 4u) *reinterpret_cast<uint32_t *>(bytes + (skip & 2u)) = __funnelshift_r(own.w[0], own.w[1], (skip & 2u) * 8u);
+        if (skip & 8u) {
+            const bool word = skip & 4u;
+            const uint32_t a = word ? own.w[1] : own.w[0], b = word ? own.w[2] : own.w[1], c = word ? own.w[3] : own.w[2];
+            *reinterpret_cast<uint2 *>(bytes + (skip & 6u)) = make_uint2(__funnelshift_r(a, b, (skip & 2u) * 8u), __funnelshift_r(b, c, (skip & 2u) * 8u));
         }
+    }
+    if (count == 8u && !last) {                          // those behind the last whole piece: 8, 4 and 2 bytes
+        bytes += sizeof(T) * 8u - off;
+        if (off & 8u) *reinterpret_cast<uint2 *>(bytes) = make_uint2(x[W - 4], x[W - 3]);
+        const uint32_t c = off & 8u ? x[W - 2] : x[W - 4], d = off & 8u ? x[W - 1] : x[W - 3];
+        if (off & 4u) *reinterpret_cast<uint32_t *>(bytes + (off & 8u)) = c;
+        if (sizeof(T) == 2 && (off & 2u)) *reinterpret_cast<uint16_t *>(bytes + (off & 12u)) = (uint16_t)(off & 4u ? d : c);
+    }
+    if (count < 8u) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; ++i)
+            if (i < count) {
+                if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t *>(p)[i] = own.w[i];
+                else reinterpret_cast<uint16_t *>(p)[i] = (uint16_t)(own.w[i / 2] >> (16u * (i & 1u)));
+            }
+    }
 }
 
 // A lane's vector v of a row; T threads to a row, by whole warps; `live`: the row is there.
