@@ -380,8 +380,8 @@ __device__ __forceinline__ void copy_async_small(void *shared, const void *globa
 template <typename Tw, typename Tg, bool MASTER, int WALIGN, int GALIGN>
 __device__ __forceinline__ void whole_blocks8(const AdamwArgs &a, const Coefficients &c, uint4 *ring, uint64_t s, uint32_t count, Tw *w, const Tg *g) {
     using R = Ring<Tw, Tg, MASTER>;
-    using W = rows::Segment<Tw, 16, WALIGN == 16 ? rows::kExactRows : rows::kAnyRows>;
-    using G = rows::Segment<Tg, 16, GALIGN == 16 ? rows::kExactRows : rows::kAnyRows>;
+    using W = rows::Segment<Tw, 16, (WALIGN > 0) ? rows::kExactRows : rows::kShiftedRows>;
+    using G = rows::Segment<Tg, 16, GALIGN == 16 ? rows::kExactRows : rows::kShiftedRows>;
     using M = rows::Segment<float, 16, rows::kExactRows>;
     constexpr uint32_t kHalf = kBlock / 2u;
     constexpr int kStages = R::kStages;
@@ -395,8 +395,15 @@ __device__ __forceinline__ void whole_blocks8(const AdamwArgs &a, const Coeffici
         for (uint32_t j = 0; j < 2u; ++j) {
             uint4 *const here = to + (half * 2u + j) * R::kHalf;
             const uint32_t e = first + j * kHalf;
-            if constexpr (MASTER) M::fetch(here + R::kAtMaster, a.d_master + s + e, lane, lane, kHalf);
-            else W::fetch(here, w + e, lane, lane, kHalf);
+            if constexpr (MASTER) {
+                M::fetch(here + R::kAtMaster, a.d_master + s + e, lane, lane, kHalf);
+            } else if constexpr (WALIGN == 8) {            // pieces of 8 bytes bring them to 16-byte boundaries
+#pragma unroll
+                for (uint32_t i = 0; i < sizeof(Tw); ++i)
+                    copy_async_small<8>(reinterpret_cast<uint2 *>(here) + i * 16u + lane, reinterpret_cast<const uint8_t *>(w + e) + (i * 16u + lane) * 8u);
+            } else {
+                W::fetch(here, w + e, lane, lane, kHalf);
+            }
             G::fetch(here + R::kAtG, g + e, lane, lane, kHalf);
             copy_async_small<8>(reinterpret_cast<uint2 *>(here + R::kAtM) + lane, static_cast<const uint8_t *>(a.d_m) + s + e + lane * 8u);
             copy_async_small<8>(reinterpret_cast<uint2 *>(here + R::kAtV) + lane, static_cast<const uint8_t *>(a.d_v) + s + e + lane * 8u);
@@ -430,7 +437,7 @@ __device__ __forceinline__ void whole_blocks8(const AdamwArgs &a, const Coeffici
             Tw *const pw = w + first + j * kHalf;
             const Tg *const pg = g + first + j * kHalf;
             if constexpr (MASTER) unpack8(M::get(here + R::kAtMaster, 0u, lane, lane, kHalf, true), e[j].w);
-            else unpack8(W::get(here, WALIGN == 8 ? 8u : elem::misalignment(pw), lane, lane, kHalf, true), e[j].w);
+            else unpack8(W::get(here, elem::misalignment(pw), lane, lane, kHalf, true), e[j].w);
             unpack8(G::get(here + R::kAtG, elem::misalignment(pg), lane, lane, kHalf, true), e[j].g);
             decode8(reinterpret_cast<const uint2 *>(here + R::kAtM)[lane], scales.x, e[j].m);
             decode8(reinterpret_cast<const uint2 *>(here + R::kAtV)[lane], scales.y, e[j].v);

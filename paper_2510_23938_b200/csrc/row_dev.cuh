@@ -9,9 +9,9 @@ namespace rows {
 using elem::Pair;
 using elem::unpair;
 
-// How rows lie: anywhere; at 16-byte boundaries and in whole vectors of eight elements; and so that all threads of a row's group
-// have the same number of vectors too.
-enum Rows { kAnyRows = 0, kAlignedRows = 1, kExactRows = 2 };
+// How rows lie: anywhere; at 16-byte boundaries and in whole vectors of eight elements; so that all threads of a row's group
+// have the same number of vectors too; or so, but anywhere.
+enum Rows { kAnyRows = 0, kAlignedRows = 1, kExactRows = 2, kShiftedRows = 3 };
 
 // Elements of vector v that are in a row of `dim`.
 __device__ __forceinline__ uint32_t left_of(uint32_t v, uint32_t dim) { return v * 8u < dim ? (dim - v * 8u < 8u ? dim - v * 8u : 8u) : 0u; }
@@ -197,7 +197,7 @@ __device__ __forceinline__ void group_sums(float (&v)[N], float *slots, F f) {
 // wait_copies and a __syncwarp.
 template <typename T, uint32_t WIDTH, int MODE>
 struct Segment {
-    static constexpr bool kAligned = MODE != kAnyRows;
+    static constexpr bool kAligned = MODE == kAlignedRows || MODE == kExactRows, kWhole = MODE == kExactRows || MODE == kShiftedRows;
     static constexpr uint32_t kEach = sizeof(T) / 2u, kPieces = WIDTH * kEach + (kAligned ? 0u : 1u);
     // v: this lane's vector, `lane` its number among the WIDTH
     static __device__ __forceinline__ void fetch(uint4 *to, const T *row, uint32_t v, uint32_t lane, uint32_t dim) {
@@ -206,6 +206,12 @@ struct Segment {
         if constexpr (MODE == kExactRows) {
 #pragma unroll
             for (uint32_t i = 0; i < kEach; ++i) copy_async16(to + i * WIDTH + lane, p + 16u * (i * WIDTH + lane));
+        } else if constexpr (MODE == kShiftedRows) {
+            const uint32_t off = elem::misalignment(p);
+            p -= off;
+#pragma unroll
+            for (uint32_t i = 0; i < kEach; ++i) copy_async16(to + i * WIDTH + lane, p + 16u * (i * WIDTH + lane));
+            if (lane == 0u && off) copy_async16(to + WIDTH * kEach, p + 16u * WIDTH * kEach);
         } else {
             if (first >= dim) return;
             const uint32_t off = kAligned ? 0u : elem::misalignment(p), bytes = off + (dim - first) * (uint32_t)sizeof(T);
@@ -222,14 +228,14 @@ struct Segment {
     // This lane's elements, zeros behind the row's end or if it is not there.  row_off: the row's bytes from a 16-byte boundary.
     static __device__ __forceinline__ elem::Packed<T, 8> get(const uint4 *from, uint32_t row_off, uint32_t v, uint32_t lane, uint32_t dim, bool live) {
         elem::Vector<T, 8, kAligned ? 16 : elem::kAny> raw;
-        const bool some = live && (MODE == kExactRows || v * 8u < dim);
+        const bool some = live && (kWhole || v * 8u < dim);
 #pragma unroll
         for (uint32_t i = 0; i < kEach + (kAligned ? 0u : 1u); ++i) {
             const uint4 x = some ? from[lane * kEach + i] : make_uint4(0u, 0u, 0u, 0u);
             raw.w[4 * i] = x.x; raw.w[4 * i + 1] = x.y; raw.w[4 * i + 2] = x.z; raw.w[4 * i + 3] = x.w;
         }
         elem::Packed<T, 8> out = raw.get(kAligned ? 0u : row_off);
-        if constexpr (!kAligned) {
+        if constexpr (MODE == kAnyRows) {
             const uint32_t left = left_of(v, dim);
             if (left < 8u) {
 #pragma unroll
