@@ -299,7 +299,7 @@ norm_grad_wide_kernel(LayerNormGradArgs a, const float2 *row_sums, float *partia
 }
 
 // The parts' sums of 32 columns: a warp adds up every 32nd part, then the warps' sums are added first to last.
-constexpr uint32_t kSlices = 32;
+constexpr uint32_t kSlices = 32, kEachSlice = (kMostParts + kSlices - 1) / kSlices;
 __global__ void __launch_bounds__(32 * kSlices)
 norm_grad_columns_kernel(const float *partial, uint32_t parts, uint32_t dim, void *dw, void *db, int type, bool accumulate) {
     __shared__ float sums[kSlices][33];
@@ -307,11 +307,14 @@ norm_grad_columns_kernel(const float *partial, uint32_t parts, uint32_t dim, voi
     const uint32_t c = blockIdx.x * 32u + lane, width = 2u * dim;
     void *out = c < dim ? dw : c < width ? db : nullptr;
     wait_for_previous_kernel();
-    float sum = 0.f;
-    if (out) {
-#pragma unroll 8
-        for (uint32_t p = slice; p < parts; p += kSlices) sum += __ldcg(partial + (uint64_t)p * width + c);
+    float part[kEachSlice], sum = 0.f;                   // all on their way at once
+#pragma unroll
+    for (uint32_t i = 0; i < kEachSlice; ++i) {
+        const uint32_t p = slice + i * kSlices;
+        part[i] = out && p < parts ? __ldcg(partial + (uint64_t)p * width + c) : 0.f;
     }
+#pragma unroll
+    for (uint32_t i = 0; i < kEachSlice; ++i) sum += part[i];
     sums[slice][lane] = sum;
     __syncthreads();
     if (slice || !out) return;
