@@ -30,8 +30,8 @@ uint64_t part_count(uint64_t n, uint32_t groups) {
     return parts < kMostParts ? (parts ? parts : 1u) : kMostParts;
 }
 
-// The ring: 16-byte pieces of x and of dy in a row of every group, rows that a group works on at a time (as many as leave room for
-// three such steps; two with fewer threads to a row, where four spill registers: 131072 x 1024 143 us, 209 with four), and steps.
+// The ring: 16-byte pieces of x and of dy in a row of every group, rows that a group works on at a time (four if three such steps
+// have room: 8192 x 2048 25.0 us, 27.7 with two), and steps.
 template <typename Tx, typename Ty, uint32_t T, int NV, int MODE>
 struct Ring {
     static constexpr uint32_t kWidth = T < 32u ? T : 32u, kSegments = kThreads / kWidth;
@@ -39,7 +39,7 @@ struct Ring {
     using Y = Segment<Ty, kWidth, MODE>;
     static constexpr uint32_t kX = kSegments * X::kPieces, kY = kSegments * Y::kPieces, kRow = NV * (kX + kY);
     static constexpr uint32_t kRoom = 12288;             // pieces: 192 KiB
-    static constexpr int kRows = NV > 1 ? 1 : T == kThreads && 12u * kRow <= kRoom ? 4 : 2;
+    static constexpr int kRows = NV > 1 ? 1 : 12u * kRow <= kRoom ? 4 : 2;
     static constexpr int kStages = (int)(kRoom / (kRow * kRows));
     static_assert(kStages >= 2 && 2u * kRows <= kWidth, "a step in flight; a lane for each of a step's statistics");
 };
