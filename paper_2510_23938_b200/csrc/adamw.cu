@@ -599,6 +599,8 @@ adamw_kernel(const __grid_constant__ AdamwArgs a, uint32_t run, uint32_t *arrive
     extern __shared__ uint4 rings[];                     // 8 bits only
     uint4 *ring = nullptr;
     if constexpr (BITS == 8) ring = rings + (threadIdx.x >> 5) * (Ring<Tw, Tg, MASTER>::kStep * Ring<Tw, Tg, MASTER>::kStages);
+    allow_next_kernel();
+    wait_for_previous_kernel();
     if (threadIdx.x == 0) make_coefficients(a, shared);
     __syncthreads();
     for (uint64_t k = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; k < a.set.n; k += (uint64_t)gridDim.x * blockDim.x)
@@ -663,8 +665,7 @@ cudaError_t launch_instance(const AdamwArgs &a, uint32_t *arrived, uint32_t *d_s
         cudaError_t e = ensure_dynamic_smem(kernel, bytes, done);
         if (e != cudaSuccess) return e;
     }
-    kernel<<<grid, kWarps * 32, bytes, stream>>>(a, run, arrived, d_status);
-    return cudaGetLastError();
+    return launch_overlapping(kernel, dim3(grid), dim3(kWarps * 32), bytes, stream, a, run, arrived, d_status);
 }
 
 }  // namespace

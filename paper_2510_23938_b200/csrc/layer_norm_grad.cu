@@ -56,6 +56,7 @@ norm_grad_kernel(const __grid_constant__ LayerNormGradArgs a, float *partial) {
     extern __shared__ uint4 ring[];                      // steps x rows x vectors x (x, dy)
     __shared__ float slots[2][2 * R * 16];
     allow_next_kernel();
+    wait_for_previous_kernel();
     const uint32_t t = threadIdx.x % T, group = threadIdx.x / T, lane = threadIdx.x % kWidth, segment = threadIdx.x / kWidth;
     const uint32_t dim = (uint32_t)a.dim;
     const uint64_t begin = a.n * blockIdx.x / gridDim.x, end = a.n * (blockIdx.x + 1u) / gridDim.x;
@@ -306,6 +307,7 @@ norm_grad_columns_kernel(const float *partial, uint32_t parts, uint32_t dim, voi
     const uint32_t lane = threadIdx.x & 31u, slice = threadIdx.x >> 5;
     const uint32_t c = blockIdx.x * 32u + lane, width = 2u * dim;
     void *out = c < dim ? dw : c < width ? db : nullptr;
+    allow_next_kernel();
     wait_for_previous_kernel();
     float part[kEachSlice], sum = 0.f;                   // all on their way at once
 #pragma unroll
@@ -337,8 +339,7 @@ cudaError_t launch_instance(const LayerNormGradArgs &a, float *partial, uint32_t
     static bool done[kMaxDevices] = {};
     cudaError_t e = ensure_dynamic_smem(kernel, shared, done);
     if (e != cudaSuccess) return e;
-    kernel<<<parts, kThreads, shared, stream>>>(a, partial);
-    return cudaGetLastError();
+    return launch_overlapping(kernel, dim3(parts), dim3(kThreads), shared, stream, a, partial);
 }
 
 constexpr uint64_t kWidest = 8u * kThreads * 2u;      // columns of the kernel that reads its rows once
