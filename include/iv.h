@@ -586,9 +586,12 @@ int iv_layer_norm_grad(iv_ctx *ctx, const void *d_dy, int y_type, uint64_t dy_st
 /* One AdamW step over a ragged tensor set, t being the number of this step (*d_step + 1):
  *   g = c * gradient,   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
  *   w = w (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps),
- * in 32 bits, w rounded once.  The weights are given as for iv_grad_norm, all
+ * in 32 bits, w rounded once (the moments' products and sums are rounded one by
+ * one; the root and the quotient are within 2^-20 of themselves, and an eps below
+ * 2^-126 counts as 0).  The weights are given as for iv_grad_norm, all
  * of one type, and updated in place (in the bytes of a weight file: the chunks
- * they lie in are then dirty).
+ * they lie in are then dirty); they must not overlap one another, the gradients
+ * or the state.
  *   d_grads, d_grad_offsets   tensor k's gradient, as many elements of
  *                    grad_type, starts at d_grads + d_grad_offsets[k] (bytes,
  *                    modulo 2^64).  The types are equal or one of them is IV_F32

@@ -8,6 +8,7 @@ raises with the build command.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Optional
 
@@ -39,7 +40,6 @@ EXPORTS = (
 )
 
 ADAMW_BLOCK = 256          # IV_ADAMW_BLOCK
-_INFINITY = float("inf")
 
 # iv_dtype of the training-step operators
 DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
@@ -795,7 +795,7 @@ class Context:
         dimensions): (x - mean) * rstd * weight + bias, rounded once to `out_dtype` (default: x's); `rms`: without the
         mean.  `mean` and `rstd` (float32, one per row) receive what `layer_norm_grad` wants."""
         dim = x.shape[-1]
-        n = x.numel() // dim if dim else 0
+        n = x.numel() // dim if dim else math.prod(x.shape[:-1])
         x_ptr, x_stride = _rows_of(x, n, dim)
         if out is None:
             out = _empty(x.shape, out_dtype or x.dtype, x.device, stream)
@@ -822,7 +822,7 @@ class Context:
         `weight_grad` and `bias_grad` (of one type), where given, receive the sums over the rows, or with `accumulate`
         have them added.  `mean` is not read with `rms` and may then be None."""
         dim = x.shape[-1]
-        n = x.numel() // dim if dim else 0
+        n = x.numel() // dim if dim else math.prod(x.shape[:-1])
         x_ptr, x_stride = _rows_of(x, n, dim)
         grad_ptr, grad_stride = _rows_of(grad_out, n, dim)
         if out is None:
@@ -868,12 +868,13 @@ class Context:
             m_scales_ptr = _vector_ptr(m_scales, blocks, torch.float32)
             v_scales_ptr = _vector_ptr(v_scales, blocks, torch.float32)
         assert step.is_cuda and step.dtype is torch.int64 and step.numel() == 1, "step: one int64 on the device"
+        assert max_norm is None or norm is not None, "clipping needs the record of the gradients' norm"
         lr_ptr = None
         if isinstance(lr, torch.Tensor):
             assert lr.is_cuda and lr.dtype is torch.float32 and lr.numel() == 1, "lr: a number or one float32 on the device"
             lr_ptr, lr = lr.data_ptr(), 0.0
         assert base.is_cuda and grads.is_cuda, "device tensors must be CUDA tensors"
-        options = AdamwOptions(lr, betas[0], betas[1], eps, weight_decay, _INFINITY if max_norm is None else max_norm, stochastic,
+        options = AdamwOptions(lr, betas[0], betas[1], eps, weight_decay, math.inf if max_norm is None else max_norm, stochastic,
                                seed & 0xffffffffffffffff)
         rc = self._lib.iv_adamw_step(
             self._h, base.data_ptr(), tensors[0], tensors[1], DTYPES[dtype or base.dtype], n, grads.data_ptr(), tensors[2],

@@ -130,6 +130,21 @@ def test_norm_defaults_and_empty_inputs(ctx):
     assert plain.shape == x.shape and torch.equal(plain.view(6, 96), ctx.layer_norm(x.view(6, 96)))
     assert ctx.layer_norm(x, out_dtype=BF16).dtype == BF16
     assert ctx.layer_norm(x[:0]).shape == (0, 3, 96) and ctx.layer_norm(x[..., :0]).shape == (2, 3, 0)
+    assert ctx.layer_norm(torch.empty(5, 0, device="cuda")).shape == (5, 0) and ctx.layer_norm(torch.empty(0, 5, device="cuda")).shape == (0, 5)
+    assert torch.equal(ctx.layer_norm(x[0, 0]), plain[0, 0])
+    wide = _randn((7, 200), 2)
+    assert torch.equal(ctx.layer_norm(wide[:, 8:104]), ctx.layer_norm(wide[:, 8:104].contiguous()))
+    empty = torch.empty(5, 0, device="cuda")
+    assert ctx.layer_norm_grad(empty, empty, torch.empty(5, device="cuda"), torch.empty(5, device="cuda")).shape == (5, 0)
+
+
+def test_moments_are_those_of_elementary_operations(ctx):
+    """Products and sums rounded one by one: bit for bit what torch's operations give."""
+    s = Set([70_000], F32, BF16, 32)
+    m, v, g = s.state["m"].clone(), s.state["v"].clone(), s.g[:70_000].float()
+    ctx.adamw_step(*s.args(), **s.state)
+    assert torch.equal(s.state["m"][:70_000], m[:70_000] * 0.9 + g * (1 - 0.9))
+    assert torch.equal(s.state["v"][:70_000], v[:70_000] * 0.999 + g * g * (1 - 0.999))
 
 
 @pytest.mark.parametrize("dim", [40, 96, 640, 4096, 20_000])
@@ -520,6 +535,19 @@ def test_bad_moments_leave_their_block_alone(ctx):
     assert torch.equal(s.w[~w_bad], clean.w[~w_bad])
 
 
+@pytest.mark.parametrize("kind", [BF16, F16])
+def test_bad_weights_stay_bad_however_they_are_rounded(ctx, kind):
+    for stochastic in (False, True):
+        s = Set([600], kind, F32, 32)
+        s.w[3], s.w[300], s.w[599], s.g[40], s.g[50] = math.inf, math.nan, -math.inf, math.nan, -math.inf
+        ctx.adamw_step(*s.args(), **s.state, stochastic=stochastic, seed=11)
+        w = s.w[:600].float()
+        assert float(w[3]) == math.inf and float(w[599]) == -math.inf
+        bad = torch.zeros(600, dtype=torch.bool, device="cuda")
+        bad[[300, 40, 50]] = True                                          # an infinite gradient: infinity / infinity
+        assert torch.equal(torch.isnan(w), bad)
+
+
 def test_averages_in_8_bits_do_not_stick(ctx):
     """Roots of 1 and gradients of 0, but for one element a block whose gradient of 1 holds the scale: rounding is unbiased, so
     the mean of the others follows 0.999^(t / 2).  A rounding goes to one of two codes at most 32 / 448 apart, so its
@@ -666,6 +694,60 @@ def test_a_captured_step_counts_on(ctx):
         assert torch.equal(eager["state"][key].view(torch.uint8), played["state"][key].view(torch.uint8))
 
 
+def test_two_graphs_take_turns(ctx):
+    """Two captured calls that share the context's scratch, replayed in turn and after calls of a larger size."""
+    inputs = [(_randn((n, 640), i), _randn((n, 640), i + 9), torch.ones(n, device="cuda"), torch.zeros(640, device="cuda"), torch.empty(n, 640, device="cuda"))
+              for i, n in enumerate((50, 900))]
+    call = lambda p: ctx.layer_norm_grad(p[0], p[1], None, p[2], rms=True, out=p[4], weight_grad=p[3])  # noqa: E731
+    want = []
+    for p in inputs:
+        call(p)
+        want.append((p[3].clone(), p[4].clone()))
+    graphs = []
+    for p in inputs:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(p)
+        graphs.append(graph)
+    big = _randn((5000, 8192), 3)
+    for turn in range(3):
+        for p, graph, (dw, dx) in zip(inputs, graphs, want):
+            p[3].zero_()
+            p[4].zero_()
+            graph.replay()
+            assert torch.equal(p[3], dw) and torch.equal(p[4], dx)
+        ctx.layer_norm_grad(big, big, None, torch.ones(5000, device="cuda"), rms=True, weight_grad=torch.empty(8192, device="cuda"))
+
+
+def test_two_contexts_at_once():
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    contexts = [binding.Context(0) for _ in range(2)]
+    sets = [Set([200_000, 31], BF16, BF16, 8, skew=k) for k in range(2)]
+    xs = [_randn((3000, 1000), k) for k in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(3):
+        for c, stream, s, x in zip(contexts, streams, sets, xs):
+            c.adamw_step(*s.args(), **s.state, stream=stream)
+            dw = torch.empty(1000, device="cuda")
+            with torch.cuda.stream(stream):
+                got.append((x, dw, c.layer_norm_grad(x, x, None, torch.ones(3000, device="cuda"), rms=True, weight_grad=dw, stream=stream)))
+    torch.cuda.synchronize()
+    for s in sets:
+        assert int(s.state["step"]) == 44
+        after = {k: v.clone() for k, v in {"w": s.w, **s.state}.items()}
+        s.back()
+        for _ in range(3):
+            contexts[0].adamw_step(*s.args(), **s.state)
+        assert all(torch.equal(after[k].view(torch.uint8), v.view(torch.uint8)) for k, v in {"w": s.w, **s.state}.items())
+    for x, dw, dx in got:
+        want = torch.empty_like(dw)
+        assert torch.equal(contexts[0].layer_norm_grad(x, x, None, torch.ones(3000, device="cuda"), rms=True, weight_grad=want), dx)
+        assert torch.equal(dw, want)
+    for c in contexts:
+        c.close()
+
+
 def test_growth_under_capture_is_refused():
     with binding.Context(0) as c:
         x, rstd, dw = _randn((64, 512), 1), torch.ones(64, device="cuda"), torch.zeros(512, device="cuda")
@@ -711,7 +793,7 @@ def test_refusals(ctx):
         with pytest.raises(binding.IvError) as err:
             ctx.adamw_step(*s.args(), **s.state, **wrong)
         assert err.value.code == binding.IV_ERR_INVALID_ARG
-    for wrong in ({"m": s.state["m"].float()}, {"m_scales": None}, {"v_scales": s.state["v_scales"][1:]}, {"step": s.state["step"].int()},
+    for wrong in ({"max_norm": 1.0}, {"m": s.state["m"].float()}, {"m_scales": None}, {"v_scales": s.state["v_scales"][1:]}, {"step": s.state["step"].int()},
                   {"state_offsets": s.state["state_offsets"].int()}, {"m": s.state["m"].view(torch.uint8)}):
         with pytest.raises(AssertionError):
             ctx.adamw_step(*s.args(), **{**s.state, **wrong})
