@@ -8,8 +8,8 @@
 // blocks, finds a block's tensor by searching the tensors' places, and needs nobody else: a block's largest moments are a reduction
 // over half a warp.  With 32-bit moments memory is the bound: on one B200 the 1.31e9 bf16 weights of a 24-layer file take 4.6 ms,
 // 6.2 TB/s (4.9 with three CTAs per SM, whose 80 registers are too few); 200 packed tensors with 32-bit copies 289 us, 5.9 TB/s.  With 8-bit
-// moments it is the instructions, 57 an element: the same file takes 3.1 ms, 4.2 TB/s, 200 packed tensors with float32 gradients
-// 208 us.  Seven small tensors take 6 to 7 us on the device.
+// moments it is the instructions, some 55 an element: the same file takes 3.05 ms, 4.3 TB/s, 200 packed tensors with float32 gradients
+// 205 us.  Seven small tensors take 6 to 7 us on the device.
 //
 // The moments' averages change by a part in a thousand a step, far less than an 8-bit code's step, so rounding to nearest would
 // hold them where they are.  They are rounded up with the probability that the lost bits give instead, by
@@ -84,12 +84,18 @@ struct Words {
 };
 
 // Root and reciprocal to 2^-22 or better (IEEE ones: 666 us against 612 for 268M weights with 8-bit moments).  The reciprocal takes what
-// is below 2^-126 for 0.
+// is below 2^-126 for 0, the root if NORMAL (its other form costs three instructions more: 557 us against 544).
+template <bool NORMAL>
 __device__ __forceinline__ Pair root_approx(Pair x) {
     float lo, hi;
     x.get(lo, hi);
-    asm("sqrt.approx.f32 %0, %0;" : "+f"(lo));
-    asm("sqrt.approx.f32 %0, %0;" : "+f"(hi));
+    if constexpr (NORMAL) {
+        asm("sqrt.approx.ftz.f32 %0, %0;" : "+f"(lo));
+        asm("sqrt.approx.ftz.f32 %0, %0;" : "+f"(hi));
+    } else {
+        asm("sqrt.approx.f32 %0, %0;" : "+f"(lo));
+        asm("sqrt.approx.f32 %0, %0;" : "+f"(hi));
+    }
     return Pair(lo, hi);
 }
 __device__ __forceinline__ Pair reciprocal_approx(Pair x) {
@@ -100,16 +106,20 @@ __device__ __forceinline__ Pair reciprocal_approx(Pair x) {
     return Pair(lo, hi);
 }
 
-// Bits of a 32-bit value with random bits added in the place of those that a 16-bit type does not have; infinities stay, NaN too.
-template <typename T> __device__ __forceinline__ uint32_t round_random(float x, uint32_t word);
-template <> __device__ __forceinline__ uint32_t round_random<__nv_bfloat16>(float x, uint32_t word) {
+// Two 32-bit values as 16-bit ones, with random bits added in the place of those that go; infinities stay, NaN too.
+template <typename T> __device__ __forceinline__ uint32_t round_random2(float lo, float hi, uint32_t word_lo, uint32_t word_hi);
+template <> __device__ __forceinline__ uint32_t round_random2<__nv_bfloat16>(float lo, float hi, uint32_t word_lo, uint32_t word_hi) {
     // the bits of a NaN that an operation gives, 0x7fffffff, would carry into the sign
-    return ((uint32_t)min((int32_t)__float_as_uint(x), 0x7fff0000) + (word >> 16)) >> 16;
+    auto sum = [](float x, uint32_t word) { return (uint32_t)min((int32_t)__float_as_uint(x), 0x7fff0000) + (word >> 16); };
+    return __byte_perm(sum(lo, word_lo), sum(hi, word_hi), 0x7632);
 }
-template <> __device__ __forceinline__ uint32_t round_random<__half>(float x, uint32_t word) {
-    if (!(fabsf(x) < 65536.f)) return __half_as_ushort(__float2half_rn(x));
-    // times 2^-112 a half's exponent and digits, small ones too, are the upper bits of the float's
-    return (__float_as_uint(fabsf(x) * 0x1p-112f) + (word >> 19)) >> 13 | __float_as_uint(x) >> 31 << 15;
+template <> __device__ __forceinline__ uint32_t round_random2<__half>(float lo, float hi, uint32_t word_lo, uint32_t word_hi) {
+    auto code = [](float x, uint32_t word) -> uint32_t {
+        if (!(fabsf(x) < 65536.f)) return __half_as_ushort(__float2half_rn(x));
+        // times 2^-112 a half's exponent and digits, small ones too, are the upper bits of the float's
+        return (__float_as_uint(fabsf(x) * 0x1p-112f) + (word >> 19)) >> 13 | __float_as_uint(x) >> 31 << 15;
+    };
+    return __byte_perm(code(lo, word_lo), code(hi, word_hi), 0x5410);
 }
 
 // Eight codes as 32-bit values times a scale.
@@ -274,9 +284,21 @@ struct Lane {
             const Pair g1 = g[i] * factor, square = BITS == 32 ? v[i] : v[i] * v[i];
             m[i] = fma2(m[i], beta1, nothing) + fma2(g1, rest1, nothing);
             v[i] = fma2(square, beta2, nothing) + fma2(g1 * g1, rest2, nothing);
-            r[i] = root_approx(v[i]);
-            w[i] = fma2(w[i], keep, m[i] * step * reciprocal_approx(fma2(r[i], root, eps)));
+            r[i] = root_approx<true>(v[i]);
         }
+        float least = __uint_as_float(0x7f800000u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float lo, hi;
+            v[i].get(lo, hi);
+            asm("min.f32 %0, %0, %1, %2;" : "+f"(least) : "f"(lo), "f"(hi));
+        }
+        if (least < 0x1p-126f) {                         // some are too small for that, or 0
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = root_approx<false>(v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = fma2(w[i], keep, m[i] * step * reciprocal_approx(fma2(r[i], root, eps)));
     }
     // The weights as elements of type T.
     template <typename T>
@@ -289,7 +311,7 @@ struct Lane {
             if (stochastic) {
 #pragma unroll
                 for (uint32_t i = 0; i < 8u; i += 2u)
-                    out.w[i / 2] = __byte_perm(round_random<T>(x[i], words.word(16u + i)), round_random<T>(x[i + 1], words.word(17u + i)), 0x5410);
+                    out.w[i / 2] = round_random2<T>(x[i], x[i + 1], words.word(16u + i), words.word(17u + i));
                 return out;
             }
         }
@@ -366,8 +388,8 @@ __device__ __forceinline__ void whole_blocks32(const AdamwArgs &a, const Coeffic
 }
 // With 8-bit moments half a warp takes a block, sixteen elements a lane in two vectors half a block apart: what a block costs
 // beside its elements (tops, scales, addresses) is shared by twice as many.  Two blocks of a warp come through a ring in shared
-// memory that the warp fills with asynchronous copies, two steps ahead (268M bf16 weights: 560 us, 617 with a block per warp and the
-// next one in registers).
+// memory that the warp fills with asynchronous copies, two steps ahead (268M bf16 weights: 560 us where a block per warp and
+// the next one in registers took 617).
 template <typename Tw, typename Tg, bool MASTER>
 struct Ring {
     // 16-byte pieces of half a block, at any alignment: weights, gradients, the 32-bit weights, the two moments' codes
