@@ -269,11 +269,14 @@ def _matrix(t: torch.Tensor) -> tuple:
 
 def _rows_of(t: torch.Tensor, n: int, dim: int) -> tuple:
     """(device pointer, elements from one row to the next) of n rows of `dim` elements."""
+    assert t.is_cuda, "device tensors must be CUDA tensors"
     if t.dim() == 2:
-        ptr, rows, columns, stride = _matrix(t)
-        assert (rows, columns) == (n, dim), "wrong number of rows or columns"
-        return ptr, stride
-    assert t.is_cuda and t.is_contiguous() and t.numel() == n * dim and t.shape[-1] == dim, "wrong number of rows or columns"
+        rows, columns = t.shape
+        assert rows == n and columns == dim, "wrong number of rows or columns"
+        stride, unit = t.stride()
+        assert unit == 1 or dim <= 1, "rows must be contiguous"
+        return t.data_ptr(), stride if n > 1 else dim
+    assert t.is_contiguous() and t.numel() == n * dim and t.shape[-1] == dim, "wrong number of rows or columns"
     return t.data_ptr(), dim
 
 
