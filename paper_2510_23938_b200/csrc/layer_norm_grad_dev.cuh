@@ -110,6 +110,8 @@ norm_grad_kernel(const __grid_constant__ LayerNormGradArgs a, float *partial) {
         float s[2 * R];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
+            s[2 * i] = s[2 * i + 1] = 0.f;
+            if (!decltype(whole)::value && base + i * kGroups >= end) continue;      // no group has such a row: 6001 x 1023 21.7 -> 21.1 us
             const bool live = decltype(whole)::value || base + i * kGroups + group < end;
             const uint32_t x_off = elem::misalignment(work_x + i * row_x), y_off = elem::misalignment(work_dy + i * row_dy);
             const Pair by(__shfl_sync(0xffffffffu, statistics, i, kWidth)), shift(-__shfl_sync(0xffffffffu, statistics, R + i, kWidth));
@@ -136,6 +138,7 @@ norm_grad_kernel(const __grid_constant__ LayerNormGradArgs a, float *partial) {
         group_sums<T, 2 * R>(s, sums, [scale](float sum) { return -sum * scale; });
 #pragma unroll
         for (int i = 0; i < R; ++i) {
+            if (!decltype(whole)::value && base + i * kGroups >= end) break;
             const bool live = decltype(whole)::value || base + i * kGroups + group < end;
             const Pair by(__shfl_sync(0xffffffffu, statistics, i, kWidth)), mp(a.rms ? 0.f : s[2 * i]), mh(s[2 * i + 1]);
 #pragma unroll
