@@ -440,6 +440,7 @@ __device__ __forceinline__ void whole_blocks8(const AdamwArgs &a, const Coeffici
             copy_async_small<4>(reinterpret_cast<float *>(to + 4u * R::kHalf) + half * 2u + lane / 8u, (lane ? a.d_v_scales : a.d_m_scales) + at / kBlock);
     };
     const uint32_t steps = (count + 1u) / 2u;
+    __syncwarp();                                        // the warp has read what the run of blocks before left in the ring
 #pragma unroll
     for (int i = 0; i < kStages - 1; ++i) {
         if ((uint32_t)i < steps) fetch(i, ring + i * R::kStep);
@@ -448,6 +449,7 @@ __device__ __forceinline__ void whole_blocks8(const AdamwArgs &a, const Coeffici
     uint32_t now = 0, last = (kStages - 1) * R::kStep;
 #pragma unroll 1
     for (uint32_t i = 0; i < steps; ++i) {
+        __syncwarp();                                    // and what it is filled with again now
         if (i + kStages - 1u < steps) fetch(i + kStages - 1u, ring + last);
         rows::commit_copies();
         rows::wait_copies<kStages - 1>();

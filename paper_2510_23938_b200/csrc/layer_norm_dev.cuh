@@ -91,6 +91,7 @@ layer_norm_kernel(const __grid_constant__ LayerNormArgs a) {
     };
     // `whole`: all rows of the step are there
     auto work = [&](uint64_t base, auto whole) {
+        __syncwarp();                                    // the warp has read what is overwritten now
         fetch(base + (kStages - 1) * stride, last);
         last = now;
         wait_copies<kStages - 1>();

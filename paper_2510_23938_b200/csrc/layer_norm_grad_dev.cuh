@@ -100,6 +100,7 @@ norm_grad_kernel(const __grid_constant__ LayerNormGradArgs a, float *partial) {
     float *sums = slots[0], *other = slots[1];
     // `whole`: all rows of the step are there
     auto work = [&](uint64_t base, auto whole) {
+        __syncwarp();                                    // the warp has read what is overwritten now
         fetch(base + (uint64_t)(kStages - 1) * kStep, last);
         last = now;
         const float statistics = next_statistic;
