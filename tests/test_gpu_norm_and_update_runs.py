@@ -6,7 +6,7 @@ form of the kernels goes round its ring at least once.  Bounds are those of test
 import pytest
 import torch
 
-from test_gpu_norm_and_update import BF16, F16, F32, KINDS, Set, _id, ctx  # noqa: F401
+from test_gpu_norm_and_update import BF16, F16, F32, KINDS, U, Set, _gen, _id, _randn, _true_grad, _true_norm, _within, ctx  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +49,82 @@ def test_the_longest_runs(ctx, kind, bits):  # noqa: F811
     s = Set([256 * (33 * 2 * 8 * SMS) + 100], weight, grad, bits, master, 4, 0)
     ctx.adamw_step(*s.args(), **s.state, seed=3)
     s.check(seed=3)
+
+
+# ------------------------------------------------------------------------------------------------- rows
+
+# For every number of threads to a row (8 to 512) and of vectors a thread: the full width, fewer whole vectors, an odd width.
+WIDTHS = [64, 40, 61, 128, 104, 101, 256, 200, 255, 512, 400, 511, 1024, 1000, 1023, 2048, 1600, 2047, 4096, 2560, 4095, 8192, 7168,
+          8191, 16384, 13000, 16383]
+TYPES = [(BF16, BF16), (F32, F32), (F16, F32), (F32, BF16)]
+
+
+def _groups(dim, threads=512):
+    """Rows that the threads of a CTA take side by side."""
+    t = 8
+    while t < threads and 8 * t < dim:
+        t *= 2
+    return threads // t
+
+
+def _steps(dim, size, most):
+    """Steps that a ring of 192 KiB holds at `most` rows a group, and one more turn of its places."""
+    row = _groups(dim) * max(dim, 64) * size
+    return -(-(192 << 10) // (row * most)) + 2
+
+
+@pytest.mark.parametrize("pair", TYPES, ids=_id)
+@pytest.mark.parametrize("dim", WIDTHS)
+def test_norm_of_many_rows_a_cta(ctx, dim, pair):  # noqa: F811
+    kind, out_kind = pair
+    rows = 4 if dim <= 8192 else 2
+    n = SMS * rows * _groups(dim) * min(_steps(dim, kind.itemsize, rows), 10) + 5
+    n = n * (2 if 2048 < dim <= 4096 else 1)                       # two CTAs an SM there
+    x = (_randn((n, dim), 1, 2.0) + 0.5).to(kind)
+    w, b = _randn((dim,), 2).to(out_kind), _randn((dim,), 3).to(out_kind)
+    mean, rstd = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    for rms in (False, True):
+        y = ctx.layer_norm(x, weight=w, bias=b, eps=1e-3, rms=rms, out_dtype=out_kind, mean=mean, rstd=rstd)
+        true_y, true_mean, true_rstd = _true_norm(x, w, b, 1e-3, rms)
+        _within(y, *true_y)
+        _within(mean, *true_mean)
+        _within(rstd, *true_rstd)
+
+
+def _many_rows(dim, kinds):
+    """So many that every ring of the gradient is filled again: x and dy of a row side by side, up to 4 rows a group."""
+    rows = 4 if dim <= 4096 else 1
+    return SMS * rows * _groups(dim) * min(_steps(dim, sum(k.itemsize for k in kinds), rows), 10) + 5
+
+
+@pytest.mark.parametrize("pair", TYPES, ids=_id)
+@pytest.mark.parametrize("dim", WIDTHS[:-3])
+def test_gradient_of_many_rows_a_cta(ctx, dim, pair):  # noqa: F811
+    kind, y_kind = pair
+    n = _many_rows(dim, pair)
+    x, dy, w = (_randn((n, dim), 1, 2.0) + 0.5).to(kind), _randn((n, dim), 2).to(y_kind), _randn((dim,), 3).to(y_kind)
+    mean, rstd = x.float().mean(1), 1 / (x.float().var(1, unbiased=False) + 1e-3).sqrt()
+    dw, db = torch.empty(dim, device="cuda"), torch.empty(dim, device="cuda")
+    # a thread adds up its group's rows of a CTA's run, then come the groups, and 5 + 32 sums of runs
+    depth = -(-n // (SMS * _groups(dim))) + 1 + _groups(dim) + 5 + 32
+    for rms in (False, True):
+        dx = ctx.layer_norm_grad(dy, x, None if rms else mean, rstd, weight=w, rms=rms, weight_grad=dw, bias_grad=db)
+        true_dx, (true_dw, _), (true_db, _) = _true_grad(dy, x, mean, rstd, w, rms)
+        _within(dx, *true_dx)
+        h = ((x.double() if rms else x.double() - mean.double()[:, None]) * rstd.double()[:, None]).abs_()
+        magnitude = dy.double().abs()
+        _within(db, true_db, depth * U * magnitude.sum(0))
+        _within(dw, true_dw, (depth + 3) * U * (magnitude * h).sum(0))              # h is rounded twice
+
+
+@pytest.mark.parametrize("pair", TYPES, ids=_id)
+@pytest.mark.parametrize("dim", WIDTHS[:-3])
+def test_sums_over_many_rows_are_exact_where_they_can_be(ctx, dim, pair):  # noqa: F811
+    """Small whole numbers: every row counts once, or a sum is off by a whole number."""
+    kind, y_kind = pair
+    n = _many_rows(dim, pair)
+    x = torch.randint(-4, 5, (n, dim), generator=_gen(1), device="cuda").to(kind)
+    dy = torch.randint(-2, 3, (n, dim), generator=_gen(2), device="cuda").to(y_kind)
+    dw, db = torch.empty(dim, device="cuda"), torch.empty(dim, device="cuda")
+    ctx.layer_norm_grad(dy, x, None, torch.ones(n, device="cuda"), rms=True, weight_grad=dw, bias_grad=db)
+    assert torch.equal(dw, (dy.double() * x.double()).sum(0).float()) and torch.equal(db, dy.double().sum(0).float())
