@@ -81,7 +81,7 @@ layer_norm_kernel(const __grid_constant__ LayerNormArgs a) {
         params_of(a.d_weight, a.param_type, t + j * T, dim, 1.f, w[j]);
         params_of(a.d_bias, a.param_type, t + j * T, dim, 0.f, b[j]);
     }
-    const float scale = 1.f / (float)dim;
+    const float count = (float)dim, scale = 1.f / count;
     uint32_t now = 0, last = (kStages - 1) * R * kRow;
     float *sums = slots[0], *other = slots[1];
     auto turn = [&]() {
@@ -118,7 +118,7 @@ layer_norm_kernel(const __grid_constant__ LayerNormArgs a) {
                 }
                 mean[i] = sum.sum();
             }
-            group_sums<T, R>(mean, sums, [scale](float sum) { return sum * scale; });
+            group_sums<T, R>(mean, sums, [count, scale](float sum) { return mean_of(sum, count, scale); });
             turn();
         }
 #pragma unroll
@@ -186,7 +186,7 @@ layer_norm_wide_kernel(LayerNormArgs a) {
     allow_next_kernel();
     wait_for_previous_kernel();
     const uint32_t dim = (uint32_t)a.dim, vectors = (dim + 7u) / 8u;
-    const float scale = 1.f / (float)dim;
+    const float count = (float)dim, scale = 1.f / count;
     uint32_t turn = 0;
     for (uint64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const Tx *in = static_cast<const Tx *>(a.d_x) + row * a.x_stride;
@@ -206,7 +206,7 @@ layer_norm_wide_kernel(LayerNormArgs a) {
         if (!a.rms) {
             each([&](uint32_t, Pair (&e)[4]) { sum += ((e[0] + e[1]) + (e[2] + e[3])).sum(); });
             float all[1] = {sum};
-            group_sums<kWideThreads, 1>(all, slots[turn], [scale](float s) { return s * scale; });
+            group_sums<kWideThreads, 1>(all, slots[turn], [count](float s) { return s / count; });
             turn ^= 1u;
             mean = all[0];
         }

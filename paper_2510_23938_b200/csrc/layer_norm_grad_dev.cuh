@@ -95,7 +95,7 @@ norm_grad_kernel(const __grid_constant__ LayerNormGradArgs a, float *partial) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) dw[j][i] = db[j][i] = Pair(0.f);
     }
-    const float scale = 1.f / (float)dim;
+    const float count = -(float)dim, scale = 1.f / count;
     uint32_t now = 0, last = (kStages - 1) * R * kRow;
     float *sums = slots[0], *other = slots[1];
     // `whole`: all rows of the step are there
@@ -150,7 +150,7 @@ norm_grad_kernel(const __grid_constant__ LayerNormGradArgs a, float *partial) {
             s[2 * i] = s2.sum();
             s[2 * i + 1] = sh2.sum();
         }
-        group_sums<T, 2 * R>(s, sums, [scale](float sum) { return -sum * scale; });
+        group_sums<T, 2 * R>(s, sums, [count, scale](float sum) { return mean_of(sum, count, scale); });
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             if (!decltype(whole)::value && base + i * kGroups >= end) break;
@@ -261,7 +261,7 @@ norm_grad_wide_kernel(LayerNormGradArgs a, const float2 *row_sums, float *partia
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, dim = (uint32_t)a.dim;
     const uint32_t tile = blockIdx.x / parts, part = blockIdx.x % parts, v = tile * 32u + lane, left = left_of(v, dim);
     const uint64_t begin = a.n * part / parts, end = a.n * (part + 1u) / parts;
-    const float scale = 1.f / (float)dim;
+    const float count = (float)dim;
     float w[8], dw[8], db[8];
     for (uint32_t i = 0; i < 8u; ++i) {
         w[i] = i >= left ? 0.f : a.d_weight ? param_at(a.d_weight, a.param_type, v * 8u + i) : 1.f;
@@ -276,7 +276,7 @@ norm_grad_wide_kernel(LayerNormGradArgs a, const float2 *row_sums, float *partia
         ry.load(dy, v, dim);
         const float rstd = a.d_rstd[row], mean = a.d_mean ? a.d_mean[row] : 0.f;
         const float2 sums = row_sums[row];
-        const float mp = a.rms ? 0.f : sums.x * scale, mh = sums.y * scale;
+        const float mp = a.rms ? 0.f : sums.x / count, mh = sums.y / count;
         Pair pairs[4];
         float h[8], e[8];
         elem::unpack8(rx.get(elem::misalignment(x), v, dim), pairs);

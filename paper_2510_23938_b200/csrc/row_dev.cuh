@@ -140,6 +140,15 @@ __device__ __forceinline__ void group_barrier() {
     asm volatile("bar.sync %0, %1;" ::"r"(threadIdx.x / T + 1u), "n"(T) : "memory");
 }
 
+// sum / count, `inverse` being 1 / count rounded.  Times that alone the mean of equal numbers can be off in its last place, which
+// 1 / sqrt(eps) then multiplies; what the product leaves of the sum, times it again, mends that: right to the last place
+// wherever the quotient is a 32-bit float.  (A division instead changes nothing but the code around it: norm of 131072 x 4096, root-mean-square
+// form, 388 us for 338, gradient of 32768 x 8192 307 for 281, but norm of 32768 x 16384 406 for 446.)
+__device__ __forceinline__ float mean_of(float sum, float count, float inverse) {
+    const float q = sum * inverse;
+    return fabsf(q) < __uint_as_float(0x7f800000u) ? fmaf(fmaf(-q, count, sum), inverse, q) : q;
+}
+
 __device__ __forceinline__ float param_at(const void *p, int type, uint32_t i) {
     if (type == IV_F32) return static_cast<const float *>(p)[i];
     if (type == IV_F16) return elem::to_float(static_cast<const __half *>(p)[i]);
