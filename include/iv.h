@@ -587,8 +587,8 @@ int iv_layer_norm_grad(iv_ctx *ctx, const void *d_dy, int y_type, uint64_t dy_st
  *   g = c * gradient,   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
  *   w = w (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps),
  * in 32 bits, w rounded once (the moments' products and sums are rounded one by
- * one; the root and the quotient are within 2^-20 of themselves, and an eps below
- * 2^-126 counts as 0).  The weights are given as for iv_grad_norm, all
+ * one; the root and the quotient are within 2^-23 of themselves, with 8-bit
+ * moments the quotient within 2^-22, and an eps below 2^-126 counts as 0).  The weights are given as for iv_grad_norm, all
  * of one type, and updated in place (in the bytes of a weight file: the chunks
  * they lie in are then dirty); they must not overlap one another, the gradients
  * or the state.

@@ -83,27 +83,51 @@ struct Words {
     __device__ __forceinline__ uint32_t word(uint32_t k) const { return b + (k + 1u) * a; }
 };
 
-// Root and reciprocal to 2^-22 or better (IEEE ones: 666 us against 612 for 268M weights with 8-bit moments).  The reciprocal takes what
-// is below 2^-126 for 0, the root if NORMAL (its other form costs three instructions more: 557 us against 544).
-template <bool NORMAL>
+__device__ __forceinline__ Pair negative(Pair x) {
+    float lo, hi;
+    x.get(lo, hi);
+    return Pair(-lo, -hi);
+}
+// `better` where it is a number.
+__device__ __forceinline__ Pair unless_nan(Pair better, Pair x) {
+    float a[2], b[2];
+    better.get(a[0], a[1]);
+    x.get(b[0], b[1]);
+    return Pair(a[0] == a[0] ? a[0] : b[0], a[1] == a[1] ? a[1] : b[1]);
+}
+// The root by one step of Heron's method: with y near 1 / sqrt(v), s = v y misses the root by (v - s^2) y / 2 but for the square of y's
+// error, 2^-45 of it.  So it is the root rounded, to 2^-24, or within 2^-23 where v is below 2^-100 and the difference a small one; NaN
+// where 1 / sqrt(v) is none or v is below 2^-126.  With sqrt.approx alone, 2^-23, one code in some 6e6 of the second moments' is not the one that
+// elementary operations give.  268M weights, sqrt.approx, this, an IEEE root: 540, 576, 617 us with 8-bit moments, 930, 930, 935 with 32-bit ones.
+__device__ __forceinline__ Pair root_of(Pair v) {
+    float lo, hi;
+    v.get(lo, hi);
+    asm("rsqrt.approx.ftz.f32 %0, %0;" : "+f"(lo));
+    asm("rsqrt.approx.ftz.f32 %0, %0;" : "+f"(hi));
+    const Pair y(lo, hi), s = v * y;
+    return fma2(fma2(negative(s), s, v), y * Pair(0.5f), s);
+}
+// To 2^-23, of any number.
 __device__ __forceinline__ Pair root_approx(Pair x) {
     float lo, hi;
     x.get(lo, hi);
-    if constexpr (NORMAL) {
-        asm("sqrt.approx.ftz.f32 %0, %0;" : "+f"(lo));
-        asm("sqrt.approx.ftz.f32 %0, %0;" : "+f"(hi));
-    } else {
-        asm("sqrt.approx.f32 %0, %0;" : "+f"(lo));
-        asm("sqrt.approx.f32 %0, %0;" : "+f"(hi));
-    }
+    asm("sqrt.approx.f32 %0, %0;" : "+f"(lo));
+    asm("sqrt.approx.f32 %0, %0;" : "+f"(hi));
     return Pair(lo, hi);
 }
-__device__ __forceinline__ Pair reciprocal_approx(Pair x) {
+// n / d, d below 2^-126 being taken for 0.  EXACT: what the approximate reciprocal's quotient, within 2^-22, leaves of n gives the rest, to
+// 2^-24.  That costs the step with 32-bit moments, which waits for memory, nothing (930 us either way, IEEE divisions 935 to 973); that
+// with 8-bit moments has no instructions to spare (IEEE divisions 617 -> 730 us), and 2^-22 of an update is below the
+// last place of a weight that the update changes by less than a quarter.
+template <bool EXACT>
+__device__ __forceinline__ Pair quotient(Pair n, Pair d) {
     float lo, hi;
-    x.get(lo, hi);
+    d.get(lo, hi);
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(lo));
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(hi));
-    return Pair(lo, hi);
+    const Pair inverse(lo, hi), q = n * inverse;
+    if constexpr (!EXACT) return q;
+    else return unless_nan(fma2(fma2(negative(q), d, n), inverse, q), q);
 }
 
 // Two 32-bit values as 16-bit ones, with random bits added in the place of those that go; infinities stay, NaN too.
@@ -165,10 +189,10 @@ __device__ __forceinline__ float largest_finite(const Pair (&x)[4], float top) {
     return top;
 }
 
-// A block's tops, the exact root of the second one's, factors and scales, from its lanes' largest magnitudes m and v.  WIDTH lanes
-// hold a block: half of them work out the first moments', half the second's.
+// A block's factors and scales, from its lanes' largest magnitudes m and v.  WIDTH lanes hold a block: half of them work out the
+// first moments', half the roots'.
 struct Tops {
-    float v, root, m_inverse, v_inverse, scale;          // scale: of the first moments in the block's lower lanes, of the roots in the upper ones
+    float m_inverse, v_inverse, scale;                   // scale: of the first moments in the block's lower lanes, of the roots in the upper ones
     bool bad;                                            // an infinity or a NaN in a block of the warp
 };
 template <uint32_t WIDTH, typename F>
@@ -193,8 +217,6 @@ __device__ __forceinline__ Tops block_tops(float m, float v, F finite) {
     const float root = __fsqrt_rn(top), x = second ? root : top, safe = fmaxf(x, 0x1p-110f);
     const float inverse = x > 0.f ? __fmul_rn(__frcp_rn(safe), kTop) : 0.f;
     t.scale = x > 0.f ? safe * (float)(1.0 / 447.9995) : 0.f;
-    t.v = __shfl_sync(0xffffffffu, top, WIDTH / 2u, WIDTH);
-    t.root = __shfl_sync(0xffffffffu, root, WIDTH / 2u, WIDTH);
     t.m_inverse = __shfl_sync(0xffffffffu, inverse, 0, WIDTH);
     t.v_inverse = __shfl_sync(0xffffffffu, inverse, WIDTH / 2u, WIDTH);
     return t;
@@ -234,17 +256,14 @@ __device__ __forceinline__ uint2 encode_first(const Pair (&m)[4], const Tops &s,
     }
     return upper_bytes(code);
 }
-// Of the approximate roots r, which stay above zero once they are; the elements that have the block's largest finite v get the code
-// that its exact root has.
+// Of the roots r of v; one that is not 0 keeps a code that is not 0.
 __device__ __forceinline__ uint2 encode_second(const Pair (&v)[4], const Pair (&r)[4], const Tops &s, const Words &words) {
     uint32_t code[8];
     const Pair inverse(s.v_inverse), shift(0x1p-120f);
 #pragma unroll
     for (uint32_t i = 0; i < 4u; ++i) {
-        float x[2], z[2], y[2];
-        v[i].get(x[0], x[1]);
-        r[i].get(z[0], z[1]);
-        (Pair(x[0] == s.v ? s.root : z[0], x[1] == s.v ? s.root : z[1]) * inverse * shift).get(y[0], y[1]);
+        float y[2];
+        (r[i] * inverse * shift).get(y[0], y[1]);
 #pragma unroll
         for (uint32_t k = 0; k < 2u; ++k) code[2 * i + k] = (__float_as_uint(y[k]) + (words.word(8u + 2u * i + k) >> 12)) * 16u;
     }
@@ -275,7 +294,7 @@ struct Lane {
     Pair w[4], g[4], m[4], v[4], r[4];         // before update(), 8 bits: v holds the roots
 
     // New moments, roots r and weights.  The moments' products and sums are rounded one by one, so that elementary operations
-    // give the same bits; root and reciprocal are approximate, small against the weight that an update changes.
+    // give the same bits.
     __device__ __forceinline__ void update(const Coefficients &c) {
         const Pair factor(c.factor), beta1(c.beta1), rest1(c.rest1), beta2(c.beta2), rest2(c.rest2), root(c.root), eps(c.eps), step(-c.step), keep(c.keep),
             nothing(c.nothing);
@@ -284,21 +303,21 @@ struct Lane {
             const Pair g1 = g[i] * factor, square = BITS == 32 ? v[i] : v[i] * v[i];
             m[i] = fma2(m[i], beta1, nothing) + fma2(g1, rest1, nothing);
             v[i] = fma2(square, beta2, nothing) + fma2(g1 * g1, rest2, nothing);
-            r[i] = root_approx<true>(v[i]);
+            r[i] = root_of(v[i]);
         }
-        float least = __uint_as_float(0x7f800000u);
+        float some = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float lo, hi;
-            v[i].get(lo, hi);
-            asm("min.f32 %0, %0, %1, %2;" : "+f"(least) : "f"(lo), "f"(hi));
+            r[i].get(lo, hi);
+            asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(some) : "f"(lo), "f"(hi));
         }
-        if (least < 0x1p-126f) {                         // some are too small for that, or 0
+        if (some != some) {                              // 0, a subnormal, infinity or NaN
 #pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] = root_approx<false>(v[i]);
+            for (int i = 0; i < 4; ++i) r[i] = unless_nan(r[i], root_approx(v[i]));
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = fma2(w[i], keep, m[i] * step * reciprocal_approx(fma2(r[i], root, eps)));
+        for (int i = 0; i < 4; ++i) w[i] = fma2(w[i], keep, quotient<BITS == 32>(m[i] * step, fma2(r[i], root, eps)));
     }
     // The weights as elements of type T.
     template <typename T>

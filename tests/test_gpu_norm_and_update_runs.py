@@ -6,7 +6,7 @@ form of the kernels goes round its ring at least once.  Bounds are those of test
 import pytest
 import torch
 
-from test_gpu_norm_and_update import BF16, F16, F32, KINDS, U, Set, _gen, _id, _randn, _true_grad, _true_norm, _within, ctx  # noqa: F401
+from test_gpu_norm_and_update import BF16, F16, F32, KINDS, TOP, U, Set, _gen, _id, _randn, _true_grad, _true_norm, _within, _words, ctx  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -49,6 +49,50 @@ def test_the_longest_runs(ctx, kind, bits):  # noqa: F811
     s = Set([256 * (33 * 2 * 8 * SMS) + 100], weight, grad, bits, master, 4, 0)
     ctx.adamw_step(*s.args(), **s.state, seed=3)
     s.check(seed=3)
+
+
+def _codes(x, words, name):
+    """Codes (as bytes) and scales of blocks of 256 numbers by elementary operations in 32 bits."""
+    rows = x.view(-1, 256)
+    safe = rows.abs().amax(1).clamp(min=2.0 ** -110)
+    scaled = rows.abs() * (safe.reciprocal() * TOP)[:, None] * 2.0 ** -120      # a code is the upper bits of such a float
+    code = (scaled.view(torch.int32).view(-1) + (words >> 12).int()) >> 20
+    if name == "v":
+        code = torch.maximum(code, (x > 0).int())
+    return torch.where(x < 0, code | 128, code).to(torch.uint8), safe * (1.0 / TOP)
+
+
+@pytest.mark.parametrize("seed", [1, 2, 3])
+def test_codes_are_those_of_elementary_operations(ctx, seed):  # noqa: F811
+    """Bit for bit.  A root that is off in its last place has another code with a probability of 2^-20 and less, hence so many."""
+    n = 1 << 24
+    s = Set([n], F32, F32, 8, seed=10 * seed)
+    want = {}
+    t, places = int(s.state["step"]) + 1, torch.arange(n, device="cuda")
+    old = {name: (s.state[name].float().view(-1, 256) * s.state[name + "_scales"][:, None]).view(-1) for name in ("m", "v")}
+    g = s.g[:n]
+    m, v = old["m"] * 0.9 + g * (1 - 0.9), old["v"] * old["v"] * 0.999 + g * g * (1 - 0.999)
+    for name, x, first in (("m", m, 0), ("v", v.sqrt(), 8)):
+        want[name] = _codes(x, _words(seed, t, places, first), name)
+    ctx.adamw_step(*s.args(), **s.state, seed=seed)
+    for name, (code, scale) in want.items():
+        assert torch.equal(s.state[name + "_scales"], scale)
+        assert torch.equal(s.state[name].view(torch.uint8), code)
+
+
+@pytest.mark.parametrize("lr", [1e-3, 0.7, 3e-5])
+def test_update_from_32_bit_moments_is_right_to_the_last_place(ctx, lr):  # noqa: F811
+    """Weights of 0, betas of 0 and gradients of 12 digits, whose squares are exact: the update is lr g / |g|, so the weight is the product
+    -lr g, rounded, over |g|, rounded: within 2^-24 of that quotient, and 2^-40 for what a step of correction leaves."""
+    g = torch.cat([torch.arange(2048, 4096, device="cuda").float() * 2.0 ** e for e in (-40, -19, -12, 3)])
+    s = Set([len(g)], F32, F32, 32, step=0)
+    s.w.zero_()
+    s.g[:len(g)] = g
+    s.keep()
+    ctx.adamw_step(*s.args(), **s.state, lr=lr, betas=(0.0, 0.0), eps=0.0, weight_decay=0.0)
+    assert torch.equal(s.state["m"][:len(g)], g) and torch.equal(s.state["v"][:len(g)], g * g)
+    true = (g * -lr).double() / g.double()
+    assert bool(((s.w[:len(g)].double() - true).abs() <= (U + 2.0 ** -40) * true.abs()).all())
 
 
 # ------------------------------------------------------------------------------------------------- rows
