@@ -26,8 +26,10 @@ using elem::Pair;
 constexpr uint32_t kThreads = 512;
 
 // The ring: 16-byte pieces in a row of every group, rows that a group works on at a time, and steps.  One CTA takes an SM's shared
-// memory, but for aligned 16-bit rows of 2049 to 4096 columns two share it (131072 x 4096: 342 us, 370 with one; 262144 x 1024 181
-// with two, 166 with one; float32 rows to 16 bits, 65536 x 4096: 279 and 240).
+// memory, but for aligned 16-bit rows of 2049 to 4096 columns two share it.  Two and one, us, 1 GB of bf16 rows: 2056 columns 580 and 676,
+// 2560 470 and 550, 3584 360 and 436, 4096 350 and 388; root-mean-square form 444 and 522, 367 and 419, 384 and 341, 337 and 340; half as many
+// rows to 32 bits 343 and 380, 305 and 318, 272 and 278, 280 and 257: one would be better for a few of them, which no width or
+// type sets apart.  Elsewhere two are worse: 262144 x 1024 181 and 166; float32 rows to 16 bits, 65536 x 4096, 279 and 240.
 template <typename Tx, uint32_t T, int NV, int MODE>
 struct Ring {
     static constexpr uint32_t kWidth = T < 32u ? T : 32u, kSegments = kThreads / kWidth;
@@ -177,7 +179,9 @@ layer_norm_kernel(const __grid_constant__ LayerNormArgs a) {
     if (base < end) work(base, std::false_type());
 }
 
-// Rows too wide for that: one CTA per row, which reads it three times (from the L2 cache the second and third time).
+// Rows too wide for that: one CTA per row, which reads it three times: from the L2 cache the second and third time as long as the rows
+// in flight, two for each SM, fit there (on a B200 16-bit rows of some 200,000 columns), from memory beyond.  A row has one SM.
+// 1.07e9 bf16 elements: 65,536 columns 1.53 ms, 2.8 TB/s of what must move once; 262,144 1.67 ms; 2^20 1.84 ms; 64 rows of 2^24 4.75 ms.
 constexpr uint32_t kWideThreads = 1024;
 template <typename Tx, typename Ty, bool ALIGNED>
 __global__ void __launch_bounds__(kWideThreads)

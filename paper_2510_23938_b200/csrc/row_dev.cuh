@@ -1,5 +1,5 @@
 // Rows taken by groups of threads, eight consecutive elements at a time: loads and stores at any element alignment, sums
-// over a group, weights widened into shared memory (layer norm and its gradient).
+// over a group, copies of rows into shared memory (layer norm and its gradient).
 #pragma once
 #include "element_dev.cuh"
 
