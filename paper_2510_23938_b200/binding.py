@@ -957,10 +957,11 @@ def tensor_ranges(tensors) -> tuple:
             torch.tensor([DTYPES[t.dtype] for t in tensors], dtype=torch.uint8, device=device))
 
 
-def adamw_state(elements, device, bits: int = 32, master: bool = False) -> dict:
+def adamw_state(elements, device, bits: int = 32, master=False) -> dict:
     """The state of adamw_step for tensors of `elements` elements each (a list of numbers), before the first step: places
-    (multiples of ADAMW_BLOCK), moments in 32 or 8 bits, the number of steps and, with `master`, room for the weights in
-    32 bits, which the caller fills (grad_scale by 1 into `master` at 4 * state_offsets does)."""
+    (multiples of ADAMW_BLOCK), moments in 32 or 8 bits, the number of steps and, with `master`, the weights in 32 bits: `master` is
+    the list of the weight tensors, which are copied, or True for room that the caller fills before the first step (zeros until
+    then, from which a step would set the weights; grad_scale by 1 into `master` at 4 * state_offsets fills it)."""
     assert bits in (8, 32), "moments are held in 8 or 32 bits"
     places, size = [], 0
     for n in elements:
@@ -974,8 +975,12 @@ def adamw_state(elements, device, bits: int = 32, master: bool = False) -> dict:
         else:
             state[name] = torch.zeros(size, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
             state[name + "_scales"] = torch.zeros(size // ADAMW_BLOCK, device=device)
-    if master:
+    if master is not False:
         state["master"] = torch.zeros(size, device=device)
+        if master is not True:
+            assert [w.numel() for w in master] == [int(n) for n in elements], "master: one tensor of weights per place"
+            for place, w in zip(places, master):
+                state["master"][place:place + w.numel()].copy_(w.reshape(-1))
     return state
 
 
