@@ -561,7 +561,9 @@ int iv_grad_scale(iv_ctx *ctx, void *d_base, const uint64_t *d_offsets, const ui
  *   d_mean, d_rstd   optional: n_rows floats each, mu and s (for the gradient)
  *   eps        >= 0, not NaN
  * A row's result does not depend on the other rows, nor on strides or
- * alignment.  Sums of squares are taken in 32 bits: a row whose squares leave
+ * alignment.  mu is a sum of 32 bits over dim: what it is off, some of its last
+ * places, is multiplied by s (nothing in a row of equal numbers the sum of which
+ * is exact in 24 bits).  Sums of squares are taken in 32 bits: a row whose squares leave
  * that range has s = 0.  IV_ERR_TOO_LARGE for n_rows > 2^30, dim > 2^24. */
 int iv_layer_norm(iv_ctx *ctx, const void *d_x, int x_type, uint64_t x_stride, uint64_t n_rows, uint64_t dim,
                   const void *d_weight, const void *d_bias, int param_type, float eps, int rms, void *d_y, int y_type,

@@ -6,10 +6,10 @@
 // Weights, gradients and moments are read once, weights and moments written once: 22 bytes an element with 16-bit weights and gradients, 10
 // with 8-bit moments.  The moments of all tensors lie in one array, every tensor at a multiple of a block; a warp takes a run of
 // blocks, finds a block's tensor by searching the tensors' places, and needs nobody else: a block's largest moments are a reduction
-// over half a warp.  With 32-bit moments memory is the bound: on one B200 the 1.31e9 bf16 weights of a 24-layer file take 4.6 ms,
-// 6.2 TB/s (4.9 with three CTAs per SM, whose 80 registers are too few); 200 packed tensors with 32-bit copies 289 us, 5.9 TB/s.  With 8-bit
-// moments it is the instructions, some 55 an element: the same file takes 3.05 ms, 4.3 TB/s, 200 packed tensors with float32 gradients
-// 205 us.  Seven small tensors take 6 to 7 us on the device.
+// over half a warp.  With 32-bit moments memory is the bound: on one B200 the 1.31e9 bf16 weights of a 24-layer file take 4.65 ms,
+// 6.2 TB/s (4.9 with three CTAs per SM, whose 80 registers are too few); 200 packed tensors with 32-bit copies 290 us, 5.8 TB/s.  With 8-bit
+// moments it is the instructions, some 54 an element: the same file takes 3.14 ms, 4.2 TB/s, 200 packed tensors with float32 gradients
+// 213 us.  Seven small tensors take 5 to 7 us on the device.
 //
 // The moments' averages change by a part in a thousand a step, far less than an 8-bit code's step, so rounding to nearest would
 // hold them where they are.  They are rounded up with the probability that the lost bits give instead, by

@@ -7,8 +7,8 @@
 // launch or on the alignment.  Rows come through a ring in shared memory that each warp fills for itself with asynchronous copies,
 // several rows ahead; a group of threads works on four (or two) at a time, so that their sums cross threads together.  The kernel may
 // start while the one before it ends (8192 x 2048: 18.6 us a call without, 17.2 with).
-// On one B200, bf16: 131072 x 4096 347 us, 6.2 TB/s; 65536 x 8192 319 us, 6.7 TB/s; 262144 x 1024 165 us; a single row 2.7 us.  Rows at odd
-// places or of odd widths are shifted, which costs instructions: 65536 x 4095 368 us, 2.9 TB/s.
+// On one B200, bf16: 131072 x 4096 350 us, 6.1 TB/s; 65536 x 8192 320 us, 6.7 TB/s; 262144 x 1024 167 us; a single row 2.5 us.  Rows at odd
+// places or of odd widths are shifted, which costs instructions: 65536 x 4095 372 us, 2.9 TB/s.
 #pragma once
 #include <type_traits>
 
